@@ -143,6 +143,9 @@ typedef enum { LAMB_PHI_IDENTITY = 0, LAMB_PHI_CLIP = 1 } lamb_phi_t;
                                            Inf or NaN                       */
 #define LAMB_STATUS_SKIPPED   0x10u     /* SKIP_NONFINITE: a step was skipped
                                            for that reason                  */
+#define LAMB_STATUS_BAD_INDEX 0x20u     /* a vocabulary plan met a word id or a
+                                           label that is not below the
+                                           vocabulary, and took it as absent */
 
 /* Hyperparameters.  Doubles on purpose: (1 - beta) is formed in double and
  * rounded once to float, so e.g. beta2 = 0.999 gives 1-beta2 = 0.001 to
@@ -631,6 +634,85 @@ LAMB_API lamb_status_t lamb_layout_shard(const int64_t* sizes,
                                          int64_t tail_elems, int32_t world,
                                          int32_t rank, int64_t* chunk_begin,
                                          int64_t* chunk_end);
+
+/* ---------------------------------------------------------------------------
+ * The two ends of a language model: the word table's lookup with its gradient,
+ * and the vocabulary head's loss with its gradients.  They make the gradient of
+ * the largest tensor of a language model's layout; with a tied table both add to
+ * one buffer, which a plan bound to it (lamb_plan_bind) then steps on.
+ *
+ * A matrix is given by the DEVICE address of its first element and by its row
+ * stride in elements (>= the width; rows are contiguous).  Word ids and labels
+ * are DEVICE int64.  An id or label below 0 is absent (padding, an ignored
+ * position); one that is not below the vocabulary is taken as absent too and
+ * sets LAMB_STATUS_BAD_INDEX (lamb_vocab_query).  Calls enqueue on `stream`,
+ * allocate nothing and do not synchronise: capturable in a CUDA graph.  Calls of
+ * one plan share its workspaces and must not overlap.  Every result is the same
+ * bits in every run.
+ * ------------------------------------------------------------------------- */
+struct lamb_vocab;
+
+/* Workspaces for up to max_tokens tokens a call (1 .. 2^24), a vocabulary of
+ * 1 .. 2^30 rows and a width of 1 .. 2^20 columns, on `device`.  Synchronous. */
+LAMB_API lamb_status_t lamb_vocab_create(int64_t vocab, int32_t width,
+                                         int64_t max_tokens, int32_t device,
+                                         struct lamb_vocab** out);
+
+/* out[t] = scale * table[ids[t]], a row of zeros where the id is absent.  table
+ * and out are LAMB_F32 or LAMB_BF16 each (out is rounded once, to nearest). */
+LAMB_API lamb_status_t lamb_vocab_embed(
+    struct lamb_vocab* plan, const void* table, int32_t table_dtype,
+    int64_t table_stride, const int64_t* ids, int64_t n_tokens, double scale,
+    void* out, int32_t out_dtype, int64_t out_stride, cudaStream_t stream);
+
+/* The lookup's gradient: table_grad[v] = scale * sum of grad_out[t] over the
+ * tokens with ids[t] = v, in fp32 and in a fixed order.  accumulate = 0 writes
+ * every row of table_grad (zeros where a word has no token); accumulate = 1 adds
+ * to the rows that have tokens and leaves the others alone.  grad_out and
+ * table_grad are LAMB_F32 or LAMB_BF16 each. */
+LAMB_API lamb_status_t lamb_vocab_embed_grad(
+    struct lamb_vocab* plan, const void* grad_out, int32_t grad_dtype,
+    int64_t grad_stride, const int64_t* ids, int64_t n_tokens, double scale,
+    void* table_grad, int32_t table_dtype, int64_t table_stride,
+    int32_t accumulate, cudaStream_t stream);
+
+/* Softmax cross entropy of bf16 hidden rows [n_tokens, width] against the bf16
+ * table weight [vocab, width], logits = hidden weight^T in fp32, without
+ * keeping them.
+ *   token_loss  NULL or DEVICE float [n_tokens]: lse_t - logit of the label, 0
+ *               where the label is absent
+ *   loss        DEVICE float: the mean over the labels that are present (0 if
+ *               there are none) */
+LAMB_API lamb_status_t lamb_vocab_loss(
+    struct lamb_vocab* plan, const void* hidden, int64_t hidden_stride,
+    const void* weight, int64_t weight_stride, const int64_t* labels,
+    int64_t n_tokens, float* token_loss, float* loss, cudaStream_t stream);
+
+/* The same, and the gradients of scale * loss.
+ *   d_scale      NULL (1) or DEVICE float: the gradient that arrives at the
+ *                loss, or a loss scale
+ *   grad_hidden  bf16 [n_tokens, width]; zeros in rows without a label
+ *   grad_weight  bf16 or fp32 [vocab, width]; accumulate = 1 adds to it
+ * The gradient of the logits is rounded to bf16 on its way into the two products
+ * with weight and hidden, whose sums are fp32: an fp32 grad_weight holds sums of
+ * such terms. */
+LAMB_API lamb_status_t lamb_vocab_loss_grad(
+    struct lamb_vocab* plan, const void* hidden, int64_t hidden_stride,
+    const void* weight, int64_t weight_stride, const int64_t* labels,
+    int64_t n_tokens, const float* d_scale, float* token_loss, float* loss,
+    void* grad_hidden, int64_t grad_hidden_stride, void* grad_weight,
+    int32_t grad_weight_dtype, int64_t grad_weight_stride, int32_t accumulate,
+    cudaStream_t stream);
+
+/* Read (and optionally clear) the plan's device status word: BAD_INDEX, or
+ * WAIT_TIMEOUT (a wait inside a product gave up: never expected, results of
+ * that call are incomplete).  Synchronises `stream`; not capturable. */
+LAMB_API lamb_status_t lamb_vocab_query(struct lamb_vocab* plan,
+                                        uint32_t* status_bits, int32_t clear,
+                                        cudaStream_t stream);
+
+/* Frees the plan (synchronises its device); NULL is a no-op. */
+LAMB_API lamb_status_t lamb_vocab_destroy(struct lamb_vocab* plan);
 
 /* Message of the last failed call on this host thread ("" if none). */
 LAMB_API const char* lamb_last_error(void);

@@ -45,6 +45,7 @@ LAMB_STATUS_NONFINITE = 0x1
 LAMB_STATUS_BAD_STEP = 0x2
 LAMB_STATUS_GRAD_NONFINITE = 0x8
 LAMB_STATUS_SKIPPED = 0x10
+LAMB_STATUS_BAD_INDEX = 0x20
 
 EXPORTED = ["lamb_plan_create", "lamb_plan_bind", "lamb_step", "lars_step",
             "lamb_plan_trust_ratios", "lamb_plan_copy_trust_ratios",
@@ -55,7 +56,10 @@ EXPORTED = ["lamb_plan_create", "lamb_plan_bind", "lamb_step", "lars_step",
             "nlamb_step", "lamb_plan_grad_norms", "lamb_plan_copy_grad_norms",
             "lamb_layout_rounds", "lamb_shard_pass1", "lamb_shard_pass2",
             "lamb_plan_partials", "lamb_layout_shard",
-            "lamb_plan_copy_partials"]
+            "lamb_plan_copy_partials",
+            "lamb_vocab_create", "lamb_vocab_embed", "lamb_vocab_embed_grad",
+            "lamb_vocab_loss", "lamb_vocab_loss_grad", "lamb_vocab_query",
+            "lamb_vocab_destroy"]
 
 
 class LambError(RuntimeError):
@@ -175,6 +179,17 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.lamb_layout_rounds.argtypes = [POINTER(c_int64), c_int32, c_int32,
                                        c_int32, *([vp] * 7), c_int64,
                                        POINTER(c_int64), POINTER(c_int32)]
+    i32, i64 = c_int32, c_int64
+    lib.lamb_vocab_create.argtypes = [i64, i32, i64, i32, POINTER(vp)]
+    lib.lamb_vocab_embed.argtypes = [vp, vp, i32, i64, vp, i64, c_double, vp,
+                                     i32, i64, vp]
+    lib.lamb_vocab_embed_grad.argtypes = [vp, vp, i32, i64, vp, i64, c_double,
+                                          vp, i32, i64, i32, vp]
+    lib.lamb_vocab_loss.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp]
+    lib.lamb_vocab_loss_grad.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp,
+                                         vp, vp, i64, vp, i32, i64, i32, vp]
+    lib.lamb_vocab_query.argtypes = [vp, POINTER(c_uint32), i32, vp]
+    lib.lamb_vocab_destroy.argtypes = [vp]
     for name in EXPORTED:
         if name in ("lamb_last_error", "lamb_abi_version"):
             continue
@@ -489,3 +504,67 @@ def lamb_plan_copy_partials(plan, buf, to_plan, stream=0) -> None:
     _check(load().lamb_plan_copy_partials(c_void_p(plan), c_void_p(buf),
                                           int(bool(to_plan)),
                                           c_void_p(stream or None)))
+
+
+# ---------------------------------------------------------------------------
+# Word table and vocabulary head
+# ---------------------------------------------------------------------------
+def lamb_vocab_create(vocab, width, max_tokens, device=0) -> int:
+    out = c_void_p()
+    _check(load().lamb_vocab_create(int(vocab), int(width), int(max_tokens),
+                                    int(device), byref(out)))
+    return out.value
+
+
+def lamb_vocab_embed(plan, table, table_dtype, table_stride, ids, n_tokens,
+                     scale, out, out_dtype, out_stride, stream=0) -> None:
+    st = load().lamb_vocab_embed(plan, table, table_dtype, table_stride, ids,
+                                 n_tokens, scale, out, out_dtype, out_stride,
+                                 stream)
+    if st:
+        _check(st)
+
+
+def lamb_vocab_embed_grad(plan, grad_out, grad_dtype, grad_stride, ids,
+                          n_tokens, scale, table_grad, table_dtype,
+                          table_stride, accumulate, stream=0) -> None:
+    st = load().lamb_vocab_embed_grad(plan, grad_out, grad_dtype, grad_stride,
+                                      ids, n_tokens, scale, table_grad,
+                                      table_dtype, table_stride, accumulate,
+                                      stream)
+    if st:
+        _check(st)
+
+
+def lamb_vocab_loss(plan, hidden, hidden_stride, weight, weight_stride, labels,
+                    n_tokens, token_loss, loss, stream=0) -> None:
+    st = load().lamb_vocab_loss(plan, hidden, hidden_stride, weight,
+                                weight_stride, labels, n_tokens, token_loss,
+                                loss, stream)
+    if st:
+        _check(st)
+
+
+def lamb_vocab_loss_grad(plan, hidden, hidden_stride, weight, weight_stride,
+                         labels, n_tokens, d_scale, token_loss, loss,
+                         grad_hidden, grad_hidden_stride, grad_weight,
+                         grad_weight_dtype, grad_weight_stride, accumulate,
+                         stream=0) -> None:
+    st = load().lamb_vocab_loss_grad(
+        plan, hidden, hidden_stride, weight, weight_stride, labels, n_tokens,
+        d_scale, token_loss, loss, grad_hidden, grad_hidden_stride,
+        grad_weight, grad_weight_dtype, grad_weight_stride, accumulate, stream)
+    if st:
+        _check(st)
+
+
+def lamb_vocab_query(plan, clear=False, stream=0) -> int:
+    bits = c_uint32()
+    _check(load().lamb_vocab_query(c_void_p(plan), byref(bits), int(clear),
+                                   c_void_p(stream or None)))
+    return int(bits.value)
+
+
+def lamb_vocab_destroy(plan) -> None:
+    if plan:
+        _check(load().lamb_vocab_destroy(c_void_p(plan)))

@@ -1,0 +1,187 @@
+// Matrix products of the language-model operators: C = A B^T of bf16 or fp16
+// operands with fp32 accumulators, tile by tile, each tile handed to an
+// epilogue while the next one is multiplied.
+//
+// One persistent CTA per SM walks the tiles of a Work type:
+//   Work::kBf16                   operands bf16 (else fp16)
+//   Work::Params::status          the plan's status word
+//   Work::start(params)           what the kernel reads first: State, with the
+//                                 number of tiles (it may come from the device)
+//   Work::tile(params, state, t)  operands and extent of tile t (GemmTile)
+//   Work::epilogue(params, state, tile, acc, row)  a row of the accumulator
+// A tile is 128 rows of A by 256 of B.  Operands come through tensor maps with
+// the 128-byte swizzle, K-major (box: 64 of K by 128 rows) or MN-major (box: 64
+// rows by 64 of K); what lies outside a matrix arrives as zeros.
+//
+// Warps: 0 copies, 1 issues the products, 2 holds the tensor memory, 4-7 run the
+// epilogue (a warp reaches the quarter of the lanes with its number mod 4).
+// Two accumulators of 256 columns fill tensor memory, so a tile's epilogue runs
+// beside the next tile's products.
+#pragma once
+#include "lamb_internal.h"
+#include "lm_tc.cuh"
+
+namespace lamb {
+namespace {
+
+constexpr int kTileM = 128, kTileN = 256, kTileK = 64;
+constexpr int kGemmThreads = 256;
+constexpr int kGemmStages = 4;
+constexpr int kTileBytesA = kTileM * kTileK * 2;
+constexpr int kTileBytesB = kTileN * kTileK * 2;
+constexpr int kGemmStageBytes = kTileBytesA + kTileBytesB;
+constexpr size_t kGemmSmem = (size_t)kGemmStages * kGemmStageBytes + 1024;
+
+struct GemmTile {
+  const CUtensorMap* a;
+  const CUtensorMap* b;
+  int a0, b0;        // first row of A, of B
+  int k0, kn;        // first block of K, number of blocks
+  int b_k;           // elements that B's K starts further on
+  bool a_mn, b_mn;   // MN-major operands
+  int what, aux;     // the epilogue's
+};
+
+struct GemmShared {
+  uint64_t full[kGemmStages], empty[kGemmStages];
+  uint64_t acc_full[2], acc_empty[2];
+  uint32_t tmem;
+  volatile int gave_up;
+};
+
+template <class Work>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+gemm_kernel(const __grid_constant__ typename Work::Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ GemmShared sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem =
+      (smem_u32(smem_raw) + 1023u) & ~1023u;   // the swizzle's pattern
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kGemmStages; ++i) {
+      mbar_init(&sh.full[i], 1);
+      mbar_init(&sh.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.acc_full[i], 1);
+      mbar_init(&sh.acc_empty[i], 4);
+    }
+    sh.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
+  }
+  if (warp == 2) tmem_alloc_all(&sh.tmem);
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  const uint32_t tmem = sh.tmem;
+  after_prior_launch();
+  const typename Work::State st = Work::start(p);
+
+  if (warp == 0) {
+    if (elect_lane()) {
+      int it = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; ok && t < st.n_tiles; t += gridDim.x) {
+        const GemmTile g = Work::tile(p, st, t);
+        for (int kb = 0; kb < g.kn; ++kb, ++it) {
+          const int s = it % kGemmStages;
+          const uint32_t ph = (uint32_t)(it / kGemmStages) & 1u;
+          if (!bounded_wait(&sh.empty[s], ph ^ 1u, &sh.gave_up, p.status,
+                            kStatusWaitTimeout)) {
+            ok = false;
+            break;
+          }
+          const uint32_t at = smem + s * kGemmStageBytes;
+          const int k = (g.k0 + kb) * kTileK;
+          mbar_expect(&sh.full[s], kGemmStageBytes);
+          if (g.a_mn) {
+            tile_load(at, g.a, g.a0, k, &sh.full[s]);
+            tile_load(at + 8192, g.a, g.a0 + 64, k, &sh.full[s]);
+          } else {
+            tile_load(at, g.a, k, g.a0, &sh.full[s]);
+          }
+          const uint32_t bt = at + kTileBytesA;
+          if (g.b_mn) {
+            for (int i = 0; i < 4; ++i)
+              tile_load(bt + i * 8192, g.b, g.b0 + 64 * i, k + g.b_k,
+                        &sh.full[s]);
+          } else {
+            tile_load(bt, g.b, k + g.b_k, g.b0, &sh.full[s]);
+            tile_load(bt + 16384, g.b, k + g.b_k, g.b0 + 128, &sh.full[s]);
+          }
+        }
+      }
+      // every copy has landed before the CTA may leave
+      const int first = it > kGemmStages ? it - kGemmStages : 0;
+      for (int j = first; j < it; ++j) {
+        const uint64_t begin = global_ns();
+        while (!mbar_try(&sh.full[j % kGemmStages],
+                         (uint32_t)(j / kGemmStages) & 1u))
+          if (global_ns() - begin > kWaitLimitNs) break;
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (elect_lane()) {
+      int it = 0, n = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; ok && t < st.n_tiles; t += gridDim.x, ++n) {
+        const GemmTile g = Work::tile(p, st, t);
+        const uint64_t da = operand_desc(g.a_mn), db = operand_desc(g.b_mn);
+        const uint32_t sa = operand_step(g.a_mn), sb = operand_step(g.b_mn);
+        const uint32_t desc =
+            product_desc(Work::kBf16, g.a_mn, g.b_mn, kTileM, kTileN);
+        const int acc = n & 1;
+        const uint32_t d = tmem + acc * kTileN;
+        if (!bounded_wait(&sh.acc_empty[acc], ((uint32_t)(n >> 1) & 1u) ^ 1u,
+                          &sh.gave_up, p.status, kStatusWaitTimeout))
+          break;
+        tmem_after_sync();
+        for (int kb = 0; kb < g.kn; ++kb, ++it) {
+          const int s = it % kGemmStages;
+          if (!bounded_wait(&sh.full[s], (uint32_t)(it / kGemmStages) & 1u,
+                            &sh.gave_up, p.status, kStatusWaitTimeout)) {
+            ok = false;
+            break;
+          }
+          tmem_after_sync();
+          const uint32_t at = smem + s * kGemmStageBytes;
+          const uint64_t a = da | (at >> 4), b = db | ((at + kTileBytesA) >> 4);
+#pragma unroll
+          for (int k = 0; k < kTileK / 16; ++k)
+            product(d, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
+          products_arrive(&sh.empty[s]);
+        }
+        if (ok) products_arrive(&sh.acc_full[acc]);
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    int n = 0;
+    for (int t = blockIdx.x; t < st.n_tiles; t += gridDim.x, ++n) {
+      const GemmTile g = Work::tile(p, st, t);
+      const int acc = n & 1;
+      const bool ok =
+          bounded_wait(&sh.acc_full[acc], (uint32_t)(n >> 1) & 1u, &sh.gave_up,
+                       p.status, kStatusWaitTimeout);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      tmem_after_sync();
+      const int quarter = warp & 3;
+      Work::epilogue(p, st, g,
+                     tmem + acc * kTileN + ((uint32_t)(quarter * 32) << 16),
+                     quarter * 32 + lane);
+      tmem_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
+    }
+  }
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  if (warp == 2) tmem_free_all(tmem);
+}
+
+}  // namespace
+}  // namespace lamb

@@ -1,0 +1,918 @@
+// Vocabulary head: softmax cross entropy of hidden rows against the word table,
+// with both gradients, without keeping the logits.
+//
+//   l = h W^T,  lse_t = log sum_v exp l_tv,  loss_t = lse_t - l_t,y
+//   dl = (exp(l - lse) - onehot) * scale / n,  dh = dl W,  dW = dl^T h
+//
+// n counts the labels that are present.  A row without one has no loss and no
+// gradient, so it is left out before the first product: the rows that have a
+// label are gathered, and all sizes below come from their number on the device.
+// (Whatever an absent row holds, an Inf or NaN too, then reaches nothing.)
+// Exponentials are taken in base 2: x' = x log2 e.
+//
+// The loss is one product on the tensor cores (lm_gemm.cuh) whose epilogue
+// leaves, of each 256 columns of a row, the maximum and the sum of exponentials
+// (fp32); a small kernel joins them in a fixed order.  The gradients take the
+// vocabulary in pieces: a piece's logits are multiplied again, the epilogue
+// writes their gradient in bf16 to a workspace (the rounding that any bf16
+// operand of the following products needs; 2^-9 of each element), and one more
+// launch multiplies it with W (rows of dh) and, transposed by the operand's
+// layout, with h (rows of dW).  dh's sums over pieces and over parts of a long
+// piece stay in fp32.  8 T V D operations in all, bound by the tensor cores for
+// many tokens and by reading W for few.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <new>
+
+#include "lm_gemm.cuh"
+#include "lm_vocab.h"
+
+namespace lamb {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 32;          // tokens of a CTA, eight threads each
+constexpr int64_t kPieceElems = 64ll << 20;   // dlogits workspace, elements
+constexpr int kMinPartBlocks = 4;      // blocks of K in a part of dh, at least
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// ---- rows with a label ------------------------------------------------------
+// CTA i takes tokens [kPickRows i, ..): counts the labels before them, gathers
+// its own rows that have one, and clears what the others' results are.  The last
+// CTA leaves the number of rows and zeros up to a whole tile (one of zeros if
+// there is no row: dW's products need a K).
+constexpr int kPickThreads = 256, kPickRows = 64;
+
+template <bool kVec>
+__global__ void __launch_bounds__(kPickThreads)
+pick_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t stride,
+            const int64_t* __restrict__ labels, int tokens, int64_t vocab,
+            int width, __nv_bfloat16* __restrict__ rows, int64_t pitch,
+            int32_t* __restrict__ row_label, int32_t* __restrict__ row_token,
+            int32_t* n_rows, float* token_loss, __nv_bfloat16* grad_hidden,
+            int64_t grad_stride, uint32_t* status) {
+  __shared__ int sh_count[kPickThreads / 32];
+  __shared__ int sh_at[kPickRows];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int first = blockIdx.x * kPickRows;
+  const bool end = blockIdx.x == gridDim.x - 1;
+  int before = 0;
+  for (int t = threadIdx.x; t < first; t += kPickThreads) {
+    const int64_t y = labels[t];
+    before += y >= 0 && y < vocab;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  if (lane == 0) sh_count[warp] = before;
+  __syncthreads();
+  if (warp == 0) {
+    int at = 0;
+    for (int i = 0; i < kPickThreads / 32; ++i) at += sh_count[i];
+    for (int r = 0; r < kPickRows; r += 32) {
+      const int t = first + r + lane;
+      const int64_t y = t < tokens ? labels[t] : -1;
+      const bool real = y >= 0 && y < vocab;
+      if (y >= vocab) atomicOr(status, LAMB_STATUS_BAD_INDEX);
+      const uint32_t m = __ballot_sync(0xffffffffu, real);
+      const int to = at + __popc(m & ((1u << lane) - 1u));
+      sh_at[r + lane] = real ? to : -1;
+      if (real) {
+        row_label[to] = (int32_t)y;
+        row_token[to] = t;
+      } else if (token_loss && t < tokens) {
+        token_loss[t] = 0.f;
+      }
+      at += __popc(m);
+    }
+    if (lane == 0) {
+      sh_count[0] = at;
+      if (end) *n_rows = at;
+    }
+  }
+  __syncthreads();
+  const int own = min(kPickRows, tokens - first);
+  const int past = sh_count[0] % kTileM;
+  const int tail = end && (past || !sh_count[0]) ? kTileM - past : 0;
+  for (int r = warp; r < own + tail; r += kPickThreads / 32) {
+    const bool zero = r >= own;
+    const int t = first + r, to = zero ? sh_count[0] + r - own : sh_at[r];
+    if (to < 0 && !grad_hidden) continue;
+    const __nv_bfloat16* src = hidden + (int64_t)t * stride;
+    if (kVec) {     // 16 bytes a lane
+      uint4* dst = reinterpret_cast<uint4*>(
+          to >= 0 ? rows + (int64_t)to * pitch
+                  : grad_hidden + (int64_t)t * grad_stride);
+      for (int d = lane; d < width / 8; d += 32)
+        dst[d] = zero || to < 0 ? make_uint4(0, 0, 0, 0)
+                                : reinterpret_cast<const uint4*>(src)[d];
+    } else {
+      __nv_bfloat16* dst = to >= 0 ? rows + (int64_t)to * pitch
+                                   : grad_hidden + (int64_t)t * grad_stride;
+      for (int d = lane; d < width; d += 32)
+        dst[d] = zero || to < 0 ? __float2bfloat16_rn(0.f) : src[d];
+    }
+  }
+}
+
+// ---- the loss ---------------------------------------------------------------
+struct RowsState {
+  int n_tiles, m_tiles, rows;
+};
+
+struct StatsParams {
+  CUtensorMap hidden, weight;
+  const int32_t* n_rows;
+  const int32_t* labels;  // of the rows
+  float2* stats;          // [vocab tile][stride]
+  float* label_logit;
+  uint32_t* status;
+  int64_t stride;
+  int v_tiles, vocab, k_blocks;
+};
+
+struct StatsWork {
+  typedef StatsParams Params;
+  typedef RowsState State;
+  static constexpr bool kBf16 = true;
+  static __device__ __forceinline__ State start(const Params& p) {
+    State s;
+    s.rows = *p.n_rows;
+    s.m_tiles = s.rows ? (s.rows + kTileM - 1) / kTileM : 1;
+    s.n_tiles = s.m_tiles * p.v_tiles;
+    return s;
+  }
+  static __device__ __forceinline__ GemmTile tile(const Params& p,
+                                                  const State& s, int t) {
+    GemmTile g;
+    g.a = &p.hidden;
+    g.b = &p.weight;
+    g.a0 = (t % s.m_tiles) * kTileM;
+    g.what = t / s.m_tiles;
+    g.b0 = g.what * kTileN;
+    g.k0 = 0;
+    g.kn = p.k_blocks;
+    g.b_k = 0;
+    g.a_mn = g.b_mn = false;
+    g.aux = 0;
+    return g;
+  }
+  static __device__ __forceinline__ void epilogue(const Params& p,
+                                                  const State& s,
+                                                  const GemmTile& g,
+                                                  uint32_t acc, int row) {
+    const int r = g.a0 + row;
+    const int label = r < s.rows ? p.labels[r] : -1;
+    float top = -INFINITY, sum = 0.f;
+    for (int c = 0; c < kTileN / 32; ++c) {
+      const int v = g.b0 + c * 32;
+      if (v >= p.vocab) break;
+      float x[32];
+      tmem_ld32(acc + c * 32, x);
+      if (label >= v && label < v + 32) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (label == v + i) p.label_logit[r] = x[i];
+      }
+      if (v + 32 > p.vocab) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (v + i >= p.vocab) x[i] = -INFINITY;
+      }
+      float m = x[0];
+#pragma unroll
+      for (int i = 1; i < 32; ++i) m = fmaxf(m, x[i]);
+      m = fmaxf(m * kLog2e, top);
+      // a row of nothing but -inf keeps the sum 0
+      const float at = m == -INFINITY ? 0.f : m;
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) {
+        s0 += exp2_fast(fmaf(x[i], kLog2e, -at));
+        s1 += exp2_fast(fmaf(x[i + 1], kLog2e, -at));
+      }
+      sum = sum * exp2_fast(top - at) + (s0 + s1);
+      top = m;
+    }
+    if (r < s.rows)
+      p.stats[(int64_t)g.what * p.stride + r] = make_float2(top, sum);
+  }
+};
+
+// Joins a row's statistics in the order of the vocabulary: eight threads a row,
+// then those eight; then the mean over the rows (fp64, fixed order) by the CTA
+// that finishes last.
+__global__ void __launch_bounds__(kJoinThreads)
+join_kernel(const float2* stats, int64_t stride, int v_tiles,
+            const float* label_logit, const int32_t* row_token,
+            const int32_t* n_rows, float* lse2, float* token_loss, float* loss,
+            const float* scale, float* coef, double* block_sums,
+            uint32_t* ticket) {
+  __shared__ double sh_loss[kJoinRows];
+  __shared__ uint32_t last;
+  const int part = threadIdx.x & 7, i = threadIdx.x >> 3;
+  const int r = blockIdx.x * kJoinRows + i;
+  after_prior_launch();
+  const int rows = *n_rows;
+  float top = -INFINITY, sum = 0.f;
+  if (r < rows) {
+    const int a = v_tiles * part / 8, b = v_tiles * (part + 1) / 8;
+    for (int k = a; k < b; ++k) {
+      const float2 s = stats[(int64_t)k * stride + r];
+      const float m = fmaxf(top, s.x);
+      const float at = m == -INFINITY ? 0.f : m;
+      sum = sum * exp2_fast(top - at) + s.y * exp2_fast(s.x - at);
+      top = m;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    const float ot = __shfl_xor_sync(0xffffffffu, top, o);
+    const float os = __shfl_xor_sync(0xffffffffu, sum, o);
+    const float m = fmaxf(top, ot);
+    const float at = m == -INFINITY ? 0.f : m;
+    sum = sum * exp2_fast(top - at) + os * exp2_fast(ot - at);
+    top = m;
+  }
+  if (part == 0) {
+    float l = 0.f;
+    if (r < rows) {
+      const float lg = log2f(sum);
+      lse2[r] = top + lg;
+      l = (lg - fmaf(label_logit[r], kLog2e, -top)) * kLn2;
+      if (token_loss) token_loss[row_token[r]] = l;
+    }
+    sh_loss[i] = l;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+    for (int k = 0; k < kJoinRows; ++k) s += sh_loss[k];
+    block_sums[blockIdx.x] = s;
+    last = atom_add_acq_rel(ticket, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (last && threadIdx.x < 32) {
+    double s = 0.0;
+    for (unsigned k = threadIdx.x; k < gridDim.x; k += 32)
+      s += *reinterpret_cast<const volatile double*>(block_sums + k);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (threadIdx.x == 0) {
+      *loss = (float)(rows ? s / rows : 0.0);
+      *coef = rows ? (scale ? *scale : 1.f) / (float)rows : 0.f;
+      *ticket = 0;
+    }
+  }
+}
+
+// ---- the logits' gradient ---------------------------------------------------
+struct DlogitsParams {
+  CUtensorMap hidden, weight;
+  const int32_t* n_rows;
+  const int32_t* labels;
+  const float* lse2;
+  const float* coef;
+  __nv_bfloat16* out;     // [rows in whole tiles][stride], the piece's columns
+  uint32_t* status;
+  int64_t stride;
+  int v_tiles, vocab, v0, k_blocks;
+};
+
+struct DlogitsWork {
+  typedef DlogitsParams Params;
+  typedef RowsState State;
+  static constexpr bool kBf16 = true;
+  static __device__ __forceinline__ State start(const Params& p) {
+    State s;
+    s.rows = *p.n_rows;
+    s.m_tiles = s.rows ? (s.rows + kTileM - 1) / kTileM : 1;
+    s.n_tiles = s.m_tiles * p.v_tiles;
+    return s;
+  }
+  static __device__ __forceinline__ GemmTile tile(const Params& p,
+                                                  const State& s, int t) {
+    GemmTile g;
+    g.a = &p.hidden;
+    g.b = &p.weight;
+    g.a0 = (t % s.m_tiles) * kTileM;
+    g.what = (t / s.m_tiles) * kTileN;     // column inside the piece
+    g.b0 = p.v0 + g.what;
+    g.k0 = 0;
+    g.kn = p.k_blocks;
+    g.b_k = 0;
+    g.a_mn = g.b_mn = false;
+    g.aux = 0;
+    return g;
+  }
+  // Rows past the last and columns past the vocabulary are zeros: the products
+  // run over whole tiles.
+  static __device__ __forceinline__ void epilogue(const Params& p,
+                                                  const State& s,
+                                                  const GemmTile& g,
+                                                  uint32_t acc, int row) {
+    const int r = g.a0 + row;
+    const bool real = r < s.rows;
+    const int label = real ? p.labels[r] : -1;
+    const float l2 = real ? p.lse2[r] : 0.f;
+    const float coef = *p.coef;
+    __nv_bfloat16* out = p.out + (int64_t)r * p.stride + g.what;
+    for (int c = 0; c < kTileN / 32; ++c) {
+      const int v = g.b0 + c * 32;
+      float x[32];
+      tmem_ld32(acc + c * 32, x);
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        x[i] = exp2_fast(fmaf(x[i], kLog2e, -l2));
+      if (label >= v && label < v + 32) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (label == v + i) x[i] -= 1.f;
+      }
+      uint32_t y[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const bool a = real && v + 2 * i < p.vocab;
+        const bool b = real && v + 2 * i + 1 < p.vocab;
+        const __nv_bfloat162 h = __floats2bfloat162_rn(
+            a ? x[2 * i] * coef : 0.f, b ? x[2 * i + 1] * coef : 0.f);
+        y[i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      uint4* to = reinterpret_cast<uint4*>(out + c * 32);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        to[i] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+    }
+  }
+};
+
+// ---- the gradients of W and h ------------------------------------------------
+struct GradsParams {
+  CUtensorMap dl_rows;    // dlogits, K-major (K: the piece's columns)
+  CUtensorMap dl_cols;    // dlogits, MN-major (K: tokens)
+  CUtensorMap hidden;     // MN-major
+  CUtensorMap weight;     // MN-major
+  void* grad_weight;
+  __nv_bfloat16* grad_hidden;
+  float* slabs;           // [split][rows][width], or NULL: one sum, written out
+  const int32_t* n_rows;
+  const int32_t* row_token;
+  uint32_t* status;
+  int64_t weight_stride, hidden_stride;
+  int64_t slab;           // elements of a slab
+  int w_tiles;            // tiles of dW (taken first)
+  int d_tiles;            // column tiles of the width
+  int width, vocab, v0, piece;
+  int k_piece, splits;    // blocks of K of dh, parts that they are cut into
+  int weight_f32, accumulate, add_slab, weight_vec, hidden_vec;
+};
+
+template <bool kF32>
+__device__ __forceinline__ void store_row(void* base, int64_t at,
+                                          const float (&x)[32], int cols,
+                                          bool add, bool vec) {
+  float* f = reinterpret_cast<float*>(base) + at;
+  __nv_bfloat16* h = reinterpret_cast<__nv_bfloat16*>(base) + at;
+  if (vec && cols >= 32) {
+    if (kF32) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        float4 v = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        float4* to = reinterpret_cast<float4*>(f + i);
+        if (add) {
+          const float4 o = *to;
+          v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        }
+        *to = v;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        uint4* to = reinterpret_cast<uint4*>(h + i);
+        uint4 o = make_uint4(0, 0, 0, 0);
+        if (add) o = *to;
+        const uint32_t* ow = reinterpret_cast<const uint32_t*>(&o);
+        uint32_t y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(
+              x[i + 2 * j] + __uint_as_float(ow[j] << 16),
+              x[i + 2 * j + 1] + __uint_as_float(ow[j] & 0xffff0000u));
+          y[j] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        *to = make_uint4(y[0], y[1], y[2], y[3]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if (i < cols) {
+        if (kF32)
+          f[i] = add ? f[i] + x[i] : x[i];
+        else
+          h[i] = __float2bfloat16_rn(add ? __bfloat162float(h[i]) + x[i]
+                                         : x[i]);
+      }
+    }
+  }
+}
+
+struct GradsState {
+  int n_tiles, rows, k_rows;
+};
+
+struct GradsWork {
+  typedef GradsParams Params;
+  typedef GradsState State;
+  static constexpr bool kBf16 = true;
+  static __device__ __forceinline__ State start(const Params& p) {
+    State s;
+    s.rows = *p.n_rows;
+    s.k_rows = s.rows ? (s.rows + kTileK - 1) / kTileK : 1;   // of zeros
+    s.n_tiles = p.w_tiles +
+                (s.rows + kTileM - 1) / kTileM * p.d_tiles * p.splits;
+    return s;
+  }
+  static __device__ __forceinline__ GemmTile tile(const Params& p,
+                                                  const State& s, int t) {
+    GemmTile g;
+    if (t < p.w_tiles) {
+      g.what = 0;
+      g.aux = 0;
+      g.a = &p.dl_cols;
+      g.b = &p.hidden;
+      g.a0 = t / p.d_tiles * kTileM;
+      g.b0 = t % p.d_tiles * kTileN;
+      g.k0 = 0;
+      g.kn = s.k_rows;
+      g.b_k = 0;
+      g.a_mn = g.b_mn = true;
+    } else {
+      t -= p.w_tiles;
+      g.what = 1;
+      g.aux = t % p.splits;
+      t /= p.splits;
+      g.a = &p.dl_rows;
+      g.b = &p.weight;
+      g.a0 = t / p.d_tiles * kTileM;
+      g.b0 = t % p.d_tiles * kTileN;
+      g.k0 = (int)((int64_t)p.k_piece * g.aux / p.splits);
+      g.kn = (int)((int64_t)p.k_piece * (g.aux + 1) / p.splits) - g.k0;
+      g.b_k = p.v0;      // W's rows are the whole vocabulary's
+      g.a_mn = false;
+      g.b_mn = true;
+    }
+    return g;
+  }
+  static __device__ __forceinline__ void epilogue(const Params& p,
+                                                  const State& s,
+                                                  const GemmTile& g,
+                                                  uint32_t acc, int row) {
+    const int r = g.a0 + row;
+    const bool in = g.what ? r < s.rows : r < p.piece && p.v0 + r < p.vocab;
+    for (int c = 0; c < kTileN / 32; ++c) {
+      const int d = g.b0 + c * 32;
+      if (d >= p.width) break;
+      float x[32];
+      tmem_ld32(acc + c * 32, x);
+      if (!in) continue;
+      const int cols = p.width - d;
+      if (g.what == 0) {
+        const int64_t at = (int64_t)(p.v0 + r) * p.weight_stride + d;
+        if (p.weight_f32)
+          store_row<true>(p.grad_weight, at, x, cols, p.accumulate,
+                           p.weight_vec);
+        else
+          store_row<false>(p.grad_weight, at, x, cols, p.accumulate,
+                           p.weight_vec);
+      } else if (p.slabs) {
+        store_row<true>(p.slabs,
+                        g.aux * p.slab + (int64_t)r * p.width + d, x, cols,
+                        p.add_slab, p.width % 4 == 0);
+      } else {
+        store_row<false>(p.grad_hidden,
+                         (int64_t)p.row_token[r] * p.hidden_stride + d, x,
+                         cols, false, p.hidden_vec);
+      }
+    }
+  }
+};
+
+// dh from its partial sums: a warp a row.
+__global__ void __launch_bounds__(256)
+slabs_kernel(const float* slabs, int count, int64_t slab, int width,
+             const int32_t* n_rows, const int32_t* row_token,
+             __nv_bfloat16* out, int64_t stride) {
+  after_prior_launch();
+  const int rows = *n_rows, lane = threadIdx.x & 31;
+  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows;
+       r += gridDim.x * 8) {
+    __nv_bfloat16* to = out + (int64_t)row_token[r] * stride;
+    for (int d = lane; d < width; d += 32) {
+      float s = 0.f;
+      for (int k = 0; k < count; ++k)
+        s += slabs[k * slab + (int64_t)r * width + d];
+      to[d] = __float2bfloat16_rn(s);
+    }
+  }
+}
+
+// Rows of a bf16 matrix that no tensor map can read, on 16-byte boundaries.
+__global__ void __launch_bounds__(256)
+rows_copy_kernel(const __nv_bfloat16* in, int64_t in_stride, int64_t rows,
+                 int width, __nv_bfloat16* out, int64_t out_stride) {
+  const int64_t n = rows * width;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
+       i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / width;
+    out[r * out_stride + (i - r * width)] = in[r * in_stride + (i - r * width)];
+  }
+}
+
+__global__ void __launch_bounds__(256)
+clear_rows_kernel(void* base, int f32, int64_t rows, int width,
+                  int64_t stride) {
+  const int64_t n = rows * width;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
+       i += (int64_t)gridDim.x * 256) {
+    const int64_t at = i / width * stride + i % width;
+    if (f32) reinterpret_cast<float*>(base)[at] = 0.f;
+    else reinterpret_cast<__nv_bfloat16*>(base)[at] = __float2bfloat16_rn(0.f);
+  }
+}
+
+template <class Work>
+cudaError_t launch_gemm(const typename Work::Params& p, int64_t most_tiles,
+                        int sms, cudaStream_t stream) {
+  const int grid = (int)std::min<int64_t>(most_tiles, sms);
+  gemm_kernel<Work><<<grid, kGemmThreads, kGemmSmem, stream>>>(p);
+  return cudaGetLastError();
+}
+
+template <class Work>
+cudaError_t allow_smem() {
+  return cudaFuncSetAttribute(gemm_kernel<Work>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)kGemmSmem);
+}
+
+int grid_for(int64_t n, int sms) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(lm_ceil_div(n, 256),
+                                                     (int64_t)sms * 8));
+}
+
+// The rows that have a label, and W as a tensor map can read it.
+struct HeadInputs {
+  const __nv_bfloat16* weight;
+  int64_t weight_stride;
+  int64_t pitch;        // of the gathered rows
+};
+
+cudaError_t head_inputs(const lamb_vocab* v, const void* hidden, int64_t hs,
+                        const void* weight, int64_t ws, const int64_t* labels,
+                        int64_t n, float* token_loss, void* grad_hidden,
+                        int64_t gs, cudaStream_t stream, HeadInputs* in) {
+  in->pitch = lm_round_up(v->width, 8);
+  in->weight = (const __nv_bfloat16*)weight;
+  in->weight_stride = ws;
+  const bool vec = lm_mappable(hidden, hs) && v->width % 8 == 0 &&
+                   (!grad_hidden || lm_mappable(grad_hidden, gs));
+  const unsigned grid = (unsigned)lm_ceil_div(n, kPickRows);
+  if (vec)
+    pick_kernel<true><<<grid, kPickThreads, 0, stream>>>(
+        (const __nv_bfloat16*)hidden, hs, labels, (int)n, v->vocab, v->width,
+        v->rows, in->pitch, v->row_label, v->row_token, v->n_rows, token_loss,
+        (__nv_bfloat16*)grad_hidden, gs, v->status);
+  else
+    pick_kernel<false><<<grid, kPickThreads, 0, stream>>>(
+        (const __nv_bfloat16*)hidden, hs, labels, (int)n, v->vocab, v->width,
+        v->rows, in->pitch, v->row_label, v->row_token, v->n_rows, token_loss,
+        (__nv_bfloat16*)grad_hidden, gs, v->status);
+  if (!lm_mappable(weight, ws)) {
+    rows_copy_kernel<<<grid_for(v->vocab * v->width, v->sms), 256, 0, stream>>>(
+        in->weight, ws, v->vocab, v->width, v->weight_copy, in->pitch);
+    in->weight = v->weight_copy;
+    in->weight_stride = in->pitch;
+  }
+  return cudaGetLastError();
+}
+
+lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
+                        const float* scale, float* token_loss, float* loss,
+                        cudaStream_t stream) {
+  StatsParams p;
+  if (!lm_map(v->encode, &p.hidden, true, v->rows, lm_round_up(n, kTileM),
+              v->width, in.pitch, kTileM) ||
+      !lm_map(v->encode, &p.weight, true, in.weight, v->vocab, v->width,
+              in.weight_stride, kTileM))
+    return lm_fail(LAMB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+  p.n_rows = v->n_rows;
+  p.labels = v->row_label;
+  p.stats = v->stats;
+  p.label_logit = v->label_logit;
+  p.status = v->status;
+  p.stride = v->max_tokens;
+  p.v_tiles = (int)lm_ceil_div(v->vocab, kTileN);
+  p.vocab = (int)v->vocab;
+  p.k_blocks = (int)lm_ceil_div(v->width, kTileK);
+  cudaError_t e = launch_gemm<StatsWork>(
+      p, lm_ceil_div(n, kTileM) * p.v_tiles, v->sms, stream);
+  if (e != cudaSuccess) return lm_cuda_fail(e, "head loss launch");
+  join_kernel<<<(unsigned)lm_ceil_div(n, kJoinRows), kJoinThreads, 0, stream>>>(
+      v->stats, v->max_tokens, p.v_tiles, v->label_logit, v->row_token,
+      v->n_rows, v->lse2, token_loss, loss, scale, v->coef, v->block_sums,
+      v->ticket);
+  e = cudaGetLastError();
+  return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "head join launch");
+}
+
+lamb_status_t check_head(const lamb_vocab* v, const void* hidden, int64_t hs,
+                         const void* weight, int64_t ws, const int64_t* labels,
+                         int64_t n, const float* loss) {
+  if (!v) return lm_fail(LAMB_ERR_INVALID_ARG, "plan is NULL");
+  if (n < 0 || n > v->max_tokens)
+    return lm_fail(LAMB_ERR_INVALID_ARG,
+                   "n_tokens %lld is not in [0, max_tokens = %lld]",
+                   (long long)n, (long long)v->max_tokens);
+  if (!weight || !loss || (n && (!hidden || !labels)))
+    return lm_fail(LAMB_ERR_INVALID_ARG,
+                   "hidden, weight, labels and loss are required");
+  if (hs < v->width || ws < v->width)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "a row stride is below the width %d",
+                   v->width);
+  if ((uintptr_t)hidden % 2 || (uintptr_t)weight % 2 || (uintptr_t)loss % 4 ||
+      (uintptr_t)labels % 8)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "a pointer is not aligned");
+  return LAMB_OK;
+}
+
+}  // namespace
+
+int lm_head_setup() {
+  cudaError_t e = allow_smem<StatsWork>();
+  if (e == cudaSuccess) e = allow_smem<DlogitsWork>();
+  if (e == cudaSuccess) e = allow_smem<GradsWork>();
+  return (int)e;
+}
+
+void lm_head_carve(lamb_vocab* v, LmArena* a) {
+  const int64_t n = v->max_tokens, pitch = lm_round_up(v->width, 8);
+  const int64_t whole = lm_round_up(n, kTileM);
+  a->take(&v->rows, whole * pitch);
+  a->take(&v->row_label, n);
+  a->take(&v->row_token, n);
+  a->take(&v->n_rows, 1);
+  a->take(&v->stats, lm_ceil_div(v->vocab, kTileN) * n);
+  a->take(&v->label_logit, n);
+  a->take(&v->lse2, n);
+  a->take(&v->block_sums, lm_ceil_div(n, kJoinRows));
+  a->take(&v->ticket, 1);
+  a->take(&v->coef, 1);
+  // a whole vocabulary where that is small, else kPieceElems
+  v->dlogits_elems = std::min(whole * lm_round_up(v->vocab, kTileN),
+                              std::max(kPieceElems, whole * (int64_t)kTileN));
+  a->take(&v->dlogits, v->dlogits_elems);
+  // parts of dh never have more tiles than there are SMs, unless it is one part
+  a->take(&v->slabs, std::max(n * v->width,
+                              (int64_t)v->sms * kTileM * kTileN));
+  a->take(&v->weight_copy, v->vocab * pitch);
+}
+
+}  // namespace lamb
+
+using namespace lamb;
+
+extern "C" lamb_status_t lamb_vocab_loss(
+    struct lamb_vocab* v, const void* hidden, int64_t hidden_stride,
+    const void* weight, int64_t weight_stride, const int64_t* labels,
+    int64_t n_tokens, float* token_loss, float* loss, cudaStream_t stream) {
+  lamb_status_t st = check_head(v, hidden, hidden_stride, weight, weight_stride,
+                                labels, n_tokens, loss);
+  if (st != LAMB_OK) return st;
+  LmDevice dev(v->device);
+  if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");
+  if (!n_tokens) {
+    const cudaError_t e = cudaMemsetAsync(loss, 0, sizeof(float), stream);
+    return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "clearing the loss");
+  }
+  HeadInputs in;
+  const cudaError_t e = head_inputs(v, hidden, hidden_stride, weight,
+                                    weight_stride, labels, n_tokens, token_loss,
+                                    nullptr, 0, stream, &in);
+  if (e != cudaSuccess) return lm_cuda_fail(e, "head copy launch");
+  return head_loss(v, in, n_tokens, nullptr, token_loss, loss, stream);
+}
+
+extern "C" lamb_status_t lamb_vocab_loss_grad(
+    struct lamb_vocab* v, const void* hidden, int64_t hidden_stride,
+    const void* weight, int64_t weight_stride, const int64_t* labels,
+    int64_t n_tokens, const float* d_scale, float* token_loss, float* loss,
+    void* grad_hidden, int64_t grad_hidden_stride, void* grad_weight,
+    int32_t grad_weight_dtype, int64_t grad_weight_stride, int32_t accumulate,
+    cudaStream_t stream) {
+  lamb_status_t st = check_head(v, hidden, hidden_stride, weight, weight_stride,
+                                labels, n_tokens, loss);
+  if (st != LAMB_OK) return st;
+  const int64_t n = n_tokens;
+  if (grad_weight_dtype != LAMB_F32 && grad_weight_dtype != LAMB_BF16)
+    return lm_fail(LAMB_ERR_UNSUPPORTED_DTYPE, "grad_weight: dtype %d unsupported",
+                   grad_weight_dtype);
+  if (!grad_weight || (n && !grad_hidden))
+    return lm_fail(LAMB_ERR_INVALID_ARG,
+                   "grad_hidden and grad_weight are required");
+  if (grad_hidden_stride < v->width || grad_weight_stride < v->width)
+    return lm_fail(LAMB_ERR_INVALID_ARG,
+                   "a gradient's row stride is below the width %d", v->width);
+  const bool f32 = grad_weight_dtype == LAMB_F32;
+  if ((uintptr_t)grad_hidden % 2 || (uintptr_t)grad_weight % (f32 ? 4 : 2))
+    return lm_fail(LAMB_ERR_INVALID_ARG, "a gradient's pointer is not aligned");
+  LmDevice dev(v->device);
+  if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");
+  cudaError_t e;
+  if (!n) {
+    e = cudaMemsetAsync(loss, 0, sizeof(float), stream);
+    if (e == cudaSuccess && !accumulate) {
+      clear_rows_kernel<<<grid_for(v->vocab * v->width, v->sms), 256, 0,
+                          stream>>>(grad_weight, f32, v->vocab, v->width,
+                                    grad_weight_stride);
+      e = cudaGetLastError();
+    }
+    return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "clearing the gradient");
+  }
+  HeadInputs in;
+  e = head_inputs(v, hidden, hidden_stride, weight, weight_stride, labels, n,
+                  token_loss, grad_hidden, grad_hidden_stride, stream, &in);
+  if (e != cudaSuccess) return lm_cuda_fail(e, "head copy launch");
+  st = head_loss(v, in, n, d_scale, token_loss, loss, stream);
+  if (st != LAMB_OK) return st;
+
+  // pieces of the vocabulary, of equal widths in whole tiles
+  const int64_t whole = lm_round_up(n, kTileM);
+  const int64_t most = v->dlogits_elems / whole / kTileN * kTileN;
+  const int64_t pieces = lm_ceil_div(v->vocab, most);
+  const int64_t piece =
+      lm_round_up(lm_ceil_div(v->vocab, pieces), kTileN);
+
+  DlogitsParams d;
+  GradsParams g;
+  const bool ok =
+      lm_map(v->encode, &d.hidden, true, v->rows, whole, v->width, in.pitch,
+             kTileM) &&
+      lm_map(v->encode, &d.weight, true, in.weight, v->vocab, v->width,
+             in.weight_stride, kTileM) &&
+      lm_map(v->encode, &g.hidden, true, v->rows, whole, v->width, in.pitch,
+             kTileK) &&
+      lm_map(v->encode, &g.weight, true, in.weight, v->vocab, v->width,
+             in.weight_stride, kTileK) &&
+      lm_map(v->encode, &g.dl_rows, true, v->dlogits, whole, piece, piece,
+             kTileM) &&
+      lm_map(v->encode, &g.dl_cols, true, v->dlogits, whole, piece, piece,
+             kTileK);
+  if (!ok) return lm_fail(LAMB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+  const int m_tiles = (int)(whole / kTileM);
+  d.n_rows = v->n_rows;
+  d.labels = v->row_label;
+  d.lse2 = v->lse2;
+  d.coef = v->coef;
+  d.out = v->dlogits;
+  d.status = v->status;
+  d.stride = piece;
+  d.vocab = (int)v->vocab;
+  d.k_blocks = (int)lm_ceil_div(v->width, kTileK);
+
+  g.d_tiles = (int)lm_ceil_div(v->width, kTileN);
+  const int h_tiles = m_tiles * g.d_tiles;
+  g.grad_weight = grad_weight;
+  g.weight_stride = grad_weight_stride;
+  g.grad_hidden = (__nv_bfloat16*)grad_hidden;
+  g.hidden_stride = grad_hidden_stride;
+  g.status = v->status;
+  g.n_rows = v->n_rows;
+  g.row_token = v->row_token;
+  g.slab = n * v->width;
+  g.width = v->width;
+  g.vocab = (int)v->vocab;
+  g.piece = (int)piece;
+  g.weight_f32 = f32;
+  g.accumulate = accumulate != 0;
+  g.weight_vec = (uintptr_t)grad_weight % 16 == 0 &&
+                 grad_weight_stride % (f32 ? 4 : 8) == 0;
+  g.hidden_vec =
+      (uintptr_t)grad_hidden % 16 == 0 && grad_hidden_stride % 8 == 0;
+  // dh of few tokens is few tiles over a long K: cut K so that every SM has one
+  const int k_first = (int)lm_ceil_div(std::min(piece, v->vocab), kTileK);
+  g.splits = std::max(1, std::min(v->sms / h_tiles, k_first / kMinPartBlocks));
+  g.slabs = pieces > 1 || g.splits > 1 ? v->slabs : nullptr;
+  for (int64_t i = 0; i < pieces; ++i) {
+    const int64_t v0 = i * piece, cols = std::min(piece, v->vocab - v0);
+    d.v0 = g.v0 = (int)v0;
+    d.v_tiles = (int)lm_ceil_div(cols, kTileN);
+    e = launch_gemm<DlogitsWork>(d, (int64_t)m_tiles * d.v_tiles, v->sms,
+                                 stream);
+    if (e != cudaSuccess) return lm_cuda_fail(e, "logit gradient launch");
+    g.w_tiles = (int)lm_ceil_div(cols, kTileM) * g.d_tiles;
+    g.k_piece = (int)lm_ceil_div(cols, kTileK);
+    // the last piece may be short: fewer parts, the others' sums stay
+    const int parts = std::min(g.splits, g.k_piece);
+    GradsParams gi = g;
+    gi.splits = parts;
+    gi.add_slab = i > 0;
+    e = launch_gemm<GradsWork>(gi, g.w_tiles + (int64_t)h_tiles * parts,
+                               v->sms, stream);
+    if (e != cudaSuccess) return lm_cuda_fail(e, "head gradient launch");
+  }
+  if (g.slabs) {
+    slabs_kernel<<<grid_for(n * 32, v->sms), 256, 0, stream>>>(
+        v->slabs, g.splits, g.slab, v->width, v->n_rows, v->row_token,
+        (__nv_bfloat16*)grad_hidden, grad_hidden_stride);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return lm_cuda_fail(e, "hidden gradient launch");
+  }
+  return LAMB_OK;
+}
+
+// ---------------------------------------------------------------------------
+// The plan
+// ---------------------------------------------------------------------------
+extern "C" lamb_status_t lamb_vocab_create(int64_t vocab, int32_t width,
+                                           int64_t max_tokens, int32_t device,
+                                           struct lamb_vocab** out) {
+  if (!out) return lm_fail(LAMB_ERR_INVALID_ARG, "out is NULL");
+  *out = nullptr;
+  if (vocab < 1 || vocab > (1ll << 30))
+    return lm_fail(LAMB_ERR_INVALID_ARG, "vocab is not in [1, 2^30]");
+  if (width < 1 || width > (1 << 20))
+    return lm_fail(LAMB_ERR_INVALID_ARG, "width is not in [1, 2^20]");
+  if (max_tokens < 1 || max_tokens > (1ll << 24))
+    return lm_fail(LAMB_ERR_INVALID_ARG, "max_tokens is not in [1, 2^24]");
+  if (device < 0) return lm_fail(LAMB_ERR_INVALID_ARG, "device < 0");
+  LmDevice dev(device);
+  if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");
+  lamb_vocab* v = new (std::nothrow) lamb_vocab;
+  if (!v) return lm_fail(LAMB_ERR_OOM, "host allocation failed");
+  v->device = device;
+  v->vocab = vocab;
+  v->width = width;
+  v->max_tokens = max_tokens;
+  v->encode = lm_encoder();
+  cudaError_t e =
+      cudaDeviceGetAttribute(&v->sms, cudaDevAttrMultiProcessorCount, device);
+  if (e == cudaSuccess && !v->encode) {
+    delete v;
+    return lm_fail(LAMB_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+  }
+  if (e == cudaSuccess) e = (cudaError_t)lm_head_setup();
+  LmArena a;
+  for (int pass = 0; e == cudaSuccess && pass < 2; ++pass) {
+    a.used = 0;
+    a.take(&v->status, 1);
+    lm_head_carve(v, &a);
+    lm_embed_carve(v, &a);
+    if (pass == 0) {
+      e = cudaMalloc(&v->arena, a.used);
+      a.base = (char*)v->arena;
+    }
+  }
+  if (e == cudaSuccess) e = cudaMemset(v->status, 0, sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaMemset(v->ticket, 0, sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) {
+    if (v->arena) cudaFree(v->arena);
+    delete v;
+    return lm_cuda_fail(e, "vocabulary plan");
+  }
+  *out = v;
+  return LAMB_OK;
+}
+
+extern "C" lamb_status_t lamb_vocab_query(struct lamb_vocab* v,
+                                          uint32_t* status_bits, int32_t clear,
+                                          cudaStream_t stream) {
+  if (!v) return lm_fail(LAMB_ERR_INVALID_ARG, "plan is NULL");
+  if (!status_bits)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "status_bits is NULL");
+  LmDevice dev(v->device);
+  cudaError_t e = dev.err;
+  if (e == cudaSuccess)
+    e = cudaMemcpyAsync(status_bits, v->status, sizeof(uint32_t),
+                        cudaMemcpyDeviceToHost, stream);
+  if (e == cudaSuccess && clear)
+    e = cudaMemsetAsync(v->status, 0, sizeof(uint32_t), stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+  return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "status query");
+}
+
+extern "C" lamb_status_t lamb_vocab_destroy(struct lamb_vocab* v) {
+  if (!v) return LAMB_OK;
+  LmDevice dev(v->device);
+  cudaError_t e = dev.err;
+  if (e == cudaSuccess) e = cudaFree(v->arena);
+  delete v;
+  return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "cudaFree(plan)");
+}

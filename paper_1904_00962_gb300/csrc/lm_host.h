@@ -1,0 +1,106 @@
+// Host helpers of the language-model operators: errors, the device guard, and
+// tensor maps.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdarg.h>
+#include <stdint.h>
+#include <stdio.h>
+
+#include "lamb.h"
+#include "lamb_internal.h"
+
+namespace lamb {
+
+inline lamb_status_t lm_fail(lamb_status_t st, const char* fmt, ...) {
+  char msg[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(msg, sizeof(msg), fmt, ap);
+  va_end(ap);
+  set_last_error(msg);
+  return st;
+}
+
+inline lamb_status_t lm_cuda_fail(cudaError_t e, const char* what) {
+  return lm_fail(e == cudaErrorMemoryAllocation ? LAMB_ERR_OOM : LAMB_ERR_CUDA,
+                 "%s: %s (%d)", what, cudaGetErrorString(e), (int)e);
+}
+
+// Makes a device current for a scope.
+struct LmDevice {
+  int prev = -1;
+  cudaError_t err;
+  explicit LmDevice(int dev) {
+    err = cudaGetDevice(&prev);
+    if (err == cudaSuccess && prev != dev) {
+      err = cudaSetDevice(dev);
+    } else {
+      prev = -1;
+    }
+  }
+  ~LmDevice() {
+    if (prev >= 0) cudaSetDevice(prev);
+  }
+};
+
+constexpr int64_t lm_round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+constexpr int64_t lm_ceil_div(int64_t x, int64_t a) { return (x + a - 1) / a; }
+
+// Pieces of one device allocation, each on a 1024-byte boundary.
+struct LmArena {
+  char* base = nullptr;
+  size_t used = 0;
+  template <class T>
+  void take(T** p, int64_t n) {
+    *p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+    used += (size_t)lm_round_up(n * (int64_t)sizeof(T), 1024);
+  }
+};
+
+inline int lm_elem_size(int dtype) { return dtype == LAMB_F32 ? 4 : 2; }
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
+                                void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*,
+                                CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion,
+                                CUtensorMapFloatOOBfill);
+
+// The driver's encoder; NULL if the driver has none.
+inline EncodeTiled lm_encoder() {
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000,
+                                       cudaEnableDefault, &found) !=
+          cudaSuccess ||
+      found != cudaDriverEntryPointSuccess) {
+    return nullptr;
+  }
+  return reinterpret_cast<EncodeTiled>(fn);
+}
+
+// A 16-bit matrix of `rows` lines of `cols` elements, row_stride elements apart
+// (a multiple of 8, the base on 16 bytes), copied in boxes of 64 columns by
+// box_rows lines.
+inline bool lm_map(EncodeTiled encode, CUtensorMap* map, bool bf16,
+                   const void* base, int64_t rows, int64_t cols,
+                   int64_t row_stride, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)row_stride * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  const cuuint32_t step[2] = {1, 1};
+  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                          : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                2, const_cast<void*>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Whether a 16-bit matrix can be copied by a tensor map where it lies.
+inline bool lm_mappable(const void* p, int64_t row_stride) {
+  return ((uintptr_t)p & 15) == 0 && row_stride % 8 == 0;
+}
+
+}  // namespace lamb

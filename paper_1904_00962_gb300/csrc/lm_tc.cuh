@@ -1,0 +1,127 @@
+// PTX of the tensor-core products (lm_gemm.cuh): tensor copies, matrix
+// descriptors, tcgen05 products with accumulators in tensor memory, and waits
+// that give up.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "lamb_sync.cuh"
+
+namespace lamb {
+namespace {
+
+// ---- bounded waits ----------------------------------------------------------
+// A wait of a product's CTA for its own copies, products or readers ends within
+// microseconds.  One that lasts kWaitLimitNs sets the CTA's flag and the status
+// word, and every role leaves its loop.
+constexpr uint64_t kWaitLimitNs = 2000000000ull;
+
+__device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity,
+                                             volatile int* gave_up,
+                                             uint32_t* status, uint32_t bit) {
+  if (mbar_try(bar, parity)) return true;
+  const uint64_t begin = global_ns();
+  while (!mbar_try(bar, parity)) {
+    if (*gave_up) return false;
+    if (global_ns() - begin > kWaitLimitNs) {
+      *gave_up = 1;
+      atomicOr(status, bit);
+      return false;
+    }
+  }
+  return true;
+}
+
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok));
+  return ok != 0;
+}
+
+// ---- tensor copies ----------------------------------------------------------
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+__device__ __forceinline__ void tile_load(uint32_t smem, const CUtensorMap* map,
+                                          int x, int y, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile"
+      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+      : "memory");
+}
+
+// ---- products ---------------------------------------------------------------
+// Descriptor of a shared-memory operand in the 128-byte swizzle (start address
+// added later, all in units of 16 bytes).  K-major: rows of 64 elements (128
+// bytes), eight rows to a swizzle pattern of 1024 bytes.  MN-major: blocks of 64
+// rows of the operand by 64 of K, a line of 128 bytes for each k; the next 64
+// rows are a block (8192 bytes) on, the next eight k 1024 bytes.
+__device__ __forceinline__ uint64_t operand_desc(bool mn_major) {
+  const uint64_t lbo = mn_major ? 8192 >> 4 : 1;
+  const uint64_t sbo = 1024 >> 4;
+  return (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
+}
+// 16 elements further along K.
+__device__ __forceinline__ uint32_t operand_step(bool mn_major) {
+  return (mn_major ? 16 * 128 : 32) >> 4;
+}
+// Accumulators in fp32; the operands both bf16 or both fp16.
+__device__ __forceinline__ uint32_t product_desc(bool bf16, bool a_mn,
+                                                 bool b_mn, int m, int n) {
+  const uint32_t f = bf16 ? 1u : 0u;
+  return (1u << 4) | (f << 7) | (f << 10) | ((a_mn ? 1u : 0u) << 15) |
+         ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void product(uint32_t tmem, uint64_t a, uint64_t b,
+                                        uint32_t desc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+      : "memory");
+}
+// Arrives at the barrier once the products issued so far are complete.
+__device__ __forceinline__ void products_arrive(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 "
+      "[%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tmem_before_sync() {
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_after_sync() {
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+
+// 32 consecutive columns of the warp's 32 lanes: lane i gets its row's values.
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&x)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, "
+      "%30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(addr) : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+
+}  // namespace
+}  // namespace lamb
