@@ -714,6 +714,84 @@ LAMB_API lamb_status_t lamb_vocab_query(struct lamb_vocab* plan,
 /* Frees the plan (synchronises its device); NULL is a no-op. */
 LAMB_API lamb_status_t lamb_vocab_destroy(struct lamb_vocab* plan);
 
+/* ---------------------------------------------------------------------------
+ * Orthogonalised (Muon) update of matrices, for the two-dimensional parameters
+ * of a model whose other tensors a plan steps on.  Per matrix:
+ *     m <- momentum m + (1 - momentum) g
+ *     u  = (1 - momentum) g + momentum m   with NESTEROV, else m
+ *     X  = u / (||u||_F + eps); `steps` times: G = X X^T,
+ *          X <- a X + (b G + c G G) X
+ *     w <- (1 - eta lambda_k) w - eta s X
+ * s is update_scale times 1, sqrt(max(1, rows / cols)) or 0.2 sqrt(max(rows,
+ * cols)).  The products take 16-bit operands (11 significant bits, the large
+ * terms apart in 32): X is within about 1e-3 of the exact one in the Frobenius
+ * norm.  Sums of squares of u are formed in fp32: entries beyond 1e19 in size
+ * make a norm infinite (LAMB_STATUS_NONFINITE), those below 1e-20 count as 0.
+ * The same bits in every run.
+ * ------------------------------------------------------------------------- */
+#define LAMB_MUON_SCALE_ONE 0
+#define LAMB_MUON_SCALE_SPECTRAL 1   /* sqrt(max(1, rows / cols))            */
+#define LAMB_MUON_SCALE_RMS 2        /* 0.2 sqrt(max(rows, cols)): the size of
+                                        an Adam or LAMB step per element     */
+#define LAMB_MUON_FLAG_NESTEROV 0x1u
+
+typedef struct {
+  double momentum;       /* in [0, 1)                                        */
+  double weight_decay;   /* lambda >= 0, decoupled; where the mask is 1       */
+  double eps;            /* >= 0                                             */
+  double a, b, c;        /* of the odd polynomial, up to 16 in size; the usual
+                            ones are 3.4445, -4.7750, 2.0315                 */
+  double update_scale;
+  int32_t steps;         /* 1 .. 64, usually 5                               */
+  int32_t scale_kind;    /* LAMB_MUON_SCALE_*                                */
+  uint32_t flags;        /* LAMB_MUON_FLAG_*                                 */
+} lamb_muon_hyper_t;
+
+struct lamb_muon;
+
+/* A plan for n_matrices row-major matrices (contiguous): rows, cols host arrays,
+ * sides 0 .. 2^20, the shorter one up to 2^15.  decay_mask, grad_dtype,
+ * copy_dtype and device as in lamb_plan_create.  Synchronous. */
+LAMB_API lamb_status_t lamb_muon_create(
+    const int64_t* rows, const int64_t* cols, int32_t n_matrices,
+    const uint8_t* decay_mask, int32_t grad_dtype, int32_t copy_dtype,
+    int32_t device, struct lamb_muon** out);
+
+/* Bind the matrices of lamb_muon_step: host arrays of DEVICE pointers as in
+ * lamb_plan_bind (w, m fp32; g of grad_dtype; w_copy iff the plan has a copy).
+ * Synchronises `stream`; not capturable. */
+LAMB_API lamb_status_t lamb_muon_bind(struct lamb_muon* plan, void* const* w,
+                                      const void* const* g, void* const* m,
+                                      void* const* w_copy, cudaStream_t stream);
+
+/* Bind the matrices of lamb_muon_direction: u of grad_dtype, o bf16 (what X
+ * holds of correct bits fits).  o[k] may be u[k] if that is bf16. */
+LAMB_API lamb_status_t lamb_muon_bind_direction(struct lamb_muon* plan,
+                                                const void* const* u,
+                                                void* const* o,
+                                                cudaStream_t stream);
+
+/* One update of every matrix, enqueued on `stream`; d_lr is DEVICE float eta.
+ * Updates w, m (and the copy) in place.  Capturable; calls of one plan share its
+ * workspace and must not overlap. */
+LAMB_API lamb_status_t lamb_muon_step(struct lamb_muon* plan,
+                                      const lamb_muon_hyper_t* hyper,
+                                      const float* d_lr, cudaStream_t stream);
+
+/* o = X of u for every matrix, without momentum, scale and weights. */
+LAMB_API lamb_status_t lamb_muon_direction(struct lamb_muon* plan,
+                                           const lamb_muon_hyper_t* hyper,
+                                           cudaStream_t stream);
+
+/* Read (and optionally clear) the plan's device status word: NONFINITE (a norm
+ * was Inf or NaN) or WAIT_TIMEOUT (as in lamb_vocab_query). */
+LAMB_API lamb_status_t lamb_muon_query(struct lamb_muon* plan,
+                                       uint32_t* status_bits, int32_t clear,
+                                       cudaStream_t stream);
+
+/* Frees the plan (synchronises its device); NULL is a no-op. */
+LAMB_API lamb_status_t lamb_muon_destroy(struct lamb_muon* plan);
+
 /* Message of the last failed call on this host thread ("" if none). */
 LAMB_API const char* lamb_last_error(void);
 

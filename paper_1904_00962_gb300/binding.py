@@ -59,7 +59,10 @@ EXPORTED = ["lamb_plan_create", "lamb_plan_bind", "lamb_step", "lars_step",
             "lamb_plan_copy_partials",
             "lamb_vocab_create", "lamb_vocab_embed", "lamb_vocab_embed_grad",
             "lamb_vocab_loss", "lamb_vocab_loss_grad", "lamb_vocab_query",
-            "lamb_vocab_destroy"]
+            "lamb_vocab_destroy",
+            "lamb_muon_create", "lamb_muon_bind", "lamb_muon_bind_direction",
+            "lamb_muon_step", "lamb_muon_direction", "lamb_muon_query",
+            "lamb_muon_destroy"]
 
 
 class LambError(RuntimeError):
@@ -81,6 +84,18 @@ class lamb_hyper_t(Structure):
                 ("lr_total_steps", c_int64)]
 
 
+class lamb_muon_hyper_t(Structure):
+    _fields_ = [("momentum", c_double), ("weight_decay", c_double),
+                ("eps", c_double), ("a", c_double), ("b", c_double),
+                ("c", c_double), ("update_scale", c_double),
+                ("steps", c_int32), ("scale_kind", c_int32),
+                ("flags", c_uint32)]
+
+
+LAMB_MUON_SCALE_ONE = 0
+LAMB_MUON_SCALE_SPECTRAL = 1
+LAMB_MUON_SCALE_RMS = 2
+LAMB_MUON_FLAG_NESTEROV = 0x1
 LAMB_ALGO_AUTO = 0
 LAMB_ALGO_TWO_PASS = 1
 LAMB_ALGO_ON_CHIP = 3
@@ -190,6 +205,16 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                          vp, vp, i64, vp, i32, i64, i32, vp]
     lib.lamb_vocab_query.argtypes = [vp, POINTER(c_uint32), i32, vp]
     lib.lamb_vocab_destroy.argtypes = [vp]
+    lib.lamb_muon_create.argtypes = [POINTER(i64), POINTER(i64), i32,
+                                     POINTER(c_uint8), i32, i32, i32,
+                                     POINTER(vp)]
+    lib.lamb_muon_bind.argtypes = [vp, POINTER(vp), POINTER(vp), POINTER(vp),
+                                   POINTER(vp), vp]
+    lib.lamb_muon_bind_direction.argtypes = [vp, POINTER(vp), POINTER(vp), vp]
+    lib.lamb_muon_step.argtypes = [vp, POINTER(lamb_muon_hyper_t), vp, vp]
+    lib.lamb_muon_direction.argtypes = [vp, POINTER(lamb_muon_hyper_t), vp]
+    lib.lamb_muon_query.argtypes = [vp, POINTER(c_uint32), i32, vp]
+    lib.lamb_muon_destroy.argtypes = [vp]
     for name in EXPORTED:
         if name in ("lamb_last_error", "lamb_abi_version"):
             continue
@@ -568,3 +593,72 @@ def lamb_vocab_query(plan, clear=False, stream=0) -> int:
 def lamb_vocab_destroy(plan) -> None:
     if plan:
         _check(load().lamb_vocab_destroy(c_void_p(plan)))
+
+
+# ---------------------------------------------------------------------------
+# Orthogonalised (Muon) update
+# ---------------------------------------------------------------------------
+_MUON_SCALES = {"one": LAMB_MUON_SCALE_ONE,
+                "spectral": LAMB_MUON_SCALE_SPECTRAL,
+                "rms": LAMB_MUON_SCALE_RMS}
+
+
+def make_muon_hyper(*, momentum=0.95, weight_decay=0.01, eps=1e-7,
+                    coefficients=(3.4445, -4.7750, 2.0315), steps=5,
+                    scale="spectral", update_scale=1.0, nesterov=True
+                    ) -> lamb_muon_hyper_t:
+    """Fill a lamb_muon_hyper_t (plain field copy); scale: "one", "spectral"
+    or "rms"."""
+    a, b, c = coefficients
+    return lamb_muon_hyper_t(momentum, weight_decay, eps, a, b, c,
+                             update_scale, int(steps), _MUON_SCALES[scale],
+                             LAMB_MUON_FLAG_NESTEROV if nesterov else 0)
+
+
+def lamb_muon_create(rows, cols, decay_mask=None, grad_dtype=LAMB_F32,
+                     copy_dtype=LAMB_DTYPE_NONE, device=0) -> int:
+    n = len(rows)
+    r = (c_int64 * max(n, 1))(*[int(x) for x in rows])
+    c = (c_int64 * max(n, 1))(*[int(x) for x in cols])
+    mask = None
+    if decay_mask is not None:
+        mask = (c_uint8 * max(n, 1))(*[1 if d else 0 for d in decay_mask])
+    out = c_void_p()
+    _check(load().lamb_muon_create(r, c, n, mask, int(grad_dtype),
+                                   int(copy_dtype), int(device), byref(out)))
+    return out.value
+
+
+def lamb_muon_bind(plan, w, g, m, w_copy=None, stream=0) -> None:
+    _check(load().lamb_muon_bind(c_void_p(plan), _ptr_array(w), _ptr_array(g),
+                                 _ptr_array(m), _ptr_array(w_copy),
+                                 c_void_p(stream or None)))
+
+
+def lamb_muon_bind_direction(plan, u, o, stream=0) -> None:
+    _check(load().lamb_muon_bind_direction(c_void_p(plan), _ptr_array(u),
+                                           _ptr_array(o),
+                                           c_void_p(stream or None)))
+
+
+def lamb_muon_step(plan, hyper: lamb_muon_hyper_t, d_lr, stream=0) -> None:
+    _check(load().lamb_muon_step(c_void_p(plan), byref(hyper),
+                                 c_void_p(d_lr or None),
+                                 c_void_p(stream or None)))
+
+
+def lamb_muon_direction(plan, hyper: lamb_muon_hyper_t, stream=0) -> None:
+    _check(load().lamb_muon_direction(c_void_p(plan), byref(hyper),
+                                      c_void_p(stream or None)))
+
+
+def lamb_muon_query(plan, clear=False, stream=0) -> int:
+    bits = c_uint32()
+    _check(load().lamb_muon_query(c_void_p(plan), byref(bits), int(clear),
+                                  c_void_p(stream or None)))
+    return int(bits.value)
+
+
+def lamb_muon_destroy(plan) -> None:
+    if plan:
+        _check(load().lamb_muon_destroy(c_void_p(plan)))

@@ -141,6 +141,9 @@ struct StatsWork {
   typedef StatsParams Params;
   typedef RowsState State;
   static constexpr bool kBf16 = true;
+  static constexpr int kStages = 4, kStaging = 0;
+  static __device__ __forceinline__ void before(const Params&, const GemmTile&,
+                                                Epilogue&) {}
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
@@ -166,8 +169,8 @@ struct StatsWork {
   static __device__ __forceinline__ void epilogue(const Params& p,
                                                   const State& s,
                                                   const GemmTile& g,
-                                                  uint32_t acc, int row) {
-    const int r = g.a0 + row;
+                                                  uint32_t acc, Epilogue& epi) {
+    const int r = g.a0 + epi.row;
     const int label = r < s.rows ? p.labels[r] : -1;
     float top = -INFINITY, sum = 0.f;
     for (int c = 0; c < kTileN / 32; ++c) {
@@ -289,6 +292,9 @@ struct DlogitsWork {
   typedef DlogitsParams Params;
   typedef RowsState State;
   static constexpr bool kBf16 = true;
+  static constexpr int kStages = 4, kStaging = 0;
+  static __device__ __forceinline__ void before(const Params&, const GemmTile&,
+                                                Epilogue&) {}
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
@@ -316,8 +322,8 @@ struct DlogitsWork {
   static __device__ __forceinline__ void epilogue(const Params& p,
                                                   const State& s,
                                                   const GemmTile& g,
-                                                  uint32_t acc, int row) {
-    const int r = g.a0 + row;
+                                                  uint32_t acc, Epilogue& epi) {
+    const int r = g.a0 + epi.row;
     const bool real = r < s.rows;
     const int label = real ? p.labels[r] : -1;
     const float l2 = real ? p.lse2[r] : 0.f;
@@ -431,6 +437,9 @@ struct GradsWork {
   typedef GradsParams Params;
   typedef GradsState State;
   static constexpr bool kBf16 = true;
+  static constexpr int kStages = 4, kStaging = 0;
+  static __device__ __forceinline__ void before(const Params&, const GemmTile&,
+                                                Epilogue&) {}
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
@@ -473,8 +482,8 @@ struct GradsWork {
   static __device__ __forceinline__ void epilogue(const Params& p,
                                                   const State& s,
                                                   const GemmTile& g,
-                                                  uint32_t acc, int row) {
-    const int r = g.a0 + row;
+                                                  uint32_t acc, Epilogue& epi) {
+    const int r = g.a0 + epi.row;
     const bool in = g.what ? r < s.rows : r < p.piece && p.v0 + r < p.vocab;
     for (int c = 0; c < kTileN / 32; ++c) {
       const int d = g.b0 + c * 32;
@@ -551,7 +560,7 @@ template <class Work>
 cudaError_t launch_gemm(const typename Work::Params& p, int64_t most_tiles,
                         int sms, cudaStream_t stream) {
   const int grid = (int)std::min<int64_t>(most_tiles, sms);
-  gemm_kernel<Work><<<grid, kGemmThreads, kGemmSmem, stream>>>(p);
+  gemm_kernel<Work><<<grid, kGemmThreads, kGemmSmem<Work>, stream>>>(p);
   return cudaGetLastError();
 }
 
@@ -559,7 +568,7 @@ template <class Work>
 cudaError_t allow_smem() {
   return cudaFuncSetAttribute(gemm_kernel<Work>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)kGemmSmem);
+                              (int)kGemmSmem<Work>);
 }
 
 int grid_for(int64_t n, int sms) {

@@ -1,0 +1,1209 @@
+// Orthogonalised (Muon) update of matrices.
+//
+//   m <- beta m + (1 - beta) g,  u = (1 - beta) g + beta m  (Nesterov) or m
+//   X = u / (|u|_F + eps); `steps` times, with G the Gram matrix of X's shorter
+//   side:  X <- a X + (b G + c G G) X      (X (b G + c G G) for a tall X)
+//   w <- (1 - eta lambda) w - eta s X
+//
+// Three products a step on the tensor cores (lm_gemm.cuh), in fp16 with fp32
+// accumulators.  Eleven significant bits are enough only where the large terms
+// stay out of the rounding, so
+//   X is a pair of halves hi + lo (22 bits; the products read hi),
+//   G is kept as its diagonal in fp32 and the rest D in fp16, and so is
+//   b G + c G G = diag(beta) + E:  with G = diag(l) + D,
+//     E_ij = b D_ij + c ((l_i + l_j) D_ij + (D D)_ij),   i != j
+//     beta_i = b l_i + c (l_i^2 + (D D)_ii)
+//   and X <- (a + beta_i) X + E X takes X whole from the pair.
+// The direction is then within 3e-4 .. 1e-3 of the exact one (Gaussian, low-rank
+// and power-law spectra, 10 x 10 to 1536 x 1600): half a bf16 rounding; with G
+// rounded as it is, 1.7e-3 .. 1.2e-2, in bf16 1.3e-2 .. 1e-1.  Scales that are
+// powers of two keep the entries inside fp16's range.
+//
+// G and G G are symmetric: tiles on or above the diagonal are multiplied and
+// written to both places.  All matrices of a group go through one launch a
+// product, longest K first.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "lm_gemm.cuh"
+#include "lm_host.h"
+
+namespace lamb {
+namespace {
+
+constexpr int kMuonThreads = 256;
+constexpr int kMuonChunk = 8192;             // elements of a chunk
+constexpr float kScaleD = 1024.f;            // D is stored times this
+constexpr float kScaleE = 256.f;             // and E times this
+constexpr float kScaleLo = 2048.f;           // lo: the rest of hi, times this
+
+struct MuonMatrix {
+  CUtensorMap x_k[2], x_mn[2];   // hi (two buffers, taken in turn)
+  CUtensorMap lo_k;
+  CUtensorMap d, e;              // boxes of 128 rows
+  CUtensorMap d_t, e_t;          // boxes of 64 rows: mirrored blocks
+  __half* hi[2];
+  __half* lo;
+  __half* D;
+  __half* E;
+  float* diag;                   // l
+  float* beta;
+  float scale;                   // hi + lo = X scale
+  int rows, cols, m, n;          // m = min, n = max
+  int tall;                      // rows > cols
+  int pitch, pitch_m;            // of X, of D and E
+  int first_chunk, n_chunks;
+  float decay;
+};
+
+struct MuonPtrs {
+  float* w;
+  const void* g;                 // or the direction's input
+  float* m;
+  __nv_bfloat16* out;            // copy of w, or the direction
+};
+
+struct MuonChunk {
+  int matrix;
+  int len;
+  int64_t offset;
+};
+
+struct MuonTile {
+  int matrix, i, j, pad;
+};
+
+struct MuonConsts {
+  float a, b, c;
+  float beta, omb;               // momentum
+  float eps;
+  float wd, size;                // lambda, s without its shape's part
+  int nesterov, scale_kind;
+};
+
+enum { kGram = 0, kSquare = 1, kApply = 2 };
+
+struct MuonParams {
+  const MuonMatrix* mats;
+  const MuonPtrs* ptrs;
+  const MuonTile* tiles;
+  const float* d_lr;             // NULL: the direction alone
+  uint32_t* status;
+  MuonConsts k;
+  int n_tiles;
+  int from;                      // which hi is read
+  int last;
+};
+
+struct MuonState {
+  int n_tiles;
+};
+
+// s of a matrix.
+__device__ __forceinline__ float muon_size(const MuonConsts& k,
+                                           const MuonMatrix& x) {
+  if (k.scale_kind == LAMB_MUON_SCALE_RMS)
+    return k.size * 0.2f * sqrtf((float)x.n);
+  if (k.scale_kind == LAMB_MUON_SCALE_SPECTRAL)
+    return k.size * sqrtf(fmaxf(1.f, (float)x.rows / (float)x.cols));
+  return k.size;
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The epilogues take 64 columns at a time through staging memory: a chunk's
+// inputs arrive there by tensor copies (while the chunk before is worked on),
+// each thread turns its row over, and tensor copies take the result out.  Rows of
+// 128 bytes in the copies' swizzle, 16 KB a matrix; two such buffers of 32 KB.
+// (With plain accesses, a row a thread, the epilogue took 20 times the products.)
+constexpr int kChunkCols = 64;
+constexpr int kHalfBuffer = kTileM * kChunkCols * 2;
+constexpr int kChunkBuffer = 2 * kHalfBuffer;
+
+// The 16-byte unit q of row r.
+__device__ __forceinline__ uint32_t unit16(uint32_t base, int r, int q) {
+  return base + r * 128 + ((q ^ (r & 7)) << 4);
+}
+// Entry (j, i) of a mirrored block: two halves of 64 columns, 64 rows each.
+__device__ __forceinline__ uint32_t mirrored(uint32_t base, int j, int i) {
+  return base + (i >> 6) * 8192 + j * 128 + ((((i & 63) >> 3) ^ (j & 7)) << 4) +
+         (i & 7) * 2;
+}
+// Unit q of row r of 64 floats.
+__device__ __forceinline__ uint32_t unit16_f(uint32_t base, int r, int q) {
+  return base + r * 256 + ((q ^ (r & 7)) << 4);
+}
+__device__ __forceinline__ float2 half2_at(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+__device__ __forceinline__ uint16_t half_bits(uint32_t w, int i) {
+  return (uint16_t)(i ? w >> 16 : w & 0xffffu);
+}
+
+template <int kPhase>
+struct MuonWork {
+  typedef MuonParams Params;
+  typedef MuonState State;
+  static constexpr bool kBf16 = false;
+  static constexpr int kStages = 3, kStaging = 2 * kChunkBuffer;
+  static __device__ __forceinline__ State start(const Params& p) {
+    return State{p.n_tiles};
+  }
+  static __device__ __forceinline__ GemmTile tile(const Params& p, const State&,
+                                                  int t) {
+    const MuonTile mt = p.tiles[t];
+    const MuonMatrix* x = p.mats + mt.matrix;
+    GemmTile g;
+    g.what = mt.matrix;
+    g.aux = 0;
+    g.k0 = g.b_k = 0;
+    g.a0 = mt.i * kTileM;
+    g.b0 = mt.j * kTileN;
+    if (kPhase == kGram) {
+      g.a_mn = g.b_mn = x->tall;
+      g.a = g.b = x->tall ? &x->x_mn[p.from] : &x->x_k[p.from];
+      g.kn = (x->n + kTileK - 1) / kTileK;
+    } else {
+      g.kn = (x->m + kTileK - 1) / kTileK;
+      if (kPhase == kSquare) {
+        g.a = g.b = &x->d;
+        g.a_mn = g.b_mn = false;
+      } else if (x->tall) {
+        g.a = &x->x_k[p.from];
+        g.b = &x->e;
+        g.a_mn = g.b_mn = false;
+      } else {
+        g.a = &x->e;
+        g.b = &x->x_mn[p.from];
+        g.a_mn = false;
+        g.b_mn = true;
+      }
+    }
+    return g;
+  }
+
+  // Copies chunk `c` of the tile into the buffer whose turn it is.
+  static __device__ __forceinline__ void fetch(const Params& p,
+                                               const MuonMatrix& x,
+                                               const GemmTile& g, int c,
+                                               Epilogue& epi) {
+    const int at = epi.issued++;
+    const uint32_t to = epi.staging + (at & 1) * kChunkBuffer;
+    uint64_t* bar = &epi.sh->in_full[at & 1];
+    const int c0 = g.b0 + c * kChunkCols;
+    if (kPhase == kSquare) {
+      mbar_expect(bar, kHalfBuffer);
+      tile_load(to, &x.d, c0, g.a0, bar);
+    } else {
+      mbar_expect(bar, 2 * kHalfBuffer);
+      tile_load(to, &x.x_k[p.from], c0, g.a0, bar);
+      tile_load(to + kHalfBuffer, &x.lo_k, c0, g.a0, bar);
+    }
+  }
+
+  static __device__ __forceinline__ void before(const Params& p,
+                                                const GemmTile& g,
+                                                Epilogue& epi) {
+    if (kPhase == kGram || epi.row != 0) return;
+    stores_have_read<1>();      // the buffer's own store, two chunks ago
+    fetch(p, p.mats[g.what], g, 0, epi);
+  }
+
+  static __device__ __forceinline__ void epilogue(const Params& p,
+                                                  const State&,
+                                                  const GemmTile& g,
+                                                  uint32_t acc, Epilogue& epi) {
+    const MuonMatrix& x = p.mats[g.what];
+    const int width = kPhase == kApply ? x.cols : x.m;
+    const bool last = kPhase == kApply && p.last;
+    for (int c = 0; c < kTileN / kChunkCols; ++c) {
+      const int c0 = g.b0 + c * kChunkCols;
+      if (c0 >= width) break;
+      const int n = epi.chunks;
+      const uint32_t buf = epi.staging + (n & 1) * kChunkBuffer;
+      if (kPhase == kGram) {
+        if (epi.row == 0) stores_have_read<1>();
+        epi.sync();
+      } else {
+        if (epi.row == 0 && c + 1 < kTileN / kChunkCols &&
+            c0 + kChunkCols < width) {
+          stores_have_read<0>();
+          fetch(p, x, g, c + 1, epi);
+        }
+        bounded_wait(&epi.sh->in_full[n & 1], (uint32_t)(n >> 1) & 1u,
+                     &epi.sh->gave_up, epi.status, LAMB_STATUS_WAIT_TIMEOUT);
+      }
+      if (kPhase == kApply)
+        apply(p, x, g, acc + c * kChunkCols, c0, buf, epi);
+      else
+        symmetric(p, x, g, acc + c * kChunkCols, c0, buf, epi);
+      epi.chunks = n + 1;
+      if (!last) {
+        fence_proxy_async();
+        epi.sync();
+        if (epi.row == 0) {
+          if (kPhase == kApply) {
+            tile_store(&x.x_k[p.from ^ 1], c0, g.a0, buf);
+            tile_store(&x.lo_k, c0, g.a0, buf + kHalfBuffer);
+          } else {
+            const CUtensorMap* t = kPhase == kGram ? &x.d : &x.e;
+            tile_store(t, c0, g.a0, buf);
+            if (mirror(g, c0)) {
+              const CUtensorMap* m = kPhase == kGram ? &x.d_t : &x.e_t;
+              tile_store(m, g.a0, c0, buf + kHalfBuffer);
+              if (g.a0 + 64 < x.m)
+                tile_store(m, g.a0 + 64, c0, buf + kHalfBuffer + 8192);
+            }
+          }
+          stores_commit();
+        }
+      } else {
+        epi.sync();
+        write_out(p, x, g, c0, buf, epi);
+        fence_proxy_async();
+        epi.sync();      // the buffer may be copied into again
+      }
+    }
+  }
+
+  // Whether the block of rows c0 .. and columns a0 .. is another tile's own.
+  static __device__ __forceinline__ bool mirror(const GemmTile& g, int c0) {
+    return g.a0 / kTileN * kTileN + kTileN - 1 < c0 / kTileM * kTileM;
+  }
+
+  static __device__ __forceinline__ void symmetric(const Params& p,
+                                                   const MuonMatrix& x,
+                                                   const GemmTile& g,
+                                                   uint32_t acc, int c0,
+                                                   uint32_t buf,
+                                                   const Epilogue& epi) {
+    const int i = g.a0 + epi.row, m = x.m;
+    const float li = kPhase == kSquare && i < m ? x.diag[i] : 0.f;
+    const bool both = mirror(g, c0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int j0 = c0 + 32 * h;
+      float y[32];
+      tmem_ld32(acc + 32 * h, y);
+      if (kPhase == kGram) {
+        const float s = 1.f / (x.scale * x.scale);     // a power of two
+        if (i >= j0 && i < j0 + 32 && i < m) {
+#pragma unroll
+          for (int q = 0; q < 32; ++q)
+            if (j0 + q == i) {
+              x.diag[i] = y[q] * s;
+              y[q] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 32; ++q) y[q] *= s * kScaleD;
+      } else {
+        const float s = 1.f / (kScaleD * kScaleD);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint4 d = lds16(unit16(buf, epi.row, 4 * h + u));
+          const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int q = 8 * u + k;
+            const float2 dd2 = half2_at(dw[k >> 1]);
+            const float dd = (k & 1 ? dd2.y : dd2.x) * (1.f / kScaleD);
+            const float lj = x.diag[min(j0 + q, m - 1)];
+            const float sq = y[q] * s;
+            const float sum = li + lj;
+            if (j0 + q == i) {
+              if (i < m) x.beta[i] = p.k.b * li + p.k.c * (li * li + sq);
+              y[q] = 0.f;
+            } else {
+              y[q] = (p.k.b * dd + p.k.c * (sum * dd + sq)) * kScaleE;
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          w[k] = pack_half2(y[8 * u + 2 * k], y[8 * u + 2 * k + 1]);
+        sts16(unit16(buf, epi.row, 4 * h + u),
+              make_uint4(w[0], w[1], w[2], w[3]));
+        if (both) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            sts2(mirrored(buf + kHalfBuffer, 32 * h + 8 * u + k, epi.row),
+                 half_bits(w[k >> 1], k & 1));
+        }
+      }
+    }
+  }
+
+  static __device__ __forceinline__ void apply(const Params& p,
+                                               const MuonMatrix& x,
+                                               const GemmTile& g, uint32_t acc,
+                                               int c0, uint32_t buf,
+                                               const Epilogue& epi) {
+    const int r = g.a0 + epi.row;
+    const float br = !x.tall && r < x.rows ? p.k.a + x.beta[r] : 0.f;
+    const float inv = 1.f / x.scale;
+    float y[64];
+    tmem_ld32(acc, *reinterpret_cast<float(*)[32]>(y));
+    tmem_ld32(acc + 32, *reinterpret_cast<float(*)[32]>(y + 32));
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const uint32_t ah = unit16(buf, epi.row, u), al = ah + kHalfBuffer;
+      const uint4 hi = lds16(ah), lo = lds16(al);
+      const uint32_t hw[4] = {hi.x, hi.y, hi.z, hi.w};
+      const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w};
+      uint32_t oh[4], ol[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 a = half2_at(hw[k]), b = half2_at(lw[k]);
+        float v[2] = {fmaf(b.x, 1.f / kScaleLo, a.x),
+                      fmaf(b.y, 1.f / kScaleLo, a.y)};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int q = 8 * u + 2 * k + e;
+          const float f =
+              x.tall ? p.k.a + x.beta[min(c0 + q, x.cols - 1)] : br;
+          // in units of 1 / scale
+          v[e] = fmaf(f, v[e], y[q] * (1.f / kScaleE));
+          y[q] = v[e] * inv;
+        }
+        oh[k] = pack_half2(v[0], v[1]);
+        const float2 h = half2_at(oh[k]);
+        ol[k] = pack_half2((v[0] - h.x) * kScaleLo, (v[1] - h.y) * kScaleLo);
+      }
+      if (!p.last) {
+        sts16(ah, make_uint4(oh[0], oh[1], oh[2], oh[3]));
+        sts16(al, make_uint4(ol[0], ol[1], ol[2], ol[3]));
+      }
+    }
+    if (p.last) {
+      epi.sync();          // everybody has read its inputs
+#pragma unroll
+      for (int u = 0; u < 16; ++u)
+        sts16(unit16_f(buf, epi.row, u),
+              make_uint4(__float_as_uint(y[4 * u]),
+                         __float_as_uint(y[4 * u + 1]),
+                         __float_as_uint(y[4 * u + 2]),
+                         __float_as_uint(y[4 * u + 3])));
+    }
+  }
+
+  // The last X to the weights or the direction, half a warp a row.
+  static __device__ __forceinline__ void write_out(const Params& p,
+                                                   const MuonMatrix& x,
+                                                   const GemmTile& g, int c0,
+                                                   uint32_t buf,
+                                                   const Epilogue& epi) {
+    const MuonPtrs ptr = p.ptrs[g.what];
+    const float lr = p.d_lr ? *p.d_lr : 0.f;
+    const float keep = 1.f - lr * p.k.wd * x.decay;
+    const float move = lr * muon_size(p.k, x);
+    const int u = epi.row & 15, c = c0 + 4 * u;
+    if (c >= x.cols) return;
+    const int cols = min(4, x.cols - c);
+    const bool vec = cols == 4 && x.cols % 4 == 0 && (uintptr_t)ptr.w % 16 == 0 &&
+                     (uintptr_t)ptr.out % 8 == 0;
+#pragma unroll 4
+    for (int r = epi.row >> 4; r < kTileM; r += kEpiThreads / 16) {
+      if (g.a0 + r >= x.rows) break;
+      const uint4 w = lds16(unit16_f(buf, r, u));
+      float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y),
+                    __uint_as_float(w.z), __uint_as_float(w.w)};
+      const int64_t at = (int64_t)(g.a0 + r) * x.cols + c;
+      if (vec) {
+        if (p.d_lr) {
+          float4* to = reinterpret_cast<float4*>(ptr.w + at);
+          const float4 o = *to;
+          v[0] = keep * o.x - move * v[0];
+          v[1] = keep * o.y - move * v[1];
+          v[2] = keep * o.z - move * v[2];
+          v[3] = keep * o.w - move * v[3];
+          *to = make_float4(v[0], v[1], v[2], v[3]);
+        }
+        if (ptr.out) {
+          const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]);
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2], v[3]);
+          *reinterpret_cast<uint2*>(ptr.out + at) =
+              make_uint2(*reinterpret_cast<const uint32_t*>(&a),
+                         *reinterpret_cast<const uint32_t*>(&b));
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (k >= cols) break;
+          if (p.d_lr) {
+            v[k] = keep * ptr.w[at + k] - move * v[k];
+            ptr.w[at + k] = v[k];
+          }
+          if (ptr.out) ptr.out[at + k] = __float2bfloat16_rn(v[k]);
+        }
+      }
+    }
+  }
+};
+
+// ---- momentum and norm --------------------------------------------------------
+template <class TG>
+__device__ __forceinline__ float load_grad(const void* p, int64_t i);
+template <>
+__device__ __forceinline__ float load_grad<float>(const void* p, int64_t i) {
+  return reinterpret_cast<const float*>(p)[i];
+}
+template <>
+__device__ __forceinline__ float load_grad<__nv_bfloat16>(const void* p,
+                                                          int64_t i) {
+  return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
+}
+
+__device__ __forceinline__ float update_of(const MuonConsts& k, float g,
+                                           float m) {
+  return k.nesterov ? fmaf(k.beta, m, k.omb * g) : m;
+}
+
+__device__ __forceinline__ double block_sum(double s, double* sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int i = 0; i < kMuonThreads / 32; ++i) s += sh[i];
+  return s;
+}
+
+// New momentum (kStep) and the sum of squares of a chunk's u.
+template <class TG, bool kStep>
+__global__ void __launch_bounds__(kMuonThreads)
+muon_norm_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
+                 const MuonChunk* chunks, MuonConsts k, double* part) {
+  __shared__ double sh[kMuonThreads / 32];
+  const MuonChunk c = chunks[blockIdx.x];
+  const MuonPtrs p = ptrs[c.matrix];
+  float s = 0.f;
+  for (int i = threadIdx.x; i < c.len; i += kMuonThreads) {
+    const int64_t at = c.offset + i;
+    float u = load_grad<TG>(p.g, at);
+    if (kStep) {
+      const float m = fmaf(k.beta, p.m[at], k.omb * u);
+      p.m[at] = m;
+      u = update_of(k, u, m);
+    }
+    s = fmaf(u, u, s);
+  }
+  const double sum = block_sum((double)s, sh);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+// X = u / (|u| + eps) as a pair of halves.
+template <class TG, bool kStep>
+__global__ void __launch_bounds__(kMuonThreads)
+muon_start_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
+                  const MuonChunk* chunks, MuonConsts k, const double* part,
+                  int chunk0, uint32_t* status) {
+  __shared__ double sh[kMuonThreads / 32];
+  const MuonChunk c = chunks[blockIdx.x];
+  const MuonMatrix& x = mats[c.matrix];
+  const MuonPtrs p = ptrs[c.matrix];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < x.n_chunks; i += kMuonThreads)
+    s += part[x.first_chunk - chunk0 + i];
+  const float norm = (float)sqrt(block_sum(s, sh));
+  if (threadIdx.x == 0 && !isfinite(norm))
+    atomicOr(status, LAMB_STATUS_NONFINITE);
+  const float f = 1.f / (norm + k.eps);
+  for (int i = threadIdx.x; i < c.len; i += kMuonThreads) {
+    const int64_t at = c.offset + i;
+    float u = load_grad<TG>(p.g, at);
+    if (kStep) u = update_of(k, u, p.m[at]);
+    const float v = u * f * x.scale;
+    const int64_t r = at / x.cols;
+    const int64_t to = r * x.pitch + (at - r * x.cols);
+    const __half h = __float2half_rn(v);
+    x.hi[0][to] = h;
+    x.lo[to] = __float2half_rn((v - __half2float(h)) * kScaleLo);
+  }
+}
+
+// ---- small matrices ------------------------------------------------------------
+// A matrix whose X fits in shared memory twice goes through all of its steps in
+// one CTA, in fp32 on the CUDA cores: momentum, norm, products, update.  A chain
+// of launches on the tensor cores costs some 15 launches' latency, and an entry of
+// a tiny matrix is too few terms for its 11-bit roundings to average out.
+constexpr int kSmallThreads = 512;
+constexpr int kSmallSide = 64;               // m up to
+constexpr int64_t kSmallElems = 20480;       // m n up to
+constexpr int64_t kSmallProduct = 1 << 19;   // m m n up to
+
+bool muon_is_small(int64_t m, int64_t n) {
+  return m <= kSmallSide && m * n <= kSmallElems && m * m * n <= kSmallProduct;
+}
+int64_t small_smem(int64_t m, int64_t n) {
+  return (2 * m * lm_round_up(n, 4) + 2 * m * lm_round_up(m, 8)) * 4;
+}
+
+// out = b in + c (in in^T), or in in^T (kPlain), both symmetric: blocks of 4 x 4,
+// each by S neighbouring lanes that take every S-th k.
+template <bool kPlain>
+__device__ __forceinline__ void small_gram(const float* in, int pitch, int m,
+                                           int n, float b, float c, float* out,
+                                           int out_pitch) {
+  const int nb = (m + 3) >> 2, tasks = nb * (nb + 1) / 2;
+  int S = 32;
+  while (S > 1 && S * tasks > kSmallThreads) S >>= 1;
+  const int s = threadIdx.x % S, groups = kSmallThreads / S;
+  for (int base = 0; base < tasks; base += groups) {
+    const int task = base + threadIdx.x / S;
+    int t = min(task, tasks - 1), bi = 0;
+    while (t >= nb - bi) {
+      t -= nb - bi;
+      ++bi;
+    }
+    const int i0 = 4 * bi, j0 = 4 * (bi + t);
+    const float *ri[4], *rj[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      ri[q] = in + min(i0 + q, m - 1) * pitch;
+      rj[q] = in + min(j0 + q, m - 1) * pitch;
+    }
+    float acc[4][4] = {};
+    for (int k = s; k < n; k += S) {
+      float x[4], y[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        x[q] = ri[q][k];
+        y[q] = rj[q][k];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(x[u], y[v], acc[u][v]);
+    }
+    for (int o = S >> 1; o > 0; o >>= 1)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          acc[u][v] += __shfl_xor_sync(0xffffffffu, acc[u][v], o);
+    if (task < tasks && s == 0) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int i = i0 + u, j = j0 + v;
+          if (i >= m || j >= m) continue;
+          const float r =
+              kPlain ? acc[u][v] : fmaf(b, in[i * pitch + j], c * acc[u][v]);
+          out[i * out_pitch + j] = r;
+          out[j * out_pitch + i] = r;
+        }
+    }
+  }
+}
+
+template <class TG, bool kStep>
+__global__ void __launch_bounds__(kSmallThreads)
+muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
+                  const int* which, MuonConsts k, int steps, const float* d_lr,
+                  uint32_t* status) {
+  extern __shared__ float sm[];
+  __shared__ double sh[kSmallThreads / 32];
+  const MuonMatrix& x = mats[which[blockIdx.x]];
+  const MuonPtrs p = ptrs[which[blockIdx.x]];
+  const int m = x.m, n = x.n, cols = x.cols, total = m * n;
+  const int np = (n + 3) & ~3, mp = (m + 7) & ~7;
+  const bool tall = x.tall;
+  float *X = sm, *Y = X + m * np, *G = Y + m * np, *H = G + m * mp;
+  for (int i = threadIdx.x; i < m * mp; i += kSmallThreads) H[i] = 0.f;
+
+  float s = 0.f;
+  for (int i = threadIdx.x; i < total; i += kSmallThreads) {
+    float u = load_grad<TG>(p.g, i);
+    if (kStep) {
+      const float mm = fmaf(k.beta, p.m[i], k.omb * u);
+      p.m[i] = mm;
+      u = update_of(k, u, mm);
+    }
+    s = fmaf(u, u, s);
+    const int r = i / cols, c = i - r * cols;
+    X[tall ? c * np + r : r * np + c] = u;
+  }
+  double d = (double)s;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = d;
+  __syncthreads();
+  d = 0.0;
+  for (int i = 0; i < kSmallThreads / 32; ++i) d += sh[i];
+  const float norm = (float)sqrt(d);
+  if (threadIdx.x == 0 && !isfinite(norm))
+    atomicOr(status, LAMB_STATUS_NONFINITE);
+  const float f = 1.f / (norm + k.eps);
+  for (int i = threadIdx.x; i < total; i += kSmallThreads) {
+    const int r = i / n;
+    X[r * np + (i - r * n)] *= f;
+  }
+  __syncthreads();
+
+  for (int it = 0; it < steps; ++it) {
+    small_gram<true>(X, np, m, n, 0.f, 0.f, G, mp);
+    __syncthreads();
+    small_gram<false>(G, mp, m, m, k.b, k.c, H, mp);
+    __syncthreads();
+    // Y = a X + H X, eight rows of a column a thread
+    const int tasks = ((m + 7) >> 3) * n;
+    for (int t = threadIdx.x; t < tasks; t += kSmallThreads) {
+      const int i0 = t / n * 8, j = t % n;
+      float acc[8] = {};
+      for (int q = 0; q < m; ++q) {
+        const float v = X[q * np + j];
+        const float4* h = reinterpret_cast<const float4*>(H + q * mp + i0);
+        const float4 a = h[0], b = h[1];
+        acc[0] = fmaf(a.x, v, acc[0]);
+        acc[1] = fmaf(a.y, v, acc[1]);
+        acc[2] = fmaf(a.z, v, acc[2]);
+        acc[3] = fmaf(a.w, v, acc[3]);
+        acc[4] = fmaf(b.x, v, acc[4]);
+        acc[5] = fmaf(b.y, v, acc[5]);
+        acc[6] = fmaf(b.z, v, acc[6]);
+        acc[7] = fmaf(b.w, v, acc[7]);
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (i0 + q < m)
+          Y[(i0 + q) * np + j] = fmaf(k.a, X[(i0 + q) * np + j], acc[q]);
+    }
+    __syncthreads();
+    float* z = X;
+    X = Y;
+    Y = z;
+  }
+
+  const float lr = kStep ? *d_lr : 0.f;
+  const float size = muon_size(k, x);
+  const float keep = 1.f - lr * k.wd * x.decay, move = lr * size;
+  for (int i = threadIdx.x; i < total; i += kSmallThreads) {
+    const int r = i / cols, c = i - r * cols;
+    float v = X[tall ? c * np + r : r * np + c];
+    if (kStep) {
+      v = keep * p.w[i] - move * v;
+      p.w[i] = v;
+    }
+    if (p.out) p.out[i] = __float2bfloat16_rn(v);
+  }
+}
+
+template <class TG, bool kStep>
+cudaError_t small_smem_limit(int64_t bytes) {
+  return cudaFuncSetAttribute(muon_small_kernel<TG, kStep>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)bytes);
+}
+
+template <class Work>
+cudaError_t muon_smem() {
+  return cudaFuncSetAttribute(gemm_kernel<Work>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)kGemmSmem<Work>);
+}
+
+}  // namespace
+
+// Matrices that go through the products together, on one workspace.
+struct MuonGroup {
+  int chunk0 = 0, chunks = 0;
+  int sym0 = 0, sym = 0;      // tiles of the Gram matrix, by its K
+  int sq0 = 0;                // the same tiles, by the square's K
+  int app0 = 0, app = 0;
+};
+
+}  // namespace lamb
+
+using namespace lamb;
+
+struct lamb_muon {
+  int device = 0, sms = 0, n = 0;
+  bool grad_bf16 = false, copy = false;
+  bool bound = false, bound_direction = false;
+  void* arena = nullptr;
+  void* work = nullptr;
+  MuonMatrix* mats = nullptr;
+  MuonPtrs* ptrs = nullptr;            // of the step
+  MuonPtrs* dir_ptrs = nullptr;        // of the direction
+  MuonChunk* chunks = nullptr;
+  MuonTile* tiles = nullptr;
+  double* part = nullptr;
+  int* small = nullptr;                // matrices of the small kernel
+  int n_small = 0;
+  int64_t small_bytes = 0;             // shared memory of the largest
+  uint32_t* status = nullptr;
+  std::vector<int64_t> numel;
+  std::vector<MuonGroup> groups;
+};
+
+namespace {
+
+// Bytes of working matrices that a group may take.
+constexpr int64_t kGroupBytes = 1ll << 40;
+
+struct MuonLayout {
+  std::vector<MuonMatrix> mats;
+  std::vector<MuonChunk> chunks;
+  std::vector<MuonTile> tiles;
+  std::vector<int> small;
+  std::vector<int64_t> at[7];     // byte offsets in the workspace, per matrix
+  int64_t work_bytes = 0;
+};
+
+int64_t take(int64_t* used, int64_t bytes) {
+  const int64_t at = *used;
+  *used = lm_round_up(at + bytes, 1024);
+  return at;
+}
+
+// Groups, workspace offsets, chunks and tiles of the matrices (host only).
+void muon_layout(const int64_t* rows, const int64_t* cols, int n,
+                 const uint8_t* mask, MuonLayout* L,
+                 std::vector<MuonGroup>* groups) {
+  L->mats.resize(n);
+  for (auto& v : L->at) v.assign(n, 0);
+  std::vector<int> open;
+  int64_t used = 0;
+  auto close = [&]() {
+    if (open.empty()) return;
+    MuonGroup g;
+    g.chunk0 = (int)L->chunks.size();
+    for (int k : open) {
+      MuonMatrix& x = L->mats[k];
+      x.first_chunk = (int)L->chunks.size();
+      const int64_t total = (int64_t)x.rows * x.cols;
+      for (int64_t o = 0; o < total; o += kMuonChunk)
+        L->chunks.push_back(
+            {k, (int)std::min<int64_t>(kMuonChunk, total - o), o});
+      x.n_chunks = (int)L->chunks.size() - x.first_chunk;
+    }
+    g.chunks = (int)L->chunks.size() - g.chunk0;
+    auto by = [&](bool longer) {
+      std::stable_sort(open.begin(), open.end(), [&](int p, int q) {
+        return longer ? L->mats[p].n > L->mats[q].n
+                      : L->mats[p].m > L->mats[q].m;
+      });
+    };
+    auto symmetric = [&]() {
+      for (int k : open)
+        for (int i = 0; i * kTileM < L->mats[k].m; ++i)
+          for (int j = i * kTileM / kTileN; j * kTileN < L->mats[k].m; ++j)
+            L->tiles.push_back({k, i, j, 0});
+    };
+    by(true);
+    g.sym0 = (int)L->tiles.size();
+    symmetric();
+    g.sym = (int)L->tiles.size() - g.sym0;
+    by(false);
+    g.sq0 = (int)L->tiles.size();
+    symmetric();
+    g.app0 = (int)L->tiles.size();
+    for (int k : open)
+      for (int i = 0; i * kTileM < L->mats[k].rows; ++i)
+        for (int j = 0; j * kTileN < L->mats[k].cols; ++j)
+          L->tiles.push_back({k, i, j, 0});
+    g.app = (int)L->tiles.size() - g.app0;
+    groups->push_back(g);
+    L->work_bytes = std::max(L->work_bytes, used);
+    open.clear();
+    used = 0;
+  };
+  for (int k = 0; k < n; ++k) {
+    MuonMatrix& x = L->mats[k];
+    memset(&x, 0, sizeof(x));
+    x.rows = (int)rows[k];
+    x.cols = (int)cols[k];
+    x.m = std::min(x.rows, x.cols);
+    x.n = std::max(x.rows, x.cols);
+    x.tall = x.rows > x.cols;
+    x.pitch = (int)lm_round_up(x.cols, 8);
+    x.pitch_m = (int)lm_round_up(x.m, 8);
+    x.scale = (float)std::exp2(std::round(0.5 * std::log2((double)std::max(
+        1, x.n))));
+    x.decay = mask ? (mask[k] ? 1.f : 0.f) : 1.f;
+    if (!x.m) continue;
+    if (muon_is_small(x.m, x.n)) {
+      L->small.push_back(k);
+      continue;
+    }
+    const int64_t sx = (int64_t)x.rows * x.pitch * 2;
+    const int64_t sm = (int64_t)x.m * x.pitch_m * 2;
+    if (!open.empty() && used + 3 * sx + 2 * sm > kGroupBytes) close();
+    for (int i = 0; i < 3; ++i) L->at[i][k] = take(&used, sx);
+    for (int i = 3; i < 5; ++i) L->at[i][k] = take(&used, sm);
+    for (int i = 5; i < 7; ++i) L->at[i][k] = take(&used, x.m * 4ll);
+    open.push_back(k);
+  }
+  close();
+}
+
+lamb_status_t muon_check(const lamb_muon* p, const lamb_muon_hyper_t* h) {
+  if (!p) return lm_fail(LAMB_ERR_INVALID_ARG, "plan is NULL");
+  if (!h) return lm_fail(LAMB_ERR_INVALID_ARG, "hyper is NULL");
+  const double v[] = {h->momentum, h->weight_decay, h->eps, h->a, h->b, h->c,
+                      h->update_scale};
+  for (double x : v)
+    if (!std::isfinite(x))
+      return lm_fail(LAMB_ERR_INVALID_ARG, "hyper: a value is not finite");
+  if (h->momentum < 0 || h->momentum >= 1 || h->eps < 0 || h->weight_decay < 0)
+    return lm_fail(LAMB_ERR_INVALID_ARG,
+                   "hyper: need 0 <= momentum < 1, eps >= 0, weight_decay >= 0");
+  if (h->steps < 1 || h->steps > 64)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "hyper: steps is not in [1, 64]");
+  if (std::fabs(h->a) > 16 || std::fabs(h->b) > 16 || std::fabs(h->c) > 16)
+    return lm_fail(LAMB_ERR_INVALID_ARG,
+                   "hyper: coefficients beyond 16 leave fp16's range");
+  if (h->scale_kind < LAMB_MUON_SCALE_ONE || h->scale_kind > LAMB_MUON_SCALE_RMS)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "hyper: unknown scale_kind %d",
+                   h->scale_kind);
+  return LAMB_OK;
+}
+
+template <class Work>
+cudaError_t muon_product(const lamb_muon* p, MuonParams& q, int first, int n,
+                         cudaStream_t stream) {
+  q.tiles = p->tiles + first;
+  q.n_tiles = n;
+  gemm_kernel<Work>
+      <<<std::min(n, p->sms), kGemmThreads, kGemmSmem<Work>, stream>>>(q);
+  return cudaGetLastError();
+}
+
+template <class TG, bool kStep>
+void muon_small(const lamb_muon* p, const MuonPtrs* ptrs, const MuonConsts& k,
+                int steps, const float* d_lr, cudaStream_t stream) {
+  if (p->n_small)
+    muon_small_kernel<TG, kStep>
+        <<<p->n_small, kSmallThreads, (size_t)p->small_bytes, stream>>>(
+            p->mats, ptrs, p->small, k, steps, d_lr, p->status);
+}
+
+template <class TG, bool kStep>
+void muon_front(const lamb_muon* p, const MuonPtrs* ptrs, const MuonGroup& g,
+                const MuonConsts& k, cudaStream_t stream) {
+  muon_norm_kernel<TG, kStep><<<g.chunks, kMuonThreads, 0, stream>>>(
+      p->mats, ptrs, p->chunks + g.chunk0, k, p->part);
+  muon_start_kernel<TG, kStep><<<g.chunks, kMuonThreads, 0, stream>>>(
+      p->mats, ptrs, p->chunks + g.chunk0, k, p->part, g.chunk0, p->status);
+}
+
+lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
+                       const float* d_lr, cudaStream_t stream) {
+  LmDevice dev(p->device);
+  if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");
+  MuonParams q;
+  q.mats = p->mats;
+  q.ptrs = d_lr ? p->ptrs : p->dir_ptrs;
+  q.d_lr = d_lr;
+  q.status = p->status;
+  q.k.a = (float)h->a;
+  q.k.b = (float)h->b;
+  q.k.c = (float)h->c;
+  q.k.beta = (float)h->momentum;
+  q.k.omb = (float)(1.0 - h->momentum);
+  q.k.eps = (float)h->eps;
+  q.k.wd = (float)h->weight_decay;
+  q.k.size = (float)h->update_scale;
+  q.k.nesterov = (h->flags & LAMB_MUON_FLAG_NESTEROV) != 0;
+  q.k.scale_kind = h->scale_kind;
+  typedef __nv_bfloat16 bf;
+  if (d_lr && p->grad_bf16)
+    muon_small<bf, true>(p, q.ptrs, q.k, h->steps, d_lr, stream);
+  else if (d_lr)
+    muon_small<float, true>(p, q.ptrs, q.k, h->steps, d_lr, stream);
+  else if (p->grad_bf16)
+    muon_small<bf, false>(p, q.ptrs, q.k, h->steps, d_lr, stream);
+  else
+    muon_small<float, false>(p, q.ptrs, q.k, h->steps, d_lr, stream);
+  const cudaError_t es = cudaGetLastError();
+  if (es != cudaSuccess) return lm_cuda_fail(es, "muon launch");
+  for (const MuonGroup& g : p->groups) {
+    if (d_lr) {
+      if (p->grad_bf16)
+        muon_front<__nv_bfloat16, true>(p, q.ptrs, g, q.k, stream);
+      else
+        muon_front<float, true>(p, q.ptrs, g, q.k, stream);
+    } else {
+      if (p->grad_bf16)
+        muon_front<__nv_bfloat16, false>(p, q.ptrs, g, q.k, stream);
+      else
+        muon_front<float, false>(p, q.ptrs, g, q.k, stream);
+    }
+    cudaError_t e = cudaGetLastError();
+    for (int i = 0; e == cudaSuccess && i < h->steps; ++i) {
+      q.from = i & 1;
+      q.last = i == h->steps - 1;
+      e = muon_product<MuonWork<kGram>>(p, q, g.sym0, g.sym, stream);
+      if (e == cudaSuccess)
+        e = muon_product<MuonWork<kSquare>>(p, q, g.sq0, g.sym, stream);
+      if (e == cudaSuccess)
+        e = muon_product<MuonWork<kApply>>(p, q, g.app0, g.app, stream);
+    }
+    if (e != cudaSuccess) return lm_cuda_fail(e, "muon launch");
+  }
+  return LAMB_OK;
+}
+
+lamb_status_t upload_ptrs(lamb_muon* p, MuonPtrs* to,
+                          const std::vector<MuonPtrs>& h, cudaStream_t stream) {
+  LmDevice dev(p->device);
+  cudaError_t e = dev.err;
+  if (e == cudaSuccess)
+    e = cudaMemcpyAsync(to, h.data(), h.size() * sizeof(MuonPtrs),
+                        cudaMemcpyHostToDevice, stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+  return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "muon bind");
+}
+
+}  // namespace
+
+extern "C" lamb_status_t lamb_muon_create(
+    const int64_t* rows, const int64_t* cols, int32_t n_matrices,
+    const uint8_t* decay_mask, int32_t grad_dtype, int32_t copy_dtype,
+    int32_t device, struct lamb_muon** out) {
+  if (!out) return lm_fail(LAMB_ERR_INVALID_ARG, "out is NULL");
+  *out = nullptr;
+  if (!rows || !cols || n_matrices < 1)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "need n_matrices >= 1, rows and cols");
+  if (grad_dtype != LAMB_F32 && grad_dtype != LAMB_BF16)
+    return lm_fail(LAMB_ERR_UNSUPPORTED_DTYPE, "grad_dtype %d unsupported",
+                   grad_dtype);
+  if (copy_dtype != LAMB_DTYPE_NONE && copy_dtype != LAMB_BF16)
+    return lm_fail(LAMB_ERR_UNSUPPORTED_DTYPE, "copy_dtype %d unsupported",
+                   copy_dtype);
+  if (device < 0) return lm_fail(LAMB_ERR_INVALID_ARG, "device < 0");
+  int64_t total = 0;
+  for (int k = 0; k < n_matrices; ++k) {
+    if (rows[k] < 0 || cols[k] < 0 || rows[k] > (1 << 20) ||
+        cols[k] > (1 << 20))
+      return lm_fail(LAMB_ERR_INVALID_ARG,
+                     "matrix %d: sides are not in [0, 2^20]", k);
+    if (std::min(rows[k], cols[k]) > (1 << 15))
+      return lm_fail(LAMB_ERR_INVALID_ARG,
+                     "matrix %d: the shorter side is above 2^15", k);
+    total += rows[k] * cols[k];
+    if (total > (1ll << 36))
+      return lm_fail(LAMB_ERR_INVALID_ARG, "more than 2^36 elements");
+  }
+  LmDevice dev(device);
+  if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");
+  lamb_muon* p = nullptr;
+  cudaError_t e = cudaSuccess;
+  const char* what = "muon plan";
+  try {
+    p = new lamb_muon;
+    p->device = device;
+    p->n = n_matrices;
+    p->grad_bf16 = grad_dtype == LAMB_BF16;
+    p->copy = copy_dtype == LAMB_BF16;
+    for (int k = 0; k < n_matrices; ++k) p->numel.push_back(rows[k] * cols[k]);
+    MuonLayout L;
+    muon_layout(rows, cols, n_matrices, decay_mask, &L, &p->groups);
+    const EncodeTiled encode = lm_encoder();
+    e = cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = muon_smem<MuonWork<kGram>>();
+    if (e == cudaSuccess) e = muon_smem<MuonWork<kSquare>>();
+    if (e == cudaSuccess) e = muon_smem<MuonWork<kApply>>();
+    LmArena a;
+    for (int pass = 0; e == cudaSuccess && pass < 2; ++pass) {
+      a.used = 0;
+      a.take(&p->status, 1);
+      a.take(&p->mats, n_matrices);
+      a.take(&p->ptrs, n_matrices);
+      a.take(&p->dir_ptrs, n_matrices);
+      a.take(&p->chunks, (int64_t)L.chunks.size());
+      a.take(&p->tiles, (int64_t)L.tiles.size());
+      a.take(&p->part, (int64_t)L.chunks.size());
+      a.take(&p->small, (int64_t)L.small.size());
+      if (pass == 0) {
+        e = cudaMalloc(&p->arena, a.used);
+        a.base = (char*)p->arena;
+      }
+    }
+    if (e == cudaSuccess && L.work_bytes)
+      e = cudaMalloc(&p->work, (size_t)L.work_bytes);
+    bool ok = encode != nullptr;
+    char* base = (char*)p->work;
+    for (int k = 0; e == cudaSuccess && ok && k < n_matrices; ++k) {
+      MuonMatrix& x = L.mats[k];
+      if (!x.m) continue;
+      for (int i = 0; i < 2; ++i) {
+        x.hi[i] = (__half*)(base + L.at[i][k]);
+        ok = ok && lm_map(encode, &x.x_k[i], false, x.hi[i], x.rows, x.cols,
+                          x.pitch, kTileM) &&
+             lm_map(encode, &x.x_mn[i], false, x.hi[i], x.rows, x.cols, x.pitch,
+                    kTileK);
+      }
+      x.lo = (__half*)(base + L.at[2][k]);
+      x.D = (__half*)(base + L.at[3][k]);
+      x.E = (__half*)(base + L.at[4][k]);
+      x.diag = (float*)(base + L.at[5][k]);
+      x.beta = (float*)(base + L.at[6][k]);
+      ok = ok &&
+           lm_map(encode, &x.lo_k, false, x.lo, x.rows, x.cols, x.pitch,
+                  kTileM) &&
+           lm_map(encode, &x.d, false, x.D, x.m, x.m, x.pitch_m, kTileM) &&
+           lm_map(encode, &x.e, false, x.E, x.m, x.m, x.pitch_m, kTileM) &&
+           lm_map(encode, &x.d_t, false, x.D, x.m, x.m, x.pitch_m, 64) &&
+           lm_map(encode, &x.e_t, false, x.E, x.m, x.m, x.pitch_m, 64);
+    }
+    if (e == cudaSuccess && !ok) {
+      e = cudaErrorNotSupported;
+      what = "cuTensorMapEncodeTiled";
+    }
+    p->n_small = (int)L.small.size();
+    for (int k : L.small)
+      p->small_bytes = std::max(p->small_bytes,
+                                small_smem(L.mats[k].m, L.mats[k].n));
+    if (e == cudaSuccess) e = small_smem_limit<__nv_bfloat16, true>(p->small_bytes);
+    if (e == cudaSuccess) e = small_smem_limit<__nv_bfloat16, false>(p->small_bytes);
+    if (e == cudaSuccess) e = small_smem_limit<float, true>(p->small_bytes);
+    if (e == cudaSuccess) e = small_smem_limit<float, false>(p->small_bytes);
+    if (e == cudaSuccess && p->n_small)
+      e = cudaMemcpy(p->small, L.small.data(), L.small.size() * sizeof(int),
+                     cudaMemcpyHostToDevice);
+    if (e == cudaSuccess) e = cudaMemset(p->status, 0, sizeof(uint32_t));
+    if (e == cudaSuccess)
+      e = cudaMemcpy(p->mats, L.mats.data(), L.mats.size() * sizeof(MuonMatrix),
+                     cudaMemcpyHostToDevice);
+    if (e == cudaSuccess && !L.chunks.empty())
+      e = cudaMemcpy(p->chunks, L.chunks.data(),
+                     L.chunks.size() * sizeof(MuonChunk),
+                     cudaMemcpyHostToDevice);
+    if (e == cudaSuccess && !L.tiles.empty())
+      e = cudaMemcpy(p->tiles, L.tiles.data(),
+                     L.tiles.size() * sizeof(MuonTile), cudaMemcpyHostToDevice);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  } catch (const std::bad_alloc&) {
+    lamb_muon_destroy(p);
+    return lm_fail(LAMB_ERR_OOM, "host allocation failed");
+  }
+  if (e != cudaSuccess) {
+    lamb_muon_destroy(p);
+    return lm_cuda_fail(e, what);
+  }
+  *out = p;
+  return LAMB_OK;
+}
+
+extern "C" lamb_status_t lamb_muon_bind(struct lamb_muon* p, void* const* w,
+                                        const void* const* g, void* const* m,
+                                        void* const* w_copy,
+                                        cudaStream_t stream) {
+  if (!p) return lm_fail(LAMB_ERR_INVALID_ARG, "plan is NULL");
+  if (!w || !g || !m)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "w, g and m are required");
+  if (p->copy != (w_copy != nullptr))
+    return lm_fail(LAMB_ERR_INVALID_ARG,
+                   "w_copy is required iff the plan has a bf16 copy");
+  try {
+    std::vector<MuonPtrs> h(p->n);
+    for (int k = 0; k < p->n; ++k) {
+      h[k] = {(float*)w[k], g[k], (float*)m[k],
+              w_copy ? (__nv_bfloat16*)w_copy[k] : nullptr};
+      if (!p->numel[k]) continue;
+      if (!w[k] || !g[k] || !m[k] || (w_copy && !w_copy[k]))
+        return lm_fail(LAMB_ERR_INVALID_ARG, "matrix %d: a pointer is NULL", k);
+      if ((uintptr_t)w[k] % 4 || (uintptr_t)m[k] % 4 ||
+          (uintptr_t)g[k] % (p->grad_bf16 ? 2 : 4) ||
+          (w_copy && (uintptr_t)w_copy[k] % 2))
+        return lm_fail(LAMB_ERR_INVALID_ARG,
+                       "matrix %d: a pointer is not aligned", k);
+    }
+    const lamb_status_t st = upload_ptrs(p, p->ptrs, h, stream);
+    if (st == LAMB_OK) p->bound = true;
+    return st;
+  } catch (const std::bad_alloc&) {
+    return lm_fail(LAMB_ERR_OOM, "host allocation failed");
+  }
+}
+
+extern "C" lamb_status_t lamb_muon_bind_direction(struct lamb_muon* p,
+                                                  const void* const* u,
+                                                  void* const* o,
+                                                  cudaStream_t stream) {
+  if (!p) return lm_fail(LAMB_ERR_INVALID_ARG, "plan is NULL");
+  if (!u || !o) return lm_fail(LAMB_ERR_INVALID_ARG, "u and o are required");
+  try {
+    std::vector<MuonPtrs> h(p->n);
+    for (int k = 0; k < p->n; ++k) {
+      h[k] = {nullptr, u[k], nullptr, (__nv_bfloat16*)o[k]};
+      if (!p->numel[k]) continue;
+      if (!u[k] || !o[k])
+        return lm_fail(LAMB_ERR_INVALID_ARG, "matrix %d: a pointer is NULL", k);
+      if ((uintptr_t)u[k] % (p->grad_bf16 ? 2 : 4) || (uintptr_t)o[k] % 2)
+        return lm_fail(LAMB_ERR_INVALID_ARG,
+                       "matrix %d: a pointer is not aligned", k);
+    }
+    const lamb_status_t st = upload_ptrs(p, p->dir_ptrs, h, stream);
+    if (st == LAMB_OK) p->bound_direction = true;
+    return st;
+  } catch (const std::bad_alloc&) {
+    return lm_fail(LAMB_ERR_OOM, "host allocation failed");
+  }
+}
+
+extern "C" lamb_status_t lamb_muon_step(struct lamb_muon* p,
+                                        const lamb_muon_hyper_t* hyper,
+                                        const float* d_lr,
+                                        cudaStream_t stream) {
+  lamb_status_t st = muon_check(p, hyper);
+  if (st != LAMB_OK) return st;
+  if (!d_lr) return lm_fail(LAMB_ERR_INVALID_ARG, "d_lr is NULL");
+  if (!p->bound)
+    return lm_fail(LAMB_ERR_NOT_BOUND, "lamb_muon_step before lamb_muon_bind");
+  return muon_run(p, hyper, d_lr, stream);
+}
+
+extern "C" lamb_status_t lamb_muon_direction(struct lamb_muon* p,
+                                             const lamb_muon_hyper_t* hyper,
+                                             cudaStream_t stream) {
+  lamb_status_t st = muon_check(p, hyper);
+  if (st != LAMB_OK) return st;
+  if (!p->bound_direction)
+    return lm_fail(LAMB_ERR_NOT_BOUND,
+                   "lamb_muon_direction before lamb_muon_bind_direction");
+  return muon_run(p, hyper, nullptr, stream);
+}
+
+extern "C" lamb_status_t lamb_muon_query(struct lamb_muon* p,
+                                         uint32_t* status_bits, int32_t clear,
+                                         cudaStream_t stream) {
+  if (!p) return lm_fail(LAMB_ERR_INVALID_ARG, "plan is NULL");
+  if (!status_bits)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "status_bits is NULL");
+  LmDevice dev(p->device);
+  cudaError_t e = dev.err;
+  if (e == cudaSuccess)
+    e = cudaMemcpyAsync(status_bits, p->status, sizeof(uint32_t),
+                        cudaMemcpyDeviceToHost, stream);
+  if (e == cudaSuccess && clear)
+    e = cudaMemsetAsync(p->status, 0, sizeof(uint32_t), stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+  return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "status query");
+}
+
+extern "C" lamb_status_t lamb_muon_destroy(struct lamb_muon* p) {
+  if (!p) return LAMB_OK;
+  LmDevice dev(p->device);
+  cudaError_t e = dev.err;
+  if (e == cudaSuccess) e = cudaFree(p->arena);
+  if (e == cudaSuccess) e = cudaFree(p->work);
+  delete p;
+  return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "cudaFree(plan)");
+}

@@ -33,6 +33,13 @@ __device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity,
   return true;
 }
 
+// Waits, whatever happened, for a copy that was issued.
+__device__ __forceinline__ void settle(uint64_t* bar, uint32_t parity) {
+  const uint64_t begin = global_ns();
+  while (!mbar_try(bar, parity))
+    if (global_ns() - begin > kWaitLimitNs) return;
+}
+
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_lane() {
   uint32_t ok;
@@ -55,6 +62,41 @@ __device__ __forceinline__ void tile_load(uint32_t smem, const CUtensorMap* map,
       ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
       ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
       : "memory");
+}
+
+// Shared memory to a tensor; part of the thread's open group of stores.
+__device__ __forceinline__ void tile_store(const CUtensorMap* map, int x, int y,
+                                           uint32_t smem) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group "
+      "[%0, {%1, %2}], [%3];"
+      ::"l"(map), "r"(x), "r"(y), "r"(smem)
+      : "memory");
+}
+__device__ __forceinline__ void stores_commit() {
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// All but the thread's newest kNewest groups have read shared memory.
+template <int kNewest>
+__device__ __forceinline__ void stores_have_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kNewest) : "memory");
+}
+__device__ __forceinline__ void stores_done() {
+  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t at, const uint4& v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+               ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void sts2(uint32_t at, uint16_t v) {
+  asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory");
 }
 
 // ---- products ---------------------------------------------------------------
