@@ -8,25 +8,34 @@
 //
 // Gradient: the token positions are sorted by id (stable, least significant
 // digit first, 8 bits a pass), so that every word's rows are added in the order
-// of the tokens, the same in each run, and every row of dE is written once.
-// Ids are Zipf-like: most words have few tokens, a handful (a mask token) have
-// thousands.  Up to kLongRow tokens a word is summed by the warp that writes
-// its row; a longer one is cut at every kChunk-th sorted position into partial
-// sums of fixed length, which that warp adds in their order.  Sums are fp32.
+// of the tokens, the same in each run.  The sorted list is cut every kChunk
+// positions, whatever the words: ids are Zipf-like, most words have few tokens and
+// a mask token thousands.  A chunk writes the rows of the words that lie inside it
+// and leaves the sum of a word that goes on; one more launch adds those, in order.
+// Rows of words without a token are cleared by other CTAs of the same launch.
+// Sums are fp32.
+//
+// Launches follow one another early (griddepcontrol): count, a move for each digit
+// (which counts the next digit), sums, joins.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
+#include "lamb_sync.cuh"
 #include "lm_vocab.h"
 
 namespace lamb {
 namespace {
 
 constexpr int kEmbedThreads = 256;
-constexpr int kSortThreads = 256;
-constexpr int kSortItems = 16;                      // keys of a thread
-constexpr int kSortTile = kSortThreads * kSortItems;
+constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kChunk = 128;                         // sorted positions
-constexpr int kLongRow = kChunk;
+constexpr int kSortTiles = 128;        // at most: each reads all tiles' counts
+constexpr int kChunk = 32;             // sorted positions
+constexpr int kClearRows = 64;         // rows of the table a clearing CTA looks at
+constexpr int kJoinThreads = 256;
+constexpr int kJoinParts = 4;          // threads that share a long join's columns
+constexpr int kJoinLong = 16;          // chunks of a long join
 constexpr uint32_t kStatusBadIndex = LAMB_STATUS_BAD_INDEX;
 
 __device__ __forceinline__ float load1(const float* p) { return *p; }
@@ -96,224 +105,294 @@ __device__ __forceinline__ uint32_t key_of(int64_t id, int64_t vocab,
   return id < 0 || id >= vocab ? (uint32_t)vocab : (uint32_t)id;
 }
 
-// How many keys of each tile have each value of the digit.
+// How many keys of each tile have each value of the first digit; clears what the
+// moves count in.  A tile is kSortWarps runs of 32 * rounds keys, a warp's each.
 __global__ void __launch_bounds__(kSortThreads)
-digit_count_kernel(const int64_t* ids, const uint32_t* keys, int64_t n,
-                   int64_t vocab, int shift, int32_t* hist, int tiles,
+digit_count_kernel(const int64_t* ids, int n, int64_t vocab, int rounds,
+                   int passes, int32_t* hist, uint32_t* seen,
                    uint32_t* status) {
   __shared__ int32_t count[256];
-  count[threadIdx.x] = 0;
+  let_next_launch();
+  if (threadIdx.x < 256) count[threadIdx.x] = 0;
   __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortTile;
-  for (int i = 0; i < kSortItems; ++i) {
-    const int64_t at = base + i * kSortThreads + threadIdx.x;
-    if (at < n) {
-      const uint32_t key = ids ? key_of(ids[at], vocab, status) : keys[at];
-      atomicAdd(&count[(key >> shift) & 255u], 1);
-    }
-  }
+  const int tile = kSortThreads * rounds;
+  const int64_t base = (int64_t)blockIdx.x * tile;
+  for (int i = threadIdx.x; i < tile && base + i < n; i += kSortThreads)
+    atomicAdd(&count[key_of(ids[base + i], vocab, status) & 255u], 1);
+  const int64_t words = (vocab + 31) / 32;
+  for (int64_t w = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; w < words;
+       w += (int64_t)gridDim.x * kSortThreads)
+    seen[w] = 0;
   __syncthreads();
-  hist[(int64_t)threadIdx.x * tiles + blockIdx.x] = count[threadIdx.x];
+  for (int i = threadIdx.x; i < 256 * passes; i += kSortThreads)
+    hist[((int64_t)(i >> 8) * kSortTiles + blockIdx.x) * 256 + (i & 255)] =
+        i < 256 ? count[i] : 0;
 }
 
-// Exclusive sums in place, one CTA.
-__global__ void __launch_bounds__(1024) scan_kernel(int32_t* x, int64_t n) {
-  __shared__ int32_t warp_sum[32];
-  __shared__ int32_t carry;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (threadIdx.x == 0) carry = 0;
-  __syncthreads();
-  for (int64_t base = 0; base < n; base += 1024) {
-    const int64_t at = base + threadIdx.x;
-    const int32_t v = at < n ? x[at] : 0;
-    int32_t s = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int32_t y = __shfl_up_sync(0xffffffffu, s, o);
-      if (lane >= o) s += y;
-    }
-    if (lane == 31) warp_sum[warp] = s;
-    __syncthreads();
-    if (warp == 0) {
-      int32_t w = warp_sum[lane];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int32_t y = __shfl_up_sync(0xffffffffu, w, o);
-        if (lane >= o) w += y;
-      }
-      warp_sum[lane] = w;
-    }
-    __syncthreads();
-    const int32_t before = carry + (warp ? warp_sum[warp - 1] : 0);
-    if (at < n) x[at] = before + s - v;
-    __syncthreads();
-    if (threadIdx.x == 0) carry += warp_sum[31];
-    __syncthreads();
-  }
-}
-
-// Moves a tile's keys to their places: hist holds where the tile's first key
-// of each digit goes.  A warp takes consecutive keys, 32 at a time in order, so
-// that equal digits keep their order.
+// Moves a tile's keys to their places in the order of one digit, equal digits in
+// the order they had, and counts the next digit of the new tiles.
 __global__ void __launch_bounds__(kSortThreads)
 digit_move_kernel(const int64_t* ids, const uint32_t* keys, const int32_t* pos,
-                  int64_t n, int64_t vocab, int shift, const int32_t* hist,
-                  int tiles, uint32_t* keys_out, int32_t* pos_out,
-                  uint32_t* status) {
+                  int n, int64_t vocab, int rounds, int shift,
+                  const int32_t* hist, int32_t* next_hist, uint32_t* keys_out,
+                  int32_t* pos_out, uint32_t* seen, uint32_t* status) {
   __shared__ int32_t count[kSortWarps][256];
+  __shared__ int32_t half[2][2][256];      // [half][before the tile, in all]
+  __shared__ int32_t scan[256];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int i = threadIdx.x; i < kSortWarps * 256; i += kSortThreads)
     count[i >> 8][i & 255] = 0;
-  __syncthreads();
-  const int64_t base =
-      (int64_t)blockIdx.x * kSortTile + warp * (kSortItems * 32);
-  uint32_t key[kSortItems];
-  int32_t rank[kSortItems];
-#pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const int64_t at = base + i * 32 + lane;
-    const bool in = at < n;
-    key[i] = !in ? 0u : ids ? key_of(ids[at], vocab, status) : keys[at];
-    const uint32_t digit = in ? (key[i] >> shift) & 255u : 256u;
-    const uint32_t same = __match_any_sync(0xffffffffu, digit);
-    const int before = __popc(same & ((1u << lane) - 1u));
-    rank[i] = 0;
-    if (in) rank[i] = count[warp][digit] + before;
-    __syncwarp();
-    if (in && before == 0) count[warp][digit] += __popc(same);
-    __syncwarp();
+  let_next_launch();
+  after_prior_launch();
+  {   // all tiles' counts of a digit, half of the tiles a thread
+    const int d = threadIdx.x & 255, h = threadIdx.x >> 8;
+    const int tiles = gridDim.x, mid = (tiles + 1) / 2;
+    int before = 0, total = 0;
+#pragma unroll 16
+    for (int t = h * mid; t < (h ? tiles : mid); ++t) {
+      const int c = hist[t * 256 + d];
+      total += c;
+      if (t < (int)blockIdx.x) before += c;
+    }
+    half[h][0][d] = before;
+    half[h][1][d] = total;
   }
   __syncthreads();
-  {   // where each warp's keys of a digit start
-    int32_t at = hist[(int64_t)threadIdx.x * tiles + blockIdx.x];
+  const int64_t base =
+      ((int64_t)blockIdx.x * kSortWarps + warp) * (rounds * 32);
+  for (int i = 0; i < rounds; ++i) {
+    const int64_t at = base + i * 32 + lane;
+    const bool in = at < n;
+    const uint32_t key =
+        !in ? 0u : ids ? key_of(ids[at], vocab, status) : keys[at];
+    const uint32_t digit = in ? (key >> shift) & 255u : 256u;
+    const uint32_t same = __match_any_sync(0xffffffffu, digit);
+    if (in && (same & ((1u << lane) - 1u)) == 0)
+      count[warp][digit] += __popc(same);
+    __syncwarp();
+  }
+  // exclusive sum over the digits, by the first warps
+  int total = 0;
+  if (threadIdx.x < 256) {
+    total = half[0][1][threadIdx.x] + half[1][1][threadIdx.x];
+    int s = total;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += y;
+    }
+    scan[threadIdx.x] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x < 256) {
+    int at = scan[threadIdx.x] - total;
+    for (int w = 0; w < warp; ++w) at += scan[w * 32 + 31];
+    at += half[0][0][threadIdx.x] + half[1][0][threadIdx.x];
     for (int w = 0; w < kSortWarps; ++w) {
-      const int32_t c = count[w][threadIdx.x];
+      const int c = count[w][threadIdx.x];
       count[w][threadIdx.x] = at;
       at += c;
     }
   }
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
+  const int tile = kSortThreads * rounds;
+  for (int i = 0; i < rounds; ++i) {
     const int64_t at = base + i * 32 + lane;
-    if (at >= n) continue;
-    const int32_t to = count[warp][(key[i] >> shift) & 255u] + rank[i];
-    keys_out[to] = key[i];
+    const bool in = at < n;
+    const uint32_t key =
+        !in ? 0u : ids ? key_of(ids[at], vocab, status) : keys[at];
+    const uint32_t digit = in ? (key >> shift) & 255u : 256u;
+    const uint32_t same = __match_any_sync(0xffffffffu, digit);
+    const int before = __popc(same & ((1u << lane) - 1u));
+    int to = 0;
+    if (in) to = count[warp][digit] + before;
+    __syncwarp();
+    if (in && before == 0) count[warp][digit] += __popc(same);
+    __syncwarp();
+    if (!in) continue;
+    keys_out[to] = key;
     pos_out[to] = pos ? pos[at] : (int32_t)at;
+    if (ids && key < (uint32_t)vocab) atomicOr(&seen[key >> 5], 1u << (key & 31));
+    if (next_hist)
+      atomicAdd(&next_hist[to / tile * 256 + ((key >> (shift + 8)) & 255u)], 1);
   }
-}
-
-// start[v]: first sorted position with a key of v or above.
-__global__ void __launch_bounds__(256)
-segments_kernel(const uint32_t* keys, int64_t n, int64_t vocab,
-                int32_t* start) {
-  const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (v > vocab) return;
-  int64_t lo = 0, hi = n;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (keys[mid] < (uint32_t)v) lo = mid + 1; else hi = mid;
-  }
-  start[v] = (int32_t)lo;
 }
 
 // ---- sums -------------------------------------------------------------------
-// Sum over sorted positions [a, b) of columns d .. d + 3.
 template <class TG, bool kVec>
-__device__ __forceinline__ void sum_rows(const TG* grad, int64_t stride,
-                                         const int32_t* pos, int a, int b,
-                                         int d, int width, float (&s)[4]) {
-  s[0] = s[1] = s[2] = s[3] = 0.f;
-#pragma unroll 4
-  for (int i = a; i < b; ++i) {
-    const TG* row = grad + (int64_t)pos[i] * stride;
-    if (kVec) {
-      float x[4];
-      load4(row + d, x);
+__device__ __forceinline__ void load_row(const TG* p, int d, int width,
+                                         float (&x)[4]) {
+  if (kVec) {
+    load4(p + d, x);
+  } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[j] += x[j];
-    } else {
+    for (int j = 0; j < 4; ++j) x[j] = d + j < width ? load1(p + d + j) : 0.f;
+  }
+}
+template <class TT, bool kVec>
+__device__ __forceinline__ void write_row(TT* p, int d, int width,
+                                          const float (&s)[4], float scale,
+                                          bool add) {
+  float x[4] = {0.f, 0.f, 0.f, 0.f};
+  if (add) load_row<TT, kVec>(p, d, width, x);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (d + j < width) s[j] += load1(row + d + j);
-    }
+  for (int j = 0; j < 4; ++j) x[j] = add ? x[j] + s[j] * scale : s[j] * scale;
+  if (kVec) {
+    store4(p + d, x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (d + j < width) store1(p + d + j, x[j]);
   }
 }
 
-// The part that each word with a long row has in chunk blockIdx.x: the word
-// that reaches into the chunk from before it (0) and the one that goes on past
-// its end, or ends with it (1).
-template <class TG, bool kVec>
-__global__ void __launch_bounds__(kEmbedThreads)
-long_rows_kernel(const TG* __restrict__ grad, int64_t stride,
-                 const uint32_t* __restrict__ keys,
-                 const int32_t* __restrict__ pos, int64_t n, int64_t vocab,
-                 const int32_t* __restrict__ start, int width,
-                 float* __restrict__ part) {
-  const int64_t c0 = (int64_t)blockIdx.x * kChunk;
-  const int64_t c1 = min(c0 + kChunk, n);
-  const uint32_t first = keys[c0], last = keys[c1 - 1];
-  for (int which = 0; which < 2; ++which) {
-    const uint32_t v = which ? last : first;
-    if (which && last == first) break;
-    if (v >= (uint32_t)vocab) continue;
-    const int64_t a = start[v], b = start[v + 1];
-    if (b - a <= kLongRow) continue;
-    const int from = (int)max(a, c0), to = (int)min(b, c1);
-    for (int d = threadIdx.x * 4; d < width; d += kEmbedThreads * 4) {
-      float s[4];
-      sum_rows<TG, kVec>(grad, stride, pos, from, to, d, width, s);
-      float* p = part + ((int64_t)blockIdx.x * 2 + which) * width + d;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (d + j < width) p[j] = s[j];
-    }
-  }
-}
-
-// One warp for each row of the table.
+// tx threads take a chunk's rows, four columns each; kEmbedThreads / tx chunks a
+// CTA.  The CTAs past the chunks clear rows without a token.
 template <class TG, class TT, bool kVec>
 __global__ void __launch_bounds__(kEmbedThreads)
-embed_grad_kernel(const TG* __restrict__ grad, int64_t stride,
+embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
                   const uint32_t* __restrict__ keys,
-                  const int32_t* __restrict__ pos,
-                  const int32_t* __restrict__ start, int64_t vocab, int width,
-                  const float* __restrict__ part, float scale, bool add,
-                  TT* __restrict__ out, int64_t out_stride) {
-  const int lane = threadIdx.x & 31;
-  const int64_t v =
-      (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5);
-  if (v >= vocab) return;
-  const int a = start[v], b = start[v + 1];
-  if (a == b && add) return;
-  TT* dst = out + v * out_stride;
-  for (int d = lane * 4; d < width; d += 128) {
-    float s[4];
-    if (b - a <= kLongRow) {
-      sum_rows<TG, kVec>(grad, stride, pos, a, b, d, width, s);
-    } else {
-      s[0] = s[1] = s[2] = s[3] = 0.f;
-      for (int c = a / kChunk; c <= (b - 1) / kChunk; ++c) {
-        const int which = keys[(int64_t)c * kChunk] == (uint32_t)v ? 0 : 1;
-        const float* p = part + ((int64_t)c * 2 + which) * width + d;
+                  const int32_t* __restrict__ pos, int n, int64_t vocab,
+                  int width, int tx, int chunk_ctas,
+                  const uint32_t* __restrict__ seen, float* __restrict__ part,
+                  float scale, bool add, TT* __restrict__ out,
+                  int64_t out_stride) {
+  __shared__ uint32_t sh_key[kEmbedThreads * 2 + 2];
+  __shared__ int32_t sh_pos[kEmbedThreads * 2];
+  static_assert(kEmbedThreads / 16 * kChunk <= kEmbedThreads * 2,
+                "the keys of a CTA's chunks");
+  let_next_launch();
+  after_prior_launch();
+  if ((int)blockIdx.x >= chunk_ctas) {
+    const int64_t v0 = (int64_t)(blockIdx.x - chunk_ctas) * kClearRows;
+    for (int r = threadIdx.x >> 5; r < kClearRows; r += kEmbedThreads / 32) {
+      const int64_t v = v0 + r;
+      if (v >= vocab || (n && (seen[v >> 5] >> (v & 31) & 1u))) continue;
+      TT* dst = out + v * out_stride;
+      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int d = (threadIdx.x & 31) * 4; d < width; d += 128)
+        write_row<TT, kVec>(dst, d, width, zero, 1.f, false);
+    }
+    return;
+  }
+  const int ty = kEmbedThreads / tx;
+  const int chunk0 = blockIdx.x * ty, first = chunk0 * kChunk;
+  const int held = min(ty * kChunk, n - first);
+  const int y = threadIdx.x / tx, x0 = threadIdx.x % tx;
+  const uint32_t none = 0xffffffffu;
+  for (int i = threadIdx.x; i < held; i += kEmbedThreads) {
+    sh_key[i + 1] = keys[first + i];
+    sh_pos[i] = pos[first + i];
+  }
+  if (threadIdx.x == 0) {
+    sh_key[0] = first ? keys[first - 1] : none;
+    sh_key[held + 1] = first + held < n ? keys[first + held] : none;
+  }
+  __syncthreads();
+  const int at0 = y * kChunk;                       // inside the CTA's keys
+  const int m = min(kChunk, held - at0);
+  if (m <= 0) return;
+  float* const mine = part + (int64_t)(chunk0 + y) * 2 * width;
+  auto key_at = [&](int i) -> uint32_t {            // -1 .. m: with neighbours
+    return sh_key[at0 + i + 1];
+  };
+  for (int d = x0 * 4; d < width; d += tx * 4) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    bool from_before = key_at(-1) == key_at(0);
+    for (int i0 = 0; i0 < m; i0 += 8) {
+      float x[8][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (d + j < width) s[j] += p[j];
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + u;
+        x[u][0] = x[u][1] = x[u][2] = x[u][3] = 0.f;
+        if (i < m && key_at(i) < (uint32_t)vocab)
+          load_row<TG, kVec>(grad + (int64_t)sh_pos[at0 + i] * stride, d, width,
+                             x[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + u;
+        if (i >= m) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] += x[u][j];
+        const uint32_t key = key_at(i);
+        const bool goes_on = key_at(i + 1) == key;
+        if (goes_on && i + 1 < m) continue;
+        if (key < (uint32_t)vocab) {
+          if (!from_before && !goes_on)
+            write_row<TT, kVec>(out + (int64_t)key * out_stride, d, width, s,
+                                scale, add);
+          else
+            write_row<float, kVec>(mine + (from_before ? 0 : width), d, width,
+                                   s, 1.f, false);
+        }
+        s[0] = s[1] = s[2] = s[3] = 0.f;
+        from_before = false;
       }
     }
-    if (kVec) {
-      float x[4] = {0.f, 0.f, 0.f, 0.f};
-      if (add) load4(dst + d, x);
+  }
+}
+
+// The words that go on past the chunk they begin in: the CTA of that chunk adds
+// the chunks' sums: in their order or, of a long word, in kJoinParts runs that are
+// added in order.
+template <class TT, bool kVec>
+__global__ void __launch_bounds__(kJoinThreads)
+embed_join_kernel(const uint32_t* __restrict__ keys, int n, int64_t vocab,
+                  int width, const float* __restrict__ part, float scale,
+                  bool add, TT* __restrict__ out, int64_t out_stride) {
+  __shared__ float4 sh[kJoinThreads];
+  after_prior_launch();
+  const int c = blockIdx.x;
+  const int64_t last = (int64_t)c * kChunk + kChunk - 1;
+  if (last + 1 >= n) return;
+  const uint32_t v = keys[last];
+  if (v >= (uint32_t)vocab || keys[last + 1] != v) return;
+  const int64_t first = (int64_t)c * kChunk;
+  if (first > 0 && keys[first] == v && keys[first - 1] == v) return;
+  // the last chunk with the word: doubling steps, then halving ones
+  const int chunks = (n + kChunk - 1) / kChunk;
+  int lo = c + 1, step = 1;
+  while (lo + step < chunks && keys[(int64_t)(lo + step) * kChunk] == v) {
+    lo += step;
+    step <<= 1;
+  }
+  for (; step > 0; step >>= 1)
+    if (lo + step < chunks && keys[(int64_t)(lo + step) * kChunk] == v)
+      lo += step;
+  const int count = lo - c;               // chunks after this one
+  const int parts = count > kJoinLong ? kJoinParts : 1;
+  const int wide = kJoinThreads / parts;
+  const int g = threadIdx.x / wide, x = threadIdx.x % wide;
+  const int a = (int)((int64_t)count * g / parts);
+  const int b = (int)((int64_t)count * (g + 1) / parts);
+  TT* dst = out + (int64_t)v * out_stride;
+  for (int d0 = 0; d0 < width; d0 += wide * 4) {
+    const int d = d0 + x * 4;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (d < width) {
+      if (g == 0)
+        load_row<float, kVec>(part + ((int64_t)c * 2 + 1) * width, d, width, s);
+#pragma unroll 16
+      for (int k = a; k < b; ++k) {
+        float y[4];
+        load_row<float, kVec>(part + (int64_t)(c + 1 + k) * 2 * width, d, width,
+                              y);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = add ? x[j] + s[j] * scale : s[j] * scale;
-      store4(dst + d, x);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (d + j < width)
-          store1(dst + d + j,
-                 add ? load1(dst + d + j) + s[j] * scale : s[j] * scale);
+        for (int j = 0; j < 4; ++j) s[j] += y[j];
+      }
     }
+    if (parts > 1) {
+      sh[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
+      __syncthreads();
+      for (int k = 1; g == 0 && k < parts; ++k) {
+        const float4 y = sh[k * wide + x];
+        s[0] += y.x; s[1] += y.y; s[2] += y.z; s[3] += y.w;
+      }
+    }
+    if (g == 0 && d < width)
+      write_row<TT, kVec>(dst, d, width, s, scale, add);
+    if (parts > 1) __syncthreads();
   }
 }
 
@@ -338,31 +417,34 @@ void launch_embed(const lamb_vocab* v, const void* table, int64_t ts,
 }
 
 template <class TG, class TT, bool kVec>
-void launch_sums(const lamb_vocab* v, const void* grad, int64_t gs, int64_t n,
-                 const uint32_t* keys, const int32_t* pos, float scale,
-                 bool add, void* out, int64_t os, cudaStream_t stream) {
-  if (n > kLongRow)
-    long_rows_kernel<TG, kVec>
-        <<<(unsigned)lm_ceil_div(n, kChunk), kEmbedThreads, 0, stream>>>(
-            (const TG*)grad, gs, keys, pos, n, v->vocab, v->start, v->width,
-            v->part);
-  embed_grad_kernel<TG, TT, kVec>
-      <<<(unsigned)lm_ceil_div(v->vocab, kEmbedThreads / 32), kEmbedThreads, 0,
-         stream>>>((const TG*)grad, gs, keys, pos, v->start, v->vocab, v->width,
-                   v->part, scale, add, (TT*)out, os);
+cudaError_t launch_sums(const lamb_vocab* v, const void* grad, int64_t gs,
+                        int n, int in, float scale, bool add, void* out,
+                        int64_t os, cudaStream_t stream) {
+  // threads of a chunk: its columns, 16 at least
+  int tx = kEmbedThreads;
+  while (tx > 16 && tx / 2 * 4 >= v->width) tx /= 2;
+  const int chunks = (int)lm_ceil_div(n, kChunk);
+  const int ctas = (int)lm_ceil_div(chunks, kEmbedThreads / tx);
+  const int64_t clears = add ? 0 : lm_ceil_div(v->vocab, kClearRows);
+  cudaError_t e = lm_launch(
+      embed_sums_kernel<TG, TT, kVec>, (unsigned)(ctas + clears), kEmbedThreads,
+      0, stream, n > 0, (const TG*)grad, gs, v->keys[in], v->pos[in], n,
+      v->vocab, v->width, tx, ctas, v->seen, v->part, scale, add, (TT*)out, os);
+  if (e == cudaSuccess && chunks > 1)
+    e = lm_launch(embed_join_kernel<TT, kVec>, (unsigned)(chunks - 1),
+                  kJoinThreads, 0, stream, true, v->keys[in], n, v->vocab,
+                  v->width, v->part, scale, add, (TT*)out, os);
+  return e;
 }
 
 template <class TG, class TT>
-void launch_grad(const lamb_vocab* v, const void* grad, int64_t gs, int64_t n,
-                 const uint32_t* keys, const int32_t* pos, float scale,
-                 bool add, void* out, int64_t os, bool vec,
-                 cudaStream_t stream) {
-  if (vec)
-    launch_sums<TG, TT, true>(v, grad, gs, n, keys, pos, scale, add, out, os,
-                              stream);
-  else
-    launch_sums<TG, TT, false>(v, grad, gs, n, keys, pos, scale, add, out, os,
-                               stream);
+cudaError_t launch_grad(const lamb_vocab* v, const void* grad, int64_t gs,
+                        int n, int in, float scale, bool add, void* out,
+                        int64_t os, bool vec, cudaStream_t stream) {
+  return vec ? launch_sums<TG, TT, true>(v, grad, gs, n, in, scale, add, out,
+                                         os, stream)
+             : launch_sums<TG, TT, false>(v, grad, gs, n, in, scale, add, out,
+                                          os, stream);
 }
 
 lamb_status_t check_common(const lamb_vocab* v, const void* a, const char* an,
@@ -397,13 +479,12 @@ void lm_embed_carve(lamb_vocab* v, LmArena* a) {
   const int64_t n = v->max_tokens;
   v->sort_passes = 1;
   while (v->vocab >> (8 * v->sort_passes)) ++v->sort_passes;
-  v->sort_tiles = lm_ceil_div(n, kSortTile);
   for (int i = 0; i < 2; ++i) {
     a->take(&v->keys[i], n);
     a->take(&v->pos[i], n);
   }
-  a->take(&v->hist, 256 * v->sort_tiles);
-  a->take(&v->start, v->vocab + 1);
+  a->take(&v->hist, (int64_t)v->sort_passes * kSortTiles * 256);
+  a->take(&v->seen, lm_ceil_div(v->vocab, 32));
   a->take(&v->part, lm_ceil_div(n, kChunk) * 2 * v->width);
 }
 
@@ -458,39 +539,42 @@ extern "C" lamb_status_t lamb_vocab_embed_grad(
   if (!n_tokens && accumulate) return LAMB_OK;
   LmDevice dev(v->device);
   if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");
-  const int64_t n = n_tokens;
-  const int tiles = (int)lm_ceil_div(n, kSortTile);
+  const int n = (int)n_tokens;
+  const int rounds =
+      (int)std::max<int64_t>(1, lm_ceil_div(n, kSortTiles * kSortThreads));
+  const unsigned tiles = (unsigned)lm_ceil_div(n, kSortThreads * rounds);
+  cudaError_t e = cudaSuccess;
   int in = 0;
-  for (int pass = 0; n && pass < v->sort_passes; ++pass) {
-    const int64_t* src = pass ? nullptr : ids;
-    digit_count_kernel<<<tiles, kSortThreads, 0, stream>>>(
-        src, v->keys[in], n, v->vocab, 8 * pass, v->hist, tiles, v->status);
-    scan_kernel<<<1, 1024, 0, stream>>>(v->hist, 256 * (int64_t)tiles);
-    digit_move_kernel<<<tiles, kSortThreads, 0, stream>>>(
-        src, v->keys[in], pass ? v->pos[in] : nullptr, n, v->vocab, 8 * pass,
-        v->hist, tiles, v->keys[in ^ 1], v->pos[in ^ 1], v->status);
+  if (n)
+    e = lm_launch(digit_count_kernel, tiles, kSortThreads, 0, stream, false,
+                  ids, n, v->vocab, rounds, v->sort_passes, v->hist, v->seen,
+                  v->status);
+  for (int pass = 0; e == cudaSuccess && n && pass < v->sort_passes; ++pass) {
+    int32_t* hist = v->hist + (int64_t)pass * kSortTiles * 256;
+    e = lm_launch(digit_move_kernel, tiles, kSortThreads, 0, stream, true,
+                  pass ? nullptr : ids, v->keys[in], pass ? v->pos[in] : nullptr,
+                  n, v->vocab, rounds, 8 * pass, hist,
+                  pass + 1 < v->sort_passes ? hist + kSortTiles * 256 : nullptr,
+                  v->keys[in ^ 1], v->pos[in ^ 1], v->seen, v->status);
     in ^= 1;
   }
-  segments_kernel<<<(unsigned)lm_ceil_div(v->vocab + 1, 256), 256, 0, stream>>>(
-      v->keys[in], n, v->vocab, v->start);
+  if (e != cudaSuccess) return lm_cuda_fail(e, "sort launch");
   const bool vec = vec_ok(grad_out, grad_dtype, grad_stride, v->width) &&
                    vec_ok(table_grad, table_dtype, table_stride, v->width);
   const float s = (float)scale;
   const bool add = accumulate != 0;
   typedef __nv_bfloat16 bf;
   if (grad_dtype == LAMB_F32 && table_dtype == LAMB_F32)
-    launch_grad<float, float>(v, grad_out, grad_stride, n, v->keys[in],
-                              v->pos[in], s, add, table_grad, table_stride, vec,
-                              stream);
+    e = launch_grad<float, float>(v, grad_out, grad_stride, n, in, s, add,
+                                  table_grad, table_stride, vec, stream);
   else if (grad_dtype == LAMB_F32)
-    launch_grad<float, bf>(v, grad_out, grad_stride, n, v->keys[in], v->pos[in],
-                           s, add, table_grad, table_stride, vec, stream);
+    e = launch_grad<float, bf>(v, grad_out, grad_stride, n, in, s, add,
+                               table_grad, table_stride, vec, stream);
   else if (table_dtype == LAMB_F32)
-    launch_grad<bf, float>(v, grad_out, grad_stride, n, v->keys[in], v->pos[in],
-                           s, add, table_grad, table_stride, vec, stream);
+    e = launch_grad<bf, float>(v, grad_out, grad_stride, n, in, s, add,
+                               table_grad, table_stride, vec, stream);
   else
-    launch_grad<bf, bf>(v, grad_out, grad_stride, n, v->keys[in], v->pos[in], s,
-                        add, table_grad, table_stride, vec, stream);
-  const cudaError_t e = cudaGetLastError();
+    e = launch_grad<bf, bf>(v, grad_out, grad_stride, n, in, s, add, table_grad,
+                            table_stride, vec, stream);
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "embed gradient launch");
 }

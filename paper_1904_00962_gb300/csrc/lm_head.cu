@@ -513,21 +513,37 @@ struct GradsWork {
   }
 };
 
-// dh from its partial sums: a warp a row.
+// dh from its partial sums, kCols columns a thread.
+template <int kCols>
 __global__ void __launch_bounds__(256)
 slabs_kernel(const float* slabs, int count, int64_t slab, int width,
              const int32_t* n_rows, const int32_t* row_token,
              __nv_bfloat16* out, int64_t stride) {
   after_prior_launch();
-  const int rows = *n_rows, lane = threadIdx.x & 31;
-  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows;
-       r += gridDim.x * 8) {
-    __nv_bfloat16* to = out + (int64_t)row_token[r] * stride;
-    for (int d = lane; d < width; d += 32) {
+  const int per = width / kCols;
+  const int64_t n = (int64_t)*n_rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
+       i += (int64_t)gridDim.x * 256) {
+    const int r = (int)(i / per), d = (int)(i - (int64_t)r * per) * kCols;
+    const float* from = slabs + (int64_t)r * width + d;
+    __nv_bfloat16* to = out + (int64_t)row_token[r] * stride + d;
+    if (kCols == 4) {
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+      for (int k = 0; k < count; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(from + k * slab);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+      const __nv_bfloat162 a = __floats2bfloat162_rn(s.x, s.y);
+      const __nv_bfloat162 b = __floats2bfloat162_rn(s.z, s.w);
+      *reinterpret_cast<uint2*>(to) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&a),
+                     *reinterpret_cast<const uint32_t*>(&b));
+    } else {
       float s = 0.f;
-      for (int k = 0; k < count; ++k)
-        s += slabs[k * slab + (int64_t)r * width + d];
-      to[d] = __float2bfloat16_rn(s);
+#pragma unroll 8
+      for (int k = 0; k < count; ++k) s += from[k * slab];
+      *to = __float2bfloat16_rn(s);
     }
   }
 }
@@ -837,7 +853,12 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
     if (e != cudaSuccess) return lm_cuda_fail(e, "head gradient launch");
   }
   if (g.slabs) {
-    slabs_kernel<<<grid_for(n * 32, v->sms), 256, 0, stream>>>(
+    const bool four = v->width % 4 == 0 && g.slab % 4 == 0 &&
+                      (uintptr_t)grad_hidden % 8 == 0 &&
+                      grad_hidden_stride % 4 == 0;
+    const int per = v->width / (four ? 4 : 1);
+    (four ? slabs_kernel<4> : slabs_kernel<1>)<<<grid_for(n * per, v->sms), 256,
+                                                 0, stream>>>(
         v->slabs, g.splits, g.slab, v->width, v->n_rows, v->row_token,
         (__nv_bfloat16*)grad_hidden, grad_hidden_stride);
     e = cudaGetLastError();

@@ -60,6 +60,25 @@ struct LmArena {
 
 inline int lm_elem_size(int dtype) { return dtype == LAMB_F32 ? 4 : 2; }
 
+// Launches a kernel.  after_prior: it may start while the launch in front of it in
+// the stream still runs, and waits for that one itself (after_prior_launch).
+template <class... P, class... A>
+cudaError_t lm_launch(void (*kernel)(P...), unsigned grid, unsigned block,
+                      size_t smem, cudaStream_t stream, bool after_prior,
+                      A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = after_prior ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                 void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*,

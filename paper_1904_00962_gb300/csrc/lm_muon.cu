@@ -287,7 +287,12 @@ struct MuonWork {
                                                    uint32_t buf,
                                                    const Epilogue& epi) {
     const int i = g.a0 + epi.row, m = x.m;
-    const float li = kPhase == kSquare && i < m ? x.diag[i] : 0.f;
+    float* const diag = x.diag;
+    const float s = kPhase == kGram
+                        ? 1.f / (x.scale * x.scale)    // powers of two
+                        : 1.f / (kScaleD * kScaleD);
+    const float li = kPhase == kSquare && i < m ? diag[i] : 0.f;
+    const float pb = p.k.b, pc = p.k.c;
     const bool both = mirror(g, c0);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -295,19 +300,30 @@ struct MuonWork {
       float y[32];
       tmem_ld32(acc + 32 * h, y);
       if (kPhase == kGram) {
-        const float s = 1.f / (x.scale * x.scale);     // a power of two
         if (i >= j0 && i < j0 + 32 && i < m) {
 #pragma unroll
           for (int q = 0; q < 32; ++q)
             if (j0 + q == i) {
-              x.diag[i] = y[q] * s;
+              diag[i] = y[q] * s;
               y[q] = 0.f;
             }
         }
 #pragma unroll
         for (int q = 0; q < 32; ++q) y[q] *= s * kScaleD;
       } else {
-        const float s = 1.f / (kScaleD * kScaleD);
+        // (diag's memory goes up to a whole tile)
+        float l[32];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float4 v = *reinterpret_cast<const float4*>(diag + j0 + 4 * u);
+          l[4 * u] = v.x; l[4 * u + 1] = v.y;
+          l[4 * u + 2] = v.z; l[4 * u + 3] = v.w;
+        }
+        if (i >= j0 && i < j0 + 32 && i < m) {
+#pragma unroll
+          for (int q = 0; q < 32; ++q)
+            if (j0 + q == i) x.beta[i] = pb * li + pc * (li * li + y[q] * s);
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const uint4 d = lds16(unit16(buf, epi.row, 4 * h + u));
@@ -316,17 +332,16 @@ struct MuonWork {
           for (int k = 0; k < 8; ++k) {
             const int q = 8 * u + k;
             const float2 dd2 = half2_at(dw[k >> 1]);
-            const float dd = (k & 1 ? dd2.y : dd2.x) * (1.f / kScaleD);
-            const float lj = x.diag[min(j0 + q, m - 1)];
-            const float sq = y[q] * s;
-            const float sum = li + lj;
-            if (j0 + q == i) {
-              if (i < m) x.beta[i] = p.k.b * li + p.k.c * (li * li + sq);
-              y[q] = 0.f;
-            } else {
-              y[q] = (p.k.b * dd + p.k.c * (sum * dd + sq)) * kScaleE;
-            }
+            const float dd = k & 1 ? dd2.y : dd2.x;
+            // E kScaleE, dd being D kScaleD
+            const float f = fmaf(pc, li + l[q], pb) * (kScaleE / kScaleD);
+            y[q] = fmaf(f, dd, y[q] * (pc * s * kScaleE));
           }
+        }
+        if (i >= j0 && i < j0 + 32) {
+#pragma unroll
+          for (int q = 0; q < 32; ++q)
+            if (j0 + q == i) y[q] = 0.f;
         }
       }
 #pragma unroll
@@ -353,7 +368,10 @@ struct MuonWork {
                                                int c0, uint32_t buf,
                                                const Epilogue& epi) {
     const int r = g.a0 + epi.row;
-    const float br = !x.tall && r < x.rows ? p.k.a + x.beta[r] : 0.f;
+    const bool tall = x.tall, last = p.last;
+    const float* const beta = x.beta;
+    const float pa = p.k.a;
+    const float br = !tall && r < x.rows ? pa + beta[r] : 0.f;
     const float inv = 1.f / x.scale;
     float y[64];
     tmem_ld32(acc, *reinterpret_cast<float(*)[32]>(y));
@@ -365,6 +383,13 @@ struct MuonWork {
       const uint32_t hw[4] = {hi.x, hi.y, hi.z, hi.w};
       const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w};
       uint32_t oh[4], ol[4];
+      float bc[8];         // (beta's memory goes up to a whole tile)
+      if (tall) {
+        const float4* b4 = reinterpret_cast<const float4*>(beta + c0 + 8 * u);
+        const float4 b0 = b4[0], b1 = b4[1];
+        bc[0] = b0.x; bc[1] = b0.y; bc[2] = b0.z; bc[3] = b0.w;
+        bc[4] = b1.x; bc[5] = b1.y; bc[6] = b1.z; bc[7] = b1.w;
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float2 a = half2_at(hw[k]), b = half2_at(lw[k]);
@@ -373,8 +398,7 @@ struct MuonWork {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int q = 8 * u + 2 * k + e;
-          const float f =
-              x.tall ? p.k.a + x.beta[min(c0 + q, x.cols - 1)] : br;
+          const float f = tall ? pa + bc[2 * k + e] : br;
           // in units of 1 / scale
           v[e] = fmaf(f, v[e], y[q] * (1.f / kScaleE));
           y[q] = v[e] * inv;
@@ -383,12 +407,12 @@ struct MuonWork {
         const float2 h = half2_at(oh[k]);
         ol[k] = pack_half2((v[0] - h.x) * kScaleLo, (v[1] - h.y) * kScaleLo);
       }
-      if (!p.last) {
+      if (!last) {
         sts16(ah, make_uint4(oh[0], oh[1], oh[2], oh[3]));
         sts16(al, make_uint4(ol[0], ol[1], ol[2], ol[3]));
       }
     }
-    if (p.last) {
+    if (last) {
       epi.sync();          // everybody has read its inputs
 #pragma unroll
       for (int u = 0; u < 16; ++u)
@@ -482,27 +506,130 @@ __device__ __forceinline__ double block_sum(double s, double* sh) {
   return s;
 }
 
+// Four consecutive values (kVec: by one access; else n of them).
+template <class TG, bool kVec>
+__device__ __forceinline__ void load_grads(const void* p, int64_t i, int n,
+                                           float (&x)[4]) {
+  if (kVec && sizeof(TG) == 4) {
+    const float4 v = *reinterpret_cast<const float4*>(
+        reinterpret_cast<const float*>(p) + i);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  } else if (kVec) {
+    const uint2 v = *reinterpret_cast<const uint2*>(
+        reinterpret_cast<const __nv_bfloat16*>(p) + i);
+    x[0] = __uint_as_float(v.x << 16);
+    x[1] = __uint_as_float(v.x & 0xffff0000u);
+    x[2] = __uint_as_float(v.y << 16);
+    x[3] = __uint_as_float(v.y & 0xffff0000u);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = k < n ? load_grad<TG>(p, i + k) : 0.f;
+  }
+}
+
+// What a vector access needs of a chunk (chunks start at multiples of 4).
+template <class TG, bool kStep>
+__device__ __forceinline__ bool chunk_vec(const MuonPtrs& p, int len) {
+  return len % 4 == 0 && (uintptr_t)p.g % (4 * sizeof(TG)) == 0 &&
+         (!kStep || (uintptr_t)p.m % 16 == 0);
+}
+
+template <class TG, bool kStep, bool kVec>
+__device__ __forceinline__ float norm_chunk(const MuonPtrs& p,
+                                            const MuonChunk& c,
+                                            const MuonConsts& k) {
+  float s = 0.f;
+#pragma unroll 4
+  for (int i = threadIdx.x * 4; i < c.len; i += kMuonThreads * 4) {
+    const int64_t at = c.offset + i;
+    const int n = min(4, c.len - i);
+    float u[4];
+    load_grads<TG, kVec>(p.g, at, n, u);
+    if (kStep) {
+      float m[4];
+      load_grads<float, kVec>(p.m, at, n, m);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        m[q] = fmaf(k.beta, m[q], k.omb * u[q]);
+        u[q] = update_of(k, u[q], m[q]);
+      }
+      if (kVec) {
+        *reinterpret_cast<float4*>(p.m + at) =
+            make_float4(m[0], m[1], m[2], m[3]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q < n) p.m[at + q] = m[q];
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) s = fmaf(u[q], u[q], s);
+  }
+  return s;
+}
+
 // New momentum (kStep) and the sum of squares of a chunk's u.
 template <class TG, bool kStep>
 __global__ void __launch_bounds__(kMuonThreads)
-muon_norm_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
-                 const MuonChunk* chunks, MuonConsts k, double* part) {
+muon_norm_kernel(const MuonPtrs* ptrs, const MuonChunk* chunks, MuonConsts k,
+                 double* part) {
   __shared__ double sh[kMuonThreads / 32];
   const MuonChunk c = chunks[blockIdx.x];
   const MuonPtrs p = ptrs[c.matrix];
-  float s = 0.f;
-  for (int i = threadIdx.x; i < c.len; i += kMuonThreads) {
-    const int64_t at = c.offset + i;
-    float u = load_grad<TG>(p.g, at);
-    if (kStep) {
-      const float m = fmaf(k.beta, p.m[at], k.omb * u);
-      p.m[at] = m;
-      u = update_of(k, u, m);
-    }
-    s = fmaf(u, u, s);
-  }
+  const float s = chunk_vec<TG, kStep>(p, c.len)
+                      ? norm_chunk<TG, kStep, true>(p, c, k)
+                      : norm_chunk<TG, kStep, false>(p, c, k);
   const double sum = block_sum((double)s, sh);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+template <class TG, bool kStep, bool kVec>
+__device__ __forceinline__ void start_chunk(const MuonMatrix& x,
+                                            const MuonPtrs& p,
+                                            const MuonChunk& c,
+                                            const MuonConsts& k, float f) {
+  __half* const hi = x.hi[0];
+  __half* const lo = x.lo;
+  const int cols = x.cols, pitch = x.pitch;
+#pragma unroll 4
+  for (int i = threadIdx.x * 4; i < c.len; i += kMuonThreads * 4) {
+    const int64_t at = c.offset + i;
+    const int n = min(4, c.len - i);
+    float u[4];
+    load_grads<TG, kVec>(p.g, at, n, u);
+    if (kStep) {
+      float m[4];
+      load_grads<float, kVec>(p.m, at, n, m);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) u[q] = update_of(k, u[q], m[q]);
+    }
+    uint32_t h[2], l[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float a = u[2 * q] * f, b = u[2 * q + 1] * f;
+      h[q] = pack_half2(a, b);
+      const float2 r = half2_at(h[q]);
+      l[q] = pack_half2((a - r.x) * kScaleLo, (b - r.y) * kScaleLo);
+    }
+    if (kVec && pitch == cols) {
+      *reinterpret_cast<uint2*>(hi + at) = make_uint2(h[0], h[1]);
+      *reinterpret_cast<uint2*>(lo + at) = make_uint2(l[0], l[1]);
+    } else {
+      int64_t r = at / cols;
+      int col = (int)(at - r * cols);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q >= n) break;
+        const int64_t to = r * pitch + col;
+        hi[to] = __ushort_as_half(half_bits(h[q >> 1], q & 1));
+        lo[to] = __ushort_as_half(half_bits(l[q >> 1], q & 1));
+        if (++col == cols) {
+          col = 0;
+          ++r;
+        }
+      }
+    }
+  }
 }
 
 // X = u / (|u| + eps) as a pair of halves.
@@ -521,18 +648,11 @@ muon_start_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
   const float norm = (float)sqrt(block_sum(s, sh));
   if (threadIdx.x == 0 && !isfinite(norm))
     atomicOr(status, LAMB_STATUS_NONFINITE);
-  const float f = 1.f / (norm + k.eps);
-  for (int i = threadIdx.x; i < c.len; i += kMuonThreads) {
-    const int64_t at = c.offset + i;
-    float u = load_grad<TG>(p.g, at);
-    if (kStep) u = update_of(k, u, p.m[at]);
-    const float v = u * f * x.scale;
-    const int64_t r = at / x.cols;
-    const int64_t to = r * x.pitch + (at - r * x.cols);
-    const __half h = __float2half_rn(v);
-    x.hi[0][to] = h;
-    x.lo[to] = __float2half_rn((v - __half2float(h)) * kScaleLo);
-  }
+  const float f = x.scale / (norm + k.eps);
+  if (chunk_vec<TG, kStep>(p, c.len))
+    start_chunk<TG, kStep, true>(x, p, c, k, f);
+  else
+    start_chunk<TG, kStep, false>(x, p, c, k, f);
 }
 
 // ---- small matrices ------------------------------------------------------------
@@ -897,7 +1017,7 @@ template <class TG, bool kStep>
 void muon_front(const lamb_muon* p, const MuonPtrs* ptrs, const MuonGroup& g,
                 const MuonConsts& k, cudaStream_t stream) {
   muon_norm_kernel<TG, kStep><<<g.chunks, kMuonThreads, 0, stream>>>(
-      p->mats, ptrs, p->chunks + g.chunk0, k, p->part);
+      ptrs, p->chunks + g.chunk0, k, p->part);
   muon_start_kernel<TG, kStep><<<g.chunks, kMuonThreads, 0, stream>>>(
       p->mats, ptrs, p->chunks + g.chunk0, k, p->part, g.chunk0, p->status);
 }

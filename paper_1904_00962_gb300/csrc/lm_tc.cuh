@@ -84,19 +84,20 @@ __device__ __forceinline__ void stores_have_read() {
 __device__ __forceinline__ void stores_done() {
   asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
+// Staging memory.  Not "memory": these keep their order among themselves and to
+// the barriers, and other loads may move past them.
 __device__ __forceinline__ uint4 lds16(uint32_t at) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at)
-               : "memory");
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
   return v;
 }
 __device__ __forceinline__ void sts16(uint32_t at, const uint4& v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
-               ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+               ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w));
 }
 __device__ __forceinline__ void sts2(uint32_t at, uint16_t v) {
-  asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory");
+  asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v));
 }
 
 // ---- products ---------------------------------------------------------------
@@ -160,7 +161,7 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&x)[32]) {
         "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
         "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
         "=r"(r[31])
-      : "r"(addr) : "memory");
+      : "r"(addr));
 #pragma unroll
   for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
 }

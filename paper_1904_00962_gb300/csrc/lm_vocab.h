@@ -13,13 +13,12 @@ struct lamb_vocab {
   void* arena = nullptr;
   uint32_t* status = nullptr;
 
-  // lookup gradient: sort buffers and the sorted order's segments
+  // lookup gradient: sort buffers, and the sums that chunks leave
   int sort_passes = 0;          // of 8 bits each
-  int64_t sort_tiles = 0;
   uint32_t* keys[2] = {nullptr, nullptr};
   int32_t* pos[2] = {nullptr, nullptr};
-  int32_t* hist = nullptr;      // [256][sort_tiles]
-  int32_t* start = nullptr;     // [vocab + 1]
+  int32_t* hist = nullptr;      // [pass][tile][256]
+  uint32_t* seen = nullptr;     // a bit for each word that has a token
   float* part = nullptr;        // [chunks][2][width]
 
   // head: the rows that have a label, and what is known of each
