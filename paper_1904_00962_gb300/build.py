@@ -23,7 +23,7 @@ LIB = os.path.join(BUILD, "liblamb.so")
 
 SOURCES = ["planner.cpp", "lamb_kernels.cu", "lamb_onchip.cu", "lamb_stash.cu",
            "lamb_capi.cu", "lamb_noalloc.cu", "lm_embed.cu", "lm_head.cu",
-           "lm_muon.cu"]
+           "lm_muon.cu", "lm_muon_steps.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -8,9 +8,7 @@
 //   Work::start(params)           what the kernel reads first: State, with the
 //                                 number of tiles (it may come from the device)
 //   Work::tile(params, state, t)  operands and extent of tile t (GemmTile)
-//   Work::kStages, kStaging       stages of the copies, bytes for the epilogue
-//   Work::before(params, tile, epi)   the epilogue's copies that need no product
-//   Work::epilogue(params, state, tile, acc, epi)  a tile of the accumulator
+//   Work::epilogue(params, state, tile, acc, epi)  a row of the accumulator
 // A tile is 128 rows of A by 256 of B.  Operands come through tensor maps with
 // the 128-byte swizzle, K-major (box: 64 of K by 128 rows) or MN-major (box: 64
 // rows by 64 of K); what lies outside a matrix arrives as zeros.
@@ -31,10 +29,8 @@ constexpr int kGemmThreads = 256;
 constexpr int kTileBytesA = kTileM * kTileK * 2;
 constexpr int kTileBytesB = kTileN * kTileK * 2;
 constexpr int kGemmStageBytes = kTileBytesA + kTileBytesB;
-template <class Work>
-constexpr size_t kGemmSmem =
-    (size_t)Work::kStages * kGemmStageBytes + Work::kStaging + 1024;
-constexpr int kMaxStages = 4;
+constexpr int kGemmStages = 4;
+constexpr size_t kGemmSmem = (size_t)kGemmStages * kGemmStageBytes + 1024;
 constexpr int kEpiThreads = 128, kEpiBarrier = 1;
 
 struct GemmTile {
@@ -48,26 +44,16 @@ struct GemmTile {
 };
 
 struct GemmShared {
-  uint64_t full[kMaxStages], empty[kMaxStages];
+  uint64_t full[kGemmStages], empty[kGemmStages];
   uint64_t acc_full[2], acc_empty[2];
-  uint64_t in_full[2];       // the epilogue's own copies
   uint32_t tmem;
   volatile int gave_up;
 };
 
-// What an epilogue thread has: its row of the tile, and staging memory.
+// What an epilogue thread has.
 struct Epilogue {
-  int row;               // 0 .. 127; thread 0 issues the copies
-  uint32_t staging;
-  GemmShared* sh;
-  uint32_t* status;
-  int chunks;            // chunks that went through the staging memory
-  int issued;            // copies into it (thread 0), one a chunk
+  int row;               // of the tile, 0 .. 127
 
-  __device__ __forceinline__ void sync() const {
-    asm volatile("bar.sync %0, %1;" ::"n"(kEpiBarrier), "n"(kEpiThreads)
-                 : "memory");
-  }
   // Every thread, whatever its wait said: one answer for all.
   __device__ __forceinline__ bool all(bool x) const {
     uint32_t r;
@@ -87,8 +73,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ typename Work::Params p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ GemmShared sh;
-  constexpr int kGemmStages = Work::kStages;
-  static_assert(kGemmStages <= kMaxStages, "stages");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem =
       (smem_u32(smem_raw) + 1023u) & ~1023u;   // the swizzle's pattern
@@ -101,7 +85,6 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.acc_full[i], 1);
       mbar_init(&sh.acc_empty[i], 4);
-      mbar_init(&sh.in_full[i], 1);
     }
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -194,15 +177,10 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
     Epilogue epi;
     const int quarter = warp & 3;
     epi.row = quarter * 32 + lane;
-    epi.staging = smem + kGemmStages * kGemmStageBytes;
-    epi.sh = &sh;
-    epi.status = p.status;
-    epi.chunks = epi.issued = 0;
     int n = 0;
     for (int t = blockIdx.x; t < st.n_tiles; t += gridDim.x, ++n) {
       const GemmTile g = Work::tile(p, st, t);
       const int acc = n & 1;
-      Work::before(p, g, epi);
       const bool ok =
           bounded_wait(&sh.acc_full[acc], (uint32_t)(n >> 1) & 1u, &sh.gave_up,
                        p.status, kStatusWaitTimeout);
@@ -214,12 +192,6 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
       tmem_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
-    }
-    // copies into and out of the staging memory end before the CTA does
-    if (Work::kStaging && epi.row == 0) {
-      if (epi.issued > epi.chunks) settle(&sh.in_full[epi.chunks & 1],
-                                          (uint32_t)(epi.chunks >> 1) & 1u);
-      stores_done();
     }
   }
   tmem_before_sync();

@@ -141,9 +141,6 @@ struct StatsWork {
   typedef StatsParams Params;
   typedef RowsState State;
   static constexpr bool kBf16 = true;
-  static constexpr int kStages = 4, kStaging = 0;
-  static __device__ __forceinline__ void before(const Params&, const GemmTile&,
-                                                Epilogue&) {}
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
@@ -292,9 +289,6 @@ struct DlogitsWork {
   typedef DlogitsParams Params;
   typedef RowsState State;
   static constexpr bool kBf16 = true;
-  static constexpr int kStages = 4, kStaging = 0;
-  static __device__ __forceinline__ void before(const Params&, const GemmTile&,
-                                                Epilogue&) {}
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
@@ -437,9 +431,6 @@ struct GradsWork {
   typedef GradsParams Params;
   typedef GradsState State;
   static constexpr bool kBf16 = true;
-  static constexpr int kStages = 4, kStaging = 0;
-  static __device__ __forceinline__ void before(const Params&, const GemmTile&,
-                                                Epilogue&) {}
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
@@ -576,7 +567,7 @@ template <class Work>
 cudaError_t launch_gemm(const typename Work::Params& p, int64_t most_tiles,
                         int sms, cudaStream_t stream) {
   const int grid = (int)std::min<int64_t>(most_tiles, sms);
-  gemm_kernel<Work><<<grid, kGemmThreads, kGemmSmem<Work>, stream>>>(p);
+  gemm_kernel<Work><<<grid, kGemmThreads, kGemmSmem, stream>>>(p);
   return cudaGetLastError();
 }
 
@@ -584,7 +575,7 @@ template <class Work>
 cudaError_t allow_smem() {
   return cudaFuncSetAttribute(gemm_kernel<Work>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)kGemmSmem<Work>);
+                              (int)kGemmSmem);
 }
 
 int grid_for(int64_t n, int sms) {

@@ -100,19 +100,21 @@ inline EncodeTiled lm_encoder() {
 }
 
 // A 16-bit matrix of `rows` lines of `cols` elements, row_stride elements apart
-// (a multiple of 8, the base on 16 bytes), copied in boxes of 64 columns by
-// box_rows lines.
+// (a multiple of 8, the base on 16 bytes), copied in boxes of 64 columns (128-byte
+// swizzle) or 32 (64-byte swizzle) by box_rows lines.
 inline bool lm_map(EncodeTiled encode, CUtensorMap* map, bool bf16,
                    const void* base, int64_t rows, int64_t cols,
-                   int64_t row_stride, int box_rows) {
+                   int64_t row_stride, int box_rows, int box_cols = 64) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)row_stride * 2};
-  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
   const cuuint32_t step[2] = {1, 1};
   return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                           : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
                 2, const_cast<void*>(base), dims, strides, box, step,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_INTERLEAVE_NONE,
+                box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B
+                               : CU_TENSOR_MAP_SWIZZLE_64B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -19,9 +19,8 @@
 // rounded as it is, 1.7e-3 .. 1.2e-2, in bf16 1.3e-2 .. 1e-1.  Scales that are
 // powers of two keep the entries inside fp16's range.
 //
-// G and G G are symmetric: tiles on or above the diagonal are multiplied and
-// written to both places.  All matrices of a group go through one launch a
-// product, longest K first.
+// lm_muon_steps.cu multiplies; here are the momentum and the norm in front of it,
+// small matrices, and the plan.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -31,453 +30,13 @@
 #include <new>
 #include <vector>
 
-#include "lm_gemm.cuh"
-#include "lm_host.h"
+#include "lm_muon.h"
 
 namespace lamb {
 namespace {
 
 constexpr int kMuonThreads = 256;
 constexpr int kMuonChunk = 8192;             // elements of a chunk
-constexpr float kScaleD = 1024.f;            // D is stored times this
-constexpr float kScaleE = 256.f;             // and E times this
-constexpr float kScaleLo = 2048.f;           // lo: the rest of hi, times this
-
-struct MuonMatrix {
-  CUtensorMap x_k[2], x_mn[2];   // hi (two buffers, taken in turn)
-  CUtensorMap lo_k;
-  CUtensorMap d, e;              // boxes of 128 rows
-  CUtensorMap d_t, e_t;          // boxes of 64 rows: mirrored blocks
-  __half* hi[2];
-  __half* lo;
-  __half* D;
-  __half* E;
-  float* diag;                   // l
-  float* beta;
-  float scale;                   // hi + lo = X scale
-  int rows, cols, m, n;          // m = min, n = max
-  int tall;                      // rows > cols
-  int pitch, pitch_m;            // of X, of D and E
-  int first_chunk, n_chunks;
-  float decay;
-};
-
-struct MuonPtrs {
-  float* w;
-  const void* g;                 // or the direction's input
-  float* m;
-  __nv_bfloat16* out;            // copy of w, or the direction
-};
-
-struct MuonChunk {
-  int matrix;
-  int len;
-  int64_t offset;
-};
-
-struct MuonTile {
-  int matrix, i, j, pad;
-};
-
-struct MuonConsts {
-  float a, b, c;
-  float beta, omb;               // momentum
-  float eps;
-  float wd, size;                // lambda, s without its shape's part
-  int nesterov, scale_kind;
-};
-
-enum { kGram = 0, kSquare = 1, kApply = 2 };
-
-struct MuonParams {
-  const MuonMatrix* mats;
-  const MuonPtrs* ptrs;
-  const MuonTile* tiles;
-  const float* d_lr;             // NULL: the direction alone
-  uint32_t* status;
-  MuonConsts k;
-  int n_tiles;
-  int from;                      // which hi is read
-  int last;
-};
-
-struct MuonState {
-  int n_tiles;
-};
-
-// s of a matrix.
-__device__ __forceinline__ float muon_size(const MuonConsts& k,
-                                           const MuonMatrix& x) {
-  if (k.scale_kind == LAMB_MUON_SCALE_RMS)
-    return k.size * 0.2f * sqrtf((float)x.n);
-  if (k.scale_kind == LAMB_MUON_SCALE_SPECTRAL)
-    return k.size * sqrtf(fmaxf(1.f, (float)x.rows / (float)x.cols));
-  return k.size;
-}
-
-__device__ __forceinline__ uint32_t pack_half2(float x, float y) {
-  const __half2 h = __floats2half2_rn(x, y);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-// The epilogues take 64 columns at a time through staging memory: a chunk's
-// inputs arrive there by tensor copies (while the chunk before is worked on),
-// each thread turns its row over, and tensor copies take the result out.  Rows of
-// 128 bytes in the copies' swizzle, 16 KB a matrix; two such buffers of 32 KB.
-// (With plain accesses, a row a thread, the epilogue took 20 times the products.)
-constexpr int kChunkCols = 64;
-constexpr int kHalfBuffer = kTileM * kChunkCols * 2;
-constexpr int kChunkBuffer = 2 * kHalfBuffer;
-
-// The 16-byte unit q of row r.
-__device__ __forceinline__ uint32_t unit16(uint32_t base, int r, int q) {
-  return base + r * 128 + ((q ^ (r & 7)) << 4);
-}
-// Entry (j, i) of a mirrored block: two halves of 64 columns, 64 rows each.
-__device__ __forceinline__ uint32_t mirrored(uint32_t base, int j, int i) {
-  return base + (i >> 6) * 8192 + j * 128 + ((((i & 63) >> 3) ^ (j & 7)) << 4) +
-         (i & 7) * 2;
-}
-// Unit q of row r of 64 floats.
-__device__ __forceinline__ uint32_t unit16_f(uint32_t base, int r, int q) {
-  return base + r * 256 + ((q ^ (r & 7)) << 4);
-}
-__device__ __forceinline__ float2 half2_at(uint32_t w) {
-  return __half22float2(*reinterpret_cast<const __half2*>(&w));
-}
-__device__ __forceinline__ uint16_t half_bits(uint32_t w, int i) {
-  return (uint16_t)(i ? w >> 16 : w & 0xffffu);
-}
-
-template <int kPhase>
-struct MuonWork {
-  typedef MuonParams Params;
-  typedef MuonState State;
-  static constexpr bool kBf16 = false;
-  static constexpr int kStages = 3, kStaging = 2 * kChunkBuffer;
-  static __device__ __forceinline__ State start(const Params& p) {
-    return State{p.n_tiles};
-  }
-  static __device__ __forceinline__ GemmTile tile(const Params& p, const State&,
-                                                  int t) {
-    const MuonTile mt = p.tiles[t];
-    const MuonMatrix* x = p.mats + mt.matrix;
-    GemmTile g;
-    g.what = mt.matrix;
-    g.aux = 0;
-    g.k0 = g.b_k = 0;
-    g.a0 = mt.i * kTileM;
-    g.b0 = mt.j * kTileN;
-    if (kPhase == kGram) {
-      g.a_mn = g.b_mn = x->tall;
-      g.a = g.b = x->tall ? &x->x_mn[p.from] : &x->x_k[p.from];
-      g.kn = (x->n + kTileK - 1) / kTileK;
-    } else {
-      g.kn = (x->m + kTileK - 1) / kTileK;
-      if (kPhase == kSquare) {
-        g.a = g.b = &x->d;
-        g.a_mn = g.b_mn = false;
-      } else if (x->tall) {
-        g.a = &x->x_k[p.from];
-        g.b = &x->e;
-        g.a_mn = g.b_mn = false;
-      } else {
-        g.a = &x->e;
-        g.b = &x->x_mn[p.from];
-        g.a_mn = false;
-        g.b_mn = true;
-      }
-    }
-    return g;
-  }
-
-  // Copies chunk `c` of the tile into the buffer whose turn it is.
-  static __device__ __forceinline__ void fetch(const Params& p,
-                                               const MuonMatrix& x,
-                                               const GemmTile& g, int c,
-                                               Epilogue& epi) {
-    const int at = epi.issued++;
-    const uint32_t to = epi.staging + (at & 1) * kChunkBuffer;
-    uint64_t* bar = &epi.sh->in_full[at & 1];
-    const int c0 = g.b0 + c * kChunkCols;
-    if (kPhase == kSquare) {
-      mbar_expect(bar, kHalfBuffer);
-      tile_load(to, &x.d, c0, g.a0, bar);
-    } else {
-      mbar_expect(bar, 2 * kHalfBuffer);
-      tile_load(to, &x.x_k[p.from], c0, g.a0, bar);
-      tile_load(to + kHalfBuffer, &x.lo_k, c0, g.a0, bar);
-    }
-  }
-
-  static __device__ __forceinline__ void before(const Params& p,
-                                                const GemmTile& g,
-                                                Epilogue& epi) {
-    if (kPhase == kGram || epi.row != 0) return;
-    stores_have_read<1>();      // the buffer's own store, two chunks ago
-    fetch(p, p.mats[g.what], g, 0, epi);
-  }
-
-  static __device__ __forceinline__ void epilogue(const Params& p,
-                                                  const State&,
-                                                  const GemmTile& g,
-                                                  uint32_t acc, Epilogue& epi) {
-    const MuonMatrix& x = p.mats[g.what];
-    const int width = kPhase == kApply ? x.cols : x.m;
-    const bool last = kPhase == kApply && p.last;
-    for (int c = 0; c < kTileN / kChunkCols; ++c) {
-      const int c0 = g.b0 + c * kChunkCols;
-      if (c0 >= width) break;
-      const int n = epi.chunks;
-      const uint32_t buf = epi.staging + (n & 1) * kChunkBuffer;
-      if (kPhase == kGram) {
-        if (epi.row == 0) stores_have_read<1>();
-        epi.sync();
-      } else {
-        if (epi.row == 0 && c + 1 < kTileN / kChunkCols &&
-            c0 + kChunkCols < width) {
-          stores_have_read<0>();
-          fetch(p, x, g, c + 1, epi);
-        }
-        bounded_wait(&epi.sh->in_full[n & 1], (uint32_t)(n >> 1) & 1u,
-                     &epi.sh->gave_up, epi.status, LAMB_STATUS_WAIT_TIMEOUT);
-      }
-      if (kPhase == kApply)
-        apply(p, x, g, acc + c * kChunkCols, c0, buf, epi);
-      else
-        symmetric(p, x, g, acc + c * kChunkCols, c0, buf, epi);
-      epi.chunks = n + 1;
-      if (!last) {
-        fence_proxy_async();
-        epi.sync();
-        if (epi.row == 0) {
-          if (kPhase == kApply) {
-            tile_store(&x.x_k[p.from ^ 1], c0, g.a0, buf);
-            tile_store(&x.lo_k, c0, g.a0, buf + kHalfBuffer);
-          } else {
-            const CUtensorMap* t = kPhase == kGram ? &x.d : &x.e;
-            tile_store(t, c0, g.a0, buf);
-            if (mirror(g, c0)) {
-              const CUtensorMap* m = kPhase == kGram ? &x.d_t : &x.e_t;
-              tile_store(m, g.a0, c0, buf + kHalfBuffer);
-              if (g.a0 + 64 < x.m)
-                tile_store(m, g.a0 + 64, c0, buf + kHalfBuffer + 8192);
-            }
-          }
-          stores_commit();
-        }
-      } else {
-        epi.sync();
-        write_out(p, x, g, c0, buf, epi);
-        fence_proxy_async();
-        epi.sync();      // the buffer may be copied into again
-      }
-    }
-  }
-
-  // Whether the block of rows c0 .. and columns a0 .. is another tile's own.
-  static __device__ __forceinline__ bool mirror(const GemmTile& g, int c0) {
-    return g.a0 / kTileN * kTileN + kTileN - 1 < c0 / kTileM * kTileM;
-  }
-
-  static __device__ __forceinline__ void symmetric(const Params& p,
-                                                   const MuonMatrix& x,
-                                                   const GemmTile& g,
-                                                   uint32_t acc, int c0,
-                                                   uint32_t buf,
-                                                   const Epilogue& epi) {
-    const int i = g.a0 + epi.row, m = x.m;
-    float* const diag = x.diag;
-    const float s = kPhase == kGram
-                        ? 1.f / (x.scale * x.scale)    // powers of two
-                        : 1.f / (kScaleD * kScaleD);
-    const float li = kPhase == kSquare && i < m ? diag[i] : 0.f;
-    const float pb = p.k.b, pc = p.k.c;
-    const bool both = mirror(g, c0);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int j0 = c0 + 32 * h;
-      float y[32];
-      tmem_ld32(acc + 32 * h, y);
-      if (kPhase == kGram) {
-        if (i >= j0 && i < j0 + 32 && i < m) {
-#pragma unroll
-          for (int q = 0; q < 32; ++q)
-            if (j0 + q == i) {
-              diag[i] = y[q] * s;
-              y[q] = 0.f;
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < 32; ++q) y[q] *= s * kScaleD;
-      } else {
-        // (diag's memory goes up to a whole tile)
-        float l[32];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const float4 v = *reinterpret_cast<const float4*>(diag + j0 + 4 * u);
-          l[4 * u] = v.x; l[4 * u + 1] = v.y;
-          l[4 * u + 2] = v.z; l[4 * u + 3] = v.w;
-        }
-        if (i >= j0 && i < j0 + 32 && i < m) {
-#pragma unroll
-          for (int q = 0; q < 32; ++q)
-            if (j0 + q == i) x.beta[i] = pb * li + pc * (li * li + y[q] * s);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint4 d = lds16(unit16(buf, epi.row, 4 * h + u));
-          const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int q = 8 * u + k;
-            const float2 dd2 = half2_at(dw[k >> 1]);
-            const float dd = k & 1 ? dd2.y : dd2.x;
-            // E kScaleE, dd being D kScaleD
-            const float f = fmaf(pc, li + l[q], pb) * (kScaleE / kScaleD);
-            y[q] = fmaf(f, dd, y[q] * (pc * s * kScaleE));
-          }
-        }
-        if (i >= j0 && i < j0 + 32) {
-#pragma unroll
-          for (int q = 0; q < 32; ++q)
-            if (j0 + q == i) y[q] = 0.f;
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        uint32_t w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          w[k] = pack_half2(y[8 * u + 2 * k], y[8 * u + 2 * k + 1]);
-        sts16(unit16(buf, epi.row, 4 * h + u),
-              make_uint4(w[0], w[1], w[2], w[3]));
-        if (both) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            sts2(mirrored(buf + kHalfBuffer, 32 * h + 8 * u + k, epi.row),
-                 half_bits(w[k >> 1], k & 1));
-        }
-      }
-    }
-  }
-
-  static __device__ __forceinline__ void apply(const Params& p,
-                                               const MuonMatrix& x,
-                                               const GemmTile& g, uint32_t acc,
-                                               int c0, uint32_t buf,
-                                               const Epilogue& epi) {
-    const int r = g.a0 + epi.row;
-    const bool tall = x.tall, last = p.last;
-    const float* const beta = x.beta;
-    const float pa = p.k.a;
-    const float br = !tall && r < x.rows ? pa + beta[r] : 0.f;
-    const float inv = 1.f / x.scale;
-    float y[64];
-    tmem_ld32(acc, *reinterpret_cast<float(*)[32]>(y));
-    tmem_ld32(acc + 32, *reinterpret_cast<float(*)[32]>(y + 32));
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const uint32_t ah = unit16(buf, epi.row, u), al = ah + kHalfBuffer;
-      const uint4 hi = lds16(ah), lo = lds16(al);
-      const uint32_t hw[4] = {hi.x, hi.y, hi.z, hi.w};
-      const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w};
-      uint32_t oh[4], ol[4];
-      float bc[8];         // (beta's memory goes up to a whole tile)
-      if (tall) {
-        const float4* b4 = reinterpret_cast<const float4*>(beta + c0 + 8 * u);
-        const float4 b0 = b4[0], b1 = b4[1];
-        bc[0] = b0.x; bc[1] = b0.y; bc[2] = b0.z; bc[3] = b0.w;
-        bc[4] = b1.x; bc[5] = b1.y; bc[6] = b1.z; bc[7] = b1.w;
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 a = half2_at(hw[k]), b = half2_at(lw[k]);
-        float v[2] = {fmaf(b.x, 1.f / kScaleLo, a.x),
-                      fmaf(b.y, 1.f / kScaleLo, a.y)};
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int q = 8 * u + 2 * k + e;
-          const float f = tall ? pa + bc[2 * k + e] : br;
-          // in units of 1 / scale
-          v[e] = fmaf(f, v[e], y[q] * (1.f / kScaleE));
-          y[q] = v[e] * inv;
-        }
-        oh[k] = pack_half2(v[0], v[1]);
-        const float2 h = half2_at(oh[k]);
-        ol[k] = pack_half2((v[0] - h.x) * kScaleLo, (v[1] - h.y) * kScaleLo);
-      }
-      if (!last) {
-        sts16(ah, make_uint4(oh[0], oh[1], oh[2], oh[3]));
-        sts16(al, make_uint4(ol[0], ol[1], ol[2], ol[3]));
-      }
-    }
-    if (last) {
-      epi.sync();          // everybody has read its inputs
-#pragma unroll
-      for (int u = 0; u < 16; ++u)
-        sts16(unit16_f(buf, epi.row, u),
-              make_uint4(__float_as_uint(y[4 * u]),
-                         __float_as_uint(y[4 * u + 1]),
-                         __float_as_uint(y[4 * u + 2]),
-                         __float_as_uint(y[4 * u + 3])));
-    }
-  }
-
-  // The last X to the weights or the direction, half a warp a row.
-  static __device__ __forceinline__ void write_out(const Params& p,
-                                                   const MuonMatrix& x,
-                                                   const GemmTile& g, int c0,
-                                                   uint32_t buf,
-                                                   const Epilogue& epi) {
-    const MuonPtrs ptr = p.ptrs[g.what];
-    const float lr = p.d_lr ? *p.d_lr : 0.f;
-    const float keep = 1.f - lr * p.k.wd * x.decay;
-    const float move = lr * muon_size(p.k, x);
-    const int u = epi.row & 15, c = c0 + 4 * u;
-    if (c >= x.cols) return;
-    const int cols = min(4, x.cols - c);
-    const bool vec = cols == 4 && x.cols % 4 == 0 && (uintptr_t)ptr.w % 16 == 0 &&
-                     (uintptr_t)ptr.out % 8 == 0;
-#pragma unroll 4
-    for (int r = epi.row >> 4; r < kTileM; r += kEpiThreads / 16) {
-      if (g.a0 + r >= x.rows) break;
-      const uint4 w = lds16(unit16_f(buf, r, u));
-      float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y),
-                    __uint_as_float(w.z), __uint_as_float(w.w)};
-      const int64_t at = (int64_t)(g.a0 + r) * x.cols + c;
-      if (vec) {
-        if (p.d_lr) {
-          float4* to = reinterpret_cast<float4*>(ptr.w + at);
-          const float4 o = *to;
-          v[0] = keep * o.x - move * v[0];
-          v[1] = keep * o.y - move * v[1];
-          v[2] = keep * o.z - move * v[2];
-          v[3] = keep * o.w - move * v[3];
-          *to = make_float4(v[0], v[1], v[2], v[3]);
-        }
-        if (ptr.out) {
-          const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]);
-          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2], v[3]);
-          *reinterpret_cast<uint2*>(ptr.out + at) =
-              make_uint2(*reinterpret_cast<const uint32_t*>(&a),
-                         *reinterpret_cast<const uint32_t*>(&b));
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (k >= cols) break;
-          if (p.d_lr) {
-            v[k] = keep * ptr.w[at + k] - move * v[k];
-            ptr.w[at + k] = v[k];
-          }
-          if (ptr.out) ptr.out[at + k] = __float2bfloat16_rn(v[k]);
-        }
-      }
-    }
-  }
-};
-
 // ---- momentum and norm --------------------------------------------------------
 template <class TG>
 __device__ __forceinline__ float load_grad(const void* p, int64_t i);
@@ -637,17 +196,20 @@ template <class TG, bool kStep>
 __global__ void __launch_bounds__(kMuonThreads)
 muon_start_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
                   const MuonChunk* chunks, MuonConsts k, const double* part,
-                  int chunk0, uint32_t* status) {
+                  uint32_t* done, uint32_t* ticket, uint32_t* status) {
   __shared__ double sh[kMuonThreads / 32];
   const MuonChunk c = chunks[blockIdx.x];
   const MuonMatrix& x = mats[c.matrix];
   const MuonPtrs p = ptrs[c.matrix];
   double s = 0.0;
   for (int i = threadIdx.x; i < x.n_chunks; i += kMuonThreads)
-    s += part[x.first_chunk - chunk0 + i];
+    s += part[x.first_chunk + i];
   const float norm = (float)sqrt(block_sum(s, sh));
-  if (threadIdx.x == 0 && !isfinite(norm))
-    atomicOr(status, LAMB_STATUS_NONFINITE);
+  if (threadIdx.x == 0) {
+    if (!isfinite(norm)) atomicOr(status, LAMB_STATUS_NONFINITE);
+    if (c.offset == 0) done[c.matrix] = 0;       // of the products to come
+    if (blockIdx.x == 0) *ticket = 0;
+  }
   const float f = x.scale / (norm + k.eps);
   if (chunk_vec<TG, kStep>(p, c.len))
     start_chunk<TG, kStep, true>(x, p, c, k, f);
@@ -830,22 +392,7 @@ cudaError_t small_smem_limit(int64_t bytes) {
                               (int)bytes);
 }
 
-template <class Work>
-cudaError_t muon_smem() {
-  return cudaFuncSetAttribute(gemm_kernel<Work>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)kGemmSmem<Work>);
-}
-
 }  // namespace
-
-// Matrices that go through the products together, on one workspace.
-struct MuonGroup {
-  int chunk0 = 0, chunks = 0;
-  int sym0 = 0, sym = 0;      // tiles of the Gram matrix, by its K
-  int sq0 = 0;                // the same tiles, by the square's K
-  int app0 = 0, app = 0;
-};
 
 }  // namespace lamb
 
@@ -862,24 +409,30 @@ struct lamb_muon {
   MuonPtrs* dir_ptrs = nullptr;        // of the direction
   MuonChunk* chunks = nullptr;
   MuonTile* tiles = nullptr;
+  MuonSpan* spans = nullptr;
+  uint32_t* done = nullptr;
+  uint32_t* ticket = nullptr;
   double* part = nullptr;
   int* small = nullptr;                // matrices of the small kernel
   int n_small = 0;
   int64_t small_bytes = 0;             // shared memory of the largest
   uint32_t* status = nullptr;
   std::vector<int64_t> numel;
-  std::vector<MuonGroup> groups;
+  int n_chunks = 0, n_spans = 0;
+  int64_t step_tiles = 0;              // tiles of one step of all matrices
 };
 
 namespace {
 
-// Bytes of working matrices that a group may take.
-constexpr int64_t kGroupBytes = 1ll << 40;
+// Bytes of the working matrices of a set: two sets go through their steps at a
+// time and have to share L2.
+constexpr int64_t kMuonSetBytes = 56ll << 20;
 
 struct MuonLayout {
   std::vector<MuonMatrix> mats;
   std::vector<MuonChunk> chunks;
   std::vector<MuonTile> tiles;
+  std::vector<MuonSpan> spans;
   std::vector<int> small;
   std::vector<int64_t> at[7];     // byte offsets in the workspace, per matrix
   int64_t work_bytes = 0;
@@ -891,58 +444,14 @@ int64_t take(int64_t* used, int64_t bytes) {
   return at;
 }
 
-// Groups, workspace offsets, chunks and tiles of the matrices (host only).
+// Workspace offsets, chunks, sets and tiles of the matrices (host only).
 void muon_layout(const int64_t* rows, const int64_t* cols, int n,
-                 const uint8_t* mask, MuonLayout* L,
-                 std::vector<MuonGroup>* groups) {
+                 const uint8_t* mask, MuonLayout* L) {
   L->mats.resize(n);
   for (auto& v : L->at) v.assign(n, 0);
-  std::vector<int> open;
+  std::vector<int> large;
+  std::vector<int64_t> bytes(n, 0);
   int64_t used = 0;
-  auto close = [&]() {
-    if (open.empty()) return;
-    MuonGroup g;
-    g.chunk0 = (int)L->chunks.size();
-    for (int k : open) {
-      MuonMatrix& x = L->mats[k];
-      x.first_chunk = (int)L->chunks.size();
-      const int64_t total = (int64_t)x.rows * x.cols;
-      for (int64_t o = 0; o < total; o += kMuonChunk)
-        L->chunks.push_back(
-            {k, (int)std::min<int64_t>(kMuonChunk, total - o), o});
-      x.n_chunks = (int)L->chunks.size() - x.first_chunk;
-    }
-    g.chunks = (int)L->chunks.size() - g.chunk0;
-    auto by = [&](bool longer) {
-      std::stable_sort(open.begin(), open.end(), [&](int p, int q) {
-        return longer ? L->mats[p].n > L->mats[q].n
-                      : L->mats[p].m > L->mats[q].m;
-      });
-    };
-    auto symmetric = [&]() {
-      for (int k : open)
-        for (int i = 0; i * kTileM < L->mats[k].m; ++i)
-          for (int j = i * kTileM / kTileN; j * kTileN < L->mats[k].m; ++j)
-            L->tiles.push_back({k, i, j, 0});
-    };
-    by(true);
-    g.sym0 = (int)L->tiles.size();
-    symmetric();
-    g.sym = (int)L->tiles.size() - g.sym0;
-    by(false);
-    g.sq0 = (int)L->tiles.size();
-    symmetric();
-    g.app0 = (int)L->tiles.size();
-    for (int k : open)
-      for (int i = 0; i * kTileM < L->mats[k].rows; ++i)
-        for (int j = 0; j * kTileN < L->mats[k].cols; ++j)
-          L->tiles.push_back({k, i, j, 0});
-    g.app = (int)L->tiles.size() - g.app0;
-    groups->push_back(g);
-    L->work_bytes = std::max(L->work_bytes, used);
-    open.clear();
-    used = 0;
-  };
   for (int k = 0; k < n; ++k) {
     MuonMatrix& x = L->mats[k];
     memset(&x, 0, sizeof(x));
@@ -963,13 +472,67 @@ void muon_layout(const int64_t* rows, const int64_t* cols, int n,
     }
     const int64_t sx = (int64_t)x.rows * x.pitch * 2;
     const int64_t sm = (int64_t)x.m * x.pitch_m * 2;
-    if (!open.empty() && used + 3 * sx + 2 * sm > kGroupBytes) close();
+    const int64_t before = used;
     for (int i = 0; i < 3; ++i) L->at[i][k] = take(&used, sx);
     for (int i = 3; i < 5; ++i) L->at[i][k] = take(&used, sm);
     for (int i = 5; i < 7; ++i) L->at[i][k] = take(&used, x.m * 4ll);
-    open.push_back(k);
+    bytes[k] = used - before;
+    large.push_back(k);
+    x.first_chunk = (int)L->chunks.size();
+    const int64_t total = (int64_t)x.rows * x.cols;
+    for (int64_t o = 0; o < total; o += kMuonChunk)
+      L->chunks.push_back(
+          {k, (int)std::min<int64_t>(kMuonChunk, total - o), o});
+    x.n_chunks = (int)L->chunks.size() - x.first_chunk;
+    for (int i = 0; i * kMuonTileM < x.m; ++i)
+      x.sym += (int)lm_ceil_div(x.m, kMuonTileN) - i * kMuonTileM / kMuonTileN;
+    x.app = (int)(lm_ceil_div(x.rows, kMuonTileM) *
+                  lm_ceil_div(x.cols, kMuonTileN));
   }
-  close();
+  L->work_bytes = used;
+  if (large.empty()) return;
+
+  // an even number of sets of about equal work, the largest matrices first, each
+  // to the set that has least so far
+  auto work = [&](int k) {
+    const MuonMatrix& x = L->mats[k];
+    return (double)x.m * x.m * x.n;
+  };
+  std::stable_sort(large.begin(), large.end(),
+                   [&](int p, int q) { return work(p) > work(q); });
+  const int64_t pairs = lm_ceil_div(used, 2 * kMuonSetBytes);
+  const int sets =
+      (int)std::min<int64_t>(2 * pairs, (int64_t)large.size());
+  std::vector<std::vector<int>> set(sets);
+  std::vector<double> load(sets, 0.0);
+  for (int k : large) {
+    const int to = (int)(std::min_element(load.begin(), load.end()) -
+                         load.begin());
+    set[to].push_back(k);
+    load[to] += work(k);
+  }
+  // the tiles of one step of two sets: product by product, the sets in turn, long
+  // products first
+  for (int s = 0; s < sets; s += 2) {
+    const int first = (int)L->tiles.size();
+    for (int phase = kGram; phase <= kApply; ++phase)
+      for (int h = s; h < std::min(s + 2, sets); ++h) {
+        std::stable_sort(set[h].begin(), set[h].end(), [&](int p, int q) {
+          const MuonMatrix &x = L->mats[p], &y = L->mats[q];
+          return phase == kGram ? x.n > y.n : x.m > y.m;
+        });
+        for (int k : set[h]) {
+          const MuonMatrix& x = L->mats[k];
+          const int r = phase == kApply ? x.rows : x.m;
+          const int c = phase == kApply ? x.cols : x.m;
+          for (int i = 0; i * kMuonTileM < r; ++i)
+            for (int j = phase == kApply ? 0 : i * kMuonTileM / kMuonTileN;
+                 j * kMuonTileN < c; ++j)
+              L->tiles.push_back({k, i, j, phase});
+        }
+      }
+    L->spans.push_back({first, (int)L->tiles.size() - first});
+  }
 }
 
 lamb_status_t muon_check(const lamb_muon* p, const lamb_muon_hyper_t* h) {
@@ -994,16 +557,6 @@ lamb_status_t muon_check(const lamb_muon* p, const lamb_muon_hyper_t* h) {
   return LAMB_OK;
 }
 
-template <class Work>
-cudaError_t muon_product(const lamb_muon* p, MuonParams& q, int first, int n,
-                         cudaStream_t stream) {
-  q.tiles = p->tiles + first;
-  q.n_tiles = n;
-  gemm_kernel<Work>
-      <<<std::min(n, p->sms), kGemmThreads, kGemmSmem<Work>, stream>>>(q);
-  return cudaGetLastError();
-}
-
 template <class TG, bool kStep>
 void muon_small(const lamb_muon* p, const MuonPtrs* ptrs, const MuonConsts& k,
                 int steps, const float* d_lr, cudaStream_t stream) {
@@ -1014,12 +567,13 @@ void muon_small(const lamb_muon* p, const MuonPtrs* ptrs, const MuonConsts& k,
 }
 
 template <class TG, bool kStep>
-void muon_front(const lamb_muon* p, const MuonPtrs* ptrs, const MuonGroup& g,
-                const MuonConsts& k, cudaStream_t stream) {
-  muon_norm_kernel<TG, kStep><<<g.chunks, kMuonThreads, 0, stream>>>(
-      ptrs, p->chunks + g.chunk0, k, p->part);
-  muon_start_kernel<TG, kStep><<<g.chunks, kMuonThreads, 0, stream>>>(
-      p->mats, ptrs, p->chunks + g.chunk0, k, p->part, g.chunk0, p->status);
+void muon_front(const lamb_muon* p, const MuonPtrs* ptrs, const MuonConsts& k,
+                cudaStream_t stream) {
+  if (!p->n_chunks) return;
+  muon_norm_kernel<TG, kStep><<<p->n_chunks, kMuonThreads, 0, stream>>>(
+      ptrs, p->chunks, k, p->part);
+  muon_start_kernel<TG, kStep><<<p->n_chunks, kMuonThreads, 0, stream>>>(
+      p->mats, ptrs, p->chunks, k, p->part, p->done, p->ticket, p->status);
 }
 
 lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
@@ -1050,33 +604,26 @@ lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
     muon_small<bf, false>(p, q.ptrs, q.k, h->steps, d_lr, stream);
   else
     muon_small<float, false>(p, q.ptrs, q.k, h->steps, d_lr, stream);
-  const cudaError_t es = cudaGetLastError();
-  if (es != cudaSuccess) return lm_cuda_fail(es, "muon launch");
-  for (const MuonGroup& g : p->groups) {
-    if (d_lr) {
-      if (p->grad_bf16)
-        muon_front<__nv_bfloat16, true>(p, q.ptrs, g, q.k, stream);
-      else
-        muon_front<float, true>(p, q.ptrs, g, q.k, stream);
-    } else {
-      if (p->grad_bf16)
-        muon_front<__nv_bfloat16, false>(p, q.ptrs, g, q.k, stream);
-      else
-        muon_front<float, false>(p, q.ptrs, g, q.k, stream);
-    }
-    cudaError_t e = cudaGetLastError();
-    for (int i = 0; e == cudaSuccess && i < h->steps; ++i) {
-      q.from = i & 1;
-      q.last = i == h->steps - 1;
-      e = muon_product<MuonWork<kGram>>(p, q, g.sym0, g.sym, stream);
-      if (e == cudaSuccess)
-        e = muon_product<MuonWork<kSquare>>(p, q, g.sq0, g.sym, stream);
-      if (e == cudaSuccess)
-        e = muon_product<MuonWork<kApply>>(p, q, g.app0, g.app, stream);
-    }
-    if (e != cudaSuccess) return lm_cuda_fail(e, "muon launch");
+  if (d_lr && p->grad_bf16)
+    muon_front<bf, true>(p, q.ptrs, q.k, stream);
+  else if (d_lr)
+    muon_front<float, true>(p, q.ptrs, q.k, stream);
+  else if (p->grad_bf16)
+    muon_front<bf, false>(p, q.ptrs, q.k, stream);
+  else
+    muon_front<float, false>(p, q.ptrs, q.k, stream);
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess && p->step_tiles) {
+    q.tiles = p->tiles;
+    q.spans = p->spans;
+    q.n_spans = p->n_spans;
+    q.done = p->done;
+    q.ticket = p->ticket;
+    q.steps = h->steps;
+    q.total = (int)(p->step_tiles * h->steps);
+    e = muon_launch_steps(q, p->sms, stream);
   }
-  return LAMB_OK;
+  return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "muon launch");
 }
 
 lamb_status_t upload_ptrs(lamb_muon* p, MuonPtrs* to,
@@ -1133,12 +680,17 @@ extern "C" lamb_status_t lamb_muon_create(
     p->copy = copy_dtype == LAMB_BF16;
     for (int k = 0; k < n_matrices; ++k) p->numel.push_back(rows[k] * cols[k]);
     MuonLayout L;
-    muon_layout(rows, cols, n_matrices, decay_mask, &L, &p->groups);
+    muon_layout(rows, cols, n_matrices, decay_mask, &L);
+    p->n_chunks = (int)L.chunks.size();
+    p->n_spans = (int)L.spans.size();
+    p->step_tiles = (int64_t)L.tiles.size();
+    if (p->step_tiles * 64 > INT32_MAX || L.chunks.size() > INT32_MAX) {
+      lamb_muon_destroy(p);
+      return lm_fail(LAMB_ERR_INVALID_ARG, "the matrices have too many tiles");
+    }
     const EncodeTiled encode = lm_encoder();
     e = cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = muon_smem<MuonWork<kGram>>();
-    if (e == cudaSuccess) e = muon_smem<MuonWork<kSquare>>();
-    if (e == cudaSuccess) e = muon_smem<MuonWork<kApply>>();
+    if (e == cudaSuccess) e = (cudaError_t)muon_steps_setup();
     LmArena a;
     for (int pass = 0; e == cudaSuccess && pass < 2; ++pass) {
       a.used = 0;
@@ -1148,6 +700,9 @@ extern "C" lamb_status_t lamb_muon_create(
       a.take(&p->dir_ptrs, n_matrices);
       a.take(&p->chunks, (int64_t)L.chunks.size());
       a.take(&p->tiles, (int64_t)L.tiles.size());
+      a.take(&p->spans, (int64_t)L.spans.size());
+      a.take(&p->done, n_matrices);
+      a.take(&p->ticket, 1);
       a.take(&p->part, (int64_t)L.chunks.size());
       a.take(&p->small, (int64_t)L.small.size());
       if (pass == 0) {
@@ -1161,26 +716,32 @@ extern "C" lamb_status_t lamb_muon_create(
     char* base = (char*)p->work;
     for (int k = 0; e == cudaSuccess && ok && k < n_matrices; ++k) {
       MuonMatrix& x = L.mats[k];
-      if (!x.m) continue;
+      if (!x.sym) continue;          // empty or small
+      bool m = true;
+      auto map = [&](CUtensorMap* t, const __half* at, int rows_, int cols_,
+                     int pitch, int box_rows, int box_cols) {
+        m = m && lm_map(encode, t, false, at, rows_, cols_, pitch, box_rows,
+                        box_cols);
+      };
       for (int i = 0; i < 2; ++i) {
         x.hi[i] = (__half*)(base + L.at[i][k]);
-        ok = ok && lm_map(encode, &x.x_k[i], false, x.hi[i], x.rows, x.cols,
-                          x.pitch, kTileM) &&
-             lm_map(encode, &x.x_mn[i], false, x.hi[i], x.rows, x.cols, x.pitch,
-                    kTileK);
+        map(&x.x_k[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileM, 64);
+        map(&x.x_mn[i], x.hi[i], x.rows, x.cols, x.pitch, 64, 64);
+        map(&x.x_c[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileM, kMuonCols);
       }
       x.lo = (__half*)(base + L.at[2][k]);
       x.D = (__half*)(base + L.at[3][k]);
       x.E = (__half*)(base + L.at[4][k]);
       x.diag = (float*)(base + L.at[5][k]);
       x.beta = (float*)(base + L.at[6][k]);
-      ok = ok &&
-           lm_map(encode, &x.lo_k, false, x.lo, x.rows, x.cols, x.pitch,
-                  kTileM) &&
-           lm_map(encode, &x.d, false, x.D, x.m, x.m, x.pitch_m, kTileM) &&
-           lm_map(encode, &x.e, false, x.E, x.m, x.m, x.pitch_m, kTileM) &&
-           lm_map(encode, &x.d_t, false, x.D, x.m, x.m, x.pitch_m, 64) &&
-           lm_map(encode, &x.e_t, false, x.E, x.m, x.m, x.pitch_m, 64);
+      map(&x.lo_c, x.lo, x.rows, x.cols, x.pitch, kMuonTileM, kMuonCols);
+      map(&x.d, x.D, x.m, x.m, x.pitch_m, kMuonTileM, 64);
+      map(&x.e, x.E, x.m, x.m, x.pitch_m, kMuonTileM, 64);
+      map(&x.d_c, x.D, x.m, x.m, x.pitch_m, kMuonTileM, kMuonCols);
+      map(&x.e_c, x.E, x.m, x.m, x.pitch_m, kMuonTileM, kMuonCols);
+      map(&x.d_t, x.D, x.m, x.m, x.pitch_m, kMuonCols, 64);
+      map(&x.e_t, x.E, x.m, x.m, x.pitch_m, kMuonCols, 64);
+      ok = m;
     }
     if (e == cudaSuccess && !ok) {
       e = cudaErrorNotSupported;
@@ -1208,6 +769,9 @@ extern "C" lamb_status_t lamb_muon_create(
     if (e == cudaSuccess && !L.tiles.empty())
       e = cudaMemcpy(p->tiles, L.tiles.data(),
                      L.tiles.size() * sizeof(MuonTile), cudaMemcpyHostToDevice);
+    if (e == cudaSuccess && !L.spans.empty())
+      e = cudaMemcpy(p->spans, L.spans.data(),
+                     L.spans.size() * sizeof(MuonSpan), cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
   } catch (const std::bad_alloc&) {
     lamb_muon_destroy(p);

@@ -1,0 +1,110 @@
+// The Muon plan's device tables, and the launch of its product steps.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "lm_host.h"
+
+namespace lamb {
+
+constexpr float kScaleD = 1024.f;            // D is stored times this
+constexpr float kScaleE = 256.f;             // and E times this
+constexpr float kScaleLo = 2048.f;           // lo: the rest of hi, times this
+
+struct MuonMatrix {
+  // the products' operands: boxes of 64 columns in the 128-byte swizzle
+  CUtensorMap x_k[2], x_mn[2];   // hi (two buffers, taken in turn)
+  CUtensorMap d, e;
+  // the epilogues' blocks: 128 rows of 32 columns (64-byte swizzle), and
+  // mirrored ones of 32 rows by 64 columns
+  CUtensorMap x_c[2], lo_c, d_c, e_c, d_t, e_t;
+  __half* hi[2];
+  __half* lo;
+  __half* D;
+  __half* E;
+  float* diag;                   // l
+  float* beta;
+  float scale;                   // hi + lo = X scale
+  int rows, cols, m, n;          // m = min, n = max
+  int tall;                      // rows > cols
+  int pitch, pitch_m;            // of X, of D and E
+  int first_chunk, n_chunks;
+  int sym, app;                  // tiles of a Gram matrix, of X
+  float decay;
+};
+
+struct MuonPtrs {
+  float* w;
+  const void* g;                 // or the direction's input
+  float* m;
+  __nv_bfloat16* out;            // copy of w, or the direction
+};
+
+struct MuonChunk {
+  int matrix;
+  int len;
+  int64_t offset;
+};
+
+enum { kGram = 0, kSquare = 1, kApply = 2, kNoTile = 3 };
+
+// A tile of one product of one matrix.
+struct MuonTile {
+  int matrix, i, j, phase;
+};
+// Tiles of matrices that go through their steps side by side, in the order of
+// one step.
+struct MuonSpan {
+  int first, count;
+};
+
+struct MuonConsts {
+  float a, b, c;
+  float beta, omb;               // momentum
+  float eps;
+  float wd, size;                // lambda, s without its shape's part
+  int nesterov, scale_kind;
+};
+
+struct MuonParams {
+  const MuonMatrix* mats;
+  const MuonPtrs* ptrs;
+  const MuonTile* tiles;
+  const MuonSpan* spans;
+  uint32_t* done;                // tiles of each matrix finished
+  uint32_t* ticket;              // tiles taken
+  const float* d_lr;             // NULL: the direction alone
+  uint32_t* status;
+  MuonConsts k;
+  int n_spans, steps;
+  int total;                     // tiles of all steps
+};
+
+// s of a matrix.
+__device__ __forceinline__ float muon_size(const MuonConsts& k,
+                                           const MuonMatrix& x) {
+  if (k.scale_kind == LAMB_MUON_SCALE_RMS)
+    return k.size * 0.2f * sqrtf((float)x.n);
+  if (k.scale_kind == LAMB_MUON_SCALE_SPECTRAL)
+    return k.size * sqrtf(fmaxf(1.f, (float)x.rows / (float)x.cols));
+  return k.size;
+}
+__device__ __forceinline__ uint32_t pack_half2(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 half2_at(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+__device__ __forceinline__ uint16_t half_bits(uint32_t w, int i) {
+  return (uint16_t)(i ? w >> 16 : w & 0xffffu);
+}
+
+constexpr int kMuonTileM = 128, kMuonTileN = 256;   // rows, columns of a tile
+constexpr int kMuonCols = 32;                       // columns of a block
+
+// lm_muon_steps.cu
+int muon_steps_setup();
+cudaError_t muon_launch_steps(const MuonParams& p, int sms, cudaStream_t stream);
+
+}  // namespace lamb

@@ -1,0 +1,707 @@
+// The products of the Muon update: all steps of all matrices in one launch.
+//
+// Per matrix and step: G = X X^T, G G, and (b G + c G G) X (lm_muon.cu has the
+// splitting of G and X that keeps their precision).  A tile is 128 x 256 of one
+// product; the symmetric ones are taken on and above the diagonal only.
+//
+// One persistent CTA per SM draws tiles from one list.  Two sets of matrices go
+// through their steps side by side in it, so that while the last tiles of one
+// set's product are still in work the other set's fill the SMs; a set is small
+// enough for both to stay in L2 (kMuonSetBytes).  A tile of a product waits for
+// all tiles of the product before it of the same matrix (a counter for each
+// matrix).  Those come earlier in the list, which is drawn in order, so the
+// earliest unfinished tile waits for nothing; all CTAs are resident (cooperative
+// launch).  Waits are bounded.
+//
+// Warps: 0 draws tiles and copies operands, 1 issues the products, 2 copies the
+// epilogue's blocks in (and holds the tensor memory), 3 copies them out, 4-7 and
+// 8-11 run the epilogue, every other block each.  A block is 32 columns of the
+// tile: its inputs (X as hi and lo; D) come to a ring of staging buffers ahead of
+// the products' end, the epilogue turns them over in place, a row a thread, and
+// tensor copies take them out (clipped at the matrix' edges).  The tile is counted
+// as done when those have landed.
+#include <algorithm>
+
+#include "lm_gemm.cuh"
+#include "lm_muon.h"
+
+namespace lamb {
+namespace {
+
+constexpr int kStages = 3;
+constexpr int kBuffers = 5;
+constexpr int kBlockBytes = kTileM * kMuonCols * 2;     // of one fp16 matrix
+constexpr int kBufferBytes = 2 * kBlockBytes;
+constexpr int kRing = 4;                                // tiles drawn ahead
+constexpr int kGroups = 2;                              // of epilogue warps
+constexpr int kStepThreads = 128 + kGroups * kEpiThreads;
+// readers of a drawn tile: products, copies in, copies out, epilogue warps
+constexpr int kReaders = 3 + 4 * kGroups;
+constexpr size_t kSmem =
+    (size_t)kStages * kGemmStageBytes + kBuffers * kBufferBytes + 1024;
+static_assert(kTileM == kMuonTileM && kTileN == kMuonTileN, "tiles");
+
+struct Drawn {
+  MuonTile t;
+  int it;            // step
+  uint32_t need;     // the matrix' finished tiles that it waits for
+};
+
+struct Shared {
+  uint64_t full[kStages], empty[kStages];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t in[kBuffers], out[kBuffers], vacant[kBuffers];
+  uint64_t drawn[kRing], read[kRing];
+  Drawn ring[kRing];
+  uint32_t tmem;
+  volatile int gave_up;
+};
+
+// Bounded wait on shared barriers.
+__device__ __forceinline__ bool wait_on(Shared& sh, const MuonParams& p,
+                                        uint64_t* bar, uint32_t parity) {
+  return bounded_wait(bar, parity, &sh.gave_up, p.status,
+                      LAMB_STATUS_WAIT_TIMEOUT);
+}
+
+// The 16-byte unit q of row r: rows of 64 bytes, rows of 128 bytes.
+__device__ __forceinline__ uint32_t unit64(uint32_t base, int r, int q) {
+  return base + r * 64 + ((q ^ ((r >> 1) & 3)) << 4);
+}
+__device__ __forceinline__ uint32_t unit128(uint32_t base, int r, int q) {
+  return base + r * 128 + ((q ^ (r & 7)) << 4);
+}
+// Entry (j, i) of a mirrored block: 32 rows in two halves of 64 columns.
+__device__ __forceinline__ uint32_t mirrored(uint32_t base, int j, int i) {
+  return unit128(base + (i >> 6) * (kBlockBytes / 2), j, (i & 63) >> 3) +
+         (i & 7) * 2;
+}
+// Whether the block of rows c0 .. and columns a0 .. lies in no tile on or above
+// the diagonal.
+__device__ __forceinline__ bool mirror(int a0, int c0) {
+  return a0 / kTileN * kTileN + kTileN - 1 < c0 / kTileM * kTileM;
+}
+
+// ---- warp 0 -------------------------------------------------------------------
+struct Operands {
+  const CUtensorMap *a, *b;
+  int kn;
+  bool a_mn, b_mn;
+};
+
+__device__ __forceinline__ Operands operands(const MuonMatrix* x,
+                                             const Drawn& d) {
+  const int from = d.it & 1;
+  Operands o;
+  o.a_mn = o.b_mn = false;
+  o.kn = ((d.t.phase == kGram ? x->n : x->m) + kTileK - 1) / kTileK;
+  if (d.t.phase == kGram) {
+    o.a_mn = o.b_mn = x->tall;
+    o.a = o.b = x->tall ? &x->x_mn[from] : &x->x_k[from];
+  } else if (d.t.phase == kSquare) {
+    o.a = o.b = &x->d;
+  } else if (x->tall) {
+    o.a = &x->x_k[from];
+    o.b = &x->e;
+  } else {
+    o.a = &x->e;
+    o.b = &x->x_mn[from];
+    o.b_mn = true;
+  }
+  return o;
+}
+
+__device__ __forceinline__ bool ready(const MuonParams& p, const Drawn& d) {
+  return ld_acquire_u32(p.done + d.t.matrix) >= d.need;
+}
+__device__ __forceinline__ bool wait_ready(Shared& sh, const MuonParams& p,
+                                           const Drawn& d) {
+  if (ready(p, d)) return true;
+  const uint64_t begin = global_ns();
+  while (!ready(p, d)) {
+    if (sh.gave_up) return false;
+    if (global_ns() - begin > kWaitLimitNs) {
+      sh.gave_up = 1;
+      atomicOr(p.status, LAMB_STATUS_WAIT_TIMEOUT);
+      return false;
+    }
+    __nanosleep(64);
+  }
+  return true;
+}
+
+__device__ __forceinline__ void draw_and_copy(Shared& sh, const MuonParams& p,
+                                              uint32_t smem) {
+  int it = 0, span = 0, base = 0;
+  int next = (int)atomicAdd(p.ticket, 1u);
+  for (int n = 0;; ++n) {
+    const int slot = n % kRing;
+    if (!wait_on(sh, p, &sh.read[slot], ((uint32_t)(n / kRing) & 1u) ^ 1u))
+      break;
+    const int t = next;
+    Drawn d;
+    d.t.phase = kNoTile;
+    if (t < p.total) {
+      next = (int)atomicAdd(p.ticket, 1u);
+      MuonSpan s = p.spans[span];
+      while (t - base >= s.count * p.steps) {
+        base += s.count * p.steps;
+        s = p.spans[++span];
+      }
+      d.it = (t - base) / s.count;
+      d.t = p.tiles[s.first + (t - base) - d.it * s.count];
+      const MuonMatrix* x = p.mats + d.t.matrix;
+      d.need = (uint32_t)(d.it * (2 * x->sym + x->app) + d.t.phase * x->sym);
+    }
+    sh.ring[slot] = d;
+    mbar_arrive(&sh.drawn[slot]);
+    if (d.t.phase == kNoTile) break;
+    const Operands o = operands(p.mats + d.t.matrix, d);
+    if (!wait_ready(sh, p, d)) break;
+    fence_proxy_async();       // other CTAs' blocks, to be read by copies
+    const int a0 = d.t.i * kTileM, b0 = d.t.j * kTileN;
+    for (int kb = 0; kb < o.kn; ++kb, ++it) {
+      const int s = it % kStages;
+      if (!wait_on(sh, p, &sh.empty[s], ((uint32_t)(it / kStages) & 1u) ^ 1u))
+        break;
+      const uint32_t at = smem + s * kGemmStageBytes;
+      const int k = kb * kTileK;
+      mbar_expect(&sh.full[s], kGemmStageBytes);
+      if (o.a_mn) {
+        tile_load(at, o.a, a0, k, &sh.full[s]);
+        tile_load(at + 8192, o.a, a0 + 64, k, &sh.full[s]);
+      } else {
+        tile_load(at, o.a, k, a0, &sh.full[s]);
+      }
+      const uint32_t bt = at + kTileBytesA;
+      if (o.b_mn) {
+        for (int i = 0; i < 4; ++i)
+          tile_load(bt + i * 8192, o.b, b0 + 64 * i, k, &sh.full[s]);
+      } else {
+        tile_load(bt, o.b, k, b0, &sh.full[s]);
+        tile_load(bt + 16384, o.b, k, b0 + 128, &sh.full[s]);
+      }
+    }
+    if (sh.gave_up) break;
+  }
+  for (int j = it > kStages ? it - kStages : 0; j < it; ++j)
+    settle(&sh.full[j % kStages], (uint32_t)(j / kStages) & 1u);
+}
+
+// ---- warp 1 -------------------------------------------------------------------
+__device__ __forceinline__ void multiply(Shared& sh, const MuonParams& p,
+                                         uint32_t smem, uint32_t tmem) {
+  int it = 0;
+  for (int n = 0;; ++n) {
+    const int slot = n % kRing;
+    if (!wait_on(sh, p, &sh.drawn[slot], (uint32_t)(n / kRing) & 1u)) return;
+    const Drawn d = sh.ring[slot];
+    mbar_arrive(&sh.read[slot]);
+    if (d.t.phase == kNoTile) return;
+    const Operands o = operands(p.mats + d.t.matrix, d);
+    const uint64_t da = operand_desc(o.a_mn), db = operand_desc(o.b_mn);
+    const uint32_t sa = operand_step(o.a_mn), sb = operand_step(o.b_mn);
+    const uint32_t desc = product_desc(false, o.a_mn, o.b_mn, kTileM, kTileN);
+    const int acc = n & 1;
+    const uint32_t to = tmem + acc * kTileN;
+    if (!wait_on(sh, p, &sh.acc_empty[acc], ((uint32_t)(n >> 1) & 1u) ^ 1u))
+      return;
+    tmem_after_sync();
+    for (int kb = 0; kb < o.kn; ++kb, ++it) {
+      const int s = it % kStages;
+      if (!wait_on(sh, p, &sh.full[s], (uint32_t)(it / kStages) & 1u)) return;
+      tmem_after_sync();
+      const uint32_t at = smem + s * kGemmStageBytes;
+      const uint64_t a = da | (at >> 4), b = db | ((at + kTileBytesA) >> 4);
+#pragma unroll
+      for (int k = 0; k < kTileK / 16; ++k)
+        product(to, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
+      products_arrive(&sh.empty[s]);
+    }
+    products_arrive(&sh.acc_full[acc]);
+  }
+}
+
+// ---- warp 2 -------------------------------------------------------------------
+__device__ __forceinline__ int block_count(const MuonMatrix& x,
+                                           const Drawn& d) {
+  const int width = d.t.phase == kApply ? x.cols : x.m;
+  const int left = (width - d.t.j * kTileN + kMuonCols - 1) / kMuonCols;
+  return left < kTileN / kMuonCols ? left : kTileN / kMuonCols;
+}
+
+// The next drawn tile: false at the end, or if a wait gave up.
+__device__ __forceinline__ bool next_tile(Shared& sh, const MuonParams& p,
+                                          int tile, Drawn* d) {
+  const int slot = tile % kRing;
+  if (!wait_on(sh, p, &sh.drawn[slot], (uint32_t)(tile / kRing) & 1u))
+    return false;
+  *d = sh.ring[slot];
+  return d->t.phase != kNoTile;
+}
+
+__device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
+                                        uint32_t staging) {
+  int n = 0;
+  Drawn d;
+  for (int tile = 0; next_tile(sh, p, tile, &d); ++tile) {
+    mbar_arrive(&sh.read[tile % kRing]);
+    const MuonMatrix& x = p.mats[d.t.matrix];
+    const int blocks = block_count(x, d), from = d.it & 1;
+    const int a0 = d.t.i * kTileM;
+    if (d.t.phase != kGram) {
+      if (!wait_ready(sh, p, d)) break;
+      fence_proxy_async();
+    }
+    for (int c = 0; c < blocks; ++c, ++n) {
+      const int b = n % kBuffers;
+      if (!wait_on(sh, p, &sh.vacant[b], ((uint32_t)(n / kBuffers) & 1u) ^ 1u))
+        break;
+      const uint32_t to = staging + b * kBufferBytes;
+      const int c0 = d.t.j * kTileN + c * kMuonCols;
+      if (d.t.phase == kGram) {
+        mbar_arrive(&sh.in[b]);
+      } else if (d.t.phase == kSquare) {
+        mbar_expect(&sh.in[b], kBlockBytes);
+        tile_load(to, &x.d_c, c0, a0, &sh.in[b]);
+      } else {
+        mbar_expect(&sh.in[b], 2 * kBlockBytes);
+        tile_load(to, &x.x_c[from], c0, a0, &sh.in[b]);
+        tile_load(to + kBlockBytes, &x.lo_c, c0, a0, &sh.in[b]);
+      }
+    }
+    if (sh.gave_up) break;
+  }
+  // copies that were started land before the CTA may leave
+  for (int j = n > kBuffers ? n - kBuffers : 0; j < n; ++j)
+    settle(&sh.in[j % kBuffers], (uint32_t)(j / kBuffers) & 1u);
+}
+
+// ---- warp 3 -------------------------------------------------------------------
+__device__ __forceinline__ void copy_out(Shared& sh, const MuonParams& p,
+                                         uint32_t staging) {
+  int n = 0;
+  Drawn d;
+  for (int tile = 0; next_tile(sh, p, tile, &d); ++tile) {
+    const MuonMatrix& x = p.mats[d.t.matrix];
+    const int blocks = block_count(x, d), m = x.m;
+    const int a0 = d.t.i * kTileM;
+    const bool last = d.t.phase == kApply && d.it == p.steps - 1;
+    const bool gram = d.t.phase == kGram;
+    const CUtensorMap* const to = d.t.phase == kApply ? &x.x_c[(d.it & 1) ^ 1]
+                                  : gram              ? &x.d_c
+                                                      : &x.e_c;
+    const CUtensorMap* const to_t = gram ? &x.d_t : &x.e_t;
+    for (int c = 0; c < blocks; ++c, ++n) {
+      const int b = n % kBuffers;
+      if (!wait_on(sh, p, &sh.out[b], (uint32_t)(n / kBuffers) & 1u)) break;
+      if (last) {
+        mbar_arrive(&sh.vacant[b]);
+        continue;
+      }
+      const uint32_t from = staging + b * kBufferBytes;
+      const int c0 = d.t.j * kTileN + c * kMuonCols;
+      tile_store(to, c0, a0, from);
+      if (d.t.phase == kApply) {
+        tile_store(&x.lo_c, c0, a0, from + kBlockBytes);
+      } else if (mirror(a0, c0)) {
+        tile_store(to_t, a0, c0, from + kBlockBytes);
+        if (a0 + 64 < m)
+          tile_store(to_t, a0 + 64, c0,
+                     from + kBlockBytes + kBlockBytes / 2);
+      }
+      stores_commit();
+      if (c > 0) {      // the tile's block before
+        stores_have_read<1>();
+        mbar_arrive(&sh.vacant[(n - 1) % kBuffers]);
+      }
+    }
+    if (!last) {
+      stores_have_read<0>();
+      mbar_arrive(&sh.vacant[(n - 1) % kBuffers]);
+      stores_done();
+      if (sh.gave_up) break;
+      fence_proxy_async();
+      __threadfence();
+      atomicAdd(p.done + d.t.matrix, 1u);
+    }
+    mbar_arrive(&sh.read[tile % kRing]);
+  }
+  stores_done();
+}
+
+// ---- warps 4-11 -----------------------------------------------------------------
+__device__ __forceinline__ void group_sync(int group) {
+  asm volatile("bar.sync %0, %1;" ::"r"(kEpiBarrier + group), "n"(kEpiThreads)
+               : "memory");
+}
+// One answer for all of a group.
+__device__ __forceinline__ bool group_all(int group, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.and.pred q, %2, %3, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"((uint32_t)x), "r"(kEpiBarrier + group), "n"(kEpiThreads)
+      : "memory");
+  return r != 0;
+}
+// What this thread wrote to staging memory is read by copies from here on.
+__device__ __forceinline__ void fence_staging() {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+// Written by other SMs while this kernel runs: not from L1.
+__device__ __forceinline__ float4 far4(const float* p) {
+  return __ldcg(reinterpret_cast<const float4*>(p));
+}
+
+struct Row {
+  int row, i;            // in the tile, in the matrix
+  int group;
+  uint32_t buf;
+};
+
+template <bool kSq>
+__device__ __forceinline__ void symmetric_block(const MuonParams& p,
+                                                const MuonMatrix& x,
+                                                float li, float s, int a0,
+                                                int c0, const Row& r,
+                                                float (&y)[32]) {
+  const bool both = mirror(a0, c0);
+  const bool on = r.i >= c0 && r.i < c0 + 32;      // the diagonal
+  if (!kSq) {
+    if (on && r.i < x.m) {
+#pragma unroll
+      for (int q = 0; q < 32; ++q)
+        if (c0 + q == r.i) x.diag[r.i] = y[q] * s;
+    }
+#pragma unroll
+    for (int q = 0; q < 32; ++q) y[q] *= s * kScaleD;
+  } else {
+    const float pb = p.k.b, pc = p.k.c;
+    if (on && r.i < x.m) {
+#pragma unroll
+      for (int q = 0; q < 32; ++q)
+        if (c0 + q == r.i) x.beta[r.i] = pb * li + pc * (li * li + y[q] * s);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      // (diag's memory goes up to a whole tile)
+      const float4 l0 = far4(x.diag + c0 + 8 * u);
+      const float4 l1 = far4(x.diag + c0 + 8 * u + 4);
+      const float l[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
+      const uint4 d = lds16(unit64(r.buf, r.row, u));
+      const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int q = 8 * u + k;
+        const float2 d2 = half2_at(dw[k >> 1]);
+        const float dd = k & 1 ? d2.y : d2.x;
+        // E kScaleE, dd being D kScaleD
+        const float f = fmaf(pc, li + l[k], pb) * (kScaleE / kScaleD);
+        y[q] = fmaf(f, dd, y[q] * (pc * s * kScaleE));
+      }
+    }
+  }
+  if (on) {
+#pragma unroll
+    for (int q = 0; q < 32; ++q)
+      if (c0 + q == r.i) y[q] = 0.f;
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      w[k] = pack_half2(y[8 * u + 2 * k], y[8 * u + 2 * k + 1]);
+    sts16(unit64(r.buf, r.row, u), make_uint4(w[0], w[1], w[2], w[3]));
+    if (both) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        sts2(mirrored(r.buf + kBlockBytes, 8 * u + k, r.row),
+             half_bits(w[k >> 1], k & 1));
+    }
+  }
+}
+
+// X <- (a + beta) X + E X of a block; y holds the product and gets X * scale.
+template <bool kLast>
+__device__ __forceinline__ void apply_block(const MuonMatrix& x, float pa,
+                                            float br, int c0, const Row& r,
+                                            float (&y)[32]) {
+  const bool tall = x.tall;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    float f[8];
+    if (tall) {          // (beta's memory goes up to a whole tile)
+      const float4 b0 = far4(x.beta + c0 + 8 * u);
+      const float4 b1 = far4(x.beta + c0 + 8 * u + 4);
+      f[0] = pa + b0.x; f[1] = pa + b0.y; f[2] = pa + b0.z; f[3] = pa + b0.w;
+      f[4] = pa + b1.x; f[5] = pa + b1.y; f[6] = pa + b1.z; f[7] = pa + b1.w;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] = br;
+    }
+    const uint32_t ah = unit64(r.buf, r.row, u), al = ah + kBlockBytes;
+    const uint4 hi = lds16(ah), lo = lds16(al);
+    const uint32_t hw[4] = {hi.x, hi.y, hi.z, hi.w};
+    const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w};
+    uint32_t oh[4], ol[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 a = half2_at(hw[k]), b = half2_at(lw[k]);
+      const int q = 8 * u + 2 * k;
+      y[q] = fmaf(f[2 * k], fmaf(b.x, 1.f / kScaleLo, a.x),
+                  y[q] * (1.f / kScaleE));
+      y[q + 1] = fmaf(f[2 * k + 1], fmaf(b.y, 1.f / kScaleLo, a.y),
+                      y[q + 1] * (1.f / kScaleE));
+      if (!kLast) {
+        oh[k] = pack_half2(y[q], y[q + 1]);
+        const float2 h = half2_at(oh[k]);
+        ol[k] = pack_half2((y[q] - h.x) * kScaleLo, (y[q + 1] - h.y) * kScaleLo);
+      }
+    }
+    if (!kLast) {
+      sts16(ah, make_uint4(oh[0], oh[1], oh[2], oh[3]));
+      sts16(al, make_uint4(ol[0], ol[1], ol[2], ol[3]));
+    }
+  }
+}
+
+// The last X to the weights or the direction: eight threads a row of a block.
+// The old weights are on their way while the block is turned over.
+struct Output {
+  float* w;
+  __nv_bfloat16* out;
+  float inv, keep, move;
+  int rows, cols;
+  bool step, vec;
+};
+
+__device__ __forceinline__ Output output_of(const MuonParams& p,
+                                            const MuonMatrix& x,
+                                            const MuonPtrs& t) {
+  Output o;
+  o.w = t.w;
+  o.out = t.out;
+  o.step = p.d_lr != nullptr;
+  const float lr = o.step ? *p.d_lr : 0.f;
+  o.inv = 1.f / x.scale;
+  o.keep = 1.f - lr * p.k.wd * x.decay;
+  o.move = lr * muon_size(p.k, x);
+  o.rows = x.rows;
+  o.cols = x.cols;
+  o.vec = x.cols % 4 == 0 && (!o.step || (uintptr_t)t.w % 16 == 0) &&
+          (uintptr_t)t.out % 8 == 0;
+  return o;
+}
+
+__device__ __forceinline__ void last_block(const Output& o, int a0, int c0,
+                                           const Row& r, float (&y)[32]) {
+  const int u = r.row & 7, c = c0 + 4 * u;
+  const int cols = min(4, o.cols - c);
+  constexpr int kRows = kEpiThreads / 8;
+  float4 old[kTileM / kRows];
+  if (o.step && o.vec && cols == 4) {
+#pragma unroll
+    for (int k = 0; k < kTileM / kRows; ++k) {
+      const int rr = a0 + k * kRows + (r.row >> 3);
+      if (rr < o.rows)
+        old[k] = *reinterpret_cast<const float4*>(o.w + (int64_t)rr * o.cols + c);
+    }
+  }
+  group_sync(r.group);          // everybody has read the block's inputs
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    sts16(unit128(r.buf, r.row, q),
+          make_uint4(__float_as_uint(y[4 * q] * o.inv),
+                     __float_as_uint(y[4 * q + 1] * o.inv),
+                     __float_as_uint(y[4 * q + 2] * o.inv),
+                     __float_as_uint(y[4 * q + 3] * o.inv)));
+  group_sync(r.group);
+#pragma unroll
+  for (int k = 0; k < kTileM / kRows; ++k) {
+    const int br = k * kRows + (r.row >> 3), rr = a0 + br;
+    const uint4 b = lds16(unit128(r.buf, br, u));
+    if (rr >= o.rows || cols <= 0) continue;
+    float v[4] = {__uint_as_float(b.x), __uint_as_float(b.y),
+                  __uint_as_float(b.z), __uint_as_float(b.w)};
+    const int64_t at = (int64_t)rr * o.cols + c;
+    if (o.vec && cols == 4) {
+      if (o.step) {
+        v[0] = o.keep * old[k].x - o.move * v[0];
+        v[1] = o.keep * old[k].y - o.move * v[1];
+        v[2] = o.keep * old[k].z - o.move * v[2];
+        v[3] = o.keep * old[k].w - o.move * v[3];
+        *reinterpret_cast<float4*>(o.w + at) =
+            make_float4(v[0], v[1], v[2], v[3]);
+      }
+      if (o.out) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+        const __nv_bfloat162 l = __floats2bfloat162_rn(v[2], v[3]);
+        *reinterpret_cast<uint2*>(o.out + at) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&h),
+                       *reinterpret_cast<const uint32_t*>(&l));
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q >= cols) break;
+        if (o.step) {
+          v[q] = o.keep * o.w[at + q] - o.move * v[q];
+          o.w[at + q] = v[q];
+        }
+        if (o.out) o.out[at + q] = __float2bfloat16_rn(v[q]);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
+                                          uint32_t staging, uint32_t tmem) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int quarter = warp & 3;
+  Row r;
+  r.row = quarter * 32 + lane;
+  r.group = (warp - 4) >> 2;
+  int n = 0;
+  for (int tile = 0;; ++tile) {
+    const int slot = tile % kRing;
+    bool ok = wait_on(sh, p, &sh.drawn[slot], (uint32_t)(tile / kRing) & 1u);
+    // one answer for all: the last step's blocks meet at barriers
+    if (!group_all(r.group, ok)) return;
+    const Drawn d = sh.ring[slot];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.read[slot]);
+    if (d.t.phase == kNoTile) return;
+    const int acc = tile & 1;
+    ok = wait_on(sh, p, &sh.acc_full[acc], (uint32_t)(tile >> 1) & 1u);
+    if (!group_all(r.group, ok)) return;
+    tmem_after_sync();
+    const uint32_t from =
+        tmem + acc * kTileN + ((uint32_t)(quarter * 32) << 16);
+    const MuonMatrix& x = p.mats[d.t.matrix];
+    const int a0 = d.t.i * kTileM, blocks = block_count(x, d);
+    r.i = a0 + r.row;
+    const bool last = d.t.phase == kApply && d.it == p.steps - 1;
+    const float li = d.t.phase == kSquare && r.i < x.m ? __ldcg(x.diag + r.i)
+                                                       : 0.f;
+    const float br = d.t.phase == kApply && !x.tall && r.i < x.rows
+                         ? p.k.a + __ldcg(x.beta + r.i) : 0.f;
+    const float s = d.t.phase == kGram ? 1.f / (x.scale * x.scale)
+                                       : 1.f / (kScaleD * kScaleD);
+    Output o;
+    if (last) o = output_of(p, x, p.ptrs[d.t.matrix]);
+    for (int c = 0; c < blocks; ++c, ++n) {
+      if (n % kGroups != r.group) continue;
+      const int b = n % kBuffers, c0 = d.t.j * kTileN + c * kMuonCols;
+      r.buf = staging + b * kBufferBytes;
+      float y[32];
+      tmem_ld32(from + c * kMuonCols, y);
+      wait_on(sh, p, &sh.in[b], (uint32_t)(n / kBuffers) & 1u);
+      if (d.t.phase == kGram) {
+        symmetric_block<false>(p, x, 0.f, s, a0, c0, r, y);
+      } else if (d.t.phase == kSquare) {
+        symmetric_block<true>(p, x, li, s, a0, c0, r, y);
+      } else if (!last) {
+        apply_block<false>(x, p.k.a, br, c0, r, y);
+      } else {
+        apply_block<true>(x, p.k.a, br, c0, r, y);
+        last_block(o, a0, c0, r, y);
+      }
+      fence_staging();
+      mbar_arrive(&sh.out[b]);
+    }
+    tmem_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
+  }
+}
+
+__global__ void __launch_bounds__(kStepThreads, 1)
+muon_steps_kernel(const __grid_constant__ MuonParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Shared sh;
+  const int warp = threadIdx.x >> 5;
+  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t staging = smem + kStages * kGemmStageBytes;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&sh.full[i], 1);
+      mbar_init(&sh.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.acc_full[i], 1);
+      mbar_init(&sh.acc_empty[i], 4 * kGroups);
+    }
+    for (int i = 0; i < kBuffers; ++i) {
+      mbar_init(&sh.in[i], 1);
+      mbar_init(&sh.out[i], kEpiThreads);
+      mbar_init(&sh.vacant[i], 1);
+    }
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&sh.drawn[i], 1);
+      mbar_init(&sh.read[i], kReaders);
+    }
+    sh.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
+  }
+  if (warp == 2) tmem_alloc_all(&sh.tmem);
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  const uint32_t tmem = sh.tmem;
+  if (warp == 0) {
+    if (elect_lane()) draw_and_copy(sh, p, smem);
+    __syncwarp();
+  } else if (warp == 1) {
+    if (elect_lane()) multiply(sh, p, smem, tmem);
+    __syncwarp();
+  } else if (warp == 2) {
+    if (elect_lane()) copy_in(sh, p, staging);
+    __syncwarp();
+  } else if (warp == 3) {
+    if (elect_lane()) copy_out(sh, p, staging);
+    __syncwarp();
+  } else {
+    turn_over(sh, p, staging, tmem);
+  }
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  if (warp == 2) tmem_free_all(tmem);
+}
+
+}  // namespace
+
+int muon_steps_setup() {
+  return (int)cudaFuncSetAttribute(muon_steps_kernel,
+                                   cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)kSmem);
+}
+
+cudaError_t muon_launch_steps(const MuonParams& p, int sms,
+                              cudaStream_t stream) {
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeCooperative;
+  at.val.cooperative = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kStepThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = stream;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  // a process that has fewer SMs than the device takes fewer CTAs
+  cudaError_t e = cudaErrorCooperativeLaunchTooLarge;
+  for (int grid = std::min(sms, p.total);
+       grid > 0 && e == cudaErrorCooperativeLaunchTooLarge; grid /= 2) {
+    cfg.gridDim = dim3((unsigned)grid);
+    e = cudaLaunchKernelEx(&cfg, muon_steps_kernel, p);
+    if (e == cudaErrorCooperativeLaunchTooLarge) cudaGetLastError();
+  }
+  return e;
+}
+
+}  // namespace lamb
