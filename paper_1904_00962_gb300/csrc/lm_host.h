@@ -119,6 +119,26 @@ inline bool lm_map(EncodeTiled encode, CUtensorMap* map, bool bf16,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same matrix in boxes of 64 lines by `blocks` times 64 columns, which arrive
+// block after block (an MN-major operand).  Whole blocks are copied, so that the
+// row stride has to be a multiple of 64; what lies between cols and it is copied
+// too.
+inline bool lm_map_blocks(EncodeTiled encode, CUtensorMap* map, bool bf16,
+                          const void* base, int64_t rows, int64_t row_stride,
+                          int blocks) {
+  const cuuint64_t dims[3] = {64, (cuuint64_t)rows,
+                              (cuuint64_t)(row_stride / 64)};
+  const cuuint64_t strides[2] = {(cuuint64_t)row_stride * 2, 128};
+  const cuuint32_t box[3] = {64, 64, (cuuint32_t)blocks};
+  const cuuint32_t step[3] = {1, 1, 1};
+  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                          : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                3, const_cast<void*>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Whether a 16-bit matrix can be copied by a tensor map where it lies.
 inline bool lm_mappable(const void* p, int64_t row_stride) {
   return ((uintptr_t)p & 15) == 0 && row_stride % 8 == 0;

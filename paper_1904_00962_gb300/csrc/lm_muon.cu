@@ -460,7 +460,7 @@ void muon_layout(const int64_t* rows, const int64_t* cols, int n,
     x.m = std::min(x.rows, x.cols);
     x.n = std::max(x.rows, x.cols);
     x.tall = x.rows > x.cols;
-    x.pitch = (int)lm_round_up(x.cols, 8);
+    x.pitch = (int)lm_round_up(x.cols, 64);   // whole blocks
     x.pitch_m = (int)lm_round_up(x.m, 8);
     x.scale = (float)std::exp2(std::round(0.5 * std::log2((double)std::max(
         1, x.n))));
@@ -725,8 +725,12 @@ extern "C" lamb_status_t lamb_muon_create(
       };
       for (int i = 0; i < 2; ++i) {
         x.hi[i] = (__half*)(base + L.at[i][k]);
-        map(&x.x_k[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileM, 64);
-        map(&x.x_mn[i], x.hi[i], x.rows, x.cols, x.pitch, 64, 64);
+        map(&x.xa_k[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileM, 64);
+        map(&x.xb_k[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileN, 64);
+        m = m && lm_map_blocks(encode, &x.xa_mn[i], false, x.hi[i], x.rows,
+                               x.pitch, kMuonTileM / 64) &&
+            lm_map_blocks(encode, &x.xb_mn[i], false, x.hi[i], x.rows, x.pitch,
+                          kMuonTileN / 64);
         map(&x.x_c[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileM, kMuonCols);
       }
       x.lo = (__half*)(base + L.at[2][k]);
@@ -735,8 +739,10 @@ extern "C" lamb_status_t lamb_muon_create(
       x.diag = (float*)(base + L.at[5][k]);
       x.beta = (float*)(base + L.at[6][k]);
       map(&x.lo_c, x.lo, x.rows, x.cols, x.pitch, kMuonTileM, kMuonCols);
-      map(&x.d, x.D, x.m, x.m, x.pitch_m, kMuonTileM, 64);
-      map(&x.e, x.E, x.m, x.m, x.pitch_m, kMuonTileM, 64);
+      map(&x.da, x.D, x.m, x.m, x.pitch_m, kMuonTileM, 64);
+      map(&x.db, x.D, x.m, x.m, x.pitch_m, kMuonTileN, 64);
+      map(&x.ea, x.E, x.m, x.m, x.pitch_m, kMuonTileM, 64);
+      map(&x.eb, x.E, x.m, x.m, x.pitch_m, kMuonTileN, 64);
       map(&x.d_c, x.D, x.m, x.m, x.pitch_m, kMuonTileM, kMuonCols);
       map(&x.e_c, x.E, x.m, x.m, x.pitch_m, kMuonTileM, kMuonCols);
       map(&x.d_t, x.D, x.m, x.m, x.pitch_m, kMuonCols, 64);

@@ -12,9 +12,10 @@ constexpr float kScaleE = 256.f;             // and E times this
 constexpr float kScaleLo = 2048.f;           // lo: the rest of hi, times this
 
 struct MuonMatrix {
-  // the products' operands: boxes of 64 columns in the 128-byte swizzle
-  CUtensorMap x_k[2], x_mn[2];   // hi (two buffers, taken in turn)
-  CUtensorMap d, e;
+  // the products' operands, a stage's A or B in one copy: K-major (_k), MN-major
+  // (_mn); hi has two buffers, taken in turn
+  CUtensorMap xa_k[2], xb_k[2], xa_mn[2], xb_mn[2];
+  CUtensorMap da, db, ea, eb;
   // the epilogues' blocks: 128 rows of 32 columns (64-byte swizzle), and
   // mirrored ones of 32 rows by 64 columns
   CUtensorMap x_c[2], lo_c, d_c, e_c, d_t, e_t;

@@ -29,7 +29,7 @@ namespace lamb {
 namespace {
 
 constexpr int kStages = 3;
-constexpr int kBuffers = 5;
+constexpr int kBuffers = 4;
 constexpr int kBlockBytes = kTileM * kMuonCols * 2;     // of one fp16 matrix
 constexpr int kBufferBytes = 2 * kBlockBytes;
 constexpr int kRing = 4;                                // tiles drawn ahead
@@ -37,8 +37,10 @@ constexpr int kGroups = 2;                              // of epilogue warps
 constexpr int kStepThreads = 128 + kGroups * kEpiThreads;
 // readers of a drawn tile: products, copies in, copies out, epilogue warps
 constexpr int kReaders = 3 + 4 * kGroups;
-constexpr size_t kSmem =
-    (size_t)kStages * kGemmStageBytes + kBuffers * kBufferBytes + 1024;
+// l or beta of a tile's columns, and of its rows
+constexpr int kColBytes = kTileN * 4, kVecBytes = kColBytes + kTileM * 4;
+constexpr size_t kSmem = (size_t)kStages * kGemmStageBytes +
+                         kBuffers * kBufferBytes + kRing * kVecBytes + 1024;
 static_assert(kTileM == kMuonTileM && kTileN == kMuonTileN, "tiles");
 
 struct Drawn {
@@ -51,7 +53,7 @@ struct Shared {
   uint64_t full[kStages], empty[kStages];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t in[kBuffers], out[kBuffers], vacant[kBuffers];
-  uint64_t drawn[kRing], read[kRing];
+  uint64_t drawn[kRing], read[kRing], vec[kRing];
   Drawn ring[kRing];
   uint32_t tmem;
   volatile int gave_up;
@@ -97,15 +99,17 @@ __device__ __forceinline__ Operands operands(const MuonMatrix* x,
   o.kn = ((d.t.phase == kGram ? x->n : x->m) + kTileK - 1) / kTileK;
   if (d.t.phase == kGram) {
     o.a_mn = o.b_mn = x->tall;
-    o.a = o.b = x->tall ? &x->x_mn[from] : &x->x_k[from];
+    o.a = x->tall ? &x->xa_mn[from] : &x->xa_k[from];
+    o.b = x->tall ? &x->xb_mn[from] : &x->xb_k[from];
   } else if (d.t.phase == kSquare) {
-    o.a = o.b = &x->d;
+    o.a = &x->da;
+    o.b = &x->db;
   } else if (x->tall) {
-    o.a = &x->x_k[from];
-    o.b = &x->e;
+    o.a = &x->xa_k[from];
+    o.b = &x->eb;
   } else {
-    o.a = &x->e;
-    o.b = &x->x_mn[from];
+    o.a = &x->ea;
+    o.b = &x->xb_mn[from];
     o.b_mn = true;
   }
   return o;
@@ -167,20 +171,11 @@ __device__ __forceinline__ void draw_and_copy(Shared& sh, const MuonParams& p,
       const uint32_t at = smem + s * kGemmStageBytes;
       const int k = kb * kTileK;
       mbar_expect(&sh.full[s], kGemmStageBytes);
-      if (o.a_mn) {
-        tile_load(at, o.a, a0, k, &sh.full[s]);
-        tile_load(at + 8192, o.a, a0 + 64, k, &sh.full[s]);
-      } else {
-        tile_load(at, o.a, k, a0, &sh.full[s]);
-      }
-      const uint32_t bt = at + kTileBytesA;
-      if (o.b_mn) {
-        for (int i = 0; i < 4; ++i)
-          tile_load(bt + i * 8192, o.b, b0 + 64 * i, k, &sh.full[s]);
-      } else {
-        tile_load(bt, o.b, k, b0, &sh.full[s]);
-        tile_load(bt + 16384, o.b, k, b0 + 128, &sh.full[s]);
-      }
+      // (issuing a copy takes this thread some 100 cycles: one an operand)
+      if (o.a_mn) blocks_load(at, o.a, k, a0 / 64, &sh.full[s]);
+      else tile_load(at, o.a, k, a0, &sh.full[s]);
+      if (o.b_mn) blocks_load(at + kTileBytesA, o.b, k, b0 / 64, &sh.full[s]);
+      else tile_load(at + kTileBytesA, o.b, k, b0, &sh.full[s]);
     }
     if (sh.gave_up) break;
   }
@@ -242,17 +237,29 @@ __device__ __forceinline__ bool next_tile(Shared& sh, const MuonParams& p,
 
 __device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
                                         uint32_t staging) {
-  int n = 0;
+  int n = 0, begun = 0;       // blocks, tiles whose copies were started
   Drawn d;
   for (int tile = 0; next_tile(sh, p, tile, &d); ++tile) {
-    mbar_arrive(&sh.read[tile % kRing]);
     const MuonMatrix& x = p.mats[d.t.matrix];
     const int blocks = block_count(x, d), from = d.it & 1;
     const int a0 = d.t.i * kTileM;
-    if (d.t.phase != kGram) {
+    const uint32_t vec = staging + kBuffers * kBufferBytes +
+                         tile % kRing * kVecBytes;
+    const float* const v = d.t.phase == kSquare ? x.diag : x.beta;
+    uint64_t* const vb = &sh.vec[tile % kRing];
+    if (d.t.phase == kGram) {
+      mbar_arrive(vb);
+    } else {
       if (!wait_ready(sh, p, d)) break;
       fence_proxy_async();
+      // the tile's l or beta (their memory goes up to a whole tile)
+      const bool cols = d.t.phase == kSquare || x.tall;
+      const bool rows = d.t.phase == kSquare || !x.tall;
+      mbar_expect(vb, (cols ? kColBytes : 0) + (rows ? kTileM * 4 : 0));
+      if (cols) bulk_load_at(vec, v + d.t.j * kTileN, kColBytes, vb);
+      if (rows) bulk_load_at(vec + kColBytes, v + a0, kTileM * 4, vb);
     }
+    begun = tile + 1;
     for (int c = 0; c < blocks; ++c, ++n) {
       const int b = n % kBuffers;
       if (!wait_on(sh, p, &sh.vacant[b], ((uint32_t)(n / kBuffers) & 1u) ^ 1u))
@@ -271,10 +278,13 @@ __device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
       }
     }
     if (sh.gave_up) break;
+    mbar_arrive(&sh.read[tile % kRing]);
   }
   // copies that were started land before the CTA may leave
   for (int j = n > kBuffers ? n - kBuffers : 0; j < n; ++j)
     settle(&sh.in[j % kBuffers], (uint32_t)(j / kBuffers) & 1u);
+  if (begun) settle(&sh.vec[(begun - 1) % kRing],
+                    (uint32_t)((begun - 1) / kRing) & 1u);
 }
 
 // ---- warp 3 -------------------------------------------------------------------
@@ -351,45 +361,46 @@ __device__ __forceinline__ bool group_all(int group, bool x) {
 __device__ __forceinline__ void fence_staging() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
-// Written by other SMs while this kernel runs: not from L1.
-__device__ __forceinline__ float4 far4(const float* p) {
-  return __ldcg(reinterpret_cast<const float4*>(p));
+__device__ __forceinline__ float4 lds_f4(uint32_t at) {
+  const uint4 v = lds16(at);
+  return make_float4(__uint_as_float(v.x), __uint_as_float(v.y),
+                     __uint_as_float(v.z), __uint_as_float(v.w));
+}
+__device__ __forceinline__ float lds_f(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+  return v;
 }
 
 struct Row {
   int row, i;            // in the tile, in the matrix
   int group;
+  uint32_t col;          // l or beta of the block's columns
   uint32_t buf;
 };
 
+// A block of G (kSq: of b G + c G G) without its diagonal, which goes to diag
+// (beta); li: the row's l.
 template <bool kSq>
-__device__ __forceinline__ void symmetric_block(const MuonParams& p,
-                                                const MuonMatrix& x,
-                                                float li, float s, int a0,
-                                                int c0, const Row& r,
+__device__ __forceinline__ void symmetric_block(float pb, float pc, int m,
+                                                float* diag, float li, float s,
+                                                int a0, int c0, const Row& r,
                                                 float (&y)[32]) {
   const bool both = mirror(a0, c0);
   const bool on = r.i >= c0 && r.i < c0 + 32;      // the diagonal
-  if (!kSq) {
-    if (on && r.i < x.m) {
+  if (on && r.i < m) {
 #pragma unroll
-      for (int q = 0; q < 32; ++q)
-        if (c0 + q == r.i) x.diag[r.i] = y[q] * s;
-    }
+    for (int q = 0; q < 32; ++q)
+      if (c0 + q == r.i)
+        diag[r.i] = kSq ? pb * li + pc * (li * li + y[q] * s) : y[q] * s;
+  }
+  if (!kSq) {
 #pragma unroll
     for (int q = 0; q < 32; ++q) y[q] *= s * kScaleD;
   } else {
-    const float pb = p.k.b, pc = p.k.c;
-    if (on && r.i < x.m) {
-#pragma unroll
-      for (int q = 0; q < 32; ++q)
-        if (c0 + q == r.i) x.beta[r.i] = pb * li + pc * (li * li + y[q] * s);
-    }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      // (diag's memory goes up to a whole tile)
-      const float4 l0 = far4(x.diag + c0 + 8 * u);
-      const float4 l1 = far4(x.diag + c0 + 8 * u + 4);
+      const float4 l0 = lds_f4(r.col + 32 * u), l1 = lds_f4(r.col + 32 * u + 16);
       const float l[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
       const uint4 d = lds16(unit64(r.buf, r.row, u));
       const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
@@ -427,16 +438,13 @@ __device__ __forceinline__ void symmetric_block(const MuonParams& p,
 
 // X <- (a + beta) X + E X of a block; y holds the product and gets X * scale.
 template <bool kLast>
-__device__ __forceinline__ void apply_block(const MuonMatrix& x, float pa,
-                                            float br, int c0, const Row& r,
-                                            float (&y)[32]) {
-  const bool tall = x.tall;
+__device__ __forceinline__ void apply_block(bool tall, float pa, float br,
+                                            const Row& r, float (&y)[32]) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     float f[8];
-    if (tall) {          // (beta's memory goes up to a whole tile)
-      const float4 b0 = far4(x.beta + c0 + 8 * u);
-      const float4 b1 = far4(x.beta + c0 + 8 * u + 4);
+    if (tall) {
+      const float4 b0 = lds_f4(r.col + 32 * u), b1 = lds_f4(r.col + 32 * u + 16);
       f[0] = pa + b0.x; f[1] = pa + b0.y; f[2] = pa + b0.z; f[3] = pa + b0.w;
       f[4] = pa + b1.x; f[5] = pa + b1.y; f[6] = pa + b1.z; f[7] = pa + b1.w;
     } else {
@@ -572,8 +580,6 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
     // one answer for all: the last step's blocks meet at barriers
     if (!group_all(r.group, ok)) return;
     const Drawn d = sh.ring[slot];
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.read[slot]);
     if (d.t.phase == kNoTile) return;
     const int acc = tile & 1;
     ok = wait_on(sh, p, &sh.acc_full[acc], (uint32_t)(tile >> 1) & 1u);
@@ -585,29 +591,36 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
     const int a0 = d.t.i * kTileM, blocks = block_count(x, d);
     r.i = a0 + r.row;
     const bool last = d.t.phase == kApply && d.it == p.steps - 1;
-    const float li = d.t.phase == kSquare && r.i < x.m ? __ldcg(x.diag + r.i)
-                                                       : 0.f;
-    const float br = d.t.phase == kApply && !x.tall && r.i < x.rows
-                         ? p.k.a + __ldcg(x.beta + r.i) : 0.f;
+    const bool tall = x.tall;
+    const int m = x.m;
     const float s = d.t.phase == kGram ? 1.f / (x.scale * x.scale)
                                        : 1.f / (kScaleD * kScaleD);
+    float* const diag = d.t.phase == kGram ? x.diag : x.beta;
+    const float pa = p.k.a, pb = p.k.b, pc = p.k.c;
+    const uint32_t vec = staging + kBuffers * kBufferBytes + slot * kVecBytes;
+    float row_v = 0.f;            // the row's l or beta
     Output o;
     if (last) o = output_of(p, x, p.ptrs[d.t.matrix]);
+    if (d.t.phase != kGram) {
+      wait_on(sh, p, &sh.vec[slot], (uint32_t)(tile / kRing) & 1u);
+      row_v = lds_f(vec + kColBytes + 4 * r.row);
+    }
     for (int c = 0; c < blocks; ++c, ++n) {
       if (n % kGroups != r.group) continue;
       const int b = n % kBuffers, c0 = d.t.j * kTileN + c * kMuonCols;
       r.buf = staging + b * kBufferBytes;
+      r.col = vec + c * (kMuonCols * 4);
       float y[32];
       tmem_ld32(from + c * kMuonCols, y);
       wait_on(sh, p, &sh.in[b], (uint32_t)(n / kBuffers) & 1u);
       if (d.t.phase == kGram) {
-        symmetric_block<false>(p, x, 0.f, s, a0, c0, r, y);
+        symmetric_block<false>(pb, pc, m, diag, 0.f, s, a0, c0, r, y);
       } else if (d.t.phase == kSquare) {
-        symmetric_block<true>(p, x, li, s, a0, c0, r, y);
+        symmetric_block<true>(pb, pc, m, diag, row_v, s, a0, c0, r, y);
       } else if (!last) {
-        apply_block<false>(x, p.k.a, br, c0, r, y);
+        apply_block<false>(tall, pa, pa + row_v, r, y);
       } else {
-        apply_block<true>(x, p.k.a, br, c0, r, y);
+        apply_block<true>(tall, pa, pa + row_v, r, y);
         last_block(o, a0, c0, r, y);
       }
       fence_staging();
@@ -615,7 +628,10 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
     }
     tmem_before_sync();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
+    if (lane == 0) {
+      mbar_arrive(&sh.acc_empty[acc]);
+      mbar_arrive(&sh.read[slot]);
+    }
   }
 }
 
@@ -643,6 +659,7 @@ muon_steps_kernel(const __grid_constant__ MuonParams p) {
     for (int i = 0; i < kRing; ++i) {
       mbar_init(&sh.drawn[i], 1);
       mbar_init(&sh.read[i], kReaders);
+      mbar_init(&sh.vec[i], 1);
     }
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");

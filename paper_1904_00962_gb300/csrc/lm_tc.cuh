@@ -64,6 +64,23 @@ __device__ __forceinline__ void tile_load(uint32_t smem, const CUtensorMap* map,
       : "memory");
 }
 
+// bulk_load to a shared-memory address.
+__device__ __forceinline__ void bulk_load_at(uint32_t smem, const void* gmem,
+                                             uint32_t bytes, uint64_t* b) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes "
+      "[%0], [%1], %2, [%3];"
+      ::"r"(smem), "l"(gmem), "r"(bytes), "r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void blocks_load(uint32_t smem,
+                                            const CUtensorMap* map, int line,
+                                            int block, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile"
+      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(smem), "l"(map), "r"(0), "r"(line), "r"(block), "r"(smem_u32(bar))
+      : "memory");
+}
 // Shared memory to a tensor; part of the thread's open group of stores.
 __device__ __forceinline__ void tile_store(const CUtensorMap* map, int x, int y,
                                            uint32_t smem) {
