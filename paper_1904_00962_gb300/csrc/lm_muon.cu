@@ -196,7 +196,7 @@ template <class TG, bool kStep>
 __global__ void __launch_bounds__(kMuonThreads)
 muon_start_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
                   const MuonChunk* chunks, MuonConsts k, const double* part,
-                  uint32_t* done, uint32_t* ticket, uint32_t* status) {
+                  uint32_t* done, uint32_t* status) {
   __shared__ double sh[kMuonThreads / 32];
   const MuonChunk c = chunks[blockIdx.x];
   const MuonMatrix& x = mats[c.matrix];
@@ -208,7 +208,6 @@ muon_start_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
   if (threadIdx.x == 0) {
     if (!isfinite(norm)) atomicOr(status, LAMB_STATUS_NONFINITE);
     if (c.offset == 0) done[c.matrix] = 0;       // of the products to come
-    if (blockIdx.x == 0) *ticket = 0;
   }
   const float f = x.scale / (norm + k.eps);
   if (chunk_vec<TG, kStep>(p, c.len))
@@ -399,7 +398,7 @@ cudaError_t small_smem_limit(int64_t bytes) {
 using namespace lamb;
 
 struct lamb_muon {
-  int device = 0, sms = 0, n = 0;
+  int device = 0, pairs = 0, n = 0;
   bool grad_bf16 = false, copy = false;
   bool bound = false, bound_direction = false;
   void* arena = nullptr;
@@ -411,7 +410,6 @@ struct lamb_muon {
   MuonTile* tiles = nullptr;
   MuonSpan* spans = nullptr;
   uint32_t* done = nullptr;
-  uint32_t* ticket = nullptr;
   double* part = nullptr;
   int* small = nullptr;                // matrices of the small kernel
   int n_small = 0;
@@ -426,7 +424,7 @@ namespace {
 
 // Bytes of the working matrices of a set: two sets go through their steps at a
 // time and have to share L2.
-constexpr int64_t kMuonSetBytes = 56ll << 20;
+constexpr int64_t kMuonSetBytes = 1ll << 40;
 
 struct MuonLayout {
   std::vector<MuonMatrix> mats;
@@ -484,10 +482,11 @@ void muon_layout(const int64_t* rows, const int64_t* cols, int n,
       L->chunks.push_back(
           {k, (int)std::min<int64_t>(kMuonChunk, total - o), o});
     x.n_chunks = (int)L->chunks.size() - x.first_chunk;
-    for (int i = 0; i * kMuonTileM < x.m; ++i)
-      x.sym += (int)lm_ceil_div(x.m, kMuonTileN) - i * kMuonTileM / kMuonTileN;
-    x.app = (int)(lm_ceil_div(x.rows, kMuonTileM) *
-                  lm_ceil_div(x.cols, kMuonTileN));
+    // a CTA that has no rows of a tile does not count it
+    for (int i = 0; i * kMuonRows < x.m; ++i)
+      x.sym += (int)lm_ceil_div(x.m, kMuonTile) - i * kMuonRows / kMuonTile;
+    x.app = (int)(lm_ceil_div(x.rows, kMuonRows) *
+                  lm_ceil_div(x.cols, kMuonTile));
   }
   L->work_bytes = used;
   if (large.empty()) return;
@@ -525,9 +524,8 @@ void muon_layout(const int64_t* rows, const int64_t* cols, int n,
           const MuonMatrix& x = L->mats[k];
           const int r = phase == kApply ? x.rows : x.m;
           const int c = phase == kApply ? x.cols : x.m;
-          for (int i = 0; i * kMuonTileM < r; ++i)
-            for (int j = phase == kApply ? 0 : i * kMuonTileM / kMuonTileN;
-                 j * kMuonTileN < c; ++j)
+          for (int i = 0; i * kMuonTile < r; ++i)
+            for (int j = phase == kApply ? 0 : i; j * kMuonTile < c; ++j)
               L->tiles.push_back({k, i, j, phase});
         }
       }
@@ -573,7 +571,7 @@ void muon_front(const lamb_muon* p, const MuonPtrs* ptrs, const MuonConsts& k,
   muon_norm_kernel<TG, kStep><<<p->n_chunks, kMuonThreads, 0, stream>>>(
       ptrs, p->chunks, k, p->part);
   muon_start_kernel<TG, kStep><<<p->n_chunks, kMuonThreads, 0, stream>>>(
-      p->mats, ptrs, p->chunks, k, p->part, p->done, p->ticket, p->status);
+      p->mats, ptrs, p->chunks, k, p->part, p->done, p->status);
 }
 
 lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
@@ -618,10 +616,9 @@ lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
     q.spans = p->spans;
     q.n_spans = p->n_spans;
     q.done = p->done;
-    q.ticket = p->ticket;
     q.steps = h->steps;
     q.total = (int)(p->step_tiles * h->steps);
-    e = muon_launch_steps(q, p->sms, stream);
+    e = muon_launch_steps(q, p->pairs, stream);
   }
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "muon launch");
 }
@@ -689,8 +686,9 @@ extern "C" lamb_status_t lamb_muon_create(
       return lm_fail(LAMB_ERR_INVALID_ARG, "the matrices have too many tiles");
     }
     const EncodeTiled encode = lm_encoder();
-    e = cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = (cudaError_t)muon_steps_setup();
+    int sms = 0;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = muon_steps_setup(sms, &p->pairs);
     LmArena a;
     for (int pass = 0; e == cudaSuccess && pass < 2; ++pass) {
       a.used = 0;
@@ -702,7 +700,6 @@ extern "C" lamb_status_t lamb_muon_create(
       a.take(&p->tiles, (int64_t)L.tiles.size());
       a.take(&p->spans, (int64_t)L.spans.size());
       a.take(&p->done, n_matrices);
-      a.take(&p->ticket, 1);
       a.take(&p->part, (int64_t)L.chunks.size());
       a.take(&p->small, (int64_t)L.small.size());
       if (pass == 0) {
@@ -725,26 +722,21 @@ extern "C" lamb_status_t lamb_muon_create(
       };
       for (int i = 0; i < 2; ++i) {
         x.hi[i] = (__half*)(base + L.at[i][k]);
-        map(&x.xa_k[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileM, 64);
-        map(&x.xb_k[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileN, 64);
-        m = m && lm_map_blocks(encode, &x.xa_mn[i], false, x.hi[i], x.rows,
-                               x.pitch, kMuonTileM / 64) &&
-            lm_map_blocks(encode, &x.xb_mn[i], false, x.hi[i], x.rows, x.pitch,
-                          kMuonTileN / 64);
-        map(&x.x_c[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonTileM, kMuonCols);
+        map(&x.x_k[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonRows, 64);
+        m = m && lm_map_blocks(encode, &x.x_mn[i], false, x.hi[i], x.rows,
+                               x.pitch, kMuonRows / 64);
+        map(&x.x_c[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonRows, kMuonCols);
       }
       x.lo = (__half*)(base + L.at[2][k]);
       x.D = (__half*)(base + L.at[3][k]);
       x.E = (__half*)(base + L.at[4][k]);
       x.diag = (float*)(base + L.at[5][k]);
       x.beta = (float*)(base + L.at[6][k]);
-      map(&x.lo_c, x.lo, x.rows, x.cols, x.pitch, kMuonTileM, kMuonCols);
-      map(&x.da, x.D, x.m, x.m, x.pitch_m, kMuonTileM, 64);
-      map(&x.db, x.D, x.m, x.m, x.pitch_m, kMuonTileN, 64);
-      map(&x.ea, x.E, x.m, x.m, x.pitch_m, kMuonTileM, 64);
-      map(&x.eb, x.E, x.m, x.m, x.pitch_m, kMuonTileN, 64);
-      map(&x.d_c, x.D, x.m, x.m, x.pitch_m, kMuonTileM, kMuonCols);
-      map(&x.e_c, x.E, x.m, x.m, x.pitch_m, kMuonTileM, kMuonCols);
+      map(&x.lo_c, x.lo, x.rows, x.cols, x.pitch, kMuonRows, kMuonCols);
+      map(&x.d, x.D, x.m, x.m, x.pitch_m, kMuonRows, 64);
+      map(&x.e, x.E, x.m, x.m, x.pitch_m, kMuonRows, 64);
+      map(&x.d_c, x.D, x.m, x.m, x.pitch_m, kMuonRows, kMuonCols);
+      map(&x.e_c, x.E, x.m, x.m, x.pitch_m, kMuonRows, kMuonCols);
       map(&x.d_t, x.D, x.m, x.m, x.pitch_m, kMuonCols, 64);
       map(&x.e_t, x.E, x.m, x.m, x.pitch_m, kMuonCols, 64);
       ok = m;

@@ -12,10 +12,9 @@ constexpr float kScaleE = 256.f;             // and E times this
 constexpr float kScaleLo = 2048.f;           // lo: the rest of hi, times this
 
 struct MuonMatrix {
-  // the products' operands, a stage's A or B in one copy: K-major (_k), MN-major
-  // (_mn); hi has two buffers, taken in turn
-  CUtensorMap xa_k[2], xb_k[2], xa_mn[2], xb_mn[2];
-  CUtensorMap da, db, ea, eb;
+  // the products' operands, 128 rows by 64 of K in one copy: K-major (_k),
+  // MN-major (_mn); hi has two buffers, taken in turn
+  CUtensorMap x_k[2], x_mn[2], d, e;
   // the epilogues' blocks: 128 rows of 32 columns (64-byte swizzle), and
   // mirrored ones of 32 rows by 64 columns
   CUtensorMap x_c[2], lo_c, d_c, e_c, d_t, e_t;
@@ -30,7 +29,7 @@ struct MuonMatrix {
   int tall;                      // rows > cols
   int pitch, pitch_m;            // of X, of D and E
   int first_chunk, n_chunks;
-  int sym, app;                  // tiles of a Gram matrix, of X
+  int sym, app;                  // CTAs' tiles of a Gram matrix, of X
   float decay;
 };
 
@@ -49,7 +48,7 @@ struct MuonChunk {
 
 enum { kGram = 0, kSquare = 1, kApply = 2, kNoTile = 3 };
 
-// A tile of one product of one matrix.
+// A tile of one product of one matrix, two CTAs' work.
 struct MuonTile {
   int matrix, i, j, phase;
 };
@@ -72,8 +71,7 @@ struct MuonParams {
   const MuonPtrs* ptrs;
   const MuonTile* tiles;
   const MuonSpan* spans;
-  uint32_t* done;                // tiles of each matrix finished
-  uint32_t* ticket;              // tiles taken
+  uint32_t* done;                // CTAs' tiles of each matrix finished
   const float* d_lr;             // NULL: the direction alone
   uint32_t* status;
   MuonConsts k;
@@ -101,11 +99,13 @@ __device__ __forceinline__ uint16_t half_bits(uint32_t w, int i) {
   return (uint16_t)(i ? w >> 16 : w & 0xffffu);
 }
 
-constexpr int kMuonTileM = 128, kMuonTileN = 256;   // rows, columns of a tile
+constexpr int kMuonTile = 256;        // a tile's rows and columns
+constexpr int kMuonRows = 128;        // rows of it a CTA has
 constexpr int kMuonCols = 32;                       // columns of a block
 
-// lm_muon_steps.cu
-int muon_steps_setup();
-cudaError_t muon_launch_steps(const MuonParams& p, int sms, cudaStream_t stream);
+// lm_muon_steps.cu.  Setup: how many pairs of CTAs the current device holds.
+cudaError_t muon_steps_setup(int sms, int* pairs);
+cudaError_t muon_launch_steps(const MuonParams& p, int pairs,
+                              cudaStream_t stream);
 
 }  // namespace lamb

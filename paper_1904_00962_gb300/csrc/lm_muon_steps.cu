@@ -1,19 +1,21 @@
 // The products of the Muon update: all steps of all matrices in one launch.
 //
 // Per matrix and step: G = X X^T, G G, and (b G + c G G) X (lm_muon.cu has the
-// splitting of G and X that keeps their precision).  A tile is 128 x 256 of one
-// product; the symmetric ones are taken on and above the diagonal only.
+// splitting of G and X that keeps their precision).  A tile is 256 x 256 of one
+// product; the symmetric ones are taken on and above the diagonal only.  A pair of
+// CTAs multiplies it (cta_group::2), 128 rows each: an operand block is copied to
+// one of them only, so that a stage takes 32 KB and four of them fit beside the
+// epilogue's buffers.
 //
-// One persistent CTA per SM draws tiles from one list.  Two sets of matrices go
-// through their steps side by side in it, so that while the last tiles of one
-// set's product are still in work the other set's fill the SMs; a set is small
-// enough for both to stay in L2 (kMuonSetBytes).  A tile of a product waits for
-// all tiles of the product before it of the same matrix (a counter for each
-// matrix).  Those come earlier in the list, which is drawn in order, so the
-// earliest unfinished tile waits for nothing; all CTAs are resident (cooperative
-// launch).  Waits are bounded.
+// Persistent pairs, one CTA an SM, take the tiles of one list in turn.  Two sets
+// of matrices go through their steps side by side in it, so that while the last
+// tiles of one set's product are still in work the other set's fill the SMs.  A
+// tile of a product waits for all tiles of the product before it of the same
+// matrix (a counter for each matrix).  Those come earlier in the list, which every
+// pair takes in order, so the earliest unfinished tile waits for nothing; all CTAs
+// are resident (cooperative launch).  Waits are bounded.
 //
-// Warps: 0 draws tiles and copies operands, 1 issues the products, 2 copies the
+// Warps: 0 lists tiles and copies operands, 1 issues the products, 2 copies the
 // epilogue's blocks in (and holds the tensor memory), 3 copies them out, 4-7 and
 // 8-11 run the epilogue, every other block each.  A block is 32 columns of the
 // tile: its inputs (X as hi and lo; D) come to a ring of staging buffers ahead of
@@ -28,20 +30,21 @@
 namespace lamb {
 namespace {
 
-constexpr int kStages = 3;
-constexpr int kBuffers = 4;
+constexpr int kStages = 4;
+constexpr int kStageBytes = 2 * kTileBytesA;      // a CTA's rows of A and of B
+constexpr int kBuffers = 5;
 constexpr int kBlockBytes = kTileM * kMuonCols * 2;     // of one fp16 matrix
 constexpr int kBufferBytes = 2 * kBlockBytes;
-constexpr int kRing = 4;                                // tiles drawn ahead
+constexpr int kRing = 4;                                // tiles listed ahead
 constexpr int kGroups = 2;                              // of epilogue warps
 constexpr int kStepThreads = 128 + kGroups * kEpiThreads;
-// readers of a drawn tile: products, copies in, copies out, epilogue warps
+// readers of a listed tile: products, copies in, copies out, epilogue warps
 constexpr int kReaders = 3 + 4 * kGroups;
 // l or beta of a tile's columns, and of its rows
 constexpr int kColBytes = kTileN * 4, kVecBytes = kColBytes + kTileM * 4;
-constexpr size_t kSmem = (size_t)kStages * kGemmStageBytes +
+constexpr size_t kSmem = (size_t)kStages * kStageBytes +
                          kBuffers * kBufferBytes + kRing * kVecBytes + 1024;
-static_assert(kTileM == kMuonTileM && kTileN == kMuonTileN, "tiles");
+static_assert(kTileM == kMuonRows && kTileN == kMuonTile, "tiles");
 
 struct Drawn {
   MuonTile t;
@@ -81,7 +84,7 @@ __device__ __forceinline__ uint32_t mirrored(uint32_t base, int j, int i) {
 // Whether the block of rows c0 .. and columns a0 .. lies in no tile on or above
 // the diagonal.
 __device__ __forceinline__ bool mirror(int a0, int c0) {
-  return a0 / kTileN * kTileN + kTileN - 1 < c0 / kTileM * kTileM;
+  return a0 / kMuonTile < c0 / kMuonTile;
 }
 
 // ---- warp 0 -------------------------------------------------------------------
@@ -99,17 +102,15 @@ __device__ __forceinline__ Operands operands(const MuonMatrix* x,
   o.kn = ((d.t.phase == kGram ? x->n : x->m) + kTileK - 1) / kTileK;
   if (d.t.phase == kGram) {
     o.a_mn = o.b_mn = x->tall;
-    o.a = x->tall ? &x->xa_mn[from] : &x->xa_k[from];
-    o.b = x->tall ? &x->xb_mn[from] : &x->xb_k[from];
+    o.a = o.b = x->tall ? &x->x_mn[from] : &x->x_k[from];
   } else if (d.t.phase == kSquare) {
-    o.a = &x->da;
-    o.b = &x->db;
+    o.a = o.b = &x->d;
   } else if (x->tall) {
-    o.a = &x->xa_k[from];
-    o.b = &x->eb;
+    o.a = &x->x_k[from];
+    o.b = &x->e;
   } else {
-    o.a = &x->ea;
-    o.b = &x->xb_mn[from];
+    o.a = &x->e;
+    o.b = &x->x_mn[from];
     o.b_mn = true;
   }
   return o;
@@ -134,19 +135,13 @@ __device__ __forceinline__ bool wait_ready(Shared& sh, const MuonParams& p,
   return true;
 }
 
-__device__ __forceinline__ void draw_and_copy(Shared& sh, const MuonParams& p,
-                                              uint32_t smem) {
-  int it = 0, span = 0, base = 0;
-  int next = (int)atomicAdd(p.ticket, 1u);
-  for (int n = 0;; ++n) {
-    const int slot = n % kRing;
-    if (!wait_on(sh, p, &sh.read[slot], ((uint32_t)(n / kRing) & 1u) ^ 1u))
-      break;
-    const int t = next;
+// Walks over this pair's tiles of the list.
+struct Lister {
+  int t, span, base;
+  __device__ __forceinline__ Drawn next(const MuonParams& p, int pairs) {
     Drawn d;
     d.t.phase = kNoTile;
     if (t < p.total) {
-      next = (int)atomicAdd(p.ticket, 1u);
       MuonSpan s = p.spans[span];
       while (t - base >= s.count * p.steps) {
         base += s.count * p.steps;
@@ -157,35 +152,57 @@ __device__ __forceinline__ void draw_and_copy(Shared& sh, const MuonParams& p,
       const MuonMatrix* x = p.mats + d.t.matrix;
       d.need = (uint32_t)(d.it * (2 * x->sym + x->app) + d.t.phase * x->sym);
     }
+    t += pairs;
+    return d;
+  }
+};
+
+__device__ __forceinline__ void list_and_copy(Shared& sh, const MuonParams& p,
+                                              uint32_t smem, uint32_t rank) {
+  const int pairs = gridDim.x / 2;
+  Lister list = {(int)blockIdx.x / 2, 0, 0};
+  int it = 0;
+  Drawn d = list.next(p, pairs);
+  for (int n = 0;; ++n) {
+    const int slot = n % kRing;
+    if (!wait_on(sh, p, &sh.read[slot], ((uint32_t)(n / kRing) & 1u) ^ 1u))
+      break;
     sh.ring[slot] = d;
     mbar_arrive(&sh.drawn[slot]);
     if (d.t.phase == kNoTile) break;
+    const Drawn now = d;
     const Operands o = operands(p.mats + d.t.matrix, d);
-    if (!wait_ready(sh, p, d)) break;
+    d = list.next(p, pairs);
+    if (!wait_ready(sh, p, now)) break;
     fence_proxy_async();       // other CTAs' blocks, to be read by copies
-    const int a0 = d.t.i * kTileM, b0 = d.t.j * kTileN;
+    const int a0 = now.t.i * kMuonTile + (int)rank * kTileM;
+    const int b0 = now.t.j * kMuonTile + (int)rank * kTileM;
     for (int kb = 0; kb < o.kn; ++kb, ++it) {
       const int s = it % kStages;
       if (!wait_on(sh, p, &sh.empty[s], ((uint32_t)(it / kStages) & 1u) ^ 1u))
         break;
-      const uint32_t at = smem + s * kGemmStageBytes;
+      const uint32_t at = smem + s * kStageBytes;
+      const uint32_t bar = at_rank(&sh.full[s], 0);    // the issuing CTA's
       const int k = kb * kTileK;
-      mbar_expect(&sh.full[s], kGemmStageBytes);
+      if (rank == 0) mbar_expect(&sh.full[s], 2 * kStageBytes);
       // (issuing a copy takes this thread some 100 cycles: one an operand)
-      if (o.a_mn) blocks_load(at, o.a, k, a0 / 64, &sh.full[s]);
-      else tile_load(at, o.a, k, a0, &sh.full[s]);
-      if (o.b_mn) blocks_load(at + kTileBytesA, o.b, k, b0 / 64, &sh.full[s]);
-      else tile_load(at + kTileBytesA, o.b, k, b0, &sh.full[s]);
+      if (o.a_mn) pair_blocks_load(at, o.a, k, a0 / 64, bar);
+      else pair_tile_load(at, o.a, k, a0, bar);
+      if (o.b_mn) pair_blocks_load(at + kTileBytesA, o.b, k, b0 / 64, bar);
+      else pair_tile_load(at + kTileBytesA, o.b, k, b0, bar);
     }
     if (sh.gave_up) break;
   }
-  for (int j = it > kStages ? it - kStages : 0; j < it; ++j)
-    settle(&sh.full[j % kStages], (uint32_t)(j / kStages) & 1u);
+  // the copies have landed before either CTA may leave (cluster_sync)
+  if (rank == 0)
+    for (int j = it > kStages ? it - kStages : 0; j < it; ++j)
+      settle(&sh.full[j % kStages], (uint32_t)(j / kStages) & 1u);
 }
 
 // ---- warp 1 -------------------------------------------------------------------
 __device__ __forceinline__ void multiply(Shared& sh, const MuonParams& p,
-                                         uint32_t smem, uint32_t tmem) {
+                                         uint32_t smem, uint32_t tmem,
+                                         uint32_t rank) {
   int it = 0;
   for (int n = 0;; ++n) {
     const int slot = n % kRing;
@@ -193,34 +210,44 @@ __device__ __forceinline__ void multiply(Shared& sh, const MuonParams& p,
     const Drawn d = sh.ring[slot];
     mbar_arrive(&sh.read[slot]);
     if (d.t.phase == kNoTile) return;
+    if (rank) continue;        // the other CTA issues
     const Operands o = operands(p.mats + d.t.matrix, d);
     const uint64_t da = operand_desc(o.a_mn), db = operand_desc(o.b_mn);
     const uint32_t sa = operand_step(o.a_mn), sb = operand_step(o.b_mn);
-    const uint32_t desc = product_desc(false, o.a_mn, o.b_mn, kTileM, kTileN);
+    const uint32_t desc =
+        product_desc(false, o.a_mn, o.b_mn, kMuonTile, kMuonTile);
     const int acc = n & 1;
     const uint32_t to = tmem + acc * kTileN;
-    if (!wait_on(sh, p, &sh.acc_empty[acc], ((uint32_t)(n >> 1) & 1u) ^ 1u))
-      return;
+    const uint32_t ph = ((uint32_t)(n >> 1) & 1u) ^ 1u;
+    if (!wait_on(sh, p, &sh.acc_empty[acc], ph)) return;
+    mbar_try_cluster(&sh.acc_empty[acc], ph);      // the other CTA's readers
     tmem_after_sync();
     for (int kb = 0; kb < o.kn; ++kb, ++it) {
       const int s = it % kStages;
       if (!wait_on(sh, p, &sh.full[s], (uint32_t)(it / kStages) & 1u)) return;
       tmem_after_sync();
-      const uint32_t at = smem + s * kGemmStageBytes;
+      const uint32_t at = smem + s * kStageBytes;
       const uint64_t a = da | (at >> 4), b = db | ((at + kTileBytesA) >> 4);
 #pragma unroll
       for (int k = 0; k < kTileK / 16; ++k)
-        product(to, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
-      products_arrive(&sh.empty[s]);
+        pair_product(to, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
+      pair_products_arrive(&sh.empty[s]);
     }
-    products_arrive(&sh.acc_full[acc]);
+    pair_products_arrive(&sh.acc_full[acc]);
   }
 }
 
 // ---- warp 2 -------------------------------------------------------------------
+// This CTA's first row of a tile.
+__device__ __forceinline__ int row0(const Drawn& d) {
+  return d.t.i * kMuonTile + (int)cluster_rank() * kTileM;
+}
+// Blocks of this CTA's part of a tile: none where that is past the last row.
 __device__ __forceinline__ int block_count(const MuonMatrix& x,
                                            const Drawn& d) {
   const int width = d.t.phase == kApply ? x.cols : x.m;
+  const int height = d.t.phase == kApply ? x.rows : x.m;
+  if (row0(d) >= height) return 0;
   const int left = (width - d.t.j * kTileN + kMuonCols - 1) / kMuonCols;
   return left < kTileN / kMuonCols ? left : kTileN / kMuonCols;
 }
@@ -242,7 +269,7 @@ __device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
   for (int tile = 0; next_tile(sh, p, tile, &d); ++tile) {
     const MuonMatrix& x = p.mats[d.t.matrix];
     const int blocks = block_count(x, d), from = d.it & 1;
-    const int a0 = d.t.i * kTileM;
+    const int a0 = row0(d);
     const uint32_t vec = staging + kBuffers * kBufferBytes +
                          tile % kRing * kVecBytes;
     const float* const v = d.t.phase == kSquare ? x.diag : x.beta;
@@ -295,7 +322,7 @@ __device__ __forceinline__ void copy_out(Shared& sh, const MuonParams& p,
   for (int tile = 0; next_tile(sh, p, tile, &d); ++tile) {
     const MuonMatrix& x = p.mats[d.t.matrix];
     const int blocks = block_count(x, d), m = x.m;
-    const int a0 = d.t.i * kTileM;
+    const int a0 = row0(d);
     const bool last = d.t.phase == kApply && d.it == p.steps - 1;
     const bool gram = d.t.phase == kGram;
     const CUtensorMap* const to = d.t.phase == kApply ? &x.x_c[(d.it & 1) ^ 1]
@@ -326,7 +353,7 @@ __device__ __forceinline__ void copy_out(Shared& sh, const MuonParams& p,
         mbar_arrive(&sh.vacant[(n - 1) % kBuffers]);
       }
     }
-    if (!last) {
+    if (!last && blocks) {     // (no blocks: nothing to wait for or to count)
       stores_have_read<0>();
       mbar_arrive(&sh.vacant[(n - 1) % kBuffers]);
       stores_done();
@@ -588,7 +615,7 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
     const uint32_t from =
         tmem + acc * kTileN + ((uint32_t)(quarter * 32) << 16);
     const MuonMatrix& x = p.mats[d.t.matrix];
-    const int a0 = d.t.i * kTileM, blocks = block_count(x, d);
+    const int a0 = row0(d), blocks = block_count(x, d);
     r.i = a0 + r.row;
     const bool last = d.t.phase == kApply && d.it == p.steps - 1;
     const bool tall = x.tall;
@@ -629,19 +656,19 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
     tmem_before_sync();
     __syncwarp();
     if (lane == 0) {
-      mbar_arrive(&sh.acc_empty[acc]);
+      remote_arrive(at_rank(&sh.acc_empty[acc], 0));
       mbar_arrive(&sh.read[slot]);
     }
   }
 }
 
-__global__ void __launch_bounds__(kStepThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kStepThreads, 1)
 muon_steps_kernel(const __grid_constant__ MuonParams p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ Shared sh;
   const int warp = threadIdx.x >> 5;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t staging = smem + kStages * kGemmStageBytes;
+  const uint32_t staging = smem + kStages * kStageBytes;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&sh.full[i], 1);
@@ -649,7 +676,7 @@ muon_steps_kernel(const __grid_constant__ MuonParams p) {
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.acc_full[i], 1);
-      mbar_init(&sh.acc_empty[i], 4 * kGroups);
+      mbar_init(&sh.acc_empty[i], 8 * kGroups);
     }
     for (int i = 0; i < kBuffers; ++i) {
       mbar_init(&sh.in[i], 1);
@@ -665,16 +692,17 @@ muon_steps_kernel(const __grid_constant__ MuonParams p) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   }
-  if (warp == 2) tmem_alloc_all(&sh.tmem);
+  if (warp == 2) pair_tmem_alloc_all(&sh.tmem);
   tmem_before_sync();
   __syncthreads();
+  cluster_sync();        // both CTAs' barriers are there
   tmem_after_sync();
-  const uint32_t tmem = sh.tmem;
+  const uint32_t tmem = sh.tmem, rank = cluster_rank();
   if (warp == 0) {
-    if (elect_lane()) draw_and_copy(sh, p, smem);
+    if (elect_lane()) list_and_copy(sh, p, smem, rank);
     __syncwarp();
   } else if (warp == 1) {
-    if (elect_lane()) multiply(sh, p, smem, tmem);
+    if (elect_lane()) multiply(sh, p, smem, tmem, rank);
     __syncwarp();
   } else if (warp == 2) {
     if (elect_lane()) copy_in(sh, p, staging);
@@ -687,19 +715,34 @@ muon_steps_kernel(const __grid_constant__ MuonParams p) {
   }
   tmem_before_sync();
   __syncthreads();
+  cluster_sync();        // neither CTA's memory is used any more
   tmem_after_sync();
-  if (warp == 2) tmem_free_all(tmem);
+  if (warp == 2) pair_tmem_free_all(tmem);
 }
 
 }  // namespace
 
-int muon_steps_setup() {
-  return (int)cudaFuncSetAttribute(muon_steps_kernel,
-                                   cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)kSmem);
+cudaError_t muon_steps_setup(int sms, int* pairs) {
+  cudaError_t e = cudaFuncSetAttribute(
+      muon_steps_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      (int)kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = 2;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(sms / 2 * 2));
+  cfg.blockDim = dim3(kStepThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  e = cudaOccupancyMaxActiveClusters(pairs, muon_steps_kernel, &cfg);
+  if (e == cudaSuccess && *pairs < 1) e = cudaErrorNotSupported;
+  return e;
 }
 
-cudaError_t muon_launch_steps(const MuonParams& p, int sms,
+cudaError_t muon_launch_steps(const MuonParams& p, int pairs,
                               cudaStream_t stream) {
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeCooperative;
@@ -710,11 +753,11 @@ cudaError_t muon_launch_steps(const MuonParams& p, int sms,
   cfg.stream = stream;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  // a process that has fewer SMs than the device takes fewer CTAs
+  // a process that has fewer SMs than the device takes fewer pairs
   cudaError_t e = cudaErrorCooperativeLaunchTooLarge;
-  for (int grid = std::min(sms, p.total);
-       grid > 0 && e == cudaErrorCooperativeLaunchTooLarge; grid /= 2) {
-    cfg.gridDim = dim3((unsigned)grid);
+  for (int n = std::min(pairs, p.total);
+       n > 0 && e == cudaErrorCooperativeLaunchTooLarge; n /= 2) {
+    cfg.gridDim = dim3(2u * (unsigned)n);
     e = cudaLaunchKernelEx(&cfg, muon_steps_kernel, p);
     if (e == cudaErrorCooperativeLaunchTooLarge) cudaGetLastError();
   }

@@ -117,6 +117,87 @@ __device__ __forceinline__ void sts2(uint32_t at, uint16_t v) {
   asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v));
 }
 
+// ---- pairs of CTAs ------------------------------------------------------------
+// Two CTAs of a cluster multiply one tile of 256 x 256: each holds 128 rows of A
+// and of B and gets 128 rows of the accumulator; the even one issues.
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile(
+      "barrier.cluster.arrive.release.aligned;\n\t"
+      "barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same shared variable of CTA `rank`.
+__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+               : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void remote_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];"
+               ::"r"(bar) : "memory");
+}
+// mbar_try for arrivals from the other CTA.
+__device__ __forceinline__ bool mbar_try_cluster(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Copies into this CTA's shared memory, counted by a barrier of either CTA.
+__device__ __forceinline__ void pair_tile_load(uint32_t smem,
+                                               const CUtensorMap* map, int x,
+                                               int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile"
+      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_blocks_load(uint32_t smem,
+                                                 const CUtensorMap* map,
+                                                 int line, int block,
+                                                 uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile"
+      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(smem), "l"(map), "r"(0), "r"(line), "r"(block), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void pair_product(uint32_t tmem, uint64_t a,
+                                             uint64_t b, uint32_t desc,
+                                             bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+      : "memory");
+}
+// Arrives at the barrier's place in both CTAs once the products are complete.
+__device__ __forceinline__ void pair_products_arrive(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster"
+      ".multicast::cluster.b64 [%0], %1;"
+      ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void pair_tmem_alloc_all(uint32_t* smem_out) {
+  asm volatile(
+      "tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;\n\t"
+      "tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;"
+      :: "r"(smem_u32(smem_out)) : "memory");
+}
+__device__ __forceinline__ void pair_tmem_free_all(uint32_t base) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;"
+               :: "r"(base) : "memory");
+}
+
 // ---- products ---------------------------------------------------------------
 // Descriptor of a shared-memory operand in the 128-byte swizzle (start address
 // added later, all in units of 16 bytes).  K-major: rows of 64 elements (128
