@@ -132,10 +132,15 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
           }
         }
       }
-      // every copy has landed before the CTA may leave
+      // every copy has landed, and its products' arrival is in, before the CTA
+      // may leave
       const int first = it > kGemmStages ? it - kGemmStages : 0;
-      for (int j = first; j < it; ++j)
+      for (int j = first; j < it; ++j) {
         settle(&sh.full[j % kGemmStages], (uint32_t)(j / kGemmStages) & 1u);
+        bounded_wait(&sh.empty[j % kGemmStages],
+                     (uint32_t)(j / kGemmStages) & 1u, &sh.gave_up, p.status,
+                     kStatusWaitTimeout);
+      }
     }
     __syncwarp();
   } else if (warp == 1) {

@@ -371,7 +371,7 @@ muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
   }
 
   const float lr = kStep ? *d_lr : 0.f;
-  const float size = muon_size(k, x);
+  const float size = muon_size(k, x.rows, x.cols);
   const float keep = 1.f - lr * k.wd * x.decay, move = lr * size;
   for (int i = threadIdx.x; i < total; i += kSmallThreads) {
     const int r = i / cols, c = i - r * cols;
@@ -526,7 +526,14 @@ void muon_layout(const int64_t* rows, const int64_t* cols, int n,
           const int c = phase == kApply ? x.cols : x.m;
           for (int i = 0; i * kMuonTile < r; ++i)
             for (int j = phase == kApply ? 0 : i; j * kMuonTile < c; ++j)
-              L->tiles.push_back({k, i, j, phase});
+              {
+              MuonTile t = {};
+              t.matrix = k;
+              t.i = i;
+              t.j = j;
+              t.phase = phase;
+              L->tiles.push_back(t);
+            }
         }
       }
     L->spans.push_back({first, (int)L->tiles.size() - first});
@@ -617,6 +624,7 @@ lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
     q.n_spans = p->n_spans;
     q.done = p->done;
     q.steps = h->steps;
+    q.n_mats = p->n;
     q.total = (int)(p->step_tiles * h->steps);
     e = muon_launch_steps(q, p->pairs, stream);
   }
@@ -740,6 +748,22 @@ extern "C" lamb_status_t lamb_muon_create(
       map(&x.d_t, x.D, x.m, x.m, x.pitch_m, kMuonCols, 64);
       map(&x.e_t, x.E, x.m, x.m, x.pitch_m, kMuonCols, 64);
       ok = m;
+    }
+    for (MuonTile& t : L.tiles) {
+      const MuonMatrix& x = L.mats[t.matrix];
+      t.height = t.phase == kApply ? x.rows : x.m;
+      t.width = t.phase == kApply ? x.cols : x.m;
+      t.kn = (int)lm_ceil_div(t.phase == kGram ? x.n : x.m, 64);
+      t.tall = x.tall;
+      t.sym = x.sym;
+      t.app = x.app;
+      t.scale = x.scale;
+      t.decay = x.decay;
+      t.x = p->mats + t.matrix;
+      t.diag = x.diag;
+      t.beta = x.beta;
+      t.rows = x.rows;
+      t.cols = x.cols;
     }
     if (e == cudaSuccess && !ok) {
       e = cudaErrorNotSupported;

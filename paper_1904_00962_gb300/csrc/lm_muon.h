@@ -2,6 +2,7 @@
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <stddef.h>
 
 #include "lm_host.h"
 
@@ -11,7 +12,9 @@ constexpr float kScaleD = 1024.f;            // D is stored times this
 constexpr float kScaleE = 256.f;             // and E times this
 constexpr float kScaleLo = 2048.f;           // lo: the rest of hi, times this
 
-struct MuonMatrix {
+constexpr int kMuonMaps = 13;
+
+struct MuonMatrix {               // the maps first
   // the products' operands, 128 rows by 64 of K in one copy: K-major (_k),
   // MN-major (_mn); hi has two buffers, taken in turn
   CUtensorMap x_k[2], x_mn[2], d, e;
@@ -33,6 +36,9 @@ struct MuonMatrix {
   float decay;
 };
 
+static_assert(offsetof(MuonMatrix, hi) == kMuonMaps * sizeof(CUtensorMap),
+              "kMuonMaps");
+
 struct MuonPtrs {
   float* w;
   const void* g;                 // or the direction's input
@@ -48,9 +54,18 @@ struct MuonChunk {
 
 enum { kGram = 0, kSquare = 1, kApply = 2, kNoTile = 3 };
 
-// A tile of one product of one matrix, two CTAs' work.
-struct MuonTile {
+// A tile of one product of one matrix, two CTAs' work, with what they need of the
+// matrix: one load when the tile is taken.
+struct __align__(16) MuonTile {
   int matrix, i, j, phase;
+  int height, width;     // of the product
+  int kn;                // blocks of K
+  int tall;
+  int sym, app;          // the matrix'
+  float scale, decay;
+  const MuonMatrix* x;
+  float *diag, *beta;
+  int rows, cols;
 };
 // Tiles of matrices that go through their steps side by side, in the order of
 // one step.
@@ -75,17 +90,17 @@ struct MuonParams {
   const float* d_lr;             // NULL: the direction alone
   uint32_t* status;
   MuonConsts k;
-  int n_spans, steps;
+  int n_mats, n_spans, steps;
   int total;                     // tiles of all steps
 };
 
 // s of a matrix.
-__device__ __forceinline__ float muon_size(const MuonConsts& k,
-                                           const MuonMatrix& x) {
+__device__ __forceinline__ float muon_size(const MuonConsts& k, int rows,
+                                           int cols) {
   if (k.scale_kind == LAMB_MUON_SCALE_RMS)
-    return k.size * 0.2f * sqrtf((float)x.n);
+    return k.size * 0.2f * sqrtf((float)(rows > cols ? rows : cols));
   if (k.scale_kind == LAMB_MUON_SCALE_SPECTRAL)
-    return k.size * sqrtf(fmaxf(1.f, (float)x.rows / (float)x.cols));
+    return k.size * sqrtf(fmaxf(1.f, (float)rows / (float)cols));
   return k.size;
 }
 __device__ __forceinline__ uint32_t pack_half2(float x, float y) {

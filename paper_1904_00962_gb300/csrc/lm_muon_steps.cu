@@ -15,13 +15,15 @@
 // pair takes in order, so the earliest unfinished tile waits for nothing; all CTAs
 // are resident (cooperative launch).  Waits are bounded.
 //
-// Warps: 0 lists tiles and copies operands, 1 issues the products, 2 copies the
-// epilogue's blocks in (and holds the tensor memory), 3 copies them out, 4-7 and
-// 8-11 run the epilogue, every other block each.  A block is 32 columns of the
-// tile: its inputs (X as hi and lo; D) come to a ring of staging buffers ahead of
-// the products' end, the epilogue turns them over in place, a row a thread, and
-// tensor copies take them out (clipped at the matrix' edges).  The tile is counted
-// as done when those have landed.
+// Warps: 0 lists tiles and copies operands, 1 issues the products, 2 copies the epilogue's blocks
+// in (and holds the tensor memory), 3 copies them out, 4-7 and 8-11 run the
+// epilogue, every other block each.  A block is 32 columns of the tile: its inputs
+// (X as hi and lo; D) come to a ring of staging buffers ahead of the products' end, the epilogue
+// turns them over in place, a row a thread, and tensor copies take them out
+// (clipped at the matrix' edges).  The tile is counted as done when those have
+// landed.  Warp 0 reads the list a tile ahead and leaves in shared memory all that
+// the other warps need of a tile: loads from global memory would be in their way
+// (the polls of the counters empty L1).
 #include <algorithm>
 
 #include "lm_gemm.cuh"
@@ -38,7 +40,7 @@ constexpr int kBufferBytes = 2 * kBlockBytes;
 constexpr int kRing = 4;                                // tiles listed ahead
 constexpr int kGroups = 2;                              // of epilogue warps
 constexpr int kStepThreads = 128 + kGroups * kEpiThreads;
-// readers of a listed tile: products, copies in, copies out, epilogue warps
+// readers of a listed tile: products, copies in, copies out, epilogue
 constexpr int kReaders = 3 + 4 * kGroups;
 // l or beta of a tile's columns, and of its rows
 constexpr int kColBytes = kTileN * 4, kVecBytes = kColBytes + kTileM * 4;
@@ -46,18 +48,20 @@ constexpr size_t kSmem = (size_t)kStages * kStageBytes +
                          kBuffers * kBufferBytes + kRing * kVecBytes + 1024;
 static_assert(kTileM == kMuonRows && kTileN == kMuonTile, "tiles");
 
-struct Drawn {
-  MuonTile t;
-  int it;            // step
-  uint32_t need;     // the matrix' finished tiles that it waits for
+struct Listed : MuonTile {
+  int it;                // step
+  int last;              // the step that leaves w
+  uint32_t need;         // the matrix' finished tiles that it waits for
+  float* w;
+  __nv_bfloat16* out;
 };
 
 struct Shared {
   uint64_t full[kStages], empty[kStages];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t in[kBuffers], out[kBuffers], vacant[kBuffers];
-  uint64_t drawn[kRing], read[kRing], vec[kRing];
-  Drawn ring[kRing];
+  uint64_t listed[kRing], read[kRing], vec[kRing];
+  Listed ring[kRing];
   uint32_t tmem;
   volatile int gave_up;
 };
@@ -87,40 +91,11 @@ __device__ __forceinline__ bool mirror(int a0, int c0) {
   return a0 / kMuonTile < c0 / kMuonTile;
 }
 
-// ---- warp 0 -------------------------------------------------------------------
-struct Operands {
-  const CUtensorMap *a, *b;
-  int kn;
-  bool a_mn, b_mn;
-};
-
-__device__ __forceinline__ Operands operands(const MuonMatrix* x,
-                                             const Drawn& d) {
-  const int from = d.it & 1;
-  Operands o;
-  o.a_mn = o.b_mn = false;
-  o.kn = ((d.t.phase == kGram ? x->n : x->m) + kTileK - 1) / kTileK;
-  if (d.t.phase == kGram) {
-    o.a_mn = o.b_mn = x->tall;
-    o.a = o.b = x->tall ? &x->x_mn[from] : &x->x_k[from];
-  } else if (d.t.phase == kSquare) {
-    o.a = o.b = &x->d;
-  } else if (x->tall) {
-    o.a = &x->x_k[from];
-    o.b = &x->e;
-  } else {
-    o.a = &x->e;
-    o.b = &x->x_mn[from];
-    o.b_mn = true;
-  }
-  return o;
-}
-
-__device__ __forceinline__ bool ready(const MuonParams& p, const Drawn& d) {
-  return ld_acquire_u32(p.done + d.t.matrix) >= d.need;
+__device__ __forceinline__ bool ready(const MuonParams& p, const Listed& d) {
+  return ld_acquire_u32(p.done + d.matrix) >= d.need;
 }
 __device__ __forceinline__ bool wait_ready(Shared& sh, const MuonParams& p,
-                                           const Drawn& d) {
+                                           const Listed& d) {
   if (ready(p, d)) return true;
   const uint64_t begin = global_ns();
   while (!ready(p, d)) {
@@ -130,54 +105,81 @@ __device__ __forceinline__ bool wait_ready(Shared& sh, const MuonParams& p,
       atomicOr(p.status, LAMB_STATUS_WAIT_TIMEOUT);
       return false;
     }
-    __nanosleep(64);
+    __nanosleep(32);
   }
   return true;
 }
 
+// The next listed tile: NULL at the end, or if a wait gave up.
+__device__ __forceinline__ const Listed* next_tile(Shared& sh,
+                                                   const MuonParams& p,
+                                                   int tile) {
+  const int slot = tile % kRing;
+  if (!wait_on(sh, p, &sh.listed[slot], (uint32_t)(tile / kRing) & 1u))
+    return nullptr;
+  return sh.ring[slot].phase == kNoTile ? nullptr : &sh.ring[slot];
+}
+
+// ---- warp 0 -------------------------------------------------------------------
 // Walks over this pair's tiles of the list.
 struct Lister {
   int t, span, base;
-  __device__ __forceinline__ Drawn next(const MuonParams& p, int pairs) {
-    Drawn d;
-    d.t.phase = kNoTile;
+  MuonSpan s;
+  __device__ __forceinline__ void next(const MuonParams& p, Listed& d) {
+    d.phase = kNoTile;
     if (t < p.total) {
-      MuonSpan s = p.spans[span];
       while (t - base >= s.count * p.steps) {
         base += s.count * p.steps;
         s = p.spans[++span];
       }
-      d.it = (t - base) / s.count;
-      d.t = p.tiles[s.first + (t - base) - d.it * s.count];
-      const MuonMatrix* x = p.mats + d.t.matrix;
-      d.need = (uint32_t)(d.it * (2 * x->sym + x->app) + d.t.phase * x->sym);
+      const int it = (t - base) / s.count;
+      static_cast<MuonTile&>(d) = p.tiles[s.first + (t - base) - it * s.count];
+      d.it = it;
     }
-    t += pairs;
-    return d;
+    t += gridDim.x / 2;
   }
 };
 
-__device__ __forceinline__ void list_and_copy(Shared& sh, const MuonParams& p,
+__device__ __forceinline__ void copy_operands(Shared& sh, const MuonParams& p,
                                               uint32_t smem, uint32_t rank) {
-  const int pairs = gridDim.x / 2;
-  Lister list = {(int)blockIdx.x / 2, 0, 0};
+  Lister list = {(int)blockIdx.x / 2, 0, 0, p.spans[0]};
+  Listed ahead;
+  list.next(p, ahead);
   int it = 0;
-  Drawn d = list.next(p, pairs);
   for (int n = 0;; ++n) {
     const int slot = n % kRing;
     if (!wait_on(sh, p, &sh.read[slot], ((uint32_t)(n / kRing) & 1u) ^ 1u))
       break;
-    sh.ring[slot] = d;
-    mbar_arrive(&sh.drawn[slot]);
-    if (d.t.phase == kNoTile) break;
-    const Drawn now = d;
-    const Operands o = operands(p.mats + d.t.matrix, d);
-    d = list.next(p, pairs);
-    if (!wait_ready(sh, p, now)) break;
+    Listed& d = sh.ring[slot];
+    ahead.last = ahead.phase == kApply && ahead.it == p.steps - 1;
+    ahead.need = (uint32_t)(ahead.it * (2 * ahead.sym + ahead.app) +
+                            ahead.phase * ahead.sym);
+    if (ahead.phase != kNoTile && ahead.last) {
+      ahead.w = p.ptrs[ahead.matrix].w;
+      ahead.out = p.ptrs[ahead.matrix].out;
+    }
+    d = ahead;
+    mbar_arrive(&sh.listed[slot]);
+    if (ahead.phase == kNoTile) break;
+    list.next(p, ahead);
+    const MuonMatrix* const x = d.x;
+    const int from = d.it & 1, kn = d.kn;
+    const bool gram_mn = d.phase == kGram && d.tall;
+    const bool b_mn = gram_mn || (d.phase == kApply && !d.tall);
+    const CUtensorMap *ma, *mb;
+    if (d.phase == kGram) {
+      ma = mb = d.tall ? &x->x_mn[from] : &x->x_k[from];
+    } else if (d.phase == kSquare) {
+      ma = mb = &x->d;
+    } else {
+      ma = d.tall ? &x->x_k[from] : &x->e;
+      mb = d.tall ? &x->e : &x->x_mn[from];
+    }
+    const int a0 = d.i * kMuonTile + (int)rank * kTileM;
+    const int b0 = d.j * kMuonTile + (int)rank * kTileM;
+    if (!wait_ready(sh, p, d)) break;
     fence_proxy_async();       // other CTAs' blocks, to be read by copies
-    const int a0 = now.t.i * kMuonTile + (int)rank * kTileM;
-    const int b0 = now.t.j * kMuonTile + (int)rank * kTileM;
-    for (int kb = 0; kb < o.kn; ++kb, ++it) {
+    for (int kb = 0; kb < kn; ++kb, ++it) {
       const int s = it % kStages;
       if (!wait_on(sh, p, &sh.empty[s], ((uint32_t)(it / kStages) & 1u) ^ 1u))
         break;
@@ -186,17 +188,20 @@ __device__ __forceinline__ void list_and_copy(Shared& sh, const MuonParams& p,
       const int k = kb * kTileK;
       if (rank == 0) mbar_expect(&sh.full[s], 2 * kStageBytes);
       // (issuing a copy takes this thread some 100 cycles: one an operand)
-      if (o.a_mn) pair_blocks_load(at, o.a, k, a0 / 64, bar);
-      else pair_tile_load(at, o.a, k, a0, bar);
-      if (o.b_mn) pair_blocks_load(at + kTileBytesA, o.b, k, b0 / 64, bar);
-      else pair_tile_load(at + kTileBytesA, o.b, k, b0, bar);
+      if (gram_mn) pair_blocks_load(at, ma, k, a0 / 64, bar);
+      else pair_tile_load(at, ma, k, a0, bar);
+      if (b_mn) pair_blocks_load(at + kTileBytesA, mb, k, b0 / 64, bar);
+      else pair_tile_load(at + kTileBytesA, mb, k, b0, bar);
     }
     if (sh.gave_up) break;
   }
-  // the copies have landed before either CTA may leave (cluster_sync)
-  if (rank == 0)
-    for (int j = it > kStages ? it - kStages : 0; j < it; ++j)
+  // the copies have landed, and the products' arrivals for them are in, before
+  // either CTA may leave (cluster_sync)
+  for (int j = it > kStages ? it - kStages : 0; j < it; ++j) {
+    if (rank == 0 && sh.gave_up)
       settle(&sh.full[j % kStages], (uint32_t)(j / kStages) & 1u);
+    wait_on(sh, p, &sh.empty[j % kStages], (uint32_t)(j / kStages) & 1u);
+  }
 }
 
 // ---- warp 1 -------------------------------------------------------------------
@@ -204,25 +209,22 @@ __device__ __forceinline__ void multiply(Shared& sh, const MuonParams& p,
                                          uint32_t smem, uint32_t tmem,
                                          uint32_t rank) {
   int it = 0;
-  for (int n = 0;; ++n) {
-    const int slot = n % kRing;
-    if (!wait_on(sh, p, &sh.drawn[slot], (uint32_t)(n / kRing) & 1u)) return;
-    const Drawn d = sh.ring[slot];
-    mbar_arrive(&sh.read[slot]);
-    if (d.t.phase == kNoTile) return;
+  for (int n = 0; const Listed* d = next_tile(sh, p, n); ++n) {
+    const bool a_mn = d->phase == kGram && d->tall;
+    const bool b_mn = a_mn || (d->phase == kApply && !d->tall);
+    const int kn = d->kn;
+    mbar_arrive(&sh.read[n % kRing]);
     if (rank) continue;        // the other CTA issues
-    const Operands o = operands(p.mats + d.t.matrix, d);
-    const uint64_t da = operand_desc(o.a_mn), db = operand_desc(o.b_mn);
-    const uint32_t sa = operand_step(o.a_mn), sb = operand_step(o.b_mn);
-    const uint32_t desc =
-        product_desc(false, o.a_mn, o.b_mn, kMuonTile, kMuonTile);
+    const uint64_t da = operand_desc(a_mn), db = operand_desc(b_mn);
+    const uint32_t sa = operand_step(a_mn), sb = operand_step(b_mn);
+    const uint32_t desc = product_desc(false, a_mn, b_mn, kMuonTile, kMuonTile);
     const int acc = n & 1;
     const uint32_t to = tmem + acc * kTileN;
     const uint32_t ph = ((uint32_t)(n >> 1) & 1u) ^ 1u;
     if (!wait_on(sh, p, &sh.acc_empty[acc], ph)) return;
     mbar_try_cluster(&sh.acc_empty[acc], ph);      // the other CTA's readers
     tmem_after_sync();
-    for (int kb = 0; kb < o.kn; ++kb, ++it) {
+    for (int kb = 0; kb < kn; ++kb, ++it) {
       const int s = it % kStages;
       if (!wait_on(sh, p, &sh.full[s], (uint32_t)(it / kStages) & 1u)) return;
       tmem_after_sync();
@@ -239,73 +241,60 @@ __device__ __forceinline__ void multiply(Shared& sh, const MuonParams& p,
 
 // ---- warp 2 -------------------------------------------------------------------
 // This CTA's first row of a tile.
-__device__ __forceinline__ int row0(const Drawn& d) {
-  return d.t.i * kMuonTile + (int)cluster_rank() * kTileM;
+__device__ __forceinline__ int row0(const Listed& d) {
+  return d.i * kMuonTile + (int)cluster_rank() * kTileM;
 }
 // Blocks of this CTA's part of a tile: none where that is past the last row.
-__device__ __forceinline__ int block_count(const MuonMatrix& x,
-                                           const Drawn& d) {
-  const int width = d.t.phase == kApply ? x.cols : x.m;
-  const int height = d.t.phase == kApply ? x.rows : x.m;
-  if (row0(d) >= height) return 0;
-  const int left = (width - d.t.j * kTileN + kMuonCols - 1) / kMuonCols;
+__device__ __forceinline__ int block_count(const Listed& d) {
+  if (row0(d) >= d.height) return 0;
+  const int left = (d.width - d.j * kTileN + kMuonCols - 1) / kMuonCols;
   return left < kTileN / kMuonCols ? left : kTileN / kMuonCols;
-}
-
-// The next drawn tile: false at the end, or if a wait gave up.
-__device__ __forceinline__ bool next_tile(Shared& sh, const MuonParams& p,
-                                          int tile, Drawn* d) {
-  const int slot = tile % kRing;
-  if (!wait_on(sh, p, &sh.drawn[slot], (uint32_t)(tile / kRing) & 1u))
-    return false;
-  *d = sh.ring[slot];
-  return d->t.phase != kNoTile;
 }
 
 __device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
                                         uint32_t staging) {
   int n = 0, begun = 0;       // blocks, tiles whose copies were started
-  Drawn d;
-  for (int tile = 0; next_tile(sh, p, tile, &d); ++tile) {
-    const MuonMatrix& x = p.mats[d.t.matrix];
-    const int blocks = block_count(x, d), from = d.it & 1;
-    const int a0 = row0(d);
+  for (int tile = 0; const Listed* l = next_tile(sh, p, tile); ++tile) {
+    const Listed& d = *l;
+    const MuonMatrix* const x = d.x;
+    const int blocks = block_count(d), phase = d.phase;
+    const int a0 = row0(d), b0 = d.j * kTileN;
     const uint32_t vec = staging + kBuffers * kBufferBytes +
                          tile % kRing * kVecBytes;
-    const float* const v = d.t.phase == kSquare ? x.diag : x.beta;
     uint64_t* const vb = &sh.vec[tile % kRing];
-    if (d.t.phase == kGram) {
+    const CUtensorMap* const m0 = phase == kSquare ? &x->d_c
+                                                   : &x->x_c[d.it & 1];
+    if (phase == kGram) {
       mbar_arrive(vb);
     } else {
       if (!wait_ready(sh, p, d)) break;
       fence_proxy_async();
       // the tile's l or beta (their memory goes up to a whole tile)
-      const bool cols = d.t.phase == kSquare || x.tall;
-      const bool rows = d.t.phase == kSquare || !x.tall;
+      const bool cols = phase == kSquare || d.tall;
+      const bool rows = phase == kSquare || !d.tall;
       mbar_expect(vb, (cols ? kColBytes : 0) + (rows ? kTileM * 4 : 0));
-      if (cols) bulk_load_at(vec, v + d.t.j * kTileN, kColBytes, vb);
+      const float* const v = phase == kSquare ? d.diag : d.beta;
+      if (cols) bulk_load_at(vec, v + b0, kColBytes, vb);
       if (rows) bulk_load_at(vec + kColBytes, v + a0, kTileM * 4, vb);
     }
     begun = tile + 1;
+    mbar_arrive(&sh.read[tile % kRing]);
     for (int c = 0; c < blocks; ++c, ++n) {
       const int b = n % kBuffers;
       if (!wait_on(sh, p, &sh.vacant[b], ((uint32_t)(n / kBuffers) & 1u) ^ 1u))
         break;
       const uint32_t to = staging + b * kBufferBytes;
-      const int c0 = d.t.j * kTileN + c * kMuonCols;
-      if (d.t.phase == kGram) {
+      const int c0 = b0 + c * kMuonCols;
+      if (phase == kGram) {
         mbar_arrive(&sh.in[b]);
-      } else if (d.t.phase == kSquare) {
-        mbar_expect(&sh.in[b], kBlockBytes);
-        tile_load(to, &x.d_c, c0, a0, &sh.in[b]);
       } else {
-        mbar_expect(&sh.in[b], 2 * kBlockBytes);
-        tile_load(to, &x.x_c[from], c0, a0, &sh.in[b]);
-        tile_load(to + kBlockBytes, &x.lo_c, c0, a0, &sh.in[b]);
+        mbar_expect(&sh.in[b], (phase == kSquare ? 1 : 2) * kBlockBytes);
+        tile_load(to, m0, c0, a0, &sh.in[b]);
+        if (phase == kApply)
+          tile_load(to + kBlockBytes, &x->lo_c, c0, a0, &sh.in[b]);
       }
     }
     if (sh.gave_up) break;
-    mbar_arrive(&sh.read[tile % kRing]);
   }
   // copies that were started land before the CTA may leave
   for (int j = n > kBuffers ? n - kBuffers : 0; j < n; ++j)
@@ -318,17 +307,16 @@ __device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
 __device__ __forceinline__ void copy_out(Shared& sh, const MuonParams& p,
                                          uint32_t staging) {
   int n = 0;
-  Drawn d;
-  for (int tile = 0; next_tile(sh, p, tile, &d); ++tile) {
-    const MuonMatrix& x = p.mats[d.t.matrix];
-    const int blocks = block_count(x, d), m = x.m;
-    const int a0 = row0(d);
-    const bool last = d.t.phase == kApply && d.it == p.steps - 1;
-    const bool gram = d.t.phase == kGram;
-    const CUtensorMap* const to = d.t.phase == kApply ? &x.x_c[(d.it & 1) ^ 1]
-                                  : gram              ? &x.d_c
-                                                      : &x.e_c;
-    const CUtensorMap* const to_t = gram ? &x.d_t : &x.e_t;
+  for (int tile = 0; const Listed* l = next_tile(sh, p, tile); ++tile) {
+    const MuonMatrix* const x = l->x;
+    const int blocks = block_count(*l), m = l->height, matrix = l->matrix;
+    const int a0 = row0(*l), b0 = l->j * kTileN, phase = l->phase;
+    const bool last = l->last;
+    const CUtensorMap* const to = phase == kApply ? &x->x_c[(l->it & 1) ^ 1]
+                                  : phase == kGram ? &x->d_c
+                                                   : &x->e_c;
+    const CUtensorMap* const to_t = phase == kGram ? &x->d_t : &x->e_t;
+    mbar_arrive(&sh.read[tile % kRing]);
     for (int c = 0; c < blocks; ++c, ++n) {
       const int b = n % kBuffers;
       if (!wait_on(sh, p, &sh.out[b], (uint32_t)(n / kBuffers) & 1u)) break;
@@ -337,10 +325,10 @@ __device__ __forceinline__ void copy_out(Shared& sh, const MuonParams& p,
         continue;
       }
       const uint32_t from = staging + b * kBufferBytes;
-      const int c0 = d.t.j * kTileN + c * kMuonCols;
+      const int c0 = b0 + c * kMuonCols;
       tile_store(to, c0, a0, from);
-      if (d.t.phase == kApply) {
-        tile_store(&x.lo_c, c0, a0, from + kBlockBytes);
+      if (phase == kApply) {
+        tile_store(&x->lo_c, c0, a0, from + kBlockBytes);
       } else if (mirror(a0, c0)) {
         tile_store(to_t, a0, c0, from + kBlockBytes);
         if (a0 + 64 < m)
@@ -360,9 +348,8 @@ __device__ __forceinline__ void copy_out(Shared& sh, const MuonParams& p,
       if (sh.gave_up) break;
       fence_proxy_async();
       __threadfence();
-      atomicAdd(p.done + d.t.matrix, 1u);
+      atomicAdd(p.done + matrix, 1u);
     }
-    mbar_arrive(&sh.read[tile % kRing]);
   }
   stores_done();
 }
@@ -425,11 +412,16 @@ __device__ __forceinline__ void symmetric_block(float pb, float pc, int m,
 #pragma unroll
     for (int q = 0; q < 32; ++q) y[q] *= s * kScaleD;
   } else {
+    const float ck = pc * (kScaleE / kScaleD), sk = pc * s * kScaleE;
+    const float bk = fmaf(pc, li, pb) * (kScaleE / kScaleD);
+    uint4 ds[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) ds[u] = lds16(unit64(r.buf, r.row, u));
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const float4 l0 = lds_f4(r.col + 32 * u), l1 = lds_f4(r.col + 32 * u + 16);
       const float l[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
-      const uint4 d = lds16(unit64(r.buf, r.row, u));
+      const uint4 d = ds[u];
       const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -437,8 +429,7 @@ __device__ __forceinline__ void symmetric_block(float pb, float pc, int m,
         const float2 d2 = half2_at(dw[k >> 1]);
         const float dd = k & 1 ? d2.y : d2.x;
         // E kScaleE, dd being D kScaleD
-        const float f = fmaf(pc, li + l[k], pb) * (kScaleE / kScaleD);
-        y[q] = fmaf(f, dd, y[q] * (pc * s * kScaleE));
+        y[q] = fmaf(fmaf(ck, l[k], bk), dd, y[q] * sk);
       }
     }
   }
@@ -515,20 +506,18 @@ struct Output {
 };
 
 __device__ __forceinline__ Output output_of(const MuonParams& p,
-                                            const MuonMatrix& x,
-                                            const MuonPtrs& t) {
+                                            const Listed& d, float lr) {
   Output o;
-  o.w = t.w;
-  o.out = t.out;
+  o.w = d.w;
+  o.out = d.out;
   o.step = p.d_lr != nullptr;
-  const float lr = o.step ? *p.d_lr : 0.f;
-  o.inv = 1.f / x.scale;
-  o.keep = 1.f - lr * p.k.wd * x.decay;
-  o.move = lr * muon_size(p.k, x);
-  o.rows = x.rows;
-  o.cols = x.cols;
-  o.vec = x.cols % 4 == 0 && (!o.step || (uintptr_t)t.w % 16 == 0) &&
-          (uintptr_t)t.out % 8 == 0;
+  o.inv = 1.f / d.scale;
+  o.keep = 1.f - lr * p.k.wd * d.decay;
+  o.move = lr * muon_size(p.k, d.rows, d.cols);
+  o.rows = d.height;
+  o.cols = d.width;
+  o.vec = d.width % 4 == 0 && (!o.step || (uintptr_t)d.w % 16 == 0) &&
+          (uintptr_t)d.out % 8 == 0;
   return o;
 }
 
@@ -536,16 +525,15 @@ __device__ __forceinline__ void last_block(const Output& o, int a0, int c0,
                                            const Row& r, float (&y)[32]) {
   const int u = r.row & 7, c = c0 + 4 * u;
   const int cols = min(4, o.cols - c);
-  constexpr int kRows = kEpiThreads / 8;
-  float4 old[kTileM / kRows];
-  if (o.step && o.vec && cols == 4) {
+  constexpr int kRows = kEpiThreads / 8, kAll = kTileM / kRows;
+  float4 old[kAll];
+  auto load_old = [&](int k) {
+    const int rr = a0 + k * kRows + (r.row >> 3);
+    if (o.step && o.vec && cols == 4 && rr < o.rows)
+      old[k] = *reinterpret_cast<const float4*>(o.w + (int64_t)rr * o.cols + c);
+  };
 #pragma unroll
-    for (int k = 0; k < kTileM / kRows; ++k) {
-      const int rr = a0 + k * kRows + (r.row >> 3);
-      if (rr < o.rows)
-        old[k] = *reinterpret_cast<const float4*>(o.w + (int64_t)rr * o.cols + c);
-    }
-  }
+  for (int k = 0; k < kAll / 2; ++k) load_old(k);
   group_sync(r.group);          // everybody has read the block's inputs
 #pragma unroll
   for (int q = 0; q < 8; ++q)
@@ -554,9 +542,11 @@ __device__ __forceinline__ void last_block(const Output& o, int a0, int c0,
                      __float_as_uint(y[4 * q + 1] * o.inv),
                      __float_as_uint(y[4 * q + 2] * o.inv),
                      __float_as_uint(y[4 * q + 3] * o.inv)));
+#pragma unroll
+  for (int k = kAll / 2; k < kAll; ++k) load_old(k);     // (y is gone)
   group_sync(r.group);
 #pragma unroll
-  for (int k = 0; k < kTileM / kRows; ++k) {
+  for (int k = 0; k < kAll; ++k) {
     const int br = k * kRows + (r.row >> 3), rr = a0 + br;
     const uint4 b = lds16(unit128(r.buf, br, u));
     if (rr >= o.rows || cols <= 0) continue;
@@ -600,49 +590,47 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
   Row r;
   r.row = quarter * 32 + lane;
   r.group = (warp - 4) >> 2;
+  const float lr = p.d_lr ? *p.d_lr : 0.f;
+  const float pa = p.k.a, pb = p.k.b, pc = p.k.c;
   int n = 0;
   for (int tile = 0;; ++tile) {
-    const int slot = tile % kRing;
-    bool ok = wait_on(sh, p, &sh.drawn[slot], (uint32_t)(tile / kRing) & 1u);
+    const int slot = tile % kRing, acc = tile & 1;
     // one answer for all: the last step's blocks meet at barriers
+    bool ok = wait_on(sh, p, &sh.listed[slot], (uint32_t)(tile / kRing) & 1u);
     if (!group_all(r.group, ok)) return;
-    const Drawn d = sh.ring[slot];
-    if (d.t.phase == kNoTile) return;
-    const int acc = tile & 1;
+    const Listed* const l = &sh.ring[slot];
+    if (l->phase == kNoTile) return;
     ok = wait_on(sh, p, &sh.acc_full[acc], (uint32_t)(tile >> 1) & 1u);
     if (!group_all(r.group, ok)) return;
     tmem_after_sync();
     const uint32_t from =
         tmem + acc * kTileN + ((uint32_t)(quarter * 32) << 16);
-    const MuonMatrix& x = p.mats[d.t.matrix];
-    const int a0 = row0(d), blocks = block_count(x, d);
+    const int a0 = row0(*l), blocks = block_count(*l), phase = l->phase;
+    const int b0 = l->j * kTileN, m = l->height;
+    const bool last = l->last, tall = l->tall;
     r.i = a0 + r.row;
-    const bool last = d.t.phase == kApply && d.it == p.steps - 1;
-    const bool tall = x.tall;
-    const int m = x.m;
-    const float s = d.t.phase == kGram ? 1.f / (x.scale * x.scale)
-                                       : 1.f / (kScaleD * kScaleD);
-    float* const diag = d.t.phase == kGram ? x.diag : x.beta;
-    const float pa = p.k.a, pb = p.k.b, pc = p.k.c;
+    const float s = phase == kGram ? 1.f / (l->scale * l->scale)
+                                   : 1.f / (kScaleD * kScaleD);
+    float* const diag = phase == kGram ? l->diag : l->beta;
     const uint32_t vec = staging + kBuffers * kBufferBytes + slot * kVecBytes;
     float row_v = 0.f;            // the row's l or beta
     Output o;
-    if (last) o = output_of(p, x, p.ptrs[d.t.matrix]);
-    if (d.t.phase != kGram) {
+    if (last) o = output_of(p, *l, lr);
+    if (phase != kGram) {
       wait_on(sh, p, &sh.vec[slot], (uint32_t)(tile / kRing) & 1u);
       row_v = lds_f(vec + kColBytes + 4 * r.row);
     }
     for (int c = 0; c < blocks; ++c, ++n) {
       if (n % kGroups != r.group) continue;
-      const int b = n % kBuffers, c0 = d.t.j * kTileN + c * kMuonCols;
+      const int b = n % kBuffers, c0 = b0 + c * kMuonCols;
       r.buf = staging + b * kBufferBytes;
       r.col = vec + c * (kMuonCols * 4);
       float y[32];
       tmem_ld32(from + c * kMuonCols, y);
       wait_on(sh, p, &sh.in[b], (uint32_t)(n / kBuffers) & 1u);
-      if (d.t.phase == kGram) {
+      if (phase == kGram) {
         symmetric_block<false>(pb, pc, m, diag, 0.f, s, a0, c0, r, y);
-      } else if (d.t.phase == kSquare) {
+      } else if (phase == kSquare) {
         symmetric_block<true>(pb, pc, m, diag, row_v, s, a0, c0, r, y);
       } else if (!last) {
         apply_block<false>(tall, pa, pa + row_v, r, y);
@@ -651,7 +639,8 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
         last_block(o, a0, c0, r, y);
       }
       fence_staging();
-      mbar_arrive(&sh.out[b]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.out[b]);
     }
     tmem_before_sync();
     __syncwarp();
@@ -680,11 +669,11 @@ muon_steps_kernel(const __grid_constant__ MuonParams p) {
     }
     for (int i = 0; i < kBuffers; ++i) {
       mbar_init(&sh.in[i], 1);
-      mbar_init(&sh.out[i], kEpiThreads);
+      mbar_init(&sh.out[i], kEpiThreads / 32);
       mbar_init(&sh.vacant[i], 1);
     }
     for (int i = 0; i < kRing; ++i) {
-      mbar_init(&sh.drawn[i], 1);
+      mbar_init(&sh.listed[i], 1);
       mbar_init(&sh.read[i], kReaders);
       mbar_init(&sh.vec[i], 1);
     }
@@ -693,13 +682,16 @@ muon_steps_kernel(const __grid_constant__ MuonParams p) {
     fence_proxy_async();
   }
   if (warp == 2) pair_tmem_alloc_all(&sh.tmem);
+  for (int i = threadIdx.x; i < p.n_mats * kMuonMaps; i += kStepThreads)
+    take_map(reinterpret_cast<const CUtensorMap*>(p.mats + i / kMuonMaps) +
+             i % kMuonMaps);
   tmem_before_sync();
   __syncthreads();
   cluster_sync();        // both CTAs' barriers are there
   tmem_after_sync();
   const uint32_t tmem = sh.tmem, rank = cluster_rank();
   if (warp == 0) {
-    if (elect_lane()) list_and_copy(sh, p, smem, rank);
+    if (elect_lane()) copy_operands(sh, p, smem, rank);
     __syncwarp();
   } else if (warp == 1) {
     if (elect_lane()) multiply(sh, p, smem, tmem, rank);

@@ -51,10 +51,15 @@ __device__ __forceinline__ bool elect_lane() {
   return ok != 0;
 }
 
-// ---- tensor copies ----------------------------------------------------------
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+// Tensor maps that lie in global memory and were written by a copy from the host:
+// before a CTA uses one, a thread of it has to take it over (and a barrier to
+// follow).  Without it a copy may go by the map that was at the address before.
+__device__ __forceinline__ void take_map(const CUtensorMap* map) {
+  asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;"
+               ::"l"(map) : "memory");
 }
+
+// ---- tensor copies ----------------------------------------------------------
 __device__ __forceinline__ void tile_load(uint32_t smem, const CUtensorMap* map,
                                           int x, int y, uint64_t* bar) {
   asm volatile(
