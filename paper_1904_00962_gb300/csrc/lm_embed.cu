@@ -209,45 +209,107 @@ digit_move_kernel(const int64_t* ids, const uint32_t* keys, const int32_t* pos,
     __syncwarp();
     if (in && before == 0) count[warp][digit] += __popc(same);
     __syncwarp();
-    if (!in) continue;
-    keys_out[to] = key;
-    pos_out[to] = pos ? pos[at] : (int32_t)at;
-    if (ids && key < (uint32_t)vocab) atomicOr(&seen[key >> 5], 1u << (key & 31));
-    if (next_hist)
-      atomicAdd(&next_hist[to / tile * 256 + ((key >> (shift + 8)) & 255u)], 1);
+    if (in) {
+      keys_out[to] = key;
+      pos_out[to] = pos ? pos[at] : (int32_t)at;
+      // (a mask token's thousands would queue up at its word: look first)
+      if (ids && key < (uint32_t)vocab) {
+        const uint32_t bit = 1u << (key & 31);
+        if (!(ld_relaxed_u32(&seen[key >> 5]) & bit))
+          atomicOr(&seen[key >> 5], bit);
+      }
+    }
+    if (next_hist) {      // one addition for a warp's equal places
+      const int where =
+          in ? to / tile * 256 + (int)((key >> (shift + 8)) & 255u) : -1;
+      const uint32_t m = __match_any_sync(0xffffffffu, where);
+      if (in && (m & ((1u << lane) - 1u)) == 0)
+        atomicAdd(&next_hist[where], __popc(m));
+    }
   }
 }
 
 // ---- sums -------------------------------------------------------------------
-template <class TG, bool kVec>
-__device__ __forceinline__ void load_row(const TG* p, int d, int width,
-                                         float (&x)[4]) {
-  if (kVec) {
-    load4(p + d, x);
-  } else {
+// kN columns of a row, kVec by whole accesses.
+template <class T, int kN, bool kVec>
+__device__ __forceinline__ void load_row(const T* p, int d, int width,
+                                         float (&x)[kN]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = d + j < width ? load1(p + d + j) : 0.f;
+  for (int q = 0; q < kN; q += 4) {
+    if (kVec) {
+      float v[4];
+      load4(p + d + q, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[q + j] = v[j];
+    } else {
+#pragma unroll
+      for (int j = q; j < q + 4; ++j) x[j] = d + j < width ? load1(p + d + j) : 0.f;
+    }
   }
 }
-template <class TT, bool kVec>
-__device__ __forceinline__ void write_row(TT* p, int d, int width,
-                                          const float (&s)[4], float scale,
+template <class T, int kN, bool kVec>
+__device__ __forceinline__ void write_row(T* p, int d, int width,
+                                          const float (&s)[kN], float scale,
                                           bool add) {
-  float x[4] = {0.f, 0.f, 0.f, 0.f};
-  if (add) load_row<TT, kVec>(p, d, width, x);
+  float x[kN];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = add ? x[j] + s[j] * scale : s[j] * scale;
+  for (int j = 0; j < kN; ++j) x[j] = 0.f;
+  if (add) load_row<T, kN, kVec>(p, d, width, x);
+#pragma unroll
+  for (int j = 0; j < kN; ++j) x[j] = add ? x[j] + s[j] * scale : s[j] * scale;
   if (kVec) {
-    store4(p + d, x);
+#pragma unroll
+    for (int q = 0; q < kN; q += 4) {
+      const float v[4] = {x[q], x[q + 1], x[q + 2], x[q + 3]};
+      store4(p + d + q, v);
+    }
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kN; ++j)
       if (d + j < width) store1(p + d + j, x[j]);
   }
 }
 
-// tx threads take a chunk's rows, four columns each; kEmbedThreads / tx chunks a
-// CTA.  The CTAs past the chunks clear rows without a token.
+// Rows of the gradient on their way: 16 bytes of each as they are (kVec).
+template <class T, bool kVec>
+struct Raw {
+  static constexpr int kN = kVec ? 16 / (int)sizeof(T) : 4;
+  uint4 w;
+  float x[kVec ? 1 : 4];
+  __device__ __forceinline__ void load(const T* p, int d, int width) {
+    if (kVec) {
+      w = *reinterpret_cast<const uint4*>(p + d);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x[kVec ? 0 : j] = d + j < width ? load1(p + d + j) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void add_to(float (&s)[kN]) const {
+    if (!kVec) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) s[j] += x[kVec ? 0 : j];
+    } else {
+      const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (sizeof(T) == 4) {
+          s[j] += __uint_as_float(v[j]);
+        } else {
+          s[(2 * j) % kN] += __uint_as_float(v[j] << 16);
+          s[(2 * j + 1) % kN] += __uint_as_float(v[j] & 0xffff0000u);
+        }
+      }
+    }
+  }
+};
+
+// tx threads take a chunk's rows, 16 bytes of each; kEmbedThreads / tx chunks a
+// CTA.  kBatch rows are on their way at a time: HBM's latency over rows that lie
+// anywhere takes some 100 KB in flight on an SM.  The CTAs past the chunks clear
+// rows without a token.
+constexpr int kBatch = 16, kLeastTx = 8;
+
 template <class TG, class TT, bool kVec>
 __global__ void __launch_bounds__(kEmbedThreads)
 embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
@@ -257,10 +319,10 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
                   const uint32_t* __restrict__ seen, float* __restrict__ part,
                   float scale, bool add, TT* __restrict__ out,
                   int64_t out_stride) {
-  __shared__ uint32_t sh_key[kEmbedThreads * 2 + 2];
-  __shared__ int32_t sh_pos[kEmbedThreads * 2];
-  static_assert(kEmbedThreads / 16 * kChunk <= kEmbedThreads * 2,
-                "the keys of a CTA's chunks");
+  typedef Raw<TG, kVec> R;
+  constexpr int kN = R::kN;
+  __shared__ uint32_t sh_key[kEmbedThreads / kLeastTx * kChunk + 2];
+  __shared__ int32_t sh_pos[kEmbedThreads / kLeastTx * kChunk];
   let_next_launch();
   after_prior_launch();
   if ((int)blockIdx.x >= chunk_ctas) {
@@ -269,9 +331,9 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
       const int64_t v = v0 + r;
       if (v >= vocab || (n && (seen[v >> 5] >> (v & 31) & 1u))) continue;
       TT* dst = out + v * out_stride;
-      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int d = (threadIdx.x & 31) * 4; d < width; d += 128)
-        write_row<TT, kVec>(dst, d, width, zero, 1.f, false);
+      float zero[kN] = {};
+      for (int d = (threadIdx.x & 31) * kN; d < width; d += 32 * kN)
+        write_row<TT, kN, kVec>(dst, d, width, zero, 1.f, false);
     }
     return;
   }
@@ -293,40 +355,35 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
   const int m = min(kChunk, held - at0);
   if (m <= 0) return;
   float* const mine = part + (int64_t)(chunk0 + y) * 2 * width;
-  auto key_at = [&](int i) -> uint32_t {            // -1 .. m: with neighbours
-    return sh_key[at0 + i + 1];
-  };
-  for (int d = x0 * 4; d < width; d += tx * 4) {
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    bool from_before = key_at(-1) == key_at(0);
-    for (int i0 = 0; i0 < m; i0 += 8) {
-      float x[8][4];
+  const uint32_t* const key = sh_key + at0 + 1;     // -1 .. m: with neighbours
+  for (int d = x0 * kN; d < width; d += tx * kN) {
+    float s[kN] = {};
+    bool from_before = key[-1] == key[0];
+    for (int i0 = 0; i0 < m; i0 += kBatch) {
+      R x[kBatch];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < kBatch; ++u) {
         const int i = i0 + u;
-        x[u][0] = x[u][1] = x[u][2] = x[u][3] = 0.f;
-        if (i < m && key_at(i) < (uint32_t)vocab)
-          load_row<TG, kVec>(grad + (int64_t)sh_pos[at0 + i] * stride, d, width,
-                             x[u]);
+        if (i < m && key[i] < (uint32_t)vocab)
+          x[u].load(grad + (int64_t)sh_pos[at0 + i] * stride, d, width);
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < kBatch; ++u) {
         const int i = i0 + u;
         if (i >= m) break;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] += x[u][j];
-        const uint32_t key = key_at(i);
-        const bool goes_on = key_at(i + 1) == key;
+        const uint32_t v = key[i];
+        if (v >= (uint32_t)vocab) break;            // none follows either
+        x[u].add_to(s);
+        const bool goes_on = key[i + 1] == v;
         if (goes_on && i + 1 < m) continue;
-        if (key < (uint32_t)vocab) {
-          if (!from_before && !goes_on)
-            write_row<TT, kVec>(out + (int64_t)key * out_stride, d, width, s,
-                                scale, add);
-          else
-            write_row<float, kVec>(mine + (from_before ? 0 : width), d, width,
-                                   s, 1.f, false);
-        }
-        s[0] = s[1] = s[2] = s[3] = 0.f;
+        if (!from_before && !goes_on)
+          write_row<TT, kN, kVec>(out + (int64_t)v * out_stride, d, width, s,
+                                  scale, add);
+        else
+          write_row<float, kN, kVec>(mine + (from_before ? 0 : width), d, width,
+                                     s, 1.f, false);
+#pragma unroll
+        for (int j = 0; j < kN; ++j) s[j] = 0.f;
         from_before = false;
       }
     }
@@ -337,19 +394,19 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
 // the chunks' sums: in their order or, of a long word, in kJoinParts runs that are
 // added in order.
 template <class TT, bool kVec>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinThreads, 6)
 embed_join_kernel(const uint32_t* __restrict__ keys, int n, int64_t vocab,
                   int width, const float* __restrict__ part, float scale,
                   bool add, TT* __restrict__ out, int64_t out_stride) {
   __shared__ float4 sh[kJoinThreads];
   after_prior_launch();
   const int c = blockIdx.x;
-  const int64_t last = (int64_t)c * kChunk + kChunk - 1;
+  const int64_t first = (int64_t)c * kChunk, last = first + kChunk - 1;
   if (last + 1 >= n) return;
-  const uint32_t v = keys[last];
-  if (v >= (uint32_t)vocab || keys[last + 1] != v) return;
-  const int64_t first = (int64_t)c * kChunk;
-  if (first > 0 && keys[first] == v && keys[first - 1] == v) return;
+  const uint32_t v = keys[last], after = keys[last + 1], head = keys[first];
+  const uint32_t before = keys[first > 0 ? first - 1 : 0];
+  if (v >= (uint32_t)vocab || after != v) return;
+  if (first > 0 && head == v && before == v) return;
   // the last chunk with the word: doubling steps, then halving ones
   const int chunks = (n + kChunk - 1) / kChunk;
   int lo = c + 1, step = 1;
@@ -372,11 +429,11 @@ embed_join_kernel(const uint32_t* __restrict__ keys, int n, int64_t vocab,
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (d < width) {
       if (g == 0)
-        load_row<float, kVec>(part + ((int64_t)c * 2 + 1) * width, d, width, s);
-#pragma unroll 16
+        load_row<float, 4, kVec>(part + ((int64_t)c * 2 + 1) * width, d, width, s);
+#pragma unroll 8
       for (int k = a; k < b; ++k) {
         float y[4];
-        load_row<float, kVec>(part + (int64_t)(c + 1 + k) * 2 * width, d, width,
+        load_row<float, 4, kVec>(part + (int64_t)(c + 1 + k) * 2 * width, d, width,
                               y);
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] += y[j];
@@ -391,14 +448,15 @@ embed_join_kernel(const uint32_t* __restrict__ keys, int n, int64_t vocab,
       }
     }
     if (g == 0 && d < width)
-      write_row<TT, kVec>(dst, d, width, s, scale, add);
+      write_row<TT, 4, kVec>(dst, d, width, s, scale, add);
     if (parts > 1) __syncthreads();
   }
 }
 
-bool vec_ok(const void* p, int dtype, int64_t stride, int width) {
-  const uintptr_t bytes = dtype == LAMB_F32 ? 16 : 8;
-  return (uintptr_t)p % bytes == 0 && stride % 4 == 0 && width % 4 == 0;
+// Whether rows can be taken four columns at a time (`cols`: that many).
+bool vec_ok(const void* p, int dtype, int64_t stride, int width, int cols = 4) {
+  const uintptr_t bytes = dtype == LAMB_F32 ? 16 : 2 * (uintptr_t)cols;
+  return (uintptr_t)p % bytes == 0 && stride % cols == 0 && width % cols == 0;
 }
 
 template <class TI, class TO>
@@ -420,9 +478,10 @@ template <class TG, class TT, bool kVec>
 cudaError_t launch_sums(const lamb_vocab* v, const void* grad, int64_t gs,
                         int n, int in, float scale, bool add, void* out,
                         int64_t os, cudaStream_t stream) {
-  // threads of a chunk: its columns, 16 at least
+  // threads of a chunk: its columns, kLeastTx at least
+  constexpr int kN = Raw<TG, kVec>::kN;
   int tx = kEmbedThreads;
-  while (tx > 16 && tx / 2 * 4 >= v->width) tx /= 2;
+  while (tx > kLeastTx && tx / 2 * kN >= v->width) tx /= 2;
   const int chunks = (int)lm_ceil_div(n, kChunk);
   const int ctas = (int)lm_ceil_div(chunks, kEmbedThreads / tx);
   const int64_t clears = add ? 0 : lm_ceil_div(v->vocab, kClearRows);
@@ -559,8 +618,10 @@ extern "C" lamb_status_t lamb_vocab_embed_grad(
     in ^= 1;
   }
   if (e != cudaSuccess) return lm_cuda_fail(e, "sort launch");
-  const bool vec = vec_ok(grad_out, grad_dtype, grad_stride, v->width) &&
-                   vec_ok(table_grad, table_dtype, table_stride, v->width);
+  const int cols = grad_dtype == LAMB_F32 ? 4 : 8;       // 16 bytes
+  const bool vec =
+      vec_ok(grad_out, grad_dtype, grad_stride, v->width, cols) &&
+      vec_ok(table_grad, table_dtype, table_stride, v->width);
   const float s = (float)scale;
   const bool add = accumulate != 0;
   typedef __nv_bfloat16 bf;

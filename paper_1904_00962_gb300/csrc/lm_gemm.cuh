@@ -10,8 +10,11 @@
 //   Work::tile(params, state, t)  operands and extent of tile t (GemmTile)
 //   Work::epilogue(params, state, tile, acc, epi)  a row of the accumulator
 // A tile is 128 rows of A by 256 of B.  Operands come through tensor maps with
-// the 128-byte swizzle, K-major (box: 64 of K by 128 rows) or MN-major (box: 64
-// rows by 64 of K); what lies outside a matrix arrives as zeros.
+// the 128-byte swizzle, K-major (64 of K by all the tile's rows) or MN-major
+// (blocks of 64 rows by 64 of K, all of the tile's in one copy where the map has
+// them as a third dimension); what lies outside a matrix arrives as zeros.  One
+// copy an operand counts: issuing one takes its thread some 100 cycles, and a
+// stage of products 512.
 //
 // Warps: 0 copies, 1 issues the products, 2 holds the tensor memory, 4-7 run the
 // epilogue (a warp reaches the quarter of the lanes with its number mod 4).
@@ -30,7 +33,10 @@ constexpr int kTileBytesA = kTileM * kTileK * 2;
 constexpr int kTileBytesB = kTileN * kTileK * 2;
 constexpr int kGemmStageBytes = kTileBytesA + kTileBytesB;
 constexpr int kGemmStages = 4;
-constexpr size_t kGemmSmem = (size_t)kGemmStages * kGemmStageBytes + 1024;
+// a block of 32 rows and 64 columns on its way out, two a warp
+constexpr int kOutBytes = 32 * 64 * 2, kOutBuffers = 2;
+constexpr size_t kGemmSmem = (size_t)kGemmStages * kGemmStageBytes +
+                             4 * kOutBuffers * kOutBytes + 1024;
 constexpr int kEpiThreads = 128, kEpiBarrier = 1;
 
 struct GemmTile {
@@ -40,6 +46,7 @@ struct GemmTile {
   int k0, kn;        // first block of K, number of blocks
   int b_k;           // elements that B's K starts further on
   bool a_mn, b_mn;   // MN-major operands
+  bool b_blocks;     // B's blocks are a dimension of its map (A's always are)
   int what, aux;     // the epilogue's
 };
 
@@ -53,6 +60,30 @@ struct GemmShared {
 // What an epilogue thread has.
 struct Epilogue {
   int row;               // of the tile, 0 .. 127
+  uint32_t out;          // the warp's staging memory
+  int n;                 // blocks that went through it
+
+  // A block of the warp's 32 rows and 64 columns of 16 bits, w the thread's row:
+  // out by a tensor copy to (x, y), which clips it at the matrix' edges.  Direct
+  // stores, a row a thread, take a 16-byte piece of 32 lines each.
+  __device__ __forceinline__ void store_block(const CUtensorMap* map, int x,
+                                              int y, const uint32_t (&w)[32]) {
+    const int r = row & 31;
+    const uint32_t at = out + (n & 1) * kOutBytes;
+    if (r == 0) stores_have_read<kOutBuffers - 1>();
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      sts16(at + r * 128 + ((q ^ (r & 7)) << 4),
+            make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (r == 0) {
+      tile_store(map, x, y, at);
+      stores_commit();
+    }
+    ++n;
+  }
 
   // Every thread, whatever its wait said: one answer for all.
   __device__ __forceinline__ bool all(bool x) const {
@@ -95,6 +126,7 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
   __syncthreads();
   tmem_after_sync();
   const uint32_t tmem = sh.tmem;
+  let_next_launch();
   after_prior_launch();
   const typename Work::State st = Work::start(p);
 
@@ -115,20 +147,17 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
           const uint32_t at = smem + s * kGemmStageBytes;
           const int k = (g.k0 + kb) * kTileK;
           mbar_expect(&sh.full[s], kGemmStageBytes);
-          if (g.a_mn) {
-            tile_load(at, g.a, g.a0, k, &sh.full[s]);
-            tile_load(at + 8192, g.a, g.a0 + 64, k, &sh.full[s]);
-          } else {
-            tile_load(at, g.a, k, g.a0, &sh.full[s]);
-          }
+          if (g.a_mn) blocks_load(at, g.a, k, g.a0 / 64, &sh.full[s]);
+          else tile_load(at, g.a, k, g.a0, &sh.full[s]);
           const uint32_t bt = at + kTileBytesA;
-          if (g.b_mn) {
-            for (int i = 0; i < 4; ++i)
-              tile_load(bt + i * 8192, g.b, g.b0 + 64 * i, k + g.b_k,
-                        &sh.full[s]);
+          const int bk = k + g.b_k;
+          if (!g.b_mn) {
+            tile_load(bt, g.b, bk, g.b0, &sh.full[s]);
+          } else if (g.b_blocks) {
+            blocks_load(bt, g.b, bk, g.b0 / 64, &sh.full[s]);
           } else {
-            tile_load(bt, g.b, k + g.b_k, g.b0, &sh.full[s]);
-            tile_load(bt + 16384, g.b, k + g.b_k, g.b0 + 128, &sh.full[s]);
+            for (int i = 0; i < 4; ++i)
+              tile_load(bt + i * 8192, g.b, g.b0 + 64 * i, bk, &sh.full[s]);
           }
         }
       }
@@ -182,6 +211,9 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
     Epilogue epi;
     const int quarter = warp & 3;
     epi.row = quarter * 32 + lane;
+    epi.out = smem + kGemmStages * kGemmStageBytes +
+              quarter * (kOutBuffers * kOutBytes);
+    epi.n = 0;
     int n = 0;
     for (int t = blockIdx.x; t < st.n_tiles; t += gridDim.x, ++n) {
       const GemmTile g = Work::tile(p, st, t);
@@ -198,6 +230,7 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
     }
+    if (lane == 0) stores_done();
   }
   tmem_before_sync();
   __syncthreads();

@@ -65,6 +65,7 @@ pick_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t stride,
   const int first = blockIdx.x * kPickRows;
   const bool end = blockIdx.x == gridDim.x - 1;
   int before = 0;
+  let_next_launch();
   for (int t = threadIdx.x; t < first; t += kPickThreads) {
     const int64_t y = labels[t];
     before += y >= 0 && y < vocab;
@@ -159,7 +160,7 @@ struct StatsWork {
     g.k0 = 0;
     g.kn = p.k_blocks;
     g.b_k = 0;
-    g.a_mn = g.b_mn = false;
+    g.a_mn = g.b_mn = g.b_blocks = false;
     g.aux = 0;
     return g;
   }
@@ -218,6 +219,7 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
   __shared__ uint32_t last;
   const int part = threadIdx.x & 7, i = threadIdx.x >> 3;
   const int r = blockIdx.x * kJoinRows + i;
+  let_next_launch();
   after_prior_launch();
   const int rows = *n_rows;
   float top = -INFINITY, sum = 0.f;
@@ -274,14 +276,12 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
 
 // ---- the logits' gradient ---------------------------------------------------
 struct DlogitsParams {
-  CUtensorMap hidden, weight;
+  CUtensorMap hidden, weight, out;   // out: the piece's columns
   const int32_t* n_rows;
   const int32_t* labels;
   const float* lse2;
   const float* coef;
-  __nv_bfloat16* out;     // [rows in whole tiles][stride], the piece's columns
   uint32_t* status;
-  int64_t stride;
   int v_tiles, vocab, v0, k_blocks;
 };
 
@@ -307,7 +307,7 @@ struct DlogitsWork {
     g.k0 = 0;
     g.kn = p.k_blocks;
     g.b_k = 0;
-    g.a_mn = g.b_mn = false;
+    g.a_mn = g.b_mn = g.b_blocks = false;
     g.aux = 0;
     return g;
   }
@@ -322,32 +322,35 @@ struct DlogitsWork {
     const int label = real ? p.labels[r] : -1;
     const float l2 = real ? p.lse2[r] : 0.f;
     const float coef = *p.coef;
-    __nv_bfloat16* out = p.out + (int64_t)r * p.stride + g.what;
-    for (int c = 0; c < kTileN / 32; ++c) {
-      const int v = g.b0 + c * 32;
-      float x[32];
-      tmem_ld32(acc + c * 32, x);
+    for (int c = 0; c < kTileN / 64; ++c) {
+      const int v = g.b0 + c * 64;
+      uint32_t y[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        x[i] = exp2_fast(fmaf(x[i], kLog2e, -l2));
-      if (label >= v && label < v + 32) {
+      for (int h = 0; h < 2; ++h) {
+        float x[32];
+        tmem_ld32(acc + c * 64 + h * 32, x);
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if (label == v + i) x[i] -= 1.f;
-      }
-      uint32_t y[16];
+          x[i] = exp2_fast(fmaf(x[i], kLog2e, -l2));
+        const int first = v + h * 32;
+        if (label >= first && label < first + 32) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const bool a = real && v + 2 * i < p.vocab;
-        const bool b = real && v + 2 * i + 1 < p.vocab;
-        const __nv_bfloat162 h = __floats2bfloat162_rn(
-            a ? x[2 * i] * coef : 0.f, b ? x[2 * i + 1] * coef : 0.f);
-        y[i] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-      uint4* to = reinterpret_cast<uint4*>(out + c * 32);
+          for (int i = 0; i < 32; ++i)
+            if (label == first + i) x[i] -= 1.f;
+        }
+        if (!real || first + 32 > p.vocab) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        to[i] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+          for (int i = 0; i < 32; ++i)
+            if (!real || first + i >= p.vocab) x[i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const __nv_bfloat162 b =
+              __floats2bfloat162_rn(x[2 * i] * coef, x[2 * i + 1] * coef);
+          y[h * 16 + i] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+      }
+      epi.store_block(&p.out, g.what + c * 64, g.a0 + (epi.row & ~31), y);
     }
   }
 };
@@ -358,6 +361,7 @@ struct GradsParams {
   CUtensorMap dl_cols;    // dlogits, MN-major (K: tokens)
   CUtensorMap hidden;     // MN-major
   CUtensorMap weight;     // MN-major
+  CUtensorMap out;        // grad_weight, where weight_out
   void* grad_weight;
   __nv_bfloat16* grad_hidden;
   float* slabs;           // [split][rows][width], or NULL: one sum, written out
@@ -370,6 +374,8 @@ struct GradsParams {
   int d_tiles;            // column tiles of the width
   int width, vocab, v0, piece;
   int k_piece, splits;    // blocks of K of dh, parts that they are cut into
+  int weight_blocks;      // weight's map has its blocks as a dimension
+  int weight_out;         // dW goes out by tensor copies
   int weight_f32, accumulate, add_slab, weight_vec, hidden_vec;
 };
 
@@ -452,7 +458,7 @@ struct GradsWork {
       g.k0 = 0;
       g.kn = s.k_rows;
       g.b_k = 0;
-      g.a_mn = g.b_mn = true;
+      g.a_mn = g.b_mn = g.b_blocks = true;
     } else {
       t -= p.w_tiles;
       g.what = 1;
@@ -467,6 +473,7 @@ struct GradsWork {
       g.b_k = p.v0;      // W's rows are the whole vocabulary's
       g.a_mn = false;
       g.b_mn = true;
+      g.b_blocks = p.weight_blocks;
     }
     return g;
   }
@@ -476,6 +483,30 @@ struct GradsWork {
                                                   uint32_t acc, Epilogue& epi) {
     const int r = g.a0 + epi.row;
     const bool in = g.what ? r < s.rows : r < p.piece && p.v0 + r < p.vocab;
+    if (g.what == 0 && p.weight_out) {
+      // (past the piece's rows the accumulator holds zeros, and past the
+      // vocabulary's the copy writes nothing)
+      for (int c = 0; c < kTileN / 64; ++c) {
+        const int d = g.b0 + c * 64;
+        if (d >= p.width) break;
+        uint32_t y[32];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float x[32];
+          tmem_ld32(acc + c * 64 + h * 32, x);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const __nv_bfloat162 b =
+                __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            y[h * 16 + i] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+        }
+        const int first = g.a0 + (epi.row & ~31);
+        if (first < p.piece && p.v0 + first < p.vocab)
+          epi.store_block(&p.out, d, p.v0 + first, y);
+      }
+      return;
+    }
     for (int c = 0; c < kTileN / 32; ++c) {
       const int d = g.b0 + c * 32;
       if (d >= p.width) break;
@@ -567,8 +598,8 @@ template <class Work>
 cudaError_t launch_gemm(const typename Work::Params& p, int64_t most_tiles,
                         int sms, cudaStream_t stream) {
   const int grid = (int)std::min<int64_t>(most_tiles, sms);
-  gemm_kernel<Work><<<grid, kGemmThreads, kGemmSmem, stream>>>(p);
-  return cudaGetLastError();
+  return lm_launch(gemm_kernel<Work>, (unsigned)grid, kGemmThreads, kGemmSmem,
+                   stream, true, p);
 }
 
 template <class Work>
@@ -594,7 +625,7 @@ cudaError_t head_inputs(const lamb_vocab* v, const void* hidden, int64_t hs,
                         const void* weight, int64_t ws, const int64_t* labels,
                         int64_t n, float* token_loss, void* grad_hidden,
                         int64_t gs, cudaStream_t stream, HeadInputs* in) {
-  in->pitch = lm_round_up(v->width, 8);
+  in->pitch = lm_round_up(v->width, 64);
   in->weight = (const __nv_bfloat16*)weight;
   in->weight_stride = ws;
   const bool vec = lm_mappable(hidden, hs) && v->width % 8 == 0 &&
@@ -626,7 +657,7 @@ lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
   if (!lm_map(v->encode, &p.hidden, true, v->rows, lm_round_up(n, kTileM),
               v->width, in.pitch, kTileM) ||
       !lm_map(v->encode, &p.weight, true, in.weight, v->vocab, v->width,
-              in.weight_stride, kTileM))
+              in.weight_stride, kTileN))
     return lm_fail(LAMB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   p.n_rows = v->n_rows;
   p.labels = v->row_label;
@@ -640,11 +671,10 @@ lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
   cudaError_t e = launch_gemm<StatsWork>(
       p, lm_ceil_div(n, kTileM) * p.v_tiles, v->sms, stream);
   if (e != cudaSuccess) return lm_cuda_fail(e, "head loss launch");
-  join_kernel<<<(unsigned)lm_ceil_div(n, kJoinRows), kJoinThreads, 0, stream>>>(
-      v->stats, v->max_tokens, p.v_tiles, v->label_logit, v->row_token,
-      v->n_rows, v->lse2, token_loss, loss, scale, v->coef, v->block_sums,
-      v->ticket);
-  e = cudaGetLastError();
+  e = lm_launch(join_kernel, (unsigned)lm_ceil_div(n, kJoinRows), kJoinThreads,
+                0, stream, true, v->stats, v->max_tokens, p.v_tiles,
+                v->label_logit, v->row_token, v->n_rows, v->lse2, token_loss,
+                loss, scale, v->coef, v->block_sums, v->ticket);
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "head join launch");
 }
 
@@ -678,7 +708,7 @@ int lm_head_setup() {
 }
 
 void lm_head_carve(lamb_vocab* v, LmArena* a) {
-  const int64_t n = v->max_tokens, pitch = lm_round_up(v->width, 8);
+  const int64_t n = v->max_tokens, pitch = lm_round_up(v->width, 64);
   const int64_t whole = lm_round_up(n, kTileM);
   a->take(&v->rows, whole * pitch);
   a->take(&v->row_label, n);
@@ -777,28 +807,37 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
 
   DlogitsParams d;
   GradsParams g;
+  // (the copy of W has rows of whole blocks; the user's only if the width is)
+  g.weight_blocks = v->width % 64 == 0 || in.weight == v->weight_copy;
+  g.weight_out = !f32 && !accumulate &&
+                 lm_mappable(grad_weight, grad_weight_stride);
   const bool ok =
       lm_map(v->encode, &d.hidden, true, v->rows, whole, v->width, in.pitch,
              kTileM) &&
       lm_map(v->encode, &d.weight, true, in.weight, v->vocab, v->width,
-             in.weight_stride, kTileM) &&
-      lm_map(v->encode, &g.hidden, true, v->rows, whole, v->width, in.pitch,
-             kTileK) &&
-      lm_map(v->encode, &g.weight, true, in.weight, v->vocab, v->width,
-             in.weight_stride, kTileK) &&
+             in.weight_stride, kTileN) &&
+      lm_map(v->encode, &d.out, true, v->dlogits, whole, piece, piece, 32) &&
+      lm_map_blocks(v->encode, &g.hidden, true, v->rows, whole, in.pitch,
+                    in.pitch / 64, kTileN / 64) &&
+      (g.weight_blocks
+           ? lm_map_blocks(v->encode, &g.weight, true, in.weight, v->vocab,
+                           in.weight_stride, lm_ceil_div(v->width, 64),
+                           kTileN / 64)
+           : lm_map(v->encode, &g.weight, true, in.weight, v->vocab, v->width,
+                    in.weight_stride, kTileK)) &&
       lm_map(v->encode, &g.dl_rows, true, v->dlogits, whole, piece, piece,
              kTileM) &&
-      lm_map(v->encode, &g.dl_cols, true, v->dlogits, whole, piece, piece,
-             kTileK);
+      lm_map_blocks(v->encode, &g.dl_cols, true, v->dlogits, whole, piece,
+                    piece / 64, kTileM / 64) &&
+      (!g.weight_out || lm_map(v->encode, &g.out, true, grad_weight, v->vocab,
+                               v->width, grad_weight_stride, 32));
   if (!ok) return lm_fail(LAMB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   const int m_tiles = (int)(whole / kTileM);
   d.n_rows = v->n_rows;
   d.labels = v->row_label;
   d.lse2 = v->lse2;
   d.coef = v->coef;
-  d.out = v->dlogits;
   d.status = v->status;
-  d.stride = piece;
   d.vocab = (int)v->vocab;
   d.k_blocks = (int)lm_ceil_div(v->width, kTileK);
 
@@ -848,11 +887,10 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
                       (uintptr_t)grad_hidden % 8 == 0 &&
                       grad_hidden_stride % 4 == 0;
     const int per = v->width / (four ? 4 : 1);
-    (four ? slabs_kernel<4> : slabs_kernel<1>)<<<grid_for(n * per, v->sms), 256,
-                                                 0, stream>>>(
-        v->slabs, g.splits, g.slab, v->width, v->n_rows, v->row_token,
-        (__nv_bfloat16*)grad_hidden, grad_hidden_stride);
-    e = cudaGetLastError();
+    e = lm_launch(four ? slabs_kernel<4> : slabs_kernel<1>,
+                  (unsigned)grid_for(n * per, v->sms), 256, 0, stream, true,
+                  v->slabs, g.splits, g.slab, v->width, v->n_rows, v->row_token,
+                  (__nv_bfloat16*)grad_hidden, grad_hidden_stride);
     if (e != cudaSuccess) return lm_cuda_fail(e, "hidden gradient launch");
   }
   return LAMB_OK;

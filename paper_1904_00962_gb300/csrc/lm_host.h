@@ -119,17 +119,15 @@ inline bool lm_map(EncodeTiled encode, CUtensorMap* map, bool bf16,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The same matrix in boxes of 64 lines by `blocks` times 64 columns, which arrive
-// block after block (an MN-major operand).  Whole blocks are copied, so that the
-// row stride has to be a multiple of 64; what lies between cols and it is copied
-// too.
+// A matrix of `blocks` times 64 columns in boxes of 64 lines by box_blocks blocks,
+// which arrive block after block (an MN-major operand).  Whole blocks are copied:
+// the rows have to have that many elements, whatever the last ones are.
 inline bool lm_map_blocks(EncodeTiled encode, CUtensorMap* map, bool bf16,
                           const void* base, int64_t rows, int64_t row_stride,
-                          int blocks) {
-  const cuuint64_t dims[3] = {64, (cuuint64_t)rows,
-                              (cuuint64_t)(row_stride / 64)};
+                          int64_t blocks, int box_blocks) {
+  const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)blocks};
   const cuuint64_t strides[2] = {(cuuint64_t)row_stride * 2, 128};
-  const cuuint32_t box[3] = {64, 64, (cuuint32_t)blocks};
+  const cuuint32_t box[3] = {64, 64, (cuuint32_t)box_blocks};
   const cuuint32_t step[3] = {1, 1, 1};
   return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                           : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,

@@ -732,7 +732,7 @@ extern "C" lamb_status_t lamb_muon_create(
         x.hi[i] = (__half*)(base + L.at[i][k]);
         map(&x.x_k[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonRows, 64);
         m = m && lm_map_blocks(encode, &x.x_mn[i], false, x.hi[i], x.rows,
-                               x.pitch, kMuonRows / 64);
+                               x.pitch, x.pitch / 64, kMuonRows / 64);
         map(&x.x_c[i], x.hi[i], x.rows, x.cols, x.pitch, kMuonRows, kMuonCols);
       }
       x.lo = (__half*)(base + L.at[2][k]);
