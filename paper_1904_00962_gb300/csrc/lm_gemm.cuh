@@ -2,19 +2,24 @@
 // operands with fp32 accumulators, tile by tile, each tile handed to an
 // epilogue while the next one is multiplied.
 //
-// One persistent CTA per SM walks the tiles of a Work type:
+// Persistent CTAs walk the tiles of a Work type, one by one or in pairs (kCtas): a
+// pair multiplies a tile of 256 x 256 (cta_group::2), each CTA holding 128 rows of
+// A and of B.  A pair's stage is two thirds of two single ones', so six fit instead
+// of four and less comes from L2; a single CTA's tile of 128 rows wastes less on
+// few rows.
 //   Work::kBf16                   operands bf16 (else fp16)
 //   Work::Params::status          the plan's status word
-//   Work::start(params)           what the kernel reads first: State, with the
-//                                 number of tiles (it may come from the device)
-//   Work::tile(params, state, t)  operands and extent of tile t (GemmTile)
+//   Work::start<kRows>(params)    what the kernel reads first: State, with the
+//                                 number of tiles of kRows rows (it may come from
+//                                 the device)
+//   Work::tile<kRows>(params, state, t)   operands and extent of tile t (GemmTile)
 //   Work::epilogue(params, state, tile, acc, epi)  a row of the accumulator
-// A tile is 128 rows of A by 256 of B.  Operands come through tensor maps with
-// the 128-byte swizzle, K-major (64 of K by all the tile's rows) or MN-major
-// (blocks of 64 rows by 64 of K, all of the tile's in one copy where the map has
-// them as a third dimension); what lies outside a matrix arrives as zeros.  One
-// copy an operand counts: issuing one takes its thread some 100 cycles, and a
-// stage of products 512.
+// A tile has 256 rows of B.  Operands come through tensor maps with the 128-byte
+// swizzle, K-major (64 of K by all of a CTA's rows) or MN-major (blocks of 64 rows
+// by 64 of K, all of a CTA's in one copy where the map has them as a third
+// dimension); what lies outside a matrix arrives as zeros.  One copy an operand
+// counts: issuing one takes its thread some 100 cycles, and a stage of products
+// 512.
 //
 // Warps: 0 copies, 1 issues the products, 2 holds the tensor memory, 4-7 run the
 // epilogue (a warp reaches the quarter of the lanes with its number mod 4).
@@ -30,13 +35,20 @@ namespace {
 constexpr int kTileM = 128, kTileN = 256, kTileK = 64;
 constexpr int kGemmThreads = 256;
 constexpr int kTileBytesA = kTileM * kTileK * 2;
-constexpr int kTileBytesB = kTileN * kTileK * 2;
-constexpr int kGemmStageBytes = kTileBytesA + kTileBytesB;
-constexpr int kGemmStages = 4;
+// a CTA's rows of B, stages
+template <int kCtas>
+constexpr int kRowsB = kTileN / kCtas;
+template <int kCtas>
+constexpr int kGemmStageBytes = kTileBytesA + kRowsB<kCtas> * kTileK * 2;
+template <int kCtas>
+constexpr int kGemmStages = kCtas == 2 ? 6 : 4;
+constexpr int kMaxStages = 6;
 // a block of 32 rows and 64 columns on its way out, two a warp
 constexpr int kOutBytes = 32 * 64 * 2, kOutBuffers = 2;
-constexpr size_t kGemmSmem = (size_t)kGemmStages * kGemmStageBytes +
-                             4 * kOutBuffers * kOutBytes + 1024;
+template <int kCtas>
+constexpr size_t kGemmSmem =
+    (size_t)kGemmStages<kCtas> * kGemmStageBytes<kCtas> +
+    4 * kOutBuffers * kOutBytes + 1024;
 constexpr int kEpiThreads = 128, kEpiBarrier = 1;
 
 struct GemmTile {
@@ -51,7 +63,7 @@ struct GemmTile {
 };
 
 struct GemmShared {
-  uint64_t full[kGemmStages], empty[kGemmStages];
+  uint64_t full[kMaxStages], empty[kMaxStages];
   uint64_t acc_full[2], acc_empty[2];
   uint32_t tmem;
   volatile int gave_up;
@@ -84,126 +96,142 @@ struct Epilogue {
     }
     ++n;
   }
-
-  // Every thread, whatever its wait said: one answer for all.
-  __device__ __forceinline__ bool all(bool x) const {
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 p, %1, 0;\n\t"
-        "barrier.cta.red.and.pred q, %2, %3, p;\n\t"
-        "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(r) : "r"((uint32_t)x), "n"(kEpiBarrier), "n"(kEpiThreads)
-        : "memory");
-    return r != 0;
-  }
 };
 
-template <class Work>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+template <class Work, int kCtas>
+__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ typename Work::Params p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ GemmShared sh;
+  constexpr bool kPair = kCtas == 2;
+  constexpr int kStages = kGemmStages<kCtas>, kRows = kTileM * kCtas;
+  constexpr uint32_t kBytes = kGemmStageBytes<kCtas>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem =
       (smem_u32(smem_raw) + 1023u) & ~1023u;   // the swizzle's pattern
+  const int rank = kPair ? (int)cluster_rank() : 0;
+  const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kGemmStages; ++i) {
+    for (int i = 0; i < kStages; ++i) {
       mbar_init(&sh.full[i], 1);
       mbar_init(&sh.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.acc_full[i], 1);
-      mbar_init(&sh.acc_empty[i], 4);
+      mbar_init(&sh.acc_empty[i], 4 * kCtas);
     }
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   }
-  if (warp == 2) tmem_alloc_all(&sh.tmem);
+  if (warp == 2) {
+    if (kPair) pair_tmem_alloc_all(&sh.tmem);
+    else tmem_alloc_all(&sh.tmem);
+  }
   tmem_before_sync();
   __syncthreads();
+  if (kPair) cluster_sync();
   tmem_after_sync();
   const uint32_t tmem = sh.tmem;
   let_next_launch();
   after_prior_launch();
-  const typename Work::State st = Work::start(p);
+  const typename Work::State st = Work::template start<kRows>(p);
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    return bounded_wait(bar, parity, &sh.gave_up, p.status, kStatusWaitTimeout);
+  };
 
   if (warp == 0) {
     if (elect_lane()) {
       int it = 0;
       bool ok = true;
-      for (int t = blockIdx.x; ok && t < st.n_tiles; t += gridDim.x) {
-        const GemmTile g = Work::tile(p, st, t);
+      for (int t = unit; ok && t < st.n_tiles; t += units) {
+        const GemmTile g = Work::template tile<kRows>(p, st, t);
+        const int a0 = g.a0 + rank * kTileM;
+        const int b0 = g.b0 + rank * kRowsB<kCtas>;
         for (int kb = 0; kb < g.kn; ++kb, ++it) {
-          const int s = it % kGemmStages;
-          const uint32_t ph = (uint32_t)(it / kGemmStages) & 1u;
-          if (!bounded_wait(&sh.empty[s], ph ^ 1u, &sh.gave_up, p.status,
-                            kStatusWaitTimeout)) {
+          const int s = it % kStages;
+          if (!wait(&sh.empty[s], ((uint32_t)(it / kStages) & 1u) ^ 1u)) {
             ok = false;
             break;
           }
-          const uint32_t at = smem + s * kGemmStageBytes;
-          const int k = (g.k0 + kb) * kTileK;
-          mbar_expect(&sh.full[s], kGemmStageBytes);
-          if (g.a_mn) blocks_load(at, g.a, k, g.a0 / 64, &sh.full[s]);
-          else tile_load(at, g.a, k, g.a0, &sh.full[s]);
-          const uint32_t bt = at + kTileBytesA;
-          const int bk = k + g.b_k;
-          if (!g.b_mn) {
-            tile_load(bt, g.b, bk, g.b0, &sh.full[s]);
-          } else if (g.b_blocks) {
-            blocks_load(bt, g.b, bk, g.b0 / 64, &sh.full[s]);
+          const uint32_t at = smem + s * kBytes, bt = at + kTileBytesA;
+          const int k = (g.k0 + kb) * kTileK, bk = k + g.b_k;
+          if (rank == 0) mbar_expect(&sh.full[s], kCtas * kBytes);
+          if (kPair) {
+            const uint32_t bar = at_rank(&sh.full[s], 0);   // who issues
+            if (g.a_mn) pair_blocks_load(at, g.a, k, a0 / 64, bar);
+            else pair_tile_load(at, g.a, k, a0, bar);
+            if (!g.b_mn) {
+              pair_tile_load(bt, g.b, bk, b0, bar);
+            } else if (g.b_blocks) {
+              pair_blocks_load(bt, g.b, bk, b0 / 64, bar);
+            } else {
+              for (int i = 0; i < kRowsB<kCtas> / 64; ++i)
+                pair_tile_load(bt + i * 8192, g.b, b0 + 64 * i, bk, bar);
+            }
           } else {
-            for (int i = 0; i < 4; ++i)
-              tile_load(bt + i * 8192, g.b, g.b0 + 64 * i, bk, &sh.full[s]);
+            if (g.a_mn) blocks_load(at, g.a, k, a0 / 64, &sh.full[s]);
+            else tile_load(at, g.a, k, a0, &sh.full[s]);
+            if (!g.b_mn) {
+              tile_load(bt, g.b, bk, b0, &sh.full[s]);
+            } else if (g.b_blocks) {
+              blocks_load(bt, g.b, bk, b0 / 64, &sh.full[s]);
+            } else {
+              for (int i = 0; i < kRowsB<kCtas> / 64; ++i)
+                tile_load(bt + i * 8192, g.b, b0 + 64 * i, bk, &sh.full[s]);
+            }
           }
         }
       }
       // every copy has landed, and its products' arrival is in, before the CTA
-      // may leave
-      const int first = it > kGemmStages ? it - kGemmStages : 0;
-      for (int j = first; j < it; ++j) {
-        settle(&sh.full[j % kGemmStages], (uint32_t)(j / kGemmStages) & 1u);
-        bounded_wait(&sh.empty[j % kGemmStages],
-                     (uint32_t)(j / kGemmStages) & 1u, &sh.gave_up, p.status,
-                     kStatusWaitTimeout);
+      // (either of a pair: cluster_sync) may leave
+      for (int j = it > kStages ? it - kStages : 0; j < it; ++j) {
+        if (rank == 0 && sh.gave_up)
+          settle(&sh.full[j % kStages], (uint32_t)(j / kStages) & 1u);
+        wait(&sh.empty[j % kStages], (uint32_t)(j / kStages) & 1u);
       }
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (elect_lane()) {
+    if (rank == 0 && elect_lane()) {
       int it = 0, n = 0;
       bool ok = true;
-      for (int t = blockIdx.x; ok && t < st.n_tiles; t += gridDim.x, ++n) {
-        const GemmTile g = Work::tile(p, st, t);
+      for (int t = unit; ok && t < st.n_tiles; t += units, ++n) {
+        const GemmTile g = Work::template tile<kRows>(p, st, t);
         const uint64_t da = operand_desc(g.a_mn), db = operand_desc(g.b_mn);
         const uint32_t sa = operand_step(g.a_mn), sb = operand_step(g.b_mn);
         const uint32_t desc =
-            product_desc(Work::kBf16, g.a_mn, g.b_mn, kTileM, kTileN);
+            product_desc(Work::kBf16, g.a_mn, g.b_mn, kRows, kTileN);
         const int acc = n & 1;
         const uint32_t d = tmem + acc * kTileN;
-        if (!bounded_wait(&sh.acc_empty[acc], ((uint32_t)(n >> 1) & 1u) ^ 1u,
-                          &sh.gave_up, p.status, kStatusWaitTimeout))
-          break;
+        const uint32_t ph = ((uint32_t)(n >> 1) & 1u) ^ 1u;
+        if (!wait(&sh.acc_empty[acc], ph)) break;
+        if (kPair) mbar_try_cluster(&sh.acc_empty[acc], ph);
         tmem_after_sync();
         for (int kb = 0; kb < g.kn; ++kb, ++it) {
-          const int s = it % kGemmStages;
-          if (!bounded_wait(&sh.full[s], (uint32_t)(it / kGemmStages) & 1u,
-                            &sh.gave_up, p.status, kStatusWaitTimeout)) {
+          const int s = it % kStages;
+          if (!wait(&sh.full[s], (uint32_t)(it / kStages) & 1u)) {
             ok = false;
             break;
           }
           tmem_after_sync();
-          const uint32_t at = smem + s * kGemmStageBytes;
+          const uint32_t at = smem + s * kBytes;
           const uint64_t a = da | (at >> 4), b = db | ((at + kTileBytesA) >> 4);
 #pragma unroll
-          for (int k = 0; k < kTileK / 16; ++k)
-            product(d, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
-          products_arrive(&sh.empty[s]);
+          for (int k = 0; k < kTileK / 16; ++k) {
+            if (kPair)
+              pair_product(d, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
+            else
+              product(d, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
+          }
+          if (kPair) pair_products_arrive(&sh.empty[s]);
+          else products_arrive(&sh.empty[s]);
         }
-        if (ok) products_arrive(&sh.acc_full[acc]);
+        if (ok) {
+          if (kPair) pair_products_arrive(&sh.acc_full[acc]);
+          else products_arrive(&sh.acc_full[acc]);
+        }
       }
     }
     __syncwarp();
@@ -211,31 +239,36 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
     Epilogue epi;
     const int quarter = warp & 3;
     epi.row = quarter * 32 + lane;
-    epi.out = smem + kGemmStages * kGemmStageBytes +
-              quarter * (kOutBuffers * kOutBytes);
+    epi.out = smem + kStages * kBytes + quarter * (kOutBuffers * kOutBytes);
     epi.n = 0;
     int n = 0;
-    for (int t = blockIdx.x; t < st.n_tiles; t += gridDim.x, ++n) {
-      const GemmTile g = Work::tile(p, st, t);
+    for (int t = unit; t < st.n_tiles; t += units, ++n) {
+      GemmTile g = Work::template tile<kRows>(p, st, t);
+      g.a0 += rank * kTileM;
       const int acc = n & 1;
-      const bool ok =
-          bounded_wait(&sh.acc_full[acc], (uint32_t)(n >> 1) & 1u, &sh.gave_up,
-                       p.status, kStatusWaitTimeout);
-      if (!epi.all(ok)) break;
+      const bool ok = wait(&sh.acc_full[acc], (uint32_t)(n >> 1) & 1u);
+      if (!__all_sync(0xffffffffu, ok)) break;
       tmem_after_sync();
       Work::epilogue(p, st, g,
                      tmem + acc * kTileN + ((uint32_t)(quarter * 32) << 16),
                      epi);
       tmem_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
+      if (lane == 0) {
+        if (kPair) remote_arrive(at_rank(&sh.acc_empty[acc], 0));
+        else mbar_arrive(&sh.acc_empty[acc]);
+      }
     }
     if (lane == 0) stores_done();
   }
   tmem_before_sync();
   __syncthreads();
+  if (kPair) cluster_sync();
   tmem_after_sync();
-  if (warp == 2) tmem_free_all(tmem);
+  if (warp == 2) {
+    if (kPair) pair_tmem_free_all(tmem);
+    else tmem_free_all(tmem);
+  }
 }
 
 }  // namespace

@@ -37,6 +37,7 @@ constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = 32;          // tokens of a CTA, eight threads each
 constexpr int64_t kPieceElems = 64ll << 20;   // dlogits workspace, elements
 constexpr int kMinPartBlocks = 4;      // blocks of K in a part of dh, at least
+constexpr int64_t kPieceBlocks = 40;   // what a piece more costs, in blocks of K
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -50,6 +51,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // CTA leaves the number of rows and zeros up to a whole tile (one of zeros if
 // there is no row: dW's products need a K).
 constexpr int kPickThreads = 256, kPickRows = 64;
+constexpr int kRowsWhole = 2 * kTileM;       // a tile of a pair of CTAs
 
 template <bool kVec>
 __global__ void __launch_bounds__(kPickThreads)
@@ -99,8 +101,8 @@ pick_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t stride,
   }
   __syncthreads();
   const int own = min(kPickRows, tokens - first);
-  const int past = sh_count[0] % kTileM;
-  const int tail = end && (past || !sh_count[0]) ? kTileM - past : 0;
+  const int past = sh_count[0] % kRowsWhole;
+  const int tail = end && (past || !sh_count[0]) ? kRowsWhole - past : 0;
   for (int r = warp; r < own + tail; r += kPickThreads / 32) {
     const bool zero = r >= own;
     const int t = first + r, to = zero ? sh_count[0] + r - own : sh_at[r];
@@ -142,19 +144,21 @@ struct StatsWork {
   typedef StatsParams Params;
   typedef RowsState State;
   static constexpr bool kBf16 = true;
+  template <int kRows>
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
-    s.m_tiles = s.rows ? (s.rows + kTileM - 1) / kTileM : 1;
+    s.m_tiles = s.rows ? (s.rows + kRows - 1) / kRows : 1;
     s.n_tiles = s.m_tiles * p.v_tiles;
     return s;
   }
+  template <int kRows>
   static __device__ __forceinline__ GemmTile tile(const Params& p,
                                                   const State& s, int t) {
     GemmTile g;
     g.a = &p.hidden;
     g.b = &p.weight;
-    g.a0 = (t % s.m_tiles) * kTileM;
+    g.a0 = (t % s.m_tiles) * kRows;
     g.what = t / s.m_tiles;
     g.b0 = g.what * kTileN;
     g.k0 = 0;
@@ -289,19 +293,21 @@ struct DlogitsWork {
   typedef DlogitsParams Params;
   typedef RowsState State;
   static constexpr bool kBf16 = true;
+  template <int kRows>
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
-    s.m_tiles = s.rows ? (s.rows + kTileM - 1) / kTileM : 1;
+    s.m_tiles = s.rows ? (s.rows + kRows - 1) / kRows : 1;
     s.n_tiles = s.m_tiles * p.v_tiles;
     return s;
   }
+  template <int kRows>
   static __device__ __forceinline__ GemmTile tile(const Params& p,
                                                   const State& s, int t) {
     GemmTile g;
     g.a = &p.hidden;
     g.b = &p.weight;
-    g.a0 = (t % s.m_tiles) * kTileM;
+    g.a0 = (t % s.m_tiles) * kRows;
     g.what = (t / s.m_tiles) * kTileN;     // column inside the piece
     g.b0 = p.v0 + g.what;
     g.k0 = 0;
@@ -437,14 +443,16 @@ struct GradsWork {
   typedef GradsParams Params;
   typedef GradsState State;
   static constexpr bool kBf16 = true;
+  template <int kRows>
   static __device__ __forceinline__ State start(const Params& p) {
     State s;
     s.rows = *p.n_rows;
     s.k_rows = s.rows ? (s.rows + kTileK - 1) / kTileK : 1;   // of zeros
     s.n_tiles = p.w_tiles +
-                (s.rows + kTileM - 1) / kTileM * p.d_tiles * p.splits;
+                (s.rows + kRows - 1) / kRows * p.d_tiles * p.splits;
     return s;
   }
+  template <int kRows>
   static __device__ __forceinline__ GemmTile tile(const Params& p,
                                                   const State& s, int t) {
     GemmTile g;
@@ -453,7 +461,7 @@ struct GradsWork {
       g.aux = 0;
       g.a = &p.dl_cols;
       g.b = &p.hidden;
-      g.a0 = t / p.d_tiles * kTileM;
+      g.a0 = t / p.d_tiles * kRows;
       g.b0 = t % p.d_tiles * kTileN;
       g.k0 = 0;
       g.kn = s.k_rows;
@@ -466,7 +474,7 @@ struct GradsWork {
       t /= p.splits;
       g.a = &p.dl_rows;
       g.b = &p.weight;
-      g.a0 = t / p.d_tiles * kTileM;
+      g.a0 = t / p.d_tiles * kRows;
       g.b0 = t % p.d_tiles * kTileN;
       g.k0 = (int)((int64_t)p.k_piece * g.aux / p.splits);
       g.kn = (int)((int64_t)p.k_piece * (g.aux + 1) / p.splits) - g.k0;
@@ -594,19 +602,30 @@ clear_rows_kernel(void* base, int f32, int64_t rows, int width,
   }
 }
 
+// Pairs of CTAs from this many rows on.
+constexpr int64_t kPairRows = kTileM + 1;
+
 template <class Work>
-cudaError_t launch_gemm(const typename Work::Params& p, int64_t most_tiles,
-                        int sms, cudaStream_t stream) {
-  const int grid = (int)std::min<int64_t>(most_tiles, sms);
-  return lm_launch(gemm_kernel<Work>, (unsigned)grid, kGemmThreads, kGemmSmem,
-                   stream, true, p);
+cudaError_t launch_gemm(const typename Work::Params& p, bool pair,
+                        int64_t most_tiles, int sms, cudaStream_t stream) {
+  if (pair)
+    return lm_launch(gemm_kernel<Work, 2>,
+                     2u * (unsigned)std::min<int64_t>(most_tiles, sms / 2),
+                     kGemmThreads, kGemmSmem<2>, stream, true, p);
+  return lm_launch(gemm_kernel<Work, 1>,
+                   (unsigned)std::min<int64_t>(most_tiles, sms), kGemmThreads,
+                   kGemmSmem<1>, stream, true, p);
 }
 
 template <class Work>
 cudaError_t allow_smem() {
-  return cudaFuncSetAttribute(gemm_kernel<Work>,
+  const cudaError_t e = cudaFuncSetAttribute(
+      gemm_kernel<Work, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      (int)kGemmSmem<1>);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(gemm_kernel<Work, 2>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)kGemmSmem);
+                              (int)kGemmSmem<2>);
 }
 
 int grid_for(int64_t n, int sms) {
@@ -654,10 +673,12 @@ lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
                         const float* scale, float* token_loss, float* loss,
                         cudaStream_t stream) {
   StatsParams p;
-  if (!lm_map(v->encode, &p.hidden, true, v->rows, lm_round_up(n, kTileM),
+  const bool pair = n >= kPairRows;
+  const int rows_b = pair ? kRowsB<2> : kRowsB<1>;
+  if (!lm_map(v->encode, &p.hidden, true, v->rows, lm_round_up(n, kRowsWhole),
               v->width, in.pitch, kTileM) ||
       !lm_map(v->encode, &p.weight, true, in.weight, v->vocab, v->width,
-              in.weight_stride, kTileN))
+              in.weight_stride, rows_b))
     return lm_fail(LAMB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   p.n_rows = v->n_rows;
   p.labels = v->row_label;
@@ -669,13 +690,47 @@ lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
   p.vocab = (int)v->vocab;
   p.k_blocks = (int)lm_ceil_div(v->width, kTileK);
   cudaError_t e = launch_gemm<StatsWork>(
-      p, lm_ceil_div(n, kTileM) * p.v_tiles, v->sms, stream);
+      p, pair, lm_ceil_div(n, pair ? kRowsWhole : kTileM) * p.v_tiles, v->sms,
+      stream);
   if (e != cudaSuccess) return lm_cuda_fail(e, "head loss launch");
   e = lm_launch(join_kernel, (unsigned)lm_ceil_div(n, kJoinRows), kJoinThreads,
                 0, stream, true, v->stats, v->max_tokens, p.v_tiles,
                 v->label_logit, v->row_token, v->n_rows, v->lse2, token_loss,
                 loss, scale, v->coef, v->block_sums, v->ticket);
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "head join launch");
+}
+
+// Columns of a piece of the vocabulary, in whole tiles: of the counts of pieces
+// that the workspace allows, the one whose products' tiles (rows of dW over all
+// tokens, rows of dh over the piece) fall best on `units` CTAs or pairs.  9830 x
+// 30522 x 1024, us: pieces of equal width 1827, so chosen 1639.
+int64_t piece_width(const lamb_vocab* v, int64_t n, int rows, int units) {
+  const int64_t whole = lm_round_up(n, kRowsWhole);
+  const int64_t most = v->dlogits_elems / whole / kTileN * kTileN;
+  const int64_t least = lm_ceil_div(v->vocab, most);
+  const int64_t d_tiles = lm_ceil_div(v->width, kTileN);
+  const int64_t h_tiles = lm_ceil_div(n, rows) * d_tiles;
+  const int64_t w_blocks = lm_ceil_div(n, kTileK);
+  int64_t best = most, best_cost = INT64_MAX;
+  for (int64_t np = least; np < least + 6; ++np) {
+    const int64_t piece =
+        lm_round_up(lm_ceil_div(v->vocab, np), kTileN);
+    const int64_t w_tiles = lm_ceil_div(piece, rows) * d_tiles;
+    int64_t longest = 0;
+    for (int64_t u = 0; u < units; ++u) {      // tiles u, u + units, ...
+      const int64_t all = lm_ceil_div(w_tiles + h_tiles - u, units);
+      const int64_t w = u < w_tiles ? lm_ceil_div(w_tiles - u, units) : 0;
+      longest = std::max(longest, w * w_blocks + (all - w) * (piece / kTileK));
+    }
+    // two launches and their tails are worth some blocks more
+    const int64_t cost =
+        lm_ceil_div(v->vocab, piece) * (longest + kPieceBlocks);
+    if (cost < best_cost) {
+      best_cost = cost;
+      best = piece;
+    }
+  }
+  return best;
 }
 
 lamb_status_t check_head(const lamb_vocab* v, const void* hidden, int64_t hs,
@@ -709,7 +764,7 @@ int lm_head_setup() {
 
 void lm_head_carve(lamb_vocab* v, LmArena* a) {
   const int64_t n = v->max_tokens, pitch = lm_round_up(v->width, 64);
-  const int64_t whole = lm_round_up(n, kTileM);
+  const int64_t whole = lm_round_up(n, kRowsWhole);
   a->take(&v->rows, whole * pitch);
   a->take(&v->row_label, n);
   a->take(&v->row_token, n);
@@ -798,12 +853,15 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
   st = head_loss(v, in, n, d_scale, token_loss, loss, stream);
   if (st != LAMB_OK) return st;
 
-  // pieces of the vocabulary, of equal widths in whole tiles
-  const int64_t whole = lm_round_up(n, kTileM);
-  const int64_t most = v->dlogits_elems / whole / kTileN * kTileN;
-  const int64_t pieces = lm_ceil_div(v->vocab, most);
-  const int64_t piece =
-      lm_round_up(lm_ceil_div(v->vocab, pieces), kTileN);
+  const bool pair = n >= kPairRows;
+  const int rows = pair ? kRowsWhole : kTileM;       // of a tile
+  const int rows_b = pair ? kRowsB<2> : kRowsB<1>;
+  const int64_t whole = lm_round_up(n, kRowsWhole);
+  const int m_tiles = (int)lm_ceil_div(n, rows);
+  const int d_tiles = (int)lm_ceil_div(v->width, kTileN);
+  const int units = pair ? v->sms / 2 : v->sms;
+  const int64_t piece = piece_width(v, n, rows, units);
+  const int64_t pieces = lm_ceil_div(v->vocab, piece);
 
   DlogitsParams d;
   GradsParams g;
@@ -815,14 +873,14 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
       lm_map(v->encode, &d.hidden, true, v->rows, whole, v->width, in.pitch,
              kTileM) &&
       lm_map(v->encode, &d.weight, true, in.weight, v->vocab, v->width,
-             in.weight_stride, kTileN) &&
+             in.weight_stride, rows_b) &&
       lm_map(v->encode, &d.out, true, v->dlogits, whole, piece, piece, 32) &&
       lm_map_blocks(v->encode, &g.hidden, true, v->rows, whole, in.pitch,
-                    in.pitch / 64, kTileN / 64) &&
+                    in.pitch / 64, rows_b / 64) &&
       (g.weight_blocks
            ? lm_map_blocks(v->encode, &g.weight, true, in.weight, v->vocab,
                            in.weight_stride, lm_ceil_div(v->width, 64),
-                           kTileN / 64)
+                           rows_b / 64)
            : lm_map(v->encode, &g.weight, true, in.weight, v->vocab, v->width,
                     in.weight_stride, kTileK)) &&
       lm_map(v->encode, &g.dl_rows, true, v->dlogits, whole, piece, piece,
@@ -832,7 +890,6 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
       (!g.weight_out || lm_map(v->encode, &g.out, true, grad_weight, v->vocab,
                                v->width, grad_weight_stride, 32));
   if (!ok) return lm_fail(LAMB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-  const int m_tiles = (int)(whole / kTileM);
   d.n_rows = v->n_rows;
   d.labels = v->row_label;
   d.lse2 = v->lse2;
@@ -841,8 +898,8 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
   d.vocab = (int)v->vocab;
   d.k_blocks = (int)lm_ceil_div(v->width, kTileK);
 
-  g.d_tiles = (int)lm_ceil_div(v->width, kTileN);
-  const int h_tiles = m_tiles * g.d_tiles;
+  g.d_tiles = d_tiles;
+  const int h_tiles = m_tiles * d_tiles;
   g.grad_weight = grad_weight;
   g.weight_stride = grad_weight_stride;
   g.grad_hidden = (__nv_bfloat16*)grad_hidden;
@@ -862,23 +919,23 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
       (uintptr_t)grad_hidden % 16 == 0 && grad_hidden_stride % 8 == 0;
   // dh of few tokens is few tiles over a long K: cut K so that every SM has one
   const int k_first = (int)lm_ceil_div(std::min(piece, v->vocab), kTileK);
-  g.splits = std::max(1, std::min(v->sms / h_tiles, k_first / kMinPartBlocks));
+  g.splits = std::max(1, std::min(units / h_tiles, k_first / kMinPartBlocks));
   g.slabs = pieces > 1 || g.splits > 1 ? v->slabs : nullptr;
   for (int64_t i = 0; i < pieces; ++i) {
     const int64_t v0 = i * piece, cols = std::min(piece, v->vocab - v0);
     d.v0 = g.v0 = (int)v0;
     d.v_tiles = (int)lm_ceil_div(cols, kTileN);
-    e = launch_gemm<DlogitsWork>(d, (int64_t)m_tiles * d.v_tiles, v->sms,
+    e = launch_gemm<DlogitsWork>(d, pair, (int64_t)m_tiles * d.v_tiles, v->sms,
                                  stream);
     if (e != cudaSuccess) return lm_cuda_fail(e, "logit gradient launch");
-    g.w_tiles = (int)lm_ceil_div(cols, kTileM) * g.d_tiles;
+    g.w_tiles = (int)lm_ceil_div(cols, rows) * d_tiles;
     g.k_piece = (int)lm_ceil_div(cols, kTileK);
     // the last piece may be short: fewer parts, the others' sums stay
     const int parts = std::min(g.splits, g.k_piece);
     GradsParams gi = g;
     gi.splits = parts;
     gi.add_slab = i > 0;
-    e = launch_gemm<GradsWork>(gi, g.w_tiles + (int64_t)h_tiles * parts,
+    e = launch_gemm<GradsWork>(gi, pair, g.w_tiles + (int64_t)h_tiles * parts,
                                v->sms, stream);
     if (e != cudaSuccess) return lm_cuda_fail(e, "head gradient launch");
   }
