@@ -541,46 +541,22 @@ def lamb_vocab_create(vocab, width, max_tokens, device=0) -> int:
     return out.value
 
 
-def lamb_vocab_embed(plan, table, table_dtype, table_stride, ids, n_tokens,
-                     scale, out, out_dtype, out_stride, stream=0) -> None:
-    st = load().lamb_vocab_embed(plan, table, table_dtype, table_stride, ids,
-                                 n_tokens, scale, out, out_dtype, out_stride,
-                                 stream)
-    if st:
-        _check(st)
+def _entry(name):
+    """The C entry point `name` with its status checked: the arguments go to it
+    as they are given (addresses and streams as ints, None or 0 for NULL).  For
+    calls whose latency counts."""
+    def call(*args):
+        st = getattr(_lib or load(), name)(*args)
+        if st:
+            _check(st)
+    call.__name__ = name
+    return call
 
 
-def lamb_vocab_embed_grad(plan, grad_out, grad_dtype, grad_stride, ids,
-                          n_tokens, scale, table_grad, table_dtype,
-                          table_stride, accumulate, stream=0) -> None:
-    st = load().lamb_vocab_embed_grad(plan, grad_out, grad_dtype, grad_stride,
-                                      ids, n_tokens, scale, table_grad,
-                                      table_dtype, table_stride, accumulate,
-                                      stream)
-    if st:
-        _check(st)
-
-
-def lamb_vocab_loss(plan, hidden, hidden_stride, weight, weight_stride, labels,
-                    n_tokens, token_loss, loss, stream=0) -> None:
-    st = load().lamb_vocab_loss(plan, hidden, hidden_stride, weight,
-                                weight_stride, labels, n_tokens, token_loss,
-                                loss, stream)
-    if st:
-        _check(st)
-
-
-def lamb_vocab_loss_grad(plan, hidden, hidden_stride, weight, weight_stride,
-                         labels, n_tokens, d_scale, token_loss, loss,
-                         grad_hidden, grad_hidden_stride, grad_weight,
-                         grad_weight_dtype, grad_weight_stride, accumulate,
-                         stream=0) -> None:
-    st = load().lamb_vocab_loss_grad(
-        plan, hidden, hidden_stride, weight, weight_stride, labels, n_tokens,
-        d_scale, token_loss, loss, grad_hidden, grad_hidden_stride,
-        grad_weight, grad_weight_dtype, grad_weight_stride, accumulate, stream)
-    if st:
-        _check(st)
+lamb_vocab_embed = _entry("lamb_vocab_embed")
+lamb_vocab_embed_grad = _entry("lamb_vocab_embed_grad")
+lamb_vocab_loss = _entry("lamb_vocab_loss")
+lamb_vocab_loss_grad = _entry("lamb_vocab_loss_grad")
 
 
 def lamb_vocab_query(plan, clear=False, stream=0) -> int:

@@ -34,8 +34,7 @@ constexpr int kSortTiles = 128;        // at most: each reads all tiles' counts
 constexpr int kChunk = 32;             // sorted positions
 constexpr int kClearRows = 64;         // rows of the table a clearing CTA looks at
 constexpr int kJoinThreads = 256;
-constexpr int kJoinParts = 4;          // threads that share a long join's columns
-constexpr int kJoinLong = 16;          // chunks of a long join
+constexpr int kJoinChunks = 8;         // chunks a joining CTA looks at
 constexpr uint32_t kStatusBadIndex = LAMB_STATUS_BAD_INDEX;
 
 __device__ __forceinline__ float load1(const float* p) { return *p; }
@@ -109,8 +108,7 @@ __device__ __forceinline__ uint32_t key_of(int64_t id, int64_t vocab,
 // moves count in.  A tile is kSortWarps runs of 32 * rounds keys, a warp's each.
 __global__ void __launch_bounds__(kSortThreads)
 digit_count_kernel(const int64_t* ids, int n, int64_t vocab, int rounds,
-                   int passes, int32_t* hist, uint32_t* seen,
-                   uint32_t* status) {
+                   int passes, int32_t* hist, uint32_t* status) {
   __shared__ int32_t count[256];
   let_next_launch();
   if (threadIdx.x < 256) count[threadIdx.x] = 0;
@@ -119,10 +117,6 @@ digit_count_kernel(const int64_t* ids, int n, int64_t vocab, int rounds,
   const int64_t base = (int64_t)blockIdx.x * tile;
   for (int i = threadIdx.x; i < tile && base + i < n; i += kSortThreads)
     atomicAdd(&count[key_of(ids[base + i], vocab, status) & 255u], 1);
-  const int64_t words = (vocab + 31) / 32;
-  for (int64_t w = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; w < words;
-       w += (int64_t)gridDim.x * kSortThreads)
-    seen[w] = 0;
   __syncthreads();
   for (int i = threadIdx.x; i < 256 * passes; i += kSortThreads)
     hist[((int64_t)(i >> 8) * kSortTiles + blockIdx.x) * 256 + (i & 255)] =
@@ -135,7 +129,7 @@ __global__ void __launch_bounds__(kSortThreads)
 digit_move_kernel(const int64_t* ids, const uint32_t* keys, const int32_t* pos,
                   int n, int64_t vocab, int rounds, int shift,
                   const int32_t* hist, int32_t* next_hist, uint32_t* keys_out,
-                  int32_t* pos_out, uint32_t* seen, uint32_t* status) {
+                  int32_t* pos_out, uint32_t* status) {
   __shared__ int32_t count[kSortWarps][256];
   __shared__ int32_t half[2][2][256];      // [half][before the tile, in all]
   __shared__ int32_t scan[256];
@@ -212,12 +206,6 @@ digit_move_kernel(const int64_t* ids, const uint32_t* keys, const int32_t* pos,
     if (in) {
       keys_out[to] = key;
       pos_out[to] = pos ? pos[at] : (int32_t)at;
-      // (a mask token's thousands would queue up at its word: look first)
-      if (ids && key < (uint32_t)vocab) {
-        const uint32_t bit = 1u << (key & 31);
-        if (!(ld_relaxed_u32(&seen[key >> 5]) & bit))
-          atomicOr(&seen[key >> 5], bit);
-      }
     }
     if (next_hist) {      // one addition for a warp's equal places
       const int where =
@@ -225,6 +213,94 @@ digit_move_kernel(const int64_t* ids, const uint32_t* keys, const int32_t* pos,
       const uint32_t m = __match_any_sync(0xffffffffu, where);
       if (in && (m & ((1u << lane) - 1u)) == 0)
         atomicAdd(&next_hist[where], __popc(m));
+    }
+  }
+}
+
+// All passes for up to kSmallSort keys in one CTA: a warp's keys are consecutive,
+// kSmallItems a lane.
+constexpr int kSmallThreads = 512, kSmallItems = 8;
+constexpr int kSmallSort = kSmallThreads * kSmallItems;
+
+__global__ void __launch_bounds__(kSmallThreads)
+sort_small_kernel(const int64_t* ids, int n, int64_t vocab, int passes,
+                  uint32_t* keys_out, int32_t* pos_out, uint32_t* status) {
+  constexpr int kWarps = kSmallThreads / 32;
+  __shared__ uint32_t sm_key[kSmallSort];
+  __shared__ uint16_t sm_pos[kSmallSort];
+  __shared__ uint16_t count[kWarps][256];
+  __shared__ int scan[256];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t past = 0xffffffffu;        // sorts behind every key
+  let_next_launch();
+  uint32_t key[kSmallItems], pos[kSmallItems];
+#pragma unroll
+  for (int i = 0; i < kSmallItems; ++i) {
+    const int at = (warp * kSmallItems + i) * 32 + lane;
+    key[i] = at < n ? key_of(ids[at], vocab, status) : past;
+    pos[i] = at;
+  }
+  for (int p = 0; p < passes; ++p) {
+    const int shift = 8 * p;
+    for (int i = threadIdx.x; i < kWarps * 256; i += kSmallThreads)
+      count[i >> 8][i & 255] = 0;
+    __syncthreads();
+    int rank[kSmallItems];
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+      const uint32_t digit = (key[i] >> shift) & 255u;
+      const uint32_t same = __match_any_sync(0xffffffffu, digit);
+      const int before = __popc(same & ((1u << lane) - 1u));
+      rank[i] = count[warp][digit] + before;
+      __syncwarp();
+      if (before == 0) count[warp][digit] += (uint16_t)__popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    int total = 0, s = 0;
+    if (threadIdx.x < 256) {
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) total += count[w][threadIdx.x];
+      s = total;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += y;
+      }
+      scan[threadIdx.x] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x < 256) {
+      int at = s - total;
+      for (int w = 0; w < warp; ++w) at += scan[w * 32 + 31];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const int c = count[w][threadIdx.x];
+        count[w][threadIdx.x] = (uint16_t)at;
+        at += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+      const int to = count[warp][(key[i] >> shift) & 255u] + rank[i];
+      sm_key[to] = key[i];
+      sm_pos[to] = (uint16_t)pos[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+      const int at = (warp * kSmallItems + i) * 32 + lane;
+      key[i] = sm_key[at];
+      pos[i] = sm_pos[at];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSmallItems; ++i) {
+    const int at = (warp * kSmallItems + i) * 32 + lane;
+    if (at < n) {
+      keys_out[at] = key[i];
+      pos_out[at] = (int32_t)pos[i];
     }
   }
 }
@@ -316,9 +392,8 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
                   const uint32_t* __restrict__ keys,
                   const int32_t* __restrict__ pos, int n, int64_t vocab,
                   int width, int tx, int chunk_ctas,
-                  const uint32_t* __restrict__ seen, float* __restrict__ part,
-                  float scale, bool add, TT* __restrict__ out,
-                  int64_t out_stride) {
+                  float* __restrict__ part, float scale, bool add,
+                  TT* __restrict__ out, int64_t out_stride) {
   typedef Raw<TG, kVec> R;
   constexpr int kN = R::kN;
   __shared__ uint32_t sh_key[kEmbedThreads / kLeastTx * kChunk + 2];
@@ -327,9 +402,19 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
   after_prior_launch();
   if ((int)blockIdx.x >= chunk_ctas) {
     const int64_t v0 = (int64_t)(blockIdx.x - chunk_ctas) * kClearRows;
+    if (threadIdx.x < kClearRows) {     // is the word in the sorted list?
+      const uint32_t v = (uint32_t)(v0 + threadIdx.x);
+      int lo = 0, hi = n;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (keys[mid] < v) lo = mid + 1; else hi = mid;
+      }
+      sh_key[threadIdx.x] = lo < n && keys[lo] == v;
+    }
+    __syncthreads();
     for (int r = threadIdx.x >> 5; r < kClearRows; r += kEmbedThreads / 32) {
       const int64_t v = v0 + r;
-      if (v >= vocab || (n && (seen[v >> 5] >> (v & 31) & 1u))) continue;
+      if (v >= vocab || sh_key[r]) continue;
       TT* dst = out + v * out_stride;
       float zero[kN] = {};
       for (int d = (threadIdx.x & 31) * kN; d < width; d += 32 * kN)
@@ -390,66 +475,62 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
   }
 }
 
-// The words that go on past the chunk they begin in: the CTA of that chunk adds
-// the chunks' sums: in their order or, of a long word, in kJoinParts runs that are
-// added in order.
+// The words that go on past the chunk they begin in: a CTA looks at kJoinChunks
+// chunks and adds, for each such word, the chunks' sums in their order.
 template <class TT, bool kVec>
-__global__ void __launch_bounds__(kJoinThreads, 6)
+__global__ void __launch_bounds__(kJoinThreads)
 embed_join_kernel(const uint32_t* __restrict__ keys, int n, int64_t vocab,
                   int width, const float* __restrict__ part, float scale,
                   bool add, TT* __restrict__ out, int64_t out_stride) {
-  __shared__ float4 sh[kJoinThreads];
+  __shared__ uint32_t word[kJoinChunks];
   after_prior_launch();
-  const int c = blockIdx.x;
-  const int64_t first = (int64_t)c * kChunk, last = first + kChunk - 1;
-  if (last + 1 >= n) return;
-  const uint32_t v = keys[last], after = keys[last + 1], head = keys[first];
-  const uint32_t before = keys[first > 0 ? first - 1 : 0];
-  if (v >= (uint32_t)vocab || after != v) return;
-  if (first > 0 && head == v && before == v) return;
-  // the last chunk with the word: doubling steps, then halving ones
   const int chunks = (n + kChunk - 1) / kChunk;
-  int lo = c + 1, step = 1;
-  while (lo + step < chunks && keys[(int64_t)(lo + step) * kChunk] == v) {
-    lo += step;
-    step <<= 1;
+  if (threadIdx.x < kJoinChunks) {
+    const int c = blockIdx.x * kJoinChunks + threadIdx.x;
+    const int64_t first = (int64_t)c * kChunk, last = first + kChunk - 1;
+    uint32_t w = 0xffffffffu;
+    if (last + 1 < n) {
+      const uint32_t v = keys[last], after = keys[last + 1];
+      const uint32_t head = keys[first];
+      const uint32_t before = keys[first > 0 ? first - 1 : 0];
+      if (v < (uint32_t)vocab && after == v &&
+          !(first > 0 && head == v && before == v))
+        w = v;
+    }
+    word[threadIdx.x] = w;
   }
-  for (; step > 0; step >>= 1)
-    if (lo + step < chunks && keys[(int64_t)(lo + step) * kChunk] == v)
-      lo += step;
-  const int count = lo - c;               // chunks after this one
-  const int parts = count > kJoinLong ? kJoinParts : 1;
-  const int wide = kJoinThreads / parts;
-  const int g = threadIdx.x / wide, x = threadIdx.x % wide;
-  const int a = (int)((int64_t)count * g / parts);
-  const int b = (int)((int64_t)count * (g + 1) / parts);
-  TT* dst = out + (int64_t)v * out_stride;
-  for (int d0 = 0; d0 < width; d0 += wide * 4) {
-    const int d = d0 + x * 4;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    if (d < width) {
-      if (g == 0)
-        load_row<float, 4, kVec>(part + ((int64_t)c * 2 + 1) * width, d, width, s);
-#pragma unroll 8
-      for (int k = a; k < b; ++k) {
+  __syncthreads();
+  for (int q = 0; q < kJoinChunks; ++q) {
+    const uint32_t v = word[q];
+    if (v == 0xffffffffu) continue;
+    const int c = blockIdx.x * kJoinChunks + q;
+    // how many chunks after this one begin with the word: all threads look, in
+    // steps that get shorter
+    int count = 1, step = (chunks - c + kJoinThreads - 1) / kJoinThreads;
+    for (;;) {
+      const int64_t at = c + count + (int64_t)threadIdx.x * step;
+      const int with = __syncthreads_count(
+          at < chunks && keys[at * kChunk] == v);
+      if (with > 0) count += (with - 1) * step + 1;
+      if (step == 1) break;
+      step = (step + kJoinThreads - 1) / kJoinThreads;
+    }
+    // (the steps' own finds: count is one past the last chunk that was seen)
+    count -= 1;
+    TT* dst = out + (int64_t)v * out_stride;
+    for (int d = threadIdx.x * 4; d < width; d += kJoinThreads * 4) {
+      float s[4];
+      load_row<float, 4, kVec>(part + ((int64_t)c * 2 + 1) * width, d, width, s);
+#pragma unroll 16
+      for (int k = 1; k <= count; ++k) {
         float y[4];
-        load_row<float, 4, kVec>(part + (int64_t)(c + 1 + k) * 2 * width, d, width,
-                              y);
+        load_row<float, 4, kVec>(part + (int64_t)(c + k) * 2 * width, d, width,
+                                 y);
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] += y[j];
       }
-    }
-    if (parts > 1) {
-      sh[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
-      __syncthreads();
-      for (int k = 1; g == 0 && k < parts; ++k) {
-        const float4 y = sh[k * wide + x];
-        s[0] += y.x; s[1] += y.y; s[2] += y.z; s[3] += y.w;
-      }
-    }
-    if (g == 0 && d < width)
       write_row<TT, 4, kVec>(dst, d, width, s, scale, add);
-    if (parts > 1) __syncthreads();
+    }
   }
 }
 
@@ -488,10 +569,10 @@ cudaError_t launch_sums(const lamb_vocab* v, const void* grad, int64_t gs,
   cudaError_t e = lm_launch(
       embed_sums_kernel<TG, TT, kVec>, (unsigned)(ctas + clears), kEmbedThreads,
       0, stream, n > 0, (const TG*)grad, gs, v->keys[in], v->pos[in], n,
-      v->vocab, v->width, tx, ctas, v->seen, v->part, scale, add, (TT*)out, os);
+      v->vocab, v->width, tx, ctas, v->part, scale, add, (TT*)out, os);
   if (e == cudaSuccess && chunks > 1)
-    e = lm_launch(embed_join_kernel<TT, kVec>, (unsigned)(chunks - 1),
-                  kJoinThreads, 0, stream, true, v->keys[in], n, v->vocab,
+    e = lm_launch(embed_join_kernel<TT, kVec>,
+                  (unsigned)lm_ceil_div(chunks - 1, kJoinChunks), kJoinThreads, 0, stream, true, v->keys[in], n, v->vocab,
                   v->width, v->part, scale, add, (TT*)out, os);
   return e;
 }
@@ -543,7 +624,6 @@ void lm_embed_carve(lamb_vocab* v, LmArena* a) {
     a->take(&v->pos[i], n);
   }
   a->take(&v->hist, (int64_t)v->sort_passes * kSortTiles * 256);
-  a->take(&v->seen, lm_ceil_div(v->vocab, 32));
   a->take(&v->part, lm_ceil_div(n, kChunk) * 2 * v->width);
 }
 
@@ -604,17 +684,22 @@ extern "C" lamb_status_t lamb_vocab_embed_grad(
   const unsigned tiles = (unsigned)lm_ceil_div(n, kSortThreads * rounds);
   cudaError_t e = cudaSuccess;
   int in = 0;
-  if (n)
+  // (4095 tokens: 31 us with a launch a pass, 26 with one in all)
+  const bool small = n <= kSmallSort;
+  if (n && small)
+    e = lm_launch(sort_small_kernel, 1, kSmallThreads, 0, stream, false, ids, n,
+                  v->vocab, v->sort_passes, v->keys[0], v->pos[0], v->status);
+  if (n && !small)
     e = lm_launch(digit_count_kernel, tiles, kSortThreads, 0, stream, false,
-                  ids, n, v->vocab, rounds, v->sort_passes, v->hist, v->seen,
-                  v->status);
-  for (int pass = 0; e == cudaSuccess && n && pass < v->sort_passes; ++pass) {
+                  ids, n, v->vocab, rounds, v->sort_passes, v->hist, v->status);
+  for (int pass = 0; e == cudaSuccess && !small && pass < v->sort_passes;
+       ++pass) {
     int32_t* hist = v->hist + (int64_t)pass * kSortTiles * 256;
     e = lm_launch(digit_move_kernel, tiles, kSortThreads, 0, stream, true,
                   pass ? nullptr : ids, v->keys[in], pass ? v->pos[in] : nullptr,
                   n, v->vocab, rounds, 8 * pass, hist,
                   pass + 1 < v->sort_passes ? hist + kSortTiles * 256 : nullptr,
-                  v->keys[in ^ 1], v->pos[in ^ 1], v->seen, v->status);
+                  v->keys[in ^ 1], v->pos[in ^ 1], v->status);
     in ^= 1;
   }
   if (e != cudaSuccess) return lm_cuda_fail(e, "sort launch");

@@ -75,11 +75,13 @@ struct Epilogue {
   uint32_t out;          // the warp's staging memory
   int n;                 // blocks that went through it
 
-  // A block of the warp's 32 rows and 64 columns of 16 bits, w the thread's row:
-  // out by a tensor copy to (x, y), which clips it at the matrix' edges.  Direct
-  // stores, a row a thread, take a 16-byte piece of 32 lines each.
+  // A block of the warp's 32 rows and 128 bytes of columns, w the thread's row:
+  // out by a tensor copy to (x, y), which clips it at the matrix' edges, or added
+  // to what is there (fp32).  Direct stores, a row a thread, take a 16-byte piece
+  // of 32 lines each.
   __device__ __forceinline__ void store_block(const CUtensorMap* map, int x,
-                                              int y, const uint32_t (&w)[32]) {
+                                              int y, const uint32_t (&w)[32],
+                                              bool add = false) {
     const int r = row & 31;
     const uint32_t at = out + (n & 1) * kOutBytes;
     if (r == 0) stores_have_read<kOutBuffers - 1>();
@@ -91,7 +93,8 @@ struct Epilogue {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (r == 0) {
-      tile_store(map, x, y, at);
+      if (add) tile_add(map, x, y, at);
+      else tile_store(map, x, y, at);
       stores_commit();
     }
     ++n;

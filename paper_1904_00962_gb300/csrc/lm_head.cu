@@ -229,11 +229,19 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
   float top = -INFINITY, sum = 0.f;
   if (r < rows) {
     const int a = v_tiles * part / 8, b = v_tiles * (part + 1) / 8;
-    for (int k = a; k < b; ++k) {
-      const float2 s = stats[(int64_t)k * stride + r];
-      const float m = fmaxf(top, s.x);
+    for (int k0 = a; k0 < b; k0 += 16) {      // sixteen on their way
+      float2 s[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u)
+        s[u] = k0 + u < b ? stats[(int64_t)(k0 + u) * stride + r]
+                          : make_float2(-INFINITY, 0.f);
+      float m = top;
+#pragma unroll
+      for (int u = 0; u < 16; ++u) m = fmaxf(m, s[u].x);
       const float at = m == -INFINITY ? 0.f : m;
-      sum = sum * exp2_fast(top - at) + s.y * exp2_fast(s.x - at);
+      sum *= exp2_fast(top - at);
+#pragma unroll
+      for (int u = 0; u < 16; ++u) sum += s[u].y * exp2_fast(s[u].x - at);
       top = m;
     }
   }
@@ -368,14 +376,14 @@ struct GradsParams {
   CUtensorMap hidden;     // MN-major
   CUtensorMap weight;     // MN-major
   CUtensorMap out;        // grad_weight, where weight_out
+  CUtensorMap slabs;      // [split][rows in whole tiles][width], fp32
   void* grad_weight;
   __nv_bfloat16* grad_hidden;
-  float* slabs;           // [split][rows][width], or NULL: one sum, written out
   const int32_t* n_rows;
   const int32_t* row_token;
   uint32_t* status;
   int64_t weight_stride, hidden_stride;
-  int64_t slab;           // elements of a slab
+  int slab_rows;          // of a slab; 0: one sum, written out
   int w_tiles;            // tiles of dW (taken first)
   int d_tiles;            // column tiles of the width
   int width, vocab, v0, piece;
@@ -515,6 +523,20 @@ struct GradsWork {
       }
       return;
     }
+    if (g.what == 1 && p.slab_rows) {
+      const int y = g.aux * p.slab_rows + g.a0 + (epi.row & ~31);
+      for (int c = 0; c < kTileN / 32; ++c) {
+        const int d = g.b0 + c * 32;
+        if (d >= p.width) break;
+        float x[32];
+        tmem_ld32(acc + c * 32, x);
+        uint32_t w[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(x[i]);
+        epi.store_block(&p.slabs, d, y, w, p.add_slab);
+      }
+      return;
+    }
     for (int c = 0; c < kTileN / 32; ++c) {
       const int d = g.b0 + c * 32;
       if (d >= p.width) break;
@@ -526,14 +548,10 @@ struct GradsWork {
         const int64_t at = (int64_t)(p.v0 + r) * p.weight_stride + d;
         if (p.weight_f32)
           store_row<true>(p.grad_weight, at, x, cols, p.accumulate,
-                           p.weight_vec);
+                          p.weight_vec);
         else
           store_row<false>(p.grad_weight, at, x, cols, p.accumulate,
                            p.weight_vec);
-      } else if (p.slabs) {
-        store_row<true>(p.slabs,
-                        g.aux * p.slab + (int64_t)r * p.width + d, x, cols,
-                        p.add_slab, p.width % 4 == 0);
       } else {
         store_row<false>(p.grad_hidden,
                          (int64_t)p.row_token[r] * p.hidden_stride + d, x,
@@ -546,7 +564,7 @@ struct GradsWork {
 // dh from its partial sums, kCols columns a thread.
 template <int kCols>
 __global__ void __launch_bounds__(256)
-slabs_kernel(const float* slabs, int count, int64_t slab, int width,
+slabs_kernel(const float* slabs, int count, int64_t slab, int pitch, int width,
              const int32_t* n_rows, const int32_t* row_token,
              __nv_bfloat16* out, int64_t stride) {
   after_prior_launch();
@@ -555,11 +573,11 @@ slabs_kernel(const float* slabs, int count, int64_t slab, int width,
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
        i += (int64_t)gridDim.x * 256) {
     const int r = (int)(i / per), d = (int)(i - (int64_t)r * per) * kCols;
-    const float* from = slabs + (int64_t)r * width + d;
+    const float* from = slabs + (int64_t)r * pitch + d;
     __nv_bfloat16* to = out + (int64_t)row_token[r] * stride + d;
     if (kCols == 4) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
+#pragma unroll 16
       for (int k = 0; k < count; ++k) {
         const float4 v = *reinterpret_cast<const float4*>(from + k * slab);
         s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -780,7 +798,7 @@ void lm_head_carve(lamb_vocab* v, LmArena* a) {
                               std::max(kPieceElems, whole * (int64_t)kTileN));
   a->take(&v->dlogits, v->dlogits_elems);
   // parts of dh never have more tiles than there are SMs, unless it is one part
-  a->take(&v->slabs, std::max(n * v->width,
+  a->take(&v->slabs, std::max(whole * lm_round_up(v->width, 4),
                               (int64_t)v->sms * kTileM * kTileN));
   a->take(&v->weight_copy, v->vocab * pitch);
 }
@@ -907,7 +925,6 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
   g.status = v->status;
   g.n_rows = v->n_rows;
   g.row_token = v->row_token;
-  g.slab = n * v->width;
   g.width = v->width;
   g.vocab = (int)v->vocab;
   g.piece = (int)piece;
@@ -920,7 +937,12 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
   // dh of few tokens is few tiles over a long K: cut K so that every SM has one
   const int k_first = (int)lm_ceil_div(std::min(piece, v->vocab), kTileK);
   g.splits = std::max(1, std::min(units / h_tiles, k_first / kMinPartBlocks));
-  g.slabs = pieces > 1 || g.splits > 1 ? v->slabs : nullptr;
+  g.slab_rows = pieces > 1 || g.splits > 1 ? m_tiles * rows : 0;
+  const int pitch = (int)lm_round_up(v->width, 4);
+  if (g.slab_rows &&
+      !lm_map_f32(v->encode, &g.slabs, v->slabs,
+                  (int64_t)g.splits * g.slab_rows, v->width, pitch, 32))
+    return lm_fail(LAMB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   for (int64_t i = 0; i < pieces; ++i) {
     const int64_t v0 = i * piece, cols = std::min(piece, v->vocab - v0);
     d.v0 = g.v0 = (int)v0;
@@ -939,14 +961,15 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
                                v->sms, stream);
     if (e != cudaSuccess) return lm_cuda_fail(e, "head gradient launch");
   }
-  if (g.slabs) {
-    const bool four = v->width % 4 == 0 && g.slab % 4 == 0 &&
+  if (g.slab_rows) {
+    const bool four = v->width % 4 == 0 &&
                       (uintptr_t)grad_hidden % 8 == 0 &&
                       grad_hidden_stride % 4 == 0;
     const int per = v->width / (four ? 4 : 1);
     e = lm_launch(four ? slabs_kernel<4> : slabs_kernel<1>,
                   (unsigned)grid_for(n * per, v->sms), 256, 0, stream, true,
-                  v->slabs, g.splits, g.slab, v->width, v->n_rows, v->row_token,
+                  v->slabs, g.splits, (int64_t)g.slab_rows * pitch, pitch,
+                  v->width, v->n_rows, v->row_token,
                   (__nv_bfloat16*)grad_hidden, grad_hidden_stride);
     if (e != cudaSuccess) return lm_cuda_fail(e, "hidden gradient launch");
   }

@@ -119,6 +119,22 @@ inline bool lm_map(EncodeTiled encode, CUtensorMap* map, bool bf16,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// An fp32 matrix in boxes of 32 columns (128-byte swizzle) by box_rows lines; the
+// row stride a multiple of 4.
+inline bool lm_map_f32(EncodeTiled encode, CUtensorMap* map, const void* base,
+                       int64_t rows, int64_t cols, int64_t row_stride,
+                       int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)row_stride * 4};
+  const cuuint32_t box[2] = {32, (cuuint32_t)box_rows};
+  const cuuint32_t step[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2,
+                const_cast<void*>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // A matrix of `blocks` times 64 columns in boxes of 64 lines by box_blocks blocks,
 // which arrive block after block (an MN-major operand).  Whole blocks are copied:
 // the rows have to have that many elements, whatever the last ones are.

@@ -258,6 +258,7 @@ __device__ __forceinline__ void small_gram(const float* in, int pitch, int m,
       rj[q] = in + min(j0 + q, m - 1) * pitch;
     }
     float acc[4][4] = {};
+#pragma unroll 4
     for (int k = s; k < n; k += S) {
       float x[4], y[4];
 #pragma unroll
@@ -346,6 +347,7 @@ muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
     for (int t = threadIdx.x; t < tasks; t += kSmallThreads) {
       const int i0 = t / n * 8, j = t % n;
       float acc[8] = {};
+#pragma unroll 8
       for (int q = 0; q < m; ++q) {
         const float v = X[q * np + j];
         const float4* h = reinterpret_cast<const float4*>(H + q * mp + i0);

@@ -95,6 +95,15 @@ __device__ __forceinline__ void tile_store(const CUtensorMap* map, int x, int y,
       ::"l"(map), "r"(x), "r"(y), "r"(smem)
       : "memory");
 }
+// The same, added to what is there (fp32).
+__device__ __forceinline__ void tile_add(const CUtensorMap* map, int x, int y,
+                                         uint32_t smem) {
+  asm volatile(
+      "cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group "
+      "[%0, {%1, %2}], [%3];"
+      ::"l"(map), "r"(x), "r"(y), "r"(smem)
+      : "memory");
+}
 __device__ __forceinline__ void stores_commit() {
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }

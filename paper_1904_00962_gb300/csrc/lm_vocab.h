@@ -18,7 +18,6 @@ struct lamb_vocab {
   uint32_t* keys[2] = {nullptr, nullptr};
   int32_t* pos[2] = {nullptr, nullptr};
   int32_t* hist = nullptr;      // [pass][tile][256]
-  uint32_t* seen = nullptr;     // a bit for each word that has a token
   float* part = nullptr;        // [chunks][2][width]
 
   // head: the rows that have a label, and what is known of each

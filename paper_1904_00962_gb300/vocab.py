@@ -10,11 +10,9 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
-from .state import _stream
 
-_CODES = {torch.float32: B.LAMB_F32, torch.bfloat16: B.LAMB_BF16}
-_BF16 = (torch.bfloat16,)
-_BOTH = (torch.float32, torch.bfloat16)
+_BF16 = {torch.bfloat16: B.LAMB_BF16}
+_BOTH = {torch.float32: B.LAMB_F32, torch.bfloat16: B.LAMB_BF16}
 
 
 class VocabPlan:
@@ -32,28 +30,38 @@ class VocabPlan:
     # -- checks ---------------------------------------------------------------
     def _matrix(self, name, t, rows, dtypes):
         """(address, dtype code, row stride) of a [rows, width] tensor."""
-        if t.dtype not in dtypes:
-            raise ValueError(f"{name}: {t.dtype} is not one of {dtypes}")
-        if t.shape != (rows, self.width):
+        code = dtypes.get(t.dtype)
+        if code is None:
+            raise ValueError(f"{name}: {t.dtype} is not one of "
+                             f"{list(dtypes)}")
+        width = self.width
+        if t.shape != (rows, width):
             raise ValueError(f"{name}: shape {tuple(t.shape)} is not "
-                             f"({rows}, {self.width})")
-        stride = t.stride(0) if rows > 1 else max(t.stride(0), self.width)
-        if (self.width > 1 and t.stride(1) != 1) or stride < self.width:
+                             f"({rows}, {width})")
+        stride, step = t.stride()
+        if rows <= 1:
+            stride = max(stride, width)
+        if (width > 1 and step != 1) or stride < width:
             raise ValueError(f"{name}: rows have to be contiguous")
-        self._on_device(name, t)
-        return t.data_ptr(), _CODES[t.dtype], stride
+        if t.get_device() != self._index:
+            raise ValueError(f"{name} is not on {self.device}")
+        return t.data_ptr(), code, stride
 
     def _vector(self, name, t, n, dtype):
         if t.dtype != dtype or t.shape != (n,) or \
                 (n > 1 and t.stride(0) != 1):
             raise ValueError(f"{name}: a contiguous {dtype} tensor of {n} "
                              f"elements is needed")
-        self._on_device(name, t)
+        if t.get_device() != self._index:
+            raise ValueError(f"{name} is not on {self.device}")
         return t.data_ptr()
 
-    def _on_device(self, name, t):
-        if not t.is_cuda or t.get_device() != self._index:
-            raise ValueError(f"{name} is not on {self.device}")
+    def _stream(self, stream):
+        """A raw stream handle: PyTorch's current one of the plan's device, or
+        the given one."""
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self._index)
+        return stream if isinstance(stream, int) else stream.cuda_stream
 
     def _tokens(self, name, t):
         if t.dim() != 1:
@@ -72,7 +80,7 @@ class VocabPlan:
         B.lamb_vocab_embed(
             self.handle, *self._matrix("table", table, self.vocab, _BOTH),
             self._vector("ids", ids, n, torch.int64), n, scale,
-            *self._matrix("out", out, n, _BOTH), _stream(stream))
+            *self._matrix("out", out, n, _BOTH), self._stream(stream))
         return out
 
     def embed_grad(self, grad_out, ids, table_grad, *, scale=1.0,
@@ -84,7 +92,7 @@ class VocabPlan:
             self.handle, *self._matrix("grad_out", grad_out, n, _BOTH),
             self._vector("ids", ids, n, torch.int64), n, scale,
             *self._matrix("table_grad", table_grad, self.vocab, _BOTH),
-            int(accumulate), _stream(stream))
+            int(accumulate), self._stream(stream))
         return table_grad
 
     # -- vocabulary head --------------------------------------------------------
@@ -106,7 +114,7 @@ class VocabPlan:
         hidden @ weight.T against the labels; labels below 0 do not count."""
         _, loss, ins, outs = self._head(hidden, weight, labels, token_loss,
                                         loss)
-        B.lamb_vocab_loss(self.handle, *ins, *outs, _stream(stream))
+        B.lamb_vocab_loss(self.handle, *ins, *outs, self._stream(stream))
         return loss
 
     def loss_grad(self, hidden, weight, labels, grad_hidden, grad_weight, *,
@@ -123,12 +131,12 @@ class VocabPlan:
         sp = None if scale is None else \
             self._vector("scale", scale, 1, torch.float32)
         B.lamb_vocab_loss_grad(self.handle, *ins, sp, *outs, gh, ghs, gw, code,
-                               gws, int(accumulate), _stream(stream))
+                               gws, int(accumulate), self._stream(stream))
         return loss
 
     def query(self, clear=False, stream=None) -> int:
         """The plan's LAMB_STATUS_* bits (synchronises the stream)."""
-        return B.lamb_vocab_query(self.handle, clear, _stream(stream))
+        return B.lamb_vocab_query(self.handle, clear, self._stream(stream))
 
     def destroy(self):
         if self.handle:
