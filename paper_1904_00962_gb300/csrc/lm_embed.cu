@@ -8,8 +8,8 @@
 //
 // Gradient: the token positions are sorted by id (stable, least significant
 // digit first, 8 bits a pass), so that every word's rows are added in the order
-// of the tokens, the same in each run.  The sorted list is cut every kChunk
-// positions, whatever the words: ids are Zipf-like, most words have few tokens and
+// of the tokens, the same in each run.  The sorted list is cut every 32 to
+// 128 positions, whatever the words: ids are Zipf-like, most words have few tokens and
 // a mask token thousands.  A chunk writes the rows of the words that lie inside it
 // and leaves the sum of a word that goes on; one more launch adds those, in order.
 // Rows of words without a token are cleared by other CTAs of the same launch.
@@ -31,10 +31,13 @@ constexpr int kEmbedThreads = 256;
 constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortTiles = 128;        // at most: each reads all tiles' counts
-constexpr int kChunk = 32;             // sorted positions
+// Sorted positions of a chunk: short ones fill the SMs, long ones leave fewer sums
+// to join.  us at 4095 x 768 and 65536 x 1024 tokens: 32 positions 27 / 113, 64
+// positions 36 / 85, 128 positions - / 70.
+constexpr int kLeastChunk = 32;
+int chunk_of(int64_t n) { return n <= 8192 ? 32 : n <= 32768 ? 64 : 128; }
 constexpr int kClearRows = 64;         // rows of the table a clearing CTA looks at
-constexpr int kJoinThreads = 256;
-constexpr int kJoinChunks = 8;         // chunks a joining CTA looks at
+constexpr int kJoinThreads = 256, kJoinBatch = 8;
 constexpr uint32_t kStatusBadIndex = LAMB_STATUS_BAD_INDEX;
 
 __device__ __forceinline__ float load1(const float* p) { return *p; }
@@ -391,13 +394,12 @@ __global__ void __launch_bounds__(kEmbedThreads)
 embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
                   const uint32_t* __restrict__ keys,
                   const int32_t* __restrict__ pos, int n, int64_t vocab,
-                  int width, int tx, int chunk_ctas,
+                  int width, int chunk, int tx, int chunk_ctas,
                   float* __restrict__ part, float scale, bool add,
                   TT* __restrict__ out, int64_t out_stride) {
   typedef Raw<TG, kVec> R;
   constexpr int kN = R::kN;
-  __shared__ uint32_t sh_key[kEmbedThreads / kLeastTx * kChunk + 2];
-  __shared__ int32_t sh_pos[kEmbedThreads / kLeastTx * kChunk];
+  extern __shared__ uint32_t sh_key[];       // the CTA's keys and neighbours
   let_next_launch();
   after_prior_launch();
   if ((int)blockIdx.x >= chunk_ctas) {
@@ -423,8 +425,9 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
     return;
   }
   const int ty = kEmbedThreads / tx;
-  const int chunk0 = blockIdx.x * ty, first = chunk0 * kChunk;
-  const int held = min(ty * kChunk, n - first);
+  int32_t* const sh_pos = reinterpret_cast<int32_t*>(sh_key) + ty * chunk + 2;
+  const int chunk0 = blockIdx.x * ty, first = chunk0 * chunk;
+  const int held = min(ty * chunk, n - first);
   const int y = threadIdx.x / tx, x0 = threadIdx.x % tx;
   const uint32_t none = 0xffffffffu;
   for (int i = threadIdx.x; i < held; i += kEmbedThreads) {
@@ -436,8 +439,8 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
     sh_key[held + 1] = first + held < n ? keys[first + held] : none;
   }
   __syncthreads();
-  const int at0 = y * kChunk;                       // inside the CTA's keys
-  const int m = min(kChunk, held - at0);
+  const int at0 = y * chunk;                        // inside the CTA's keys
+  const int m = min(chunk, held - at0);
   if (m <= 0) return;
   float* const mine = part + (int64_t)(chunk0 + y) * 2 * width;
   const uint32_t* const key = sh_key + at0 + 1;     // -1 .. m: with neighbours
@@ -475,62 +478,52 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
   }
 }
 
-// The words that go on past the chunk they begin in: a CTA looks at kJoinChunks
-// chunks and adds, for each such word, the chunks' sums in their order.
+// The words that go on past the chunk they begin in: the CTA of that chunk adds
+// the chunks' sums in their order, kJoinBatch on their way at a time.
 template <class TT, bool kVec>
 __global__ void __launch_bounds__(kJoinThreads)
 embed_join_kernel(const uint32_t* __restrict__ keys, int n, int64_t vocab,
-                  int width, const float* __restrict__ part, float scale,
-                  bool add, TT* __restrict__ out, int64_t out_stride) {
-  __shared__ uint32_t word[kJoinChunks];
+                  int width, int chunk, const float* __restrict__ part,
+                  float scale, bool add, TT* __restrict__ out,
+                  int64_t out_stride) {
   after_prior_launch();
-  const int chunks = (n + kChunk - 1) / kChunk;
-  if (threadIdx.x < kJoinChunks) {
-    const int c = blockIdx.x * kJoinChunks + threadIdx.x;
-    const int64_t first = (int64_t)c * kChunk, last = first + kChunk - 1;
-    uint32_t w = 0xffffffffu;
-    if (last + 1 < n) {
-      const uint32_t v = keys[last], after = keys[last + 1];
-      const uint32_t head = keys[first];
-      const uint32_t before = keys[first > 0 ? first - 1 : 0];
-      if (v < (uint32_t)vocab && after == v &&
-          !(first > 0 && head == v && before == v))
-        w = v;
-    }
-    word[threadIdx.x] = w;
+  const int chunks = (n + chunk - 1) / chunk, c = blockIdx.x;
+  const int64_t first = (int64_t)c * chunk, last = first + chunk - 1;
+  if (last + 1 >= n) return;
+  const uint32_t v = keys[last], after = keys[last + 1], head = keys[first];
+  const uint32_t before = keys[first > 0 ? first - 1 : 0];
+  if (v >= (uint32_t)vocab || after != v) return;
+  if (first > 0 && head == v && before == v) return;
+  // how many chunks after this one begin with the word: all threads look, in
+  // steps that get shorter; count is one past the last that was seen
+  int count = 1, step = (chunks - c + kJoinThreads - 1) / kJoinThreads;
+  for (;;) {
+    const int64_t at = c + count + (int64_t)threadIdx.x * step;
+    const int with =
+        __syncthreads_count(at < chunks && keys[at * chunk] == v);
+    if (with > 0) count += (with - 1) * step + 1;
+    if (step == 1) break;
+    step = (step + kJoinThreads - 1) / kJoinThreads;
   }
-  __syncthreads();
-  for (int q = 0; q < kJoinChunks; ++q) {
-    const uint32_t v = word[q];
-    if (v == 0xffffffffu) continue;
-    const int c = blockIdx.x * kJoinChunks + q;
-    // how many chunks after this one begin with the word: all threads look, in
-    // steps that get shorter
-    int count = 1, step = (chunks - c + kJoinThreads - 1) / kJoinThreads;
-    for (;;) {
-      const int64_t at = c + count + (int64_t)threadIdx.x * step;
-      const int with = __syncthreads_count(
-          at < chunks && keys[at * kChunk] == v);
-      if (with > 0) count += (with - 1) * step + 1;
-      if (step == 1) break;
-      step = (step + kJoinThreads - 1) / kJoinThreads;
-    }
-    // (the steps' own finds: count is one past the last chunk that was seen)
-    count -= 1;
-    TT* dst = out + (int64_t)v * out_stride;
-    for (int d = threadIdx.x * 4; d < width; d += kJoinThreads * 4) {
-      float s[4];
-      load_row<float, 4, kVec>(part + ((int64_t)c * 2 + 1) * width, d, width, s);
-#pragma unroll 16
-      for (int k = 1; k <= count; ++k) {
-        float y[4];
-        load_row<float, 4, kVec>(part + (int64_t)(c + k) * 2 * width, d, width,
-                                 y);
+  TT* dst = out + (int64_t)v * out_stride;
+  for (int d = threadIdx.x * 4; d < width; d += kJoinThreads * 4) {
+    float s[4];
+    load_row<float, 4, kVec>(part + ((int64_t)c * 2 + 1) * width, d, width, s);
+    for (int k0 = 1; k0 < count; k0 += kJoinBatch) {
+      float y[kJoinBatch][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] += y[j];
+      for (int u = 0; u < kJoinBatch; ++u) {
+        y[u][0] = y[u][1] = y[u][2] = y[u][3] = 0.f;
+        if (k0 + u < count)
+          load_row<float, 4, kVec>(part + (int64_t)(c + k0 + u) * 2 * width, d,
+                                   width, y[u]);
       }
-      write_row<TT, 4, kVec>(dst, d, width, s, scale, add);
+#pragma unroll
+      for (int u = 0; u < kJoinBatch; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] += y[u][j];
     }
+    write_row<TT, 4, kVec>(dst, d, width, s, scale, add);
   }
 }
 
@@ -563,17 +556,20 @@ cudaError_t launch_sums(const lamb_vocab* v, const void* grad, int64_t gs,
   constexpr int kN = Raw<TG, kVec>::kN;
   int tx = kEmbedThreads;
   while (tx > kLeastTx && tx / 2 * kN >= v->width) tx /= 2;
-  const int chunks = (int)lm_ceil_div(n, kChunk);
-  const int ctas = (int)lm_ceil_div(chunks, kEmbedThreads / tx);
+  const int chunk = chunk_of(n), ty = kEmbedThreads / tx;
+  const int chunks = (int)lm_ceil_div(n, chunk);
+  const int ctas = (int)lm_ceil_div(chunks, ty);
+  const size_t smem =
+      std::max<size_t>(2 * (size_t)ty * chunk + 2, kClearRows) * 4;
   const int64_t clears = add ? 0 : lm_ceil_div(v->vocab, kClearRows);
   cudaError_t e = lm_launch(
       embed_sums_kernel<TG, TT, kVec>, (unsigned)(ctas + clears), kEmbedThreads,
-      0, stream, n > 0, (const TG*)grad, gs, v->keys[in], v->pos[in], n,
-      v->vocab, v->width, tx, ctas, v->part, scale, add, (TT*)out, os);
+      smem, stream, n > 0, (const TG*)grad, gs, v->keys[in], v->pos[in], n,
+      v->vocab, v->width, chunk, tx, ctas, v->part, scale, add, (TT*)out, os);
   if (e == cudaSuccess && chunks > 1)
-    e = lm_launch(embed_join_kernel<TT, kVec>,
-                  (unsigned)lm_ceil_div(chunks - 1, kJoinChunks), kJoinThreads, 0, stream, true, v->keys[in], n, v->vocab,
-                  v->width, v->part, scale, add, (TT*)out, os);
+    e = lm_launch(embed_join_kernel<TT, kVec>, (unsigned)(chunks - 1),
+                  kJoinThreads, 0, stream, true, v->keys[in], n, v->vocab,
+                  v->width, chunk, v->part, scale, add, (TT*)out, os);
   return e;
 }
 
@@ -624,7 +620,7 @@ void lm_embed_carve(lamb_vocab* v, LmArena* a) {
     a->take(&v->pos[i], n);
   }
   a->take(&v->hist, (int64_t)v->sort_passes * kSortTiles * 256);
-  a->take(&v->part, lm_ceil_div(n, kChunk) * 2 * v->width);
+  a->take(&v->part, lm_ceil_div(n, kLeastChunk) * 2 * v->width);
 }
 
 }  // namespace lamb
