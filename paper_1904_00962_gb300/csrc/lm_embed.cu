@@ -222,7 +222,7 @@ digit_move_kernel(const int64_t* ids, const uint32_t* keys, const int32_t* pos,
 
 // All passes for up to kSmallSort keys in one CTA: a warp's keys are consecutive,
 // kSmallItems a lane.
-constexpr int kSmallThreads = 512, kSmallItems = 8;
+constexpr int kSmallThreads = 1024, kSmallItems = 4;
 constexpr int kSmallSort = kSmallThreads * kSmallItems;
 
 __global__ void __launch_bounds__(kSmallThreads)

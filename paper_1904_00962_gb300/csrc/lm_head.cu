@@ -12,7 +12,9 @@
 //
 // The loss is one product on the tensor cores (lm_gemm.cuh) whose epilogue
 // leaves, of each 256 columns of a row, the maximum and the sum of exponentials
-// (fp32); a small kernel joins them in a fixed order.  The gradients take the
+// (fp32); a small kernel joins them in a fixed order.  The label's own column is
+// left out of those: with R the sum of exp(l_v - l_y) over the others, the loss is
+// log1p(R), which keeps its digits where the label is nearly sure.  The gradients take the
 // vocabulary in pieces: a piece's logits are multiplied again, the epilogue
 // writes their gradient in bf16 to a workspace (the rounding that any bf16
 // operand of the following products needs; 2^-9 of each element), and one more
@@ -47,22 +49,32 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 // ---- rows with a label ------------------------------------------------------
 // CTA i takes tokens [kPickRows i, ..): counts the labels before them, gathers
-// its own rows that have one, and clears what the others' results are.  The last
-// CTA leaves the number of rows and zeros up to a whole tile (one of zeros if
-// there is no row: dW's products need a K).
-constexpr int kPickThreads = 256, kPickRows = 64;
+// its own rows that have one, and clears what the others' results are.  With a row
+// it forms the label's logit, in fp32: the tensor cores cut off what leaves the
+// accumulator's last bit at each of the some fifty additions, 1e-5 of a large
+// logit, and where the label is nearly sure that is the loss's relative error.
+// For the gradients the last CTA leaves zeros up to a whole block of K (one of
+// zeros if there is no row: dW's products need a K).
+constexpr int kPickThreads = 512, kPickRows = 32;     // two rows a warp
 constexpr int kRowsWhole = 2 * kTileM;       // a tile of a pair of CTAs
+
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b) {
+  return fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16),
+              __uint_as_float(a & 0xffff0000u) *
+                  __uint_as_float(b & 0xffff0000u));
+}
 
 template <bool kVec>
 __global__ void __launch_bounds__(kPickThreads)
 pick_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t stride,
             const int64_t* __restrict__ labels, int tokens, int64_t vocab,
+            const __nv_bfloat16* __restrict__ weight, int64_t weight_stride,
             int width, __nv_bfloat16* __restrict__ rows, int64_t pitch,
-            int32_t* __restrict__ row_label, int32_t* __restrict__ row_token,
+            float* __restrict__ label_logit, int32_t* __restrict__ row_label, int32_t* __restrict__ row_token,
             int32_t* n_rows, float* token_loss, __nv_bfloat16* grad_hidden,
             int64_t grad_stride, uint32_t* status) {
   __shared__ int sh_count[kPickThreads / 32];
-  __shared__ int sh_at[kPickRows];
+  __shared__ int sh_at[kPickRows], sh_label[kPickRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int first = blockIdx.x * kPickRows;
   const bool end = blockIdx.x == gridDim.x - 1;
@@ -86,6 +98,7 @@ pick_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t stride,
       const uint32_t m = __ballot_sync(0xffffffffu, real);
       const int to = at + __popc(m & ((1u << lane) - 1u));
       sh_at[r + lane] = real ? to : -1;
+      sh_label[r + lane] = (int)y;
       if (real) {
         row_label[to] = (int32_t)y;
         row_token[to] = t;
@@ -101,30 +114,49 @@ pick_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t stride,
   }
   __syncthreads();
   const int own = min(kPickRows, tokens - first);
-  const int past = sh_count[0] % kRowsWhole;
-  const int tail = end && (past || !sh_count[0]) ? kRowsWhole - past : 0;
+  const int past = sh_count[0] % kTileK;
+  const int tail =
+      end && grad_hidden && (past || !sh_count[0]) ? kTileK - past : 0;
   for (int r = warp; r < own + tail; r += kPickThreads / 32) {
     const bool zero = r >= own;
     const int t = first + r, to = zero ? sh_count[0] + r - own : sh_at[r];
     if (to < 0 && !grad_hidden) continue;
     const __nv_bfloat16* src = hidden + (int64_t)t * stride;
+    const bool real = !zero && to >= 0;
+    const __nv_bfloat16* w =
+        weight + (real ? (int64_t)sh_label[r] * weight_stride : 0);
+    __nv_bfloat16* to_row = to >= 0 ? rows + (int64_t)to * pitch
+                                    : grad_hidden + (int64_t)t * grad_stride;
+    float dot = 0.f;
     if (kVec) {     // 16 bytes a lane
-      uint4* dst = reinterpret_cast<uint4*>(
-          to >= 0 ? rows + (int64_t)to * pitch
-                  : grad_hidden + (int64_t)t * grad_stride);
-      for (int d = lane; d < width / 8; d += 32)
-        dst[d] = zero || to < 0 ? make_uint4(0, 0, 0, 0)
-                                : reinterpret_cast<const uint4*>(src)[d];
+      uint4* dst = reinterpret_cast<uint4*>(to_row);
+#pragma unroll 4
+      for (int d = lane; d < width / 8; d += 32) {
+        uint4 x = make_uint4(0, 0, 0, 0), y = x;
+        if (real) {
+          x = reinterpret_cast<const uint4*>(src)[d];
+          y = reinterpret_cast<const uint4*>(w)[d];
+        }
+        dst[d] = x;
+        dot += dot2(x.x, y.x) + dot2(x.y, y.y) + dot2(x.z, y.z) +
+               dot2(x.w, y.w);
+      }
     } else {
-      __nv_bfloat16* dst = to >= 0 ? rows + (int64_t)to * pitch
-                                   : grad_hidden + (int64_t)t * grad_stride;
-      for (int d = lane; d < width; d += 32)
-        dst[d] = zero || to < 0 ? __float2bfloat16_rn(0.f) : src[d];
+      for (int d = lane; d < width; d += 32) {
+        const __nv_bfloat16 x = real ? src[d] : __float2bfloat16_rn(0.f);
+        to_row[d] = x;
+        if (real) dot = fmaf(__bfloat162float(x), __bfloat162float(w[d]), dot);
+      }
+    }
+    if (real) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1)
+        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      if (lane == 0) label_logit[to] = dot;
     }
   }
 }
 
-// ---- the loss ---------------------------------------------------------------
 struct RowsState {
   int n_tiles, m_tiles, rows;
 };
@@ -134,7 +166,6 @@ struct StatsParams {
   const int32_t* n_rows;
   const int32_t* labels;  // of the rows
   float2* stats;          // [vocab tile][stride]
-  float* label_logit;
   uint32_t* status;
   int64_t stride;
   int v_tiles, vocab, k_blocks;
@@ -183,7 +214,7 @@ struct StatsWork {
       if (label >= v && label < v + 32) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if (label == v + i) p.label_logit[r] = x[i];
+          if (label == v + i) x[i] = -INFINITY;
       }
       if (v + 32 > p.vocab) {
 #pragma unroll
@@ -257,9 +288,14 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
   if (part == 0) {
     float l = 0.f;
     if (r < rows) {
-      const float lg = log2f(sum);
-      lse2[r] = top + lg;
-      l = (lg - fmaf(label_logit[r], kLog2e, -top)) * kLn2;
+      const float y = label_logit[r] * kLog2e;
+      const float m = fmaxf(top, y);
+      const float at = m == -INFINITY ? 0.f : m;
+      const float lse =
+          at + log2f(sum * exp2_fast(top - at) + exp2_fast(y - at));
+      const float others = sum * exp2_fast(top - y);
+      lse2[r] = lse;
+      l = others <= 1.f ? log1pf(others) : (lse - y) * kLn2;
       if (token_loss) token_loss[row_token[r]] = l;
     }
     sh_loss[i] = l;
@@ -269,7 +305,8 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
     double s = 0.0;
     for (int k = 0; k < kJoinRows; ++k) s += sh_loss[k];
     block_sums[blockIdx.x] = s;
-    last = atom_add_acq_rel(ticket, 1u) == gridDim.x - 1;
+    last = gridDim.x == 1 ||
+           atom_add_acq_rel(ticket, 1u) == gridDim.x - 1;
   }
   __syncthreads();
   if (last && threadIdx.x < 32) {
@@ -665,18 +702,21 @@ cudaError_t head_inputs(const lamb_vocab* v, const void* hidden, int64_t hs,
   in->pitch = lm_round_up(v->width, 64);
   in->weight = (const __nv_bfloat16*)weight;
   in->weight_stride = ws;
-  const bool vec = lm_mappable(hidden, hs) && v->width % 8 == 0 &&
+  const bool vec = lm_mappable(hidden, hs) && lm_mappable(weight, ws) &&
+                   v->width % 8 == 0 &&
                    (!grad_hidden || lm_mappable(grad_hidden, gs));
   const unsigned grid = (unsigned)lm_ceil_div(n, kPickRows);
   if (vec)
     pick_kernel<true><<<grid, kPickThreads, 0, stream>>>(
-        (const __nv_bfloat16*)hidden, hs, labels, (int)n, v->vocab, v->width,
-        v->rows, in->pitch, v->row_label, v->row_token, v->n_rows, token_loss,
+        (const __nv_bfloat16*)hidden, hs, labels, (int)n, v->vocab,
+        (const __nv_bfloat16*)weight, ws, v->width, v->rows, in->pitch,
+        v->label_logit, v->row_label, v->row_token, v->n_rows, token_loss,
         (__nv_bfloat16*)grad_hidden, gs, v->status);
   else
     pick_kernel<false><<<grid, kPickThreads, 0, stream>>>(
-        (const __nv_bfloat16*)hidden, hs, labels, (int)n, v->vocab, v->width,
-        v->rows, in->pitch, v->row_label, v->row_token, v->n_rows, token_loss,
+        (const __nv_bfloat16*)hidden, hs, labels, (int)n, v->vocab,
+        (const __nv_bfloat16*)weight, ws, v->width, v->rows, in->pitch,
+        v->label_logit, v->row_label, v->row_token, v->n_rows, token_loss,
         (__nv_bfloat16*)grad_hidden, gs, v->status);
   if (!lm_mappable(weight, ws)) {
     rows_copy_kernel<<<grid_for(v->vocab * v->width, v->sms), 256, 0, stream>>>(
@@ -701,7 +741,6 @@ lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
   p.n_rows = v->n_rows;
   p.labels = v->row_label;
   p.stats = v->stats;
-  p.label_logit = v->label_logit;
   p.status = v->status;
   p.stride = v->max_tokens;
   p.v_tiles = (int)lm_ceil_div(v->vocab, kTileN);

@@ -55,14 +55,17 @@ __device__ __forceinline__ float update_of(const MuonConsts& k, float g,
   return k.nesterov ? fmaf(k.beta, m, k.omb * g) : m;
 }
 
-__device__ __forceinline__ double block_sum(double s, double* sh) {
+// Sum over a CTA, in thread 0: each warp's in fp32, the warps' in fp64.
+template <int kThreads>
+__device__ __forceinline__ double block_sum(float s, float* sh) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
   __syncthreads();
-  s = 0.0;
-  for (int i = 0; i < kMuonThreads / 32; ++i) s += sh[i];
-  return s;
+  double d = 0.0;
+  if (threadIdx.x == 0)
+    for (int i = 0; i < kThreads / 32; ++i) d += (double)sh[i];
+  return d;
 }
 
 // Four consecutive values (kVec: by one access; else n of them).
@@ -132,13 +135,13 @@ template <class TG, bool kStep>
 __global__ void __launch_bounds__(kMuonThreads)
 muon_norm_kernel(const MuonPtrs* ptrs, const MuonChunk* chunks, MuonConsts k,
                  double* part) {
-  __shared__ double sh[kMuonThreads / 32];
+  __shared__ float sh[kMuonThreads / 32];
   const MuonChunk c = chunks[blockIdx.x];
   const MuonPtrs p = ptrs[c.matrix];
   const float s = chunk_vec<TG, kStep>(p, c.len)
                       ? norm_chunk<TG, kStep, true>(p, c, k)
                       : norm_chunk<TG, kStep, false>(p, c, k);
-  const double sum = block_sum((double)s, sh);
+  const double sum = block_sum<kMuonThreads>(s, sh);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
@@ -197,18 +200,25 @@ __global__ void __launch_bounds__(kMuonThreads)
 muon_start_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
                   const MuonChunk* chunks, MuonConsts k, const double* part,
                   uint32_t* done, uint32_t* status) {
-  __shared__ double sh[kMuonThreads / 32];
+  __shared__ float sh_norm;
   const MuonChunk c = chunks[blockIdx.x];
   const MuonMatrix& x = mats[c.matrix];
   const MuonPtrs p = ptrs[c.matrix];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < x.n_chunks; i += kMuonThreads)
-    s += part[x.first_chunk + i];
-  const float norm = (float)sqrt(block_sum(s, sh));
-  if (threadIdx.x == 0) {
-    if (!isfinite(norm)) atomicOr(status, LAMB_STATUS_NONFINITE);
-    if (c.offset == 0) done[c.matrix] = 0;       // of the products to come
+  if (threadIdx.x < 32) {       // the chunks' sums, in a fixed order
+    double s = 0.0;
+    for (int i = threadIdx.x; i < x.n_chunks; i += 32)
+      s += part[x.first_chunk + i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (threadIdx.x == 0) {
+      const float n = sqrtf((float)s);
+      sh_norm = n;
+      if (!isfinite(n)) atomicOr(status, LAMB_STATUS_NONFINITE);
+      if (c.offset == 0) done[c.matrix] = 0;       // of the products to come
+    }
   }
+  __syncthreads();
+  const float norm = sh_norm;
   const float f = x.scale / (norm + k.eps);
   if (chunk_vec<TG, kStep>(p, c.len))
     start_chunk<TG, kStep, true>(x, p, c, k, f);
@@ -230,7 +240,7 @@ bool muon_is_small(int64_t m, int64_t n) {
   return m <= kSmallSide && m * n <= kSmallElems && m * m * n <= kSmallProduct;
 }
 int64_t small_smem(int64_t m, int64_t n) {
-  return (2 * m * lm_round_up(n, 4) + 2 * m * lm_round_up(m, 8)) * 4;
+  return (m * lm_round_up(m, 8) + m * (m | 1) + 2 * m * (n | 1)) * 4;
 }
 
 // out = b in + c (in in^T), or in in^T (kPlain), both symmetric: blocks of 4 x 4,
@@ -299,13 +309,14 @@ muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
                   const int* which, MuonConsts k, int steps, const float* d_lr,
                   uint32_t* status) {
   extern __shared__ float sm[];
-  __shared__ double sh[kSmallThreads / 32];
+  __shared__ float sh[kSmallThreads / 32], sh_norm;
   const MuonMatrix& x = mats[which[blockIdx.x]];
   const MuonPtrs p = ptrs[which[blockIdx.x]];
   const int m = x.m, n = x.n, cols = x.cols, total = m * n;
-  const int np = (n + 3) & ~3, mp = (m + 7) & ~7;
+  // odd pitches: a warp's lanes are at several rows of X and G at a time
+  const int np = n | 1, gp = m | 1, mp = (m + 7) & ~7;
   const bool tall = x.tall;
-  float *X = sm, *Y = X + m * np, *G = Y + m * np, *H = G + m * mp;
+  float *H = sm, *G = H + m * mp, *X = G + m * gp, *Y = X + m * np;
   for (int i = threadIdx.x; i < m * mp; i += kSmallThreads) H[i] = 0.f;
 
   float s = 0.f;
@@ -320,16 +331,13 @@ muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
     const int r = i / cols, c = i - r * cols;
     X[tall ? c * np + r : r * np + c] = u;
   }
-  double d = (double)s;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = d;
+  const double d = block_sum<kSmallThreads>(s, sh);
+  if (threadIdx.x == 0) {
+    sh_norm = sqrtf((float)d);
+    if (!isfinite(sh_norm)) atomicOr(status, LAMB_STATUS_NONFINITE);
+  }
   __syncthreads();
-  d = 0.0;
-  for (int i = 0; i < kSmallThreads / 32; ++i) d += sh[i];
-  const float norm = (float)sqrt(d);
-  if (threadIdx.x == 0 && !isfinite(norm))
-    atomicOr(status, LAMB_STATUS_NONFINITE);
+  const float norm = sh_norm;
   const float f = 1.f / (norm + k.eps);
   for (int i = threadIdx.x; i < total; i += kSmallThreads) {
     const int r = i / n;
@@ -338,9 +346,9 @@ muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
   __syncthreads();
 
   for (int it = 0; it < steps; ++it) {
-    small_gram<true>(X, np, m, n, 0.f, 0.f, G, mp);
+    small_gram<true>(X, np, m, n, 0.f, 0.f, G, gp);
     __syncthreads();
-    small_gram<false>(G, mp, m, m, k.b, k.c, H, mp);
+    small_gram<false>(G, gp, m, m, k.b, k.c, H, mp);
     __syncthreads();
     // Y = a X + H X, eight rows of a column a thread
     const int tasks = ((m + 7) >> 3) * n;
