@@ -239,37 +239,37 @@ constexpr int64_t kSmallProduct = 1 << 19;   // m m n up to
 bool muon_is_small(int64_t m, int64_t n) {
   return m <= kSmallSide && m * n <= kSmallElems && m * m * n <= kSmallProduct;
 }
+// Rows of X: on 16 bytes, and four rows on at other banks.
+__host__ __device__ constexpr int64_t small_pitch(int64_t n) {
+  return (n + 3) / 4 * 4 + ((n + 3) / 4 % 2 ? 0 : 4);
+}
 int64_t small_smem(int64_t m, int64_t n) {
-  return (m * lm_round_up(m, 8) + m * (m | 1) + 2 * m * (n | 1)) * 4;
+  return (m * lm_round_up(m, 4) + m * lm_round_up(m | 1, 4) +
+          2 * m * small_pitch(n)) * 4;
 }
 
-// out = b in + c (in in^T), or in in^T (kPlain), both symmetric: blocks of 4 x 4,
-// each by S neighbouring lanes that take every S-th k.
+// out = b in + c (in in^T), or in in^T (kPlain), both symmetric: blocks of 4 x 4
+// (the task's places are in `where`), each by 16 neighbouring lanes that take
+// every 16th k.  Their sums are exchanged so that each lane ends with one entry.
 template <bool kPlain>
 __device__ __forceinline__ void small_gram(const float* in, int pitch, int m,
                                            int n, float b, float c, float* out,
-                                           int out_pitch) {
-  const int nb = (m + 3) >> 2, tasks = nb * (nb + 1) / 2;
-  int S = 32;
-  while (S > 1 && S * tasks > kSmallThreads) S >>= 1;
-  const int s = threadIdx.x % S, groups = kSmallThreads / S;
-  for (int base = 0; base < tasks; base += groups) {
-    const int task = base + threadIdx.x / S;
-    int t = min(task, tasks - 1), bi = 0;
-    while (t >= nb - bi) {
-      t -= nb - bi;
-      ++bi;
-    }
-    const int i0 = 4 * bi, j0 = 4 * (bi + t);
+                                           int out_pitch, const uint16_t* where,
+                                           int tasks) {
+  const int s = threadIdx.x & 15;
+  for (int base = 0; base < tasks; base += kSmallThreads / 16) {
+    const int task = base + (threadIdx.x >> 4);
+    const int w = where[min(task, tasks - 1)];
+    const int i0 = 4 * (w >> 8), j0 = 4 * (w & 255);
     const float *ri[4], *rj[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       ri[q] = in + min(i0 + q, m - 1) * pitch;
       rj[q] = in + min(j0 + q, m - 1) * pitch;
     }
-    float acc[4][4] = {};
+    float acc[16] = {};
 #pragma unroll 4
-    for (int k = s; k < n; k += S) {
+    for (int k = s; k < n; k += 16) {
       float x[4], y[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -279,26 +279,26 @@ __device__ __forceinline__ void small_gram(const float* in, int pitch, int m,
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(x[u], y[v], acc[u][v]);
-    }
-    for (int o = S >> 1; o > 0; o >>= 1)
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
         for (int v = 0; v < 4; ++v)
-          acc[u][v] += __shfl_xor_sync(0xffffffffu, acc[u][v], o);
-    if (task < tasks && s == 0) {
+          acc[4 * u + v] = fmaf(x[u], y[v], acc[4 * u + v]);
+    }
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+    for (int h = 8; h > 0; h >>= 1) {
+      const bool up = s & h;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int i = i0 + u, j = j0 + v;
-          if (i >= m || j >= m) continue;
-          const float r =
-              kPlain ? acc[u][v] : fmaf(b, in[i * pitch + j], c * acc[u][v]);
-          out[i * out_pitch + j] = r;
-          out[j * out_pitch + i] = r;
-        }
+      for (int q = 0; q < 8; ++q) {
+        if (q >= h) break;
+        const float send = up ? acc[q] : acc[q + h];
+        const float keep = up ? acc[q + h] : acc[q];
+        acc[q] = keep + __shfl_xor_sync(0xffffffffu, send, h);
+      }
+    }
+    const int i = i0 + (s >> 2), j = j0 + (s & 3);
+    if (task < tasks && i < m && j < m) {
+      const float r =
+          kPlain ? acc[0] : fmaf(b, in[i * pitch + j], c * acc[0]);
+      out[i * out_pitch + j] = r;
+      out[j * out_pitch + i] = r;
     }
   }
 }
@@ -310,14 +310,21 @@ muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
                   uint32_t* status) {
   extern __shared__ float sm[];
   __shared__ float sh[kSmallThreads / 32], sh_norm;
+  __shared__ uint16_t where[kSmallSide / 4 * (kSmallSide / 4 + 1) / 2];
   const MuonMatrix& x = mats[which[blockIdx.x]];
   const MuonPtrs p = ptrs[which[blockIdx.x]];
   const int m = x.m, n = x.n, cols = x.cols, total = m * n;
-  // odd pitches: a warp's lanes are at several rows of X and G at a time
-  const int np = n | 1, gp = m | 1, mp = (m + 7) & ~7;
+  // (a warp's lanes are at several rows of X and G at a time)
+  const int np = (int)small_pitch(n), gp = m | 1, mp = (m + 3) & ~3;
   const bool tall = x.tall;
-  float *H = sm, *G = H + m * mp, *X = G + m * gp, *Y = X + m * np;
+  float *H = sm, *G = H + m * mp, *X = G + m * ((gp + 3) & ~3), *Y = X + m * np;
   for (int i = threadIdx.x; i < m * mp; i += kSmallThreads) H[i] = 0.f;
+  const int nb = (m + 3) >> 2, blocks = nb * (nb + 1) / 2;
+  if (threadIdx.x < nb)       // the blocks on and above the diagonal
+    for (int j = threadIdx.x, t = threadIdx.x * nb -
+                                  threadIdx.x * ((int)threadIdx.x - 1) / 2;
+         j < nb; ++j, ++t)
+      where[t] = (uint16_t)(threadIdx.x << 8 | j);
 
   float s = 0.f;
   for (int i = threadIdx.x; i < total; i += kSmallThreads) {
@@ -346,33 +353,38 @@ muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
   __syncthreads();
 
   for (int it = 0; it < steps; ++it) {
-    small_gram<true>(X, np, m, n, 0.f, 0.f, G, gp);
+    small_gram<true>(X, np, m, n, 0.f, 0.f, G, gp, where, blocks);
     __syncthreads();
-    small_gram<false>(G, gp, m, m, k.b, k.c, H, mp);
+    small_gram<false>(G, gp, m, m, k.b, k.c, H, mp, where, blocks);
     __syncthreads();
-    // Y = a X + H X, eight rows of a column a thread
-    const int tasks = ((m + 7) >> 3) * n;
+    // Y = a X + H X, 4 x 4 entries a thread: two 16-byte loads for 16 products
+    // (four rows of one column were bound by shared memory)
+    const int nc = (n + 3) >> 2, tasks = nb * nc;
     for (int t = threadIdx.x; t < tasks; t += kSmallThreads) {
-      const int i0 = t / n * 8, j = t % n;
-      float acc[8] = {};
-#pragma unroll 8
+      const int i0 = t / nc * 4, j0 = t % nc * 4;
+      float acc[4][4] = {};
+#pragma unroll 4
       for (int q = 0; q < m; ++q) {
-        const float v = X[q * np + j];
-        const float4* h = reinterpret_cast<const float4*>(H + q * mp + i0);
-        const float4 a = h[0], b = h[1];
-        acc[0] = fmaf(a.x, v, acc[0]);
-        acc[1] = fmaf(a.y, v, acc[1]);
-        acc[2] = fmaf(a.z, v, acc[2]);
-        acc[3] = fmaf(a.w, v, acc[3]);
-        acc[4] = fmaf(b.x, v, acc[4]);
-        acc[5] = fmaf(b.y, v, acc[5]);
-        acc[6] = fmaf(b.z, v, acc[6]);
-        acc[7] = fmaf(b.w, v, acc[7]);
+        const float4 x = *reinterpret_cast<const float4*>(X + q * np + j0);
+        const float4 h = *reinterpret_cast<const float4*>(H + q * mp + i0);
+        const float hv[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          acc[u][0] = fmaf(hv[u], x.x, acc[u][0]);
+          acc[u][1] = fmaf(hv[u], x.y, acc[u][1]);
+          acc[u][2] = fmaf(hv[u], x.z, acc[u][2]);
+          acc[u][3] = fmaf(hv[u], x.w, acc[u][3]);
+        }
       }
 #pragma unroll
-      for (int q = 0; q < 8; ++q)
-        if (i0 + q < m)
-          Y[(i0 + q) * np + j] = fmaf(k.a, X[(i0 + q) * np + j], acc[q]);
+      for (int u = 0; u < 4; ++u) {
+        if (i0 + u >= m) break;
+        const int at = (i0 + u) * np + j0;
+        const float4 x = *reinterpret_cast<const float4*>(X + at);
+        *reinterpret_cast<float4*>(Y + at) =
+            make_float4(fmaf(k.a, x.x, acc[u][0]), fmaf(k.a, x.y, acc[u][1]),
+                        fmaf(k.a, x.z, acc[u][2]), fmaf(k.a, x.w, acc[u][3]));
+      }
     }
     __syncthreads();
     float* z = X;
