@@ -8,7 +8,7 @@
 //
 // Gradient: the token positions are sorted by id (stable, least significant
 // digit first, 8 bits a pass), so that every word's rows are added in the order
-// of the tokens, the same in each run.  The sorted list is cut every 32 to
+// of the tokens, the same in each run.  The sorted list is cut every 16 to
 // 128 positions, whatever the words: ids are Zipf-like, most words have few tokens and
 // a mask token thousands.  A chunk writes the rows of the words that lie inside it
 // and leaves the sum of a word that goes on; one more launch adds those, in order.
@@ -32,10 +32,10 @@ constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortTiles = 128;        // at most: each reads all tiles' counts
 // Sorted positions of a chunk: short ones fill the SMs, long ones leave fewer sums
-// to join.  us at 4095 x 768 and 65536 x 1024 tokens: 32 positions 27 / 113, 64
-// positions 36 / 85, 128 positions - / 70.
-constexpr int kLeastChunk = 32;
-int chunk_of(int64_t n) { return n <= 8192 ? 32 : n <= 32768 ? 64 : 128; }
+// to join.  us at 4095 x 768 tokens: 16 positions 23, 32 27, 64 36; at 65536 x 1024:
+// 32 113, 64 85, 128 70.
+constexpr int kLeastChunk = 16;
+int chunk_of(int64_t n) { return n <= 8192 ? 16 : n <= 32768 ? 64 : 128; }
 constexpr int kClearRows = 64;         // rows of the table a clearing CTA looks at
 constexpr int kJoinThreads = 256, kJoinBatch = 8;
 constexpr uint32_t kStatusBadIndex = LAMB_STATUS_BAD_INDEX;
@@ -261,9 +261,13 @@ sort_small_kernel(const int64_t* ids, int n, int64_t vocab, int passes,
     }
     __syncthreads();
     int total = 0, s = 0;
+    int held[kWarps];           // the warps' counts of a digit
     if (threadIdx.x < 256) {
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) total += count[w][threadIdx.x];
+      for (int w = 0; w < kWarps; ++w) {
+        held[w] = count[w][threadIdx.x];
+        total += held[w];
+      }
       s = total;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -278,9 +282,8 @@ sort_small_kernel(const int64_t* ids, int n, int64_t vocab, int passes,
       for (int w = 0; w < warp; ++w) at += scan[w * 32 + 31];
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const int c = count[w][threadIdx.x];
         count[w][threadIdx.x] = (uint16_t)at;
-        at += c;
+        at += held[w];
       }
     }
     __syncthreads();
@@ -680,7 +683,7 @@ extern "C" lamb_status_t lamb_vocab_embed_grad(
   const unsigned tiles = (unsigned)lm_ceil_div(n, kSortThreads * rounds);
   cudaError_t e = cudaSuccess;
   int in = 0;
-  // (4095 tokens: 31 us with a launch a pass, 26 with one in all)
+  // (4095 tokens: 31 us with a launch a pass, 29 with one in all)
   const bool small = n <= kSmallSort;
   if (n && small)
     e = lm_launch(sort_small_kernel, 1, kSmallThreads, 0, stream, false, ids, n,

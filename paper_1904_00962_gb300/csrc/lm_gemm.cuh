@@ -4,9 +4,9 @@
 //
 // Persistent CTAs walk the tiles of a Work type, one by one or in pairs (kCtas): a
 // pair multiplies a tile of 256 x 256 (cta_group::2), each CTA holding 128 rows of
-// A and of B.  A pair's stage is two thirds of two single ones', so six fit instead
-// of four and less comes from L2; a single CTA's tile of 128 rows wastes less on
-// few rows.
+// A and of B.  A pair's stage takes two thirds of what two single ones do, so six
+// fit instead of four and less comes from L2; a single CTA's tile of 128 rows wastes
+// less on few rows.
 //   Work::kBf16                   operands bf16 (else fp16)
 //   Work::Params::status          the plan's status word
 //   Work::start<kRows>(params)    what the kernel reads first: State, with the
