@@ -773,7 +773,9 @@ LAMB_API lamb_status_t lamb_muon_bind_direction(struct lamb_muon* plan,
 
 /* One update of every matrix, enqueued on `stream`; d_lr is DEVICE float eta.
  * Updates w, m (and the copy) in place.  Capturable; calls of one plan share its
- * workspace and must not overlap. */
+ * workspace and must not overlap.  The products are one cooperative launch that
+ * holds every SM (matrices that fit in one go without it): it starts when kernels
+ * of other streams leave that room. */
 LAMB_API lamb_status_t lamb_muon_step(struct lamb_muon* plan,
                                       const lamb_muon_hyper_t* hyper,
                                       const float* d_lr, cudaStream_t stream);

@@ -609,6 +609,8 @@ lamb_status_t check_common(const lamb_vocab* v, const void* a, const char* an,
       return lm_fail(LAMB_ERR_INVALID_ARG, "%s: pointer not aligned", name);
   }
   if (n && !ids) return lm_fail(LAMB_ERR_INVALID_ARG, "ids is NULL");
+  if ((uintptr_t)ids % 8)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "ids: pointer not aligned");
   return LAMB_OK;
 }
 

@@ -58,6 +58,30 @@ __device__ __forceinline__ float exp2_fast(float x) {
 constexpr int kPickThreads = 512, kPickRows = 32;     // two rows a warp
 constexpr int kRowsWhole = 2 * kTileM;       // a tile of a pair of CTAs
 
+// Labels in each kCountRows tokens, so that a CTA of pick_kernel need not look at
+// all tokens before its own where those are many.
+constexpr int kCountRows = 4096, kCountThreads = 256;
+constexpr int64_t kCountFrom = 16384;      // tokens
+
+__global__ void __launch_bounds__(kCountThreads)
+count_kernel(const int64_t* labels, int tokens, int64_t vocab, int32_t* counts) {
+  const int64_t first = (int64_t)blockIdx.x * kCountRows;
+  let_next_launch();
+  int any = 0;
+  for (int i = threadIdx.x; i < kCountRows; i += kCountThreads) {
+    const int64_t y = first + i < tokens ? labels[first + i] : -1;
+    any += y >= 0 && y < vocab;
+  }
+  __shared__ int sh[kCountThreads / 32];
+  any = __reduce_add_sync(0xffffffffu, any);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = any;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kCountThreads / 32; ++i) any += sh[i];
+    counts[blockIdx.x] = any;
+  }
+}
+
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b) {
   return fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16),
               __uint_as_float(a & 0xffff0000u) *
@@ -67,7 +91,8 @@ __device__ __forceinline__ float dot2(uint32_t a, uint32_t b) {
 template <bool kVec>
 __global__ void __launch_bounds__(kPickThreads)
 pick_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t stride,
-            const int64_t* __restrict__ labels, int tokens, int64_t vocab,
+            const int64_t* __restrict__ labels, const int32_t* counts,
+            int tokens, int64_t vocab,
             const __nv_bfloat16* __restrict__ weight, int64_t weight_stride,
             int width, __nv_bfloat16* __restrict__ rows, int64_t pitch,
             float* __restrict__ label_logit, int32_t* __restrict__ row_label, int32_t* __restrict__ row_token,
@@ -80,7 +105,10 @@ pick_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t stride,
   const bool end = blockIdx.x == gridDim.x - 1;
   int before = 0;
   let_next_launch();
-  for (int t = threadIdx.x; t < first; t += kPickThreads) {
+  after_prior_launch();
+  const int known = counts ? first / kCountRows : 0;    // whole counts
+  for (int i = threadIdx.x; i < known; i += kPickThreads) before += counts[i];
+  for (int t = known * kCountRows + threadIdx.x; t < first; t += kPickThreads) {
     const int64_t y = labels[t];
     before += y >= 0 && y < vocab;
   }
@@ -706,18 +734,20 @@ cudaError_t head_inputs(const lamb_vocab* v, const void* hidden, int64_t hs,
                    v->width % 8 == 0 &&
                    (!grad_hidden || lm_mappable(grad_hidden, gs));
   const unsigned grid = (unsigned)lm_ceil_div(n, kPickRows);
-  if (vec)
-    pick_kernel<true><<<grid, kPickThreads, 0, stream>>>(
-        (const __nv_bfloat16*)hidden, hs, labels, (int)n, v->vocab,
-        (const __nv_bfloat16*)weight, ws, v->width, v->rows, in->pitch,
-        v->label_logit, v->row_label, v->row_token, v->n_rows, token_loss,
-        (__nv_bfloat16*)grad_hidden, gs, v->status);
-  else
-    pick_kernel<false><<<grid, kPickThreads, 0, stream>>>(
-        (const __nv_bfloat16*)hidden, hs, labels, (int)n, v->vocab,
-        (const __nv_bfloat16*)weight, ws, v->width, v->rows, in->pitch,
-        v->label_logit, v->row_label, v->row_token, v->n_rows, token_loss,
-        (__nv_bfloat16*)grad_hidden, gs, v->status);
+  const bool many = n > kCountFrom;
+  cudaError_t e = cudaSuccess;
+  if (many)
+    e = lm_launch(count_kernel, (unsigned)lm_ceil_div(n, kCountRows),
+                  kCountThreads, 0, stream, false, labels, (int)n, v->vocab,
+                  v->counts);
+  if (e == cudaSuccess)
+    e = lm_launch(vec ? pick_kernel<true> : pick_kernel<false>, grid,
+                  kPickThreads, 0, stream, many, (const __nv_bfloat16*)hidden,
+                  hs, labels, many ? v->counts : nullptr, (int)n, v->vocab,
+                  (const __nv_bfloat16*)weight, ws, v->width, v->rows, in->pitch,
+                  v->label_logit, v->row_label, v->row_token, v->n_rows,
+                  token_loss, (__nv_bfloat16*)grad_hidden, gs, v->status);
+  if (e != cudaSuccess) return e;
   if (!lm_mappable(weight, ws)) {
     rows_copy_kernel<<<grid_for(v->vocab * v->width, v->sms), 256, 0, stream>>>(
         in->weight, ws, v->vocab, v->width, v->weight_copy, in->pitch);
@@ -792,7 +822,8 @@ int64_t piece_width(const lamb_vocab* v, int64_t n, int rows, int units) {
 
 lamb_status_t check_head(const lamb_vocab* v, const void* hidden, int64_t hs,
                          const void* weight, int64_t ws, const int64_t* labels,
-                         int64_t n, const float* loss) {
+                         int64_t n, const float* token_loss,
+                         const float* loss) {
   if (!v) return lm_fail(LAMB_ERR_INVALID_ARG, "plan is NULL");
   if (n < 0 || n > v->max_tokens)
     return lm_fail(LAMB_ERR_INVALID_ARG,
@@ -805,7 +836,7 @@ lamb_status_t check_head(const lamb_vocab* v, const void* hidden, int64_t hs,
     return lm_fail(LAMB_ERR_INVALID_ARG, "a row stride is below the width %d",
                    v->width);
   if ((uintptr_t)hidden % 2 || (uintptr_t)weight % 2 || (uintptr_t)loss % 4 ||
-      (uintptr_t)labels % 8)
+      (uintptr_t)token_loss % 4 || (uintptr_t)labels % 8)
     return lm_fail(LAMB_ERR_INVALID_ARG, "a pointer is not aligned");
   return LAMB_OK;
 }
@@ -826,6 +857,7 @@ void lm_head_carve(lamb_vocab* v, LmArena* a) {
   a->take(&v->row_label, n);
   a->take(&v->row_token, n);
   a->take(&v->n_rows, 1);
+  a->take(&v->counts, lm_ceil_div(n, kCountRows));
   a->take(&v->stats, lm_ceil_div(v->vocab, kTileN) * n);
   a->take(&v->label_logit, n);
   a->take(&v->lse2, n);
@@ -851,7 +883,7 @@ extern "C" lamb_status_t lamb_vocab_loss(
     const void* weight, int64_t weight_stride, const int64_t* labels,
     int64_t n_tokens, float* token_loss, float* loss, cudaStream_t stream) {
   lamb_status_t st = check_head(v, hidden, hidden_stride, weight, weight_stride,
-                                labels, n_tokens, loss);
+                                labels, n_tokens, token_loss, loss);
   if (st != LAMB_OK) return st;
   LmDevice dev(v->device);
   if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");
@@ -875,7 +907,7 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
     int32_t grad_weight_dtype, int64_t grad_weight_stride, int32_t accumulate,
     cudaStream_t stream) {
   lamb_status_t st = check_head(v, hidden, hidden_stride, weight, weight_stride,
-                                labels, n_tokens, loss);
+                                labels, n_tokens, token_loss, loss);
   if (st != LAMB_OK) return st;
   const int64_t n = n_tokens;
   if (grad_weight_dtype != LAMB_F32 && grad_weight_dtype != LAMB_BF16)
@@ -888,7 +920,8 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
     return lm_fail(LAMB_ERR_INVALID_ARG,
                    "a gradient's row stride is below the width %d", v->width);
   const bool f32 = grad_weight_dtype == LAMB_F32;
-  if ((uintptr_t)grad_hidden % 2 || (uintptr_t)grad_weight % (f32 ? 4 : 2))
+  if ((uintptr_t)grad_hidden % 2 || (uintptr_t)d_scale % 4 ||
+      (uintptr_t)grad_weight % (f32 ? 4 : 2))
     return lm_fail(LAMB_ERR_INVALID_ARG, "a gradient's pointer is not aligned");
   LmDevice dev(v->device);
   if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");
@@ -1029,6 +1062,9 @@ extern "C" lamb_status_t lamb_vocab_create(int64_t vocab, int32_t width,
     return lm_fail(LAMB_ERR_INVALID_ARG, "width is not in [1, 2^20]");
   if (max_tokens < 1 || max_tokens > (1ll << 24))
     return lm_fail(LAMB_ERR_INVALID_ARG, "max_tokens is not in [1, 2^24]");
+  if (lm_ceil_div(max_tokens, kTileM) * lm_ceil_div(vocab, kTileN) > INT32_MAX)
+    return lm_fail(LAMB_ERR_INVALID_ARG,
+                   "max_tokens times vocab is above 2^46 or so");
   if (device < 0) return lm_fail(LAMB_ERR_INVALID_ARG, "device < 0");
   LmDevice dev(device);
   if (dev.err != cudaSuccess) return lm_cuda_fail(dev.err, "cudaSetDevice");

@@ -892,7 +892,8 @@ extern "C" lamb_status_t lamb_muon_step(struct lamb_muon* p,
                                         cudaStream_t stream) {
   lamb_status_t st = muon_check(p, hyper);
   if (st != LAMB_OK) return st;
-  if (!d_lr) return lm_fail(LAMB_ERR_INVALID_ARG, "d_lr is NULL");
+  if (!d_lr || (uintptr_t)d_lr % 4)
+    return lm_fail(LAMB_ERR_INVALID_ARG, "d_lr is NULL or not aligned");
   if (!p->bound)
     return lm_fail(LAMB_ERR_NOT_BOUND, "lamb_muon_step before lamb_muon_bind");
   return muon_run(p, hyper, d_lr, stream);

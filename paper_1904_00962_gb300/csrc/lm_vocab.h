@@ -25,6 +25,7 @@ struct lamb_vocab {
   int32_t* row_label = nullptr;
   int32_t* row_token = nullptr;
   int32_t* n_rows = nullptr;
+  int32_t* counts = nullptr;    // labels in runs of tokens
   float2* stats = nullptr;      // [vocab tiles][max_tokens]
   float* label_logit = nullptr;
   float* lse2 = nullptr;

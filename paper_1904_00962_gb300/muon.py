@@ -9,7 +9,7 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
-from .state import _dtype_code, _stream
+from .state import _dtype_code
 
 _TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
 
@@ -45,6 +45,13 @@ class MuonPlan:
         self._bound[name] = tensors
         return [t.data_ptr() for t in tensors]
 
+    def _stream(self, stream):
+        """A raw stream handle: PyTorch's current one of the plan's device, or
+        the given one."""
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.device.index or 0)
+        return stream if isinstance(stream, int) else stream.cuda_stream
+
     def bind(self, w, g, m, copy=None, stream=None):
         """The weights and momenta (fp32), gradients, and bf16 copies that
         `step` works on."""
@@ -56,24 +63,29 @@ class MuonPlan:
             self._ptrs("g", g, _TORCH[self.grad_dtype]),
             self._ptrs("m", m, f32),
             None if copy is None else
-            self._ptrs("copy", copy, torch.bfloat16), _stream(stream))
+            self._ptrs("copy", copy, torch.bfloat16), self._stream(stream))
 
     def bind_direction(self, u, o, stream=None):
         """The inputs (of the gradients' type) and bf16 outputs of
         `direction`."""
         B.lamb_muon_bind_direction(
             self.handle, self._ptrs("u", u, _TORCH[self.grad_dtype]),
-            self._ptrs("o", o, torch.bfloat16), _stream(stream))
+            self._ptrs("o", o, torch.bfloat16), self._stream(stream))
 
     def step(self, hyper, d_lr: torch.Tensor, stream=None):
-        B.lamb_muon_step(self.handle, hyper, d_lr.data_ptr(), _stream(stream))
+        """One update; d_lr: a float tensor of one element on the device."""
+        if d_lr.dtype != torch.float32 or d_lr.numel() != 1 or \
+                d_lr.get_device() != (self.device.index or 0):
+            raise ValueError("d_lr: a float32 tensor of one element on "
+                             f"{self.device} is needed")
+        B.lamb_muon_step(self.handle, hyper, d_lr.data_ptr(), self._stream(stream))
 
     def direction(self, hyper, stream=None):
-        B.lamb_muon_direction(self.handle, hyper, _stream(stream))
+        B.lamb_muon_direction(self.handle, hyper, self._stream(stream))
 
     def query(self, clear=False, stream=None) -> int:
         """The plan's LAMB_STATUS_* bits (synchronises the stream)."""
-        return B.lamb_muon_query(self.handle, clear, _stream(stream))
+        return B.lamb_muon_query(self.handle, clear, self._stream(stream))
 
     def destroy(self):
         if self.handle:

@@ -32,7 +32,8 @@ def _refused(call, status=B.LAMB_ERR_INVALID_ARG, word=""):
     ((0, 64, 10, 0), "vocab"), ((-5, 64, 10, 0), "vocab"),
     ((2 ** 31, 64, 10, 0), "vocab"), ((10, 0, 10, 0), "width"),
     ((10, 2 ** 21, 10, 0), "width"), ((10, 64, 0, 0), "max_tokens"),
-    ((10, 64, 2 ** 25, 0), "max_tokens"), ((10, 64, 10, -1), "device")])
+    ((10, 64, 2 ** 25, 0), "max_tokens"), ((10, 64, 10, -1), "device"),
+    ((2 ** 30, 64, 2 ** 24, 0), "max_tokens times vocab")])
 def test_vocab_create_refuses(lib, args, word):
     _refused(lambda: B.lamb_vocab_create(*args), word=word)
 

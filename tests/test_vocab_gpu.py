@@ -296,6 +296,25 @@ def test_head_with_few_labels(ignored):
     _head_case(400, 600, 64, ignored=ignored, max_tokens=500)
 
 
+def test_head_of_many_tokens():
+    """Rows counted in runs: labels far apart, and none in most runs."""
+    g = _gen(11)
+    n, vocab, width = 40000, 40, 16
+    h, w, y = _head_inputs(n, vocab, width, g, 0.0)
+    y[5000:31000] = -1
+    y[20000] = 7
+    y[39990:] = -3
+    ref = _head_reference(h, w, y)
+    plan = VocabPlan(vocab, width, n)
+    token = torch.full((n,), 7.0, device=DEV)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    loss = plan.loss_grad(h, w, y, dh, dw, token_loss=token)
+    _close(token, ref["token"], ref["token"] * 2 ** -20 + ref["e_token"])
+    _close(loss[0], ref["loss"], ref["loss"] * 2 ** -20 + ref["e_token"])
+    _close(dh, ref["dh"], ref["dh_err"] + UBF * ref["dh"].abs())
+    _close(dw, ref["dw"], ref["dw_err"] + UBF * ref["dw"].abs())
+
+
 def test_head_in_several_pieces():
     """More logits than the workspace holds."""
     _head_case(4500, 30001, 64, ignored=0.0)
