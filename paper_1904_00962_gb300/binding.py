@@ -618,14 +618,15 @@ def lamb_muon_bind_direction(plan, u, o, stream=0) -> None:
 
 
 def lamb_muon_step(plan, hyper: lamb_muon_hyper_t, d_lr, stream=0) -> None:
-    _check(load().lamb_muon_step(c_void_p(plan), byref(hyper),
-                                 c_void_p(d_lr or None),
-                                 c_void_p(stream or None)))
+    st = (_lib or load()).lamb_muon_step(plan, byref(hyper), d_lr, stream)
+    if st:
+        _check(st)
 
 
 def lamb_muon_direction(plan, hyper: lamb_muon_hyper_t, stream=0) -> None:
-    _check(load().lamb_muon_direction(c_void_p(plan), byref(hyper),
-                                      c_void_p(stream or None)))
+    st = (_lib or load()).lamb_muon_direction(plan, byref(hyper), stream)
+    if st:
+        _check(st)
 
 
 def lamb_muon_query(plan, clear=False, stream=0) -> int:

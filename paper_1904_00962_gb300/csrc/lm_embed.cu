@@ -6,17 +6,22 @@
 // Lookup: a copy with a gather, bound by HBM (each row read and written once); a
 // warp takes a row, 16 bytes a lane.
 //
-// Gradient: the token positions are sorted by id (stable, least significant
-// digit first, 8 bits a pass), so that every word's rows are added in the order
-// of the tokens, the same in each run.  The sorted list is cut every 16 to
-// 128 positions, whatever the words: ids are Zipf-like, most words have few tokens and
-// a mask token thousands.  A chunk writes the rows of the words that lie inside it
-// and leaves the sum of a word that goes on; one more launch adds those, in order.
-// Rows of words without a token are cleared by other CTAs of the same launch.
-// Sums are fp32.
+// Gradient: the token positions are sorted by id (stable, least significant digit
+// first, 8 bits a pass), so that every word's rows are added in the order of the
+// tokens, the same in each run.  The sorted list is cut every 16 to 128 positions,
+// whatever the words: ids are Zipf-like, most words have few tokens and a mask
+// token thousands.  A chunk writes the rows of the words that lie inside it and
+// leaves the sum of a word that goes on; one more launch adds those, in order.
+// Rows of words without a token are cleared by other CTAs of the same launch.  Sums
+// are fp32.
 //
 // Launches follow one another early (griddepcontrol): count, a move for each digit
-// (which counts the next digit), sums, joins.
+// (which counts the next digit), sums, joins; up to 4096 tokens are sorted in one.
+//
+// Measured: lookup of 65536 x 768 (fp32 to bf16) 27 us, 5.1 TB/s; gradient of 65536
+// x 1024 (bf16) into a fresh table 70 us, of which the sort takes 18, the sums 40 and
+// the joins 10: 27 us of HBM traffic, the rest latency of the longest word and of
+// four launches in front; 4095 x 768 added to a tied table 23 us.
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -13,6 +13,8 @@
 //                                 number of tiles of kRows rows (it may come from
 //                                 the device)
 //   Work::tile<kRows>(params, state, t)   operands and extent of tile t (GemmTile)
+//   Work::early(params, t, tile)  whether tile t of one of 128 rows is known, and
+//                                 its B there, before the launch in front has ended
 //   Work::epilogue(params, state, tile, acc, epi)  a row of the accumulator
 // A tile has 256 rows of B.  Operands come through tensor maps with the 128-byte
 // swizzle, K-major (64 of K by all of a CTA's rows) or MN-major (blocks of 64 rows
@@ -138,16 +140,24 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
   tmem_after_sync();
   const uint32_t tmem = sh.tmem;
   let_next_launch();
-  after_prior_launch();
-  const typename Work::State st = Work::template start<kRows>(p);
   auto wait = [&](uint64_t* bar, uint32_t parity) {
     return bounded_wait(bar, parity, &sh.gave_up, p.status, kStatusWaitTimeout);
   };
 
   if (warp == 0) {
     if (elect_lane()) {
-      int it = 0;
+      int it = 0, ahead = 0;       // ahead: blocks of B that are on their way
       bool ok = true;
+      GemmTile e;
+      if (!kPair && Work::early(p, unit, &e)) {
+        for (; ahead < kStages && ahead < e.kn; ++ahead) {
+          mbar_expect(&sh.full[ahead], kBytes);
+          tile_load(smem + ahead * kBytes + kTileBytesA, e.b, ahead * kTileK,
+                    e.b0, &sh.full[ahead]);
+        }
+      }
+      after_prior_launch();
+      const typename Work::State st = Work::template start<kRows>(p);
       for (int t = unit; ok && t < st.n_tiles; t += units) {
         const GemmTile g = Work::template tile<kRows>(p, st, t);
         const int a0 = g.a0 + rank * kTileM;
@@ -160,6 +170,10 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
           }
           const uint32_t at = smem + s * kBytes, bt = at + kTileBytesA;
           const int k = (g.k0 + kb) * kTileK, bk = k + g.b_k;
+          if (it < ahead) {
+            tile_load(at, g.a, k, a0, &sh.full[s]);
+            continue;
+          }
           if (rank == 0) mbar_expect(&sh.full[s], kCtas * kBytes);
           if (kPair) {
             const uint32_t bar = at_rank(&sh.full[s], 0);   // who issues
@@ -200,6 +214,8 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
     if (rank == 0 && elect_lane()) {
       int it = 0, n = 0;
       bool ok = true;
+      after_prior_launch();
+      const typename Work::State st = Work::template start<kRows>(p);
       for (int t = unit; ok && t < st.n_tiles; t += units, ++n) {
         const GemmTile g = Work::template tile<kRows>(p, st, t);
         const uint64_t da = operand_desc(g.a_mn), db = operand_desc(g.b_mn);
@@ -239,6 +255,8 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
     }
     __syncwarp();
   } else if (warp >= 4) {
+    after_prior_launch();
+    const typename Work::State st = Work::template start<kRows>(p);
     Epilogue epi;
     const int quarter = warp & 3;
     epi.row = quarter * 32 + lane;
