@@ -9,12 +9,13 @@
 // less on few rows.
 //   Work::kBf16                   operands bf16 (else fp16)
 //   Work::Params::status          the plan's status word
-//   Work::start<kRows>(params)    what the kernel reads first: State, with the
-//                                 number of tiles of kRows rows (it may come from
-//                                 the device)
-//   Work::tile<kRows>(params, state, t)   operands and extent of tile t (GemmTile)
-//   Work::early(params, t, tile)  whether tile t of one of 128 rows is known, and
-//                                 its B there, before the launch in front has ended
+//   Work::start<kRows>(params)    what the kernel reads first: State (numbers of
+//                                 tiles of kRows rows may come from the device)
+//   Work::tile<kRows>(params, state, u, units, i, tile)   operands and extent
+//                                 (GemmTile) of the i-th tile of CTA or pair u;
+//                                 false past its last
+//   Work::early(params, u, tile)  whether the first tile of CTA u is known, and its
+//                                 B there, before the launch in front has ended
 //   Work::epilogue(params, state, tile, acc, epi)  a row of the accumulator
 // A tile has 256 rows of B.  Operands come through tensor maps with the 128-byte
 // swizzle, K-major (64 of K by all of a CTA's rows) or MN-major (blocks of 64 rows
@@ -158,8 +159,9 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
       }
       after_prior_launch();
       const typename Work::State st = Work::template start<kRows>(p);
-      for (int t = unit; ok && t < st.n_tiles; t += units) {
-        const GemmTile g = Work::template tile<kRows>(p, st, t);
+      GemmTile g;
+      for (int i = 0;
+           ok && Work::template tile<kRows>(p, st, unit, units, i, &g); ++i) {
         const int a0 = g.a0 + rank * kTileM;
         const int b0 = g.b0 + rank * kRowsB<kCtas>;
         for (int kb = 0; kb < g.kn; ++kb, ++it) {
@@ -216,8 +218,8 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
       bool ok = true;
       after_prior_launch();
       const typename Work::State st = Work::template start<kRows>(p);
-      for (int t = unit; ok && t < st.n_tiles; t += units, ++n) {
-        const GemmTile g = Work::template tile<kRows>(p, st, t);
+      GemmTile g;
+      for (; ok && Work::template tile<kRows>(p, st, unit, units, n, &g); ++n) {
         const uint64_t da = operand_desc(g.a_mn), db = operand_desc(g.b_mn);
         const uint32_t sa = operand_step(g.a_mn), sb = operand_step(g.b_mn);
         const uint32_t desc =
@@ -263,8 +265,8 @@ gemm_kernel(const __grid_constant__ typename Work::Params p) {
     epi.out = smem + kStages * kBytes + quarter * (kOutBuffers * kOutBytes);
     epi.n = 0;
     int n = 0;
-    for (int t = unit; t < st.n_tiles; t += units, ++n) {
-      GemmTile g = Work::template tile<kRows>(p, st, t);
+    GemmTile g;
+    for (; Work::template tile<kRows>(p, st, unit, units, n, &g); ++n) {
       g.a0 += rank * kTileM;
       const int acc = n & 1;
       const bool ok = wait(&sh.acc_full[acc], (uint32_t)(n >> 1) & 1u);

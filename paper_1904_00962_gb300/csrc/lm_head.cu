@@ -218,9 +218,12 @@ struct StatsWork {
     return s;
   }
   template <int kRows>
-  static __device__ __forceinline__ GemmTile tile(const Params& p,
-                                                  const State& s, int t) {
-    GemmTile g;
+  static __device__ __forceinline__ bool tile(const Params& p, const State& s,
+                                              int u, int units, int i,
+                                              GemmTile* to) {
+    const int t = u + i * units;
+    if (t >= s.n_tiles) return false;
+    GemmTile& g = *to;
     g.a = &p.hidden;
     g.b = &p.weight;
     g.a0 = (t % s.m_tiles) * kRows;
@@ -231,12 +234,12 @@ struct StatsWork {
     g.b_k = 0;
     g.a_mn = g.b_mn = g.b_blocks = false;
     g.aux = 0;
-    return g;
+    return true;
   }
-  static __device__ __forceinline__ bool early(const Params& p, int t,
+  static __device__ __forceinline__ bool early(const Params& p, int u,
                                                GemmTile* g) {
-    if (p.weight_early) *g = tile<kTileM>(p, State{p.v_tiles, 1, 0}, t);
-    return p.weight_early;
+    return p.weight_early &&
+           tile<kTileM>(p, State{p.v_tiles, 1, 0}, u, 1, 0, g);
   }
   static __device__ __forceinline__ void epilogue(const Params& p,
                                                   const State& s,
@@ -390,9 +393,12 @@ struct DlogitsWork {
     return s;
   }
   template <int kRows>
-  static __device__ __forceinline__ GemmTile tile(const Params& p,
-                                                  const State& s, int t) {
-    GemmTile g;
+  static __device__ __forceinline__ bool tile(const Params& p, const State& s,
+                                              int u, int units, int i,
+                                              GemmTile* to) {
+    const int t = u + i * units;
+    if (t >= s.n_tiles) return false;
+    GemmTile& g = *to;
     g.a = &p.hidden;
     g.b = &p.weight;
     g.a0 = (t % s.m_tiles) * kRows;
@@ -403,12 +409,12 @@ struct DlogitsWork {
     g.b_k = 0;
     g.a_mn = g.b_mn = g.b_blocks = false;
     g.aux = 0;
-    return g;
+    return true;
   }
-  static __device__ __forceinline__ bool early(const Params& p, int t,
+  static __device__ __forceinline__ bool early(const Params& p, int u,
                                                GemmTile* g) {
-    if (p.weight_early) *g = tile<kTileM>(p, State{p.v_tiles, 1, 0}, t);
-    return p.weight_early;
+    return p.weight_early &&
+           tile<kTileM>(p, State{p.v_tiles, 1, 0}, u, 1, 0, g);
   }
   // Rows past the last and columns past the vocabulary are zeros: the products
   // run over whole tiles.
@@ -469,7 +475,7 @@ struct GradsParams {
   uint32_t* status;
   int64_t weight_stride, hidden_stride;
   int slab_rows;          // of a slab; 0: one sum, written out
-  int w_tiles;            // tiles of dW (taken first)
+  int w_tiles;            // tiles of dW
   int d_tiles;            // column tiles of the width
   int width, vocab, v0, piece;
   int k_piece, splits;    // blocks of K of dh, parts that they are cut into
@@ -529,9 +535,14 @@ __device__ __forceinline__ void store_row(void* base, int64_t at,
 }
 
 struct GradsState {
-  int n_tiles, rows, k_rows;
+  int rows, k_rows;
+  int h_tiles;            // tiles of dh
 };
 
+// dh's tiles run over the piece's columns, dW's over the rows.  Unit u of U takes
+// dh's tiles u, u + U, ..; the units that then have one less take as many of dW's
+// as come to the same blocks of K, and the rest of dW goes round, those units first.
+// (One list in turn left the longest unit a quarter above the mean at 2458 x 768.)
 struct GradsWork {
   typedef GradsParams Params;
   typedef GradsState State;
@@ -541,27 +552,18 @@ struct GradsWork {
     State s;
     s.rows = *p.n_rows;
     s.k_rows = s.rows ? (s.rows + kTileK - 1) / kTileK : 1;   // of zeros
-    s.n_tiles = p.w_tiles +
-                (s.rows + kRows - 1) / kRows * p.d_tiles * p.splits;
+    s.h_tiles = (s.rows + kRows - 1) / kRows * p.d_tiles * p.splits;
     return s;
   }
   template <int kRows>
-  static __device__ __forceinline__ GemmTile tile(const Params& p,
-                                                  const State& s, int t) {
-    GemmTile g;
-    if (t < p.w_tiles) {
-      g.what = 0;
-      g.aux = 0;
-      g.a = &p.dl_cols;
-      g.b = &p.hidden;
-      g.a0 = t / p.d_tiles * kRows;
-      g.b0 = t % p.d_tiles * kTileN;
-      g.k0 = 0;
-      g.kn = s.k_rows;
-      g.b_k = 0;
-      g.a_mn = g.b_mn = g.b_blocks = true;
-    } else {
-      t -= p.w_tiles;
+  static __device__ __forceinline__ bool tile(const Params& p, const State& s,
+                                              int u, int units, int i,
+                                              GemmTile* to) {
+    GemmTile& g = *to;
+    const int turns = s.h_tiles / units, over = s.h_tiles - turns * units;
+    const int own = turns + (u < over);
+    if (i < own) {
+      int t = u + i * units;
       g.what = 1;
       g.aux = t % p.splits;
       t /= p.splits;
@@ -575,8 +577,32 @@ struct GradsWork {
       g.a_mn = false;
       g.b_mn = true;
       g.b_blocks = p.weight_blocks;
+      return true;
     }
-    return g;
+    i -= own;
+    // dW's tiles that even out the units without the last of dh's
+    const int less = units - over;
+    int even = over ? p.k_piece / p.splits / s.k_rows : 0;
+    even = min(even, p.w_tiles / less);
+    int t;
+    if (u >= over && i < even) {
+      t = u - over + i * less;
+    } else {
+      if (u >= over) i -= even;
+      t = even * less + (u >= over ? u - over : u + less) + i * units;
+      if (t >= p.w_tiles) return false;
+    }
+    g.what = 0;
+    g.aux = 0;
+    g.a = &p.dl_cols;
+    g.b = &p.hidden;
+    g.a0 = t / p.d_tiles * kRows;
+    g.b0 = t % p.d_tiles * kTileN;
+    g.k0 = 0;
+    g.kn = s.k_rows;
+    g.b_k = 0;
+    g.a_mn = g.b_mn = g.b_blocks = true;
+    return true;
   }
   static __device__ __forceinline__ bool early(const Params&, int, GemmTile*) {
     return false;         // dlogits and the rows come from the launches in front
@@ -811,10 +837,17 @@ lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "head join launch");
 }
 
+// Parts of dh's K: dh of few tokens is few tiles over a long K, cut so that every
+// CTA or pair has one.
+int64_t head_parts(int64_t units, int64_t h_tiles, int64_t k_blocks) {
+  return std::max<int64_t>(1, std::min(units / h_tiles,
+                                       k_blocks / kMinPartBlocks));
+}
+
 // Columns of a piece of the vocabulary, in whole tiles: of the counts of pieces
 // that the workspace allows, the one whose products' tiles (rows of dW over all
 // tokens, rows of dh over the piece) fall best on `units` CTAs or pairs.  9830 x
-// 30522 x 1024, us: pieces of equal width 1827, so chosen 1639.
+// 30522 x 1024, us: the fewest pieces 1827, so chosen 1639.
 int64_t piece_width(const lamb_vocab* v, int64_t n, int rows, int units) {
   const int64_t whole = lm_round_up(n, kRowsWhole);
   const int64_t most = v->dlogits_elems / whole / kTileN * kTileN;
@@ -827,12 +860,18 @@ int64_t piece_width(const lamb_vocab* v, int64_t n, int rows, int units) {
     const int64_t piece =
         lm_round_up(lm_ceil_div(v->vocab, np), kTileN);
     const int64_t w_tiles = lm_ceil_div(piece, rows) * d_tiles;
-    int64_t longest = 0;
-    for (int64_t u = 0; u < units; ++u) {      // tiles u, u + units, ...
-      const int64_t all = lm_ceil_div(w_tiles + h_tiles - u, units);
-      const int64_t w = u < w_tiles ? lm_ceil_div(w_tiles - u, units) : 0;
-      longest = std::max(longest, w * w_blocks + (all - w) * (piece / kTileK));
-    }
+    // (as GradsWork::tile hands them out)
+    const int64_t parts = head_parts(units, h_tiles, piece / kTileK);
+    const int64_t h = piece / kTileK / parts, hs = h_tiles * parts;
+    const int64_t turns = hs / units, over = hs % units, less = units - over;
+    const int64_t even =
+        over ? std::min(h / w_blocks, w_tiles / less) : 0;
+    const int64_t rest = w_tiles - even * less;
+    const int64_t longest =
+        std::max((turns + (over > 0)) * h +
+                     lm_ceil_div(std::max<int64_t>(rest - less, 0), units) *
+                         w_blocks * (over > 0),
+                 turns * h + (even + lm_ceil_div(rest, units)) * w_blocks);
     // two launches and their tails are worth some blocks more
     const int64_t cost =
         lm_ceil_div(v->vocab, piece) * (longest + kPieceBlocks);
@@ -1031,9 +1070,8 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
                  grad_weight_stride % (f32 ? 4 : 8) == 0;
   g.hidden_vec =
       (uintptr_t)grad_hidden % 16 == 0 && grad_hidden_stride % 8 == 0;
-  // dh of few tokens is few tiles over a long K: cut K so that every SM has one
   const int k_first = (int)lm_ceil_div(std::min(piece, v->vocab), kTileK);
-  g.splits = std::max(1, std::min(units / h_tiles, k_first / kMinPartBlocks));
+  g.splits = (int)head_parts(units, h_tiles, k_first);
   g.slab_rows = pieces > 1 || g.splits > 1 ? m_tiles * rows : 0;
   const int pitch = (int)lm_round_up(v->width, 4);
   if (g.slab_rows &&
