@@ -420,7 +420,8 @@ cudaError_t small_smem_limit(int64_t bytes) {
 using namespace lamb;
 
 struct lamb_muon {
-  int device = 0, pairs = 0, n = 0;
+  int device = 0, units = 0, n = 0;
+  bool pair = false;                   // tiles by pairs of CTAs
   bool grad_bf16 = false, copy = false;
   bool bound = false, bound_direction = false;
   void* arena = nullptr;
@@ -430,7 +431,6 @@ struct lamb_muon {
   MuonPtrs* dir_ptrs = nullptr;        // of the direction
   MuonChunk* chunks = nullptr;
   MuonTile* tiles = nullptr;
-  MuonSpan* spans = nullptr;
   uint32_t* done = nullptr;
   double* part = nullptr;
   int* small = nullptr;                // matrices of the small kernel
@@ -438,24 +438,33 @@ struct lamb_muon {
   int64_t small_bytes = 0;             // shared memory of the largest
   uint32_t* status = nullptr;
   std::vector<int64_t> numel;
-  int n_chunks = 0, n_spans = 0;
+  int n_chunks = 0;
   int64_t step_tiles = 0;              // tiles of one step of all matrices
 };
 
 namespace {
 
-// Bytes of the working matrices of a set: two sets go through their steps at a
-// time and have to share L2.
-constexpr int64_t kMuonSetBytes = 1ll << 40;
+// Up to so many tiles of 256 x 256 for a pair of CTAs, the smaller ones are taken.
+// Measured (us, the whole call; tiles of 128 | of 256), by tiles for a pair of 76:
+//   512 x 512            0.05    115 | 146
+//   1024 x 1024          0.2     139 | 184
+//   1024 x 4096          0.8     221 | 258
+//   9 of 1000 x 500      0.9     184 | 212
+//   1536 x 4096          1.3     285 | 330
+//   8 of 1024 x 1024     1.7     240 | 239
+//   a BERT-large layer   2.5     350 | 353
+//   16 of 1024 x 1024    3.4     488 | 373
+//   BERT-base            18     2021 | 1690 (the whole step)
+constexpr int64_t kSingleTiles = 2;
 
 struct MuonLayout {
   std::vector<MuonMatrix> mats;
   std::vector<MuonChunk> chunks;
   std::vector<MuonTile> tiles;
-  std::vector<MuonSpan> spans;
   std::vector<int> small;
   std::vector<int64_t> at[7];     // byte offsets in the workspace, per matrix
   int64_t work_bytes = 0;
+  bool pair = false;
 };
 
 int64_t take(int64_t* used, int64_t bytes) {
@@ -464,13 +473,12 @@ int64_t take(int64_t* used, int64_t bytes) {
   return at;
 }
 
-// Workspace offsets, chunks, sets and tiles of the matrices (host only).
+// Workspace offsets, chunks and tiles of the matrices (host only).
 void muon_layout(const int64_t* rows, const int64_t* cols, int n,
-                 const uint8_t* mask, MuonLayout* L) {
+                 const uint8_t* mask, int pairs, MuonLayout* L) {
   L->mats.resize(n);
   for (auto& v : L->at) v.assign(n, 0);
   std::vector<int> large;
-  std::vector<int64_t> bytes(n, 0);
   int64_t used = 0;
   for (int k = 0; k < n; ++k) {
     MuonMatrix& x = L->mats[k];
@@ -492,11 +500,9 @@ void muon_layout(const int64_t* rows, const int64_t* cols, int n,
     }
     const int64_t sx = (int64_t)x.rows * x.pitch * 2;
     const int64_t sm = (int64_t)x.m * x.pitch_m * 2;
-    const int64_t before = used;
     for (int i = 0; i < 3; ++i) L->at[i][k] = take(&used, sx);
     for (int i = 3; i < 5; ++i) L->at[i][k] = take(&used, sm);
     for (int i = 5; i < 7; ++i) L->at[i][k] = take(&used, x.m * 4ll);
-    bytes[k] = used - before;
     large.push_back(k);
     x.first_chunk = (int)L->chunks.size();
     const int64_t total = (int64_t)x.rows * x.cols;
@@ -504,62 +510,65 @@ void muon_layout(const int64_t* rows, const int64_t* cols, int n,
       L->chunks.push_back(
           {k, (int)std::min<int64_t>(kMuonChunk, total - o), o});
     x.n_chunks = (int)L->chunks.size() - x.first_chunk;
-    // a CTA that has no rows of a tile does not count it
-    for (int i = 0; i * kMuonRows < x.m; ++i)
-      x.sym += (int)lm_ceil_div(x.m, kMuonTile) - i * kMuonRows / kMuonTile;
-    x.app = (int)(lm_ceil_div(x.rows, kMuonRows) *
-                  lm_ceil_div(x.cols, kMuonTile));
   }
   L->work_bytes = used;
   if (large.empty()) return;
 
-  // an even number of sets of about equal work, the largest matrices first, each
-  // to the set that has least so far
+  // Tiles of 256 x 256 by pairs of CTAs copy half the operands for a product, tiles
+  // of 128 x 128 by single ones end sooner and are more: those where the others
+  // would be too few.
+  int64_t tiles = 0;
+  for (int k : large)
+    tiles += lm_ceil_div(L->mats[k].rows, 256) *
+             lm_ceil_div(L->mats[k].cols, 256);
+  L->pair = tiles > kSingleTiles * pairs;
+  const int tile = L->pair ? 2 * kMuonRows : kMuonRows;
+  for (int k : large) {
+    MuonMatrix& x = L->mats[k];
+    // a CTA that has no rows of a tile does not count it
+    for (int i = 0; i * kMuonRows < x.m; ++i)
+      x.sym += (int)lm_ceil_div(x.m, tile) - i * kMuonRows / tile;
+    x.app = (int)(lm_ceil_div(x.rows, kMuonRows) * lm_ceil_div(x.cols, tile));
+  }
+
+  // two sets of about equal work, the largest matrices first, each to the set that
+  // has less so far
   auto work = [&](int k) {
     const MuonMatrix& x = L->mats[k];
     return (double)x.m * x.m * x.n;
   };
   std::stable_sort(large.begin(), large.end(),
                    [&](int p, int q) { return work(p) > work(q); });
-  const int64_t pairs = lm_ceil_div(used, 2 * kMuonSetBytes);
-  const int sets =
-      (int)std::min<int64_t>(2 * pairs, (int64_t)large.size());
-  std::vector<std::vector<int>> set(sets);
-  std::vector<double> load(sets, 0.0);
+  std::vector<int> set[2];
+  double load[2] = {0.0, 0.0};
   for (int k : large) {
-    const int to = (int)(std::min_element(load.begin(), load.end()) -
-                         load.begin());
+    const int to = load[1] < load[0];
     set[to].push_back(k);
     load[to] += work(k);
   }
-  // the tiles of one step of two sets: product by product, the sets in turn, long
-  // products first
-  for (int s = 0; s < sets; s += 2) {
-    const int first = (int)L->tiles.size();
-    for (int phase = kGram; phase <= kApply; ++phase)
-      for (int h = s; h < std::min(s + 2, sets); ++h) {
-        std::stable_sort(set[h].begin(), set[h].end(), [&](int p, int q) {
-          const MuonMatrix &x = L->mats[p], &y = L->mats[q];
-          return phase == kGram ? x.n > y.n : x.m > y.m;
-        });
-        for (int k : set[h]) {
-          const MuonMatrix& x = L->mats[k];
-          const int r = phase == kApply ? x.rows : x.m;
-          const int c = phase == kApply ? x.cols : x.m;
-          for (int i = 0; i * kMuonTile < r; ++i)
-            for (int j = phase == kApply ? 0 : i; j * kMuonTile < c; ++j)
-              {
-              MuonTile t = {};
-              t.matrix = k;
-              t.i = i;
-              t.j = j;
-              t.phase = phase;
-              L->tiles.push_back(t);
-            }
-        }
+  // the tiles of one step: product by product, the sets in turn, long products
+  // first
+  for (int phase = kGram; phase <= kApply; ++phase)
+    for (std::vector<int>& of : set) {
+      std::stable_sort(of.begin(), of.end(), [&](int p, int q) {
+        const MuonMatrix &x = L->mats[p], &y = L->mats[q];
+        return phase == kGram ? x.n > y.n : x.m > y.m;
+      });
+      for (int k : of) {
+        const MuonMatrix& x = L->mats[k];
+        const int r = phase == kApply ? x.rows : x.m;
+        const int c = phase == kApply ? x.cols : x.m;
+        for (int i = 0; i * tile < r; ++i)
+          for (int j = phase == kApply ? 0 : i; j * tile < c; ++j) {
+            MuonTile t = {};
+            t.matrix = k;
+            t.i = i;
+            t.j = j;
+            t.phase = phase;
+            L->tiles.push_back(t);
+          }
       }
-    L->spans.push_back({first, (int)L->tiles.size() - first});
-  }
+    }
 }
 
 lamb_status_t muon_check(const lamb_muon* p, const lamb_muon_hyper_t* h) {
@@ -642,13 +651,12 @@ lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess && p->step_tiles) {
     q.tiles = p->tiles;
-    q.spans = p->spans;
-    q.n_spans = p->n_spans;
     q.done = p->done;
     q.steps = h->steps;
     q.n_mats = p->n;
+    q.step_tiles = (int)p->step_tiles;
     q.total = (int)(p->step_tiles * h->steps);
-    e = muon_launch_steps(q, p->pairs, stream);
+    e = muon_launch_steps(q, p->pair, p->units, stream);
   }
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "muon launch");
 }
@@ -707,18 +715,23 @@ extern "C" lamb_status_t lamb_muon_create(
     p->copy = copy_dtype == LAMB_BF16;
     for (int k = 0; k < n_matrices; ++k) p->numel.push_back(rows[k] * cols[k]);
     MuonLayout L;
-    muon_layout(rows, cols, n_matrices, decay_mask, &L);
+    int sms = 0, ctas = 0, pairs = 0;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = muon_steps_setup(sms, &ctas, &pairs);
+    if (e != cudaSuccess) {
+      lamb_muon_destroy(p);
+      return lm_cuda_fail(e, what);
+    }
+    muon_layout(rows, cols, n_matrices, decay_mask, pairs, &L);
+    p->pair = L.pair;
+    p->units = L.pair ? pairs : ctas;
     p->n_chunks = (int)L.chunks.size();
-    p->n_spans = (int)L.spans.size();
     p->step_tiles = (int64_t)L.tiles.size();
     if (p->step_tiles * 64 > INT32_MAX || L.chunks.size() > INT32_MAX) {
       lamb_muon_destroy(p);
       return lm_fail(LAMB_ERR_INVALID_ARG, "the matrices have too many tiles");
     }
     const EncodeTiled encode = lm_encoder();
-    int sms = 0;
-    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = muon_steps_setup(sms, &p->pairs);
     LmArena a;
     for (int pass = 0; e == cudaSuccess && pass < 2; ++pass) {
       a.used = 0;
@@ -728,7 +741,6 @@ extern "C" lamb_status_t lamb_muon_create(
       a.take(&p->dir_ptrs, n_matrices);
       a.take(&p->chunks, (int64_t)L.chunks.size());
       a.take(&p->tiles, (int64_t)L.tiles.size());
-      a.take(&p->spans, (int64_t)L.spans.size());
       a.take(&p->done, n_matrices);
       a.take(&p->part, (int64_t)L.chunks.size());
       a.take(&p->small, (int64_t)L.small.size());
@@ -813,9 +825,6 @@ extern "C" lamb_status_t lamb_muon_create(
     if (e == cudaSuccess && !L.tiles.empty())
       e = cudaMemcpy(p->tiles, L.tiles.data(),
                      L.tiles.size() * sizeof(MuonTile), cudaMemcpyHostToDevice);
-    if (e == cudaSuccess && !L.spans.empty())
-      e = cudaMemcpy(p->spans, L.spans.data(),
-                     L.spans.size() * sizeof(MuonSpan), cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
   } catch (const std::bad_alloc&) {
     lamb_muon_destroy(p);

@@ -67,12 +67,6 @@ struct __align__(16) MuonTile {
   float *diag, *beta;
   int rows, cols;
 };
-// Tiles of matrices that go through their steps side by side, in the order of
-// one step.
-struct MuonSpan {
-  int first, count;
-};
-
 struct MuonConsts {
   float a, b, c;
   float beta, omb;               // momentum
@@ -84,14 +78,13 @@ struct MuonConsts {
 struct MuonParams {
   const MuonMatrix* mats;
   const MuonPtrs* ptrs;
-  const MuonTile* tiles;
-  const MuonSpan* spans;
+  const MuonTile* tiles;         // of one step
   uint32_t* done;                // CTAs' tiles of each matrix finished
   const float* d_lr;             // NULL: the direction alone
   uint32_t* status;
   MuonConsts k;
-  int n_mats, n_spans, steps;
-  int total;                     // tiles of all steps
+  int n_mats, steps;
+  int step_tiles, total;         // tiles of one step, of all
 };
 
 // s of a matrix.
@@ -114,13 +107,13 @@ __device__ __forceinline__ uint16_t half_bits(uint32_t w, int i) {
   return (uint16_t)(i ? w >> 16 : w & 0xffffu);
 }
 
-constexpr int kMuonTile = 256;        // a tile's rows and columns
-constexpr int kMuonRows = 128;        // rows of it a CTA has
+constexpr int kMuonRows = 128;        // rows of a tile that a CTA has
 constexpr int kMuonCols = 32;                       // columns of a block
 
-// lm_muon_steps.cu.  Setup: how many pairs of CTAs the current device holds.
-cudaError_t muon_steps_setup(int sms, int* pairs);
-cudaError_t muon_launch_steps(const MuonParams& p, int pairs,
+// lm_muon_steps.cu: tiles of 128 x 128 by single CTAs, or of 256 x 256 by pairs.
+// Setup: how many of either the current device holds at a time.
+cudaError_t muon_steps_setup(int sms, int* ctas, int* pairs);
+cudaError_t muon_launch_steps(const MuonParams& p, bool pair, int units,
                               cudaStream_t stream);
 
 }  // namespace lamb

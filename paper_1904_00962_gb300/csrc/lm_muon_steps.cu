@@ -2,18 +2,19 @@
 //
 // Per matrix and step: G = X X^T, G G, and (b G + c G G) X (lm_muon.cu has the
 // splitting of G and X that keeps their precision).  A tile is 256 x 256 of one
-// product; the symmetric ones are taken on and above the diagonal only.  A pair of
-// CTAs multiplies it (cta_group::2), 128 rows each: an operand block is copied to
-// one of them only, so that a stage takes 32 KB and four of them fit beside the
-// epilogue's buffers.
+// product, multiplied by a pair of CTAs (cta_group::2), 128 rows each, which copies
+// an operand block to one of them only; or, where that makes too few tiles, 128 x
+// 128 by one CTA.  A CTA's stage takes 32 KB either way, and four of them fit beside
+// the epilogue's buffers.  The symmetric products' tiles are taken on and above the
+// diagonal only.
 //
-// Persistent pairs, one CTA an SM, take the tiles of one list in turn.  Two sets
-// of matrices go through their steps side by side in it, so that while the last
-// tiles of one set's product are still in work the other set's fill the SMs.  A
-// tile of a product waits for all tiles of the product before it of the same
-// matrix (a counter for each matrix).  Those come earlier in the list, which every
-// pair takes in order, so the earliest unfinished tile waits for nothing; all CTAs
-// are resident (cooperative launch).  Waits are bounded.
+// Persistent CTAs or pairs, one CTA an SM, take the tiles of one list in turn.  Two
+// sets of matrices go through their steps side by side in it, so that while the last
+// tiles of one set's product are still in work the other set's fill the SMs.  A tile
+// of a product waits for all tiles of the product before it of the same matrix (a
+// counter for each matrix).  Those come earlier in the list, which everybody takes
+// in order, so the earliest unfinished tile waits for nothing; all CTAs are resident
+// (cooperative launch).  Waits are bounded.
 //
 // Warps: 0 lists tiles and copies operands, 1 issues the products, 2 copies the
 // epilogue's blocks in (and holds the tensor memory), 3 copies them out, 4-7 and
@@ -24,11 +25,12 @@
 // as done when those have landed.  Warp 0 reads the list a tile ahead and leaves in
 // shared memory all that the other warps need of a tile.
 //
-// Measured: one BERT-large layer (four 1024 x 1024, two 4096 x 1024) 312 us, bound
-// by the chain of a matrix' products (64 blocks of K, the epilogue's drain, the
-// counters); all matrices of BERT-base 1350 us, bound by HBM: X, D and E take some
-// 1.2 GB a step and do not fit L2.  Sets that do (56 MB each) wait for one another's
-// products instead: 1500 us.  On the way there (both cases, us, with the momentum's
+// Measured: one 1024 x 1024 matrix 139 us with the momentum's launches, 15 products
+// one behind another; one BERT-large layer (four 1024 x 1024, two 4096 x 1024) 308
+// us, bound by the chain of a matrix' products (64 blocks of K, the epilogue's drain,
+// the counters); all matrices of BERT-base 1350 us, bound by HBM: X, D and E take
+// some 1.2 GB a step and do not fit L2.  Sets that do (56 MB each) wait for one
+// another's products instead: 1500 us.  On the way there (both cases, us, with the momentum's
 // launches): a launch a product with a CTA a tile 550 / 2909, one launch 419 / 2336,
 // all matrices in two sets 419 / 1812, pairs of CTAs 353 / 1683.  X in fp32 beside hi
 // in place of lo: 411 / 1963.
@@ -51,10 +53,13 @@ constexpr int kStepThreads = 128 + kGroups * kEpiThreads;
 // readers of a listed tile: products, copies in, copies out, epilogue
 constexpr int kReaders = 3 + 4 * kGroups;
 // l or beta of a tile's columns, and of its rows
-constexpr int kColBytes = kTileN * 4, kVecBytes = kColBytes + kTileM * 4;
+constexpr int kColBytes = 2 * kTileM * 4, kVecBytes = kColBytes + kTileM * 4;
 constexpr size_t kSmem = (size_t)kStages * kStageBytes +
                          kBuffers * kBufferBytes + kRing * kVecBytes + 1024;
-static_assert(kTileM == kMuonRows && kTileN == kMuonTile, "tiles");
+static_assert(kTileM == kMuonRows, "tiles");
+// a tile's rows and columns: of one CTA, of a pair
+template <int kCtas>
+constexpr int kTile = kTileM * kCtas;
 
 struct Listed : MuonTile {
   int it;                // step
@@ -95,8 +100,9 @@ __device__ __forceinline__ uint32_t mirrored(uint32_t base, int j, int i) {
 }
 // Whether the block of rows c0 .. and columns a0 .. lies in no tile on or above
 // the diagonal.
+template <int kCtas>
 __device__ __forceinline__ bool mirror(int a0, int c0) {
-  return a0 / kMuonTile < c0 / kMuonTile;
+  return a0 / kTile<kCtas> < c0 / kTile<kCtas>;
 }
 
 __device__ __forceinline__ bool ready(const MuonParams& p, const Listed& d) {
@@ -129,28 +135,24 @@ __device__ __forceinline__ const Listed* next_tile(Shared& sh,
 }
 
 // ---- warp 0 -------------------------------------------------------------------
-// Walks over this pair's tiles of the list.
+// Walks over this CTA's or pair's tiles of the list, step after step.
 struct Lister {
-  int t, span, base;
-  MuonSpan s;
+  int t, units;
   __device__ __forceinline__ void next(const MuonParams& p, Listed& d) {
     d.phase = kNoTile;
     if (t < p.total) {
-      while (t - base >= s.count * p.steps) {
-        base += s.count * p.steps;
-        s = p.spans[++span];
-      }
-      const int it = (t - base) / s.count;
-      static_cast<MuonTile&>(d) = p.tiles[s.first + (t - base) - it * s.count];
+      const int it = t / p.step_tiles;
+      static_cast<MuonTile&>(d) = p.tiles[t - it * p.step_tiles];
       d.it = it;
     }
-    t += gridDim.x / 2;
+    t += units;
   }
 };
 
+template <int kCtas>
 __device__ __forceinline__ void copy_operands(Shared& sh, const MuonParams& p,
                                               uint32_t smem, uint32_t rank) {
-  Lister list = {(int)blockIdx.x / 2, 0, 0, p.spans[0]};
+  Lister list = {(int)blockIdx.x / kCtas, (int)gridDim.x / kCtas};
   Listed ahead;
   list.next(p, ahead);
   int it = 0;
@@ -183,8 +185,8 @@ __device__ __forceinline__ void copy_operands(Shared& sh, const MuonParams& p,
       ma = d.tall ? &x->x_k[from] : &x->e;
       mb = d.tall ? &x->e : &x->x_mn[from];
     }
-    const int a0 = d.i * kMuonTile + (int)rank * kTileM;
-    const int b0 = d.j * kMuonTile + (int)rank * kTileM;
+    const int a0 = d.i * kTile<kCtas> + (int)rank * kTileM;
+    const int b0 = d.j * kTile<kCtas> + (int)rank * kTileM;
     if (!wait_ready(sh, p, d)) break;
     fence_proxy_async();       // other CTAs' blocks, to be read by copies
     for (int kb = 0; kb < kn; ++kb, ++it) {
@@ -192,14 +194,21 @@ __device__ __forceinline__ void copy_operands(Shared& sh, const MuonParams& p,
       if (!wait_on(sh, p, &sh.empty[s], ((uint32_t)(it / kStages) & 1u) ^ 1u))
         break;
       const uint32_t at = smem + s * kStageBytes;
-      const uint32_t bar = at_rank(&sh.full[s], 0);    // the issuing CTA's
       const int k = kb * kTileK;
-      if (rank == 0) mbar_expect(&sh.full[s], 2 * kStageBytes);
+      if (rank == 0) mbar_expect(&sh.full[s], kCtas * kStageBytes);
       // (issuing a copy takes this thread some 100 cycles: one an operand)
-      if (gram_mn) pair_blocks_load(at, ma, k, a0 / 64, bar);
-      else pair_tile_load(at, ma, k, a0, bar);
-      if (b_mn) pair_blocks_load(at + kTileBytesA, mb, k, b0 / 64, bar);
-      else pair_tile_load(at + kTileBytesA, mb, k, b0, bar);
+      if (kCtas == 2) {
+        const uint32_t bar = at_rank(&sh.full[s], 0);    // the issuing CTA's
+        if (gram_mn) pair_blocks_load(at, ma, k, a0 / 64, bar);
+        else pair_tile_load(at, ma, k, a0, bar);
+        if (b_mn) pair_blocks_load(at + kTileBytesA, mb, k, b0 / 64, bar);
+        else pair_tile_load(at + kTileBytesA, mb, k, b0, bar);
+      } else {
+        if (gram_mn) blocks_load(at, ma, k, a0 / 64, &sh.full[s]);
+        else tile_load(at, ma, k, a0, &sh.full[s]);
+        if (b_mn) blocks_load(at + kTileBytesA, mb, k, b0 / 64, &sh.full[s]);
+        else tile_load(at + kTileBytesA, mb, k, b0, &sh.full[s]);
+      }
     }
     if (sh.gave_up) break;
   }
@@ -213,6 +222,7 @@ __device__ __forceinline__ void copy_operands(Shared& sh, const MuonParams& p,
 }
 
 // ---- warp 1 -------------------------------------------------------------------
+template <int kCtas>
 __device__ __forceinline__ void multiply(Shared& sh, const MuonParams& p,
                                          uint32_t smem, uint32_t tmem,
                                          uint32_t rank) {
@@ -225,12 +235,14 @@ __device__ __forceinline__ void multiply(Shared& sh, const MuonParams& p,
     if (rank) continue;        // the other CTA issues
     const uint64_t da = operand_desc(a_mn), db = operand_desc(b_mn);
     const uint32_t sa = operand_step(a_mn), sb = operand_step(b_mn);
-    const uint32_t desc = product_desc(false, a_mn, b_mn, kMuonTile, kMuonTile);
+    const uint32_t desc =
+        product_desc(false, a_mn, b_mn, kTile<kCtas>, kTile<kCtas>);
     const int acc = n & 1;
-    const uint32_t to = tmem + acc * kTileN;
+    const uint32_t to = tmem + acc * kTile<kCtas>;
     const uint32_t ph = ((uint32_t)(n >> 1) & 1u) ^ 1u;
     if (!wait_on(sh, p, &sh.acc_empty[acc], ph)) return;
-    mbar_try_cluster(&sh.acc_empty[acc], ph);      // the other CTA's readers
+    if (kCtas == 2)
+      mbar_try_cluster(&sh.acc_empty[acc], ph);      // the other CTA's readers
     tmem_after_sync();
     for (int kb = 0; kb < kn; ++kb, ++it) {
       const int s = it % kStages;
@@ -239,34 +251,45 @@ __device__ __forceinline__ void multiply(Shared& sh, const MuonParams& p,
       const uint32_t at = smem + s * kStageBytes;
       const uint64_t a = da | (at >> 4), b = db | ((at + kTileBytesA) >> 4);
 #pragma unroll
-      for (int k = 0; k < kTileK / 16; ++k)
-        pair_product(to, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
-      pair_products_arrive(&sh.empty[s]);
+      for (int k = 0; k < kTileK / 16; ++k) {
+        if (kCtas == 2)
+          pair_product(to, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
+        else
+          product(to, a + k * sa, b + k * sb, desc, kb > 0 || k > 0);
+      }
+      if (kCtas == 2) pair_products_arrive(&sh.empty[s]);
+      else products_arrive(&sh.empty[s]);
     }
-    pair_products_arrive(&sh.acc_full[acc]);
+    if (kCtas == 2) pair_products_arrive(&sh.acc_full[acc]);
+    else products_arrive(&sh.acc_full[acc]);
   }
 }
 
 // ---- warp 2 -------------------------------------------------------------------
 // This CTA's first row of a tile.
+template <int kCtas>
 __device__ __forceinline__ int row0(const Listed& d) {
-  return d.i * kMuonTile + (int)cluster_rank() * kTileM;
+  return d.i * kTile<kCtas> + (kCtas == 2 ? (int)cluster_rank() * kTileM : 0);
 }
 // Blocks of this CTA's part of a tile: none where that is past the last row.
+template <int kCtas>
 __device__ __forceinline__ int block_count(const Listed& d) {
-  if (row0(d) >= d.height) return 0;
-  const int left = (d.width - d.j * kTileN + kMuonCols - 1) / kMuonCols;
-  return left < kTileN / kMuonCols ? left : kTileN / kMuonCols;
+  if (row0<kCtas>(d) >= d.height) return 0;
+  constexpr int kMost = kTile<kCtas> / kMuonCols;
+  const int left =
+      (d.width - d.j * kTile<kCtas> + kMuonCols - 1) / kMuonCols;
+  return left < kMost ? left : kMost;
 }
 
+template <int kCtas>
 __device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
                                         uint32_t staging) {
   int n = 0, begun = 0;       // blocks, tiles whose copies were started
   for (int tile = 0; const Listed* l = next_tile(sh, p, tile); ++tile) {
     const Listed& d = *l;
     const MuonMatrix* const x = d.x;
-    const int blocks = block_count(d), phase = d.phase;
-    const int a0 = row0(d), b0 = d.j * kTileN;
+    const int blocks = block_count<kCtas>(d), phase = d.phase;
+    const int a0 = row0<kCtas>(d), b0 = d.j * kTile<kCtas>;
     const uint32_t vec = staging + kBuffers * kBufferBytes +
                          tile % kRing * kVecBytes;
     uint64_t* const vb = &sh.vec[tile % kRing];
@@ -280,9 +303,9 @@ __device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
       // the tile's l or beta (their memory goes up to a whole tile)
       const bool cols = phase == kSquare || d.tall;
       const bool rows = phase == kSquare || !d.tall;
-      mbar_expect(vb, (cols ? kColBytes : 0) + (rows ? kTileM * 4 : 0));
+      mbar_expect(vb, (cols ? kTile<kCtas> * 4 : 0) + (rows ? kTileM * 4 : 0));
       const float* const v = phase == kSquare ? d.diag : d.beta;
-      if (cols) bulk_load_at(vec, v + b0, kColBytes, vb);
+      if (cols) bulk_load_at(vec, v + b0, kTile<kCtas> * 4, vb);
       if (rows) bulk_load_at(vec + kColBytes, v + a0, kTileM * 4, vb);
     }
     begun = tile + 1;
@@ -312,13 +335,15 @@ __device__ __forceinline__ void copy_in(Shared& sh, const MuonParams& p,
 }
 
 // ---- warp 3 -------------------------------------------------------------------
+template <int kCtas>
 __device__ __forceinline__ void copy_out(Shared& sh, const MuonParams& p,
                                          uint32_t staging) {
   int n = 0;
   for (int tile = 0; const Listed* l = next_tile(sh, p, tile); ++tile) {
     const MuonMatrix* const x = l->x;
-    const int blocks = block_count(*l), m = l->height, matrix = l->matrix;
-    const int a0 = row0(*l), b0 = l->j * kTileN, phase = l->phase;
+    const int blocks = block_count<kCtas>(*l), m = l->height, matrix = l->matrix;
+    const int a0 = row0<kCtas>(*l), b0 = l->j * kTile<kCtas>;
+    const int phase = l->phase;
     const bool last = l->last;
     const CUtensorMap* const to = phase == kApply ? &x->x_c[(l->it & 1) ^ 1]
                                   : phase == kGram ? &x->d_c
@@ -337,7 +362,7 @@ __device__ __forceinline__ void copy_out(Shared& sh, const MuonParams& p,
       tile_store(to, c0, a0, from);
       if (phase == kApply) {
         tile_store(&x->lo_c, c0, a0, from + kBlockBytes);
-      } else if (mirror(a0, c0)) {
+      } else if (mirror<kCtas>(a0, c0)) {
         tile_store(to_t, a0, c0, from + kBlockBytes);
         if (a0 + 64 < m)
           tile_store(to_t, a0 + 64, c0,
@@ -406,9 +431,8 @@ struct Row {
 template <bool kSq>
 __device__ __forceinline__ void symmetric_block(float pb, float pc, int m,
                                                 float* diag, float li, float s,
-                                                int a0, int c0, const Row& r,
+                                                bool both, int c0, const Row& r,
                                                 float (&y)[32]) {
-  const bool both = mirror(a0, c0);
   const bool on = r.i >= c0 && r.i < c0 + 32;      // the diagonal
   if (on && r.i < m) {
 #pragma unroll
@@ -591,6 +615,7 @@ __device__ __forceinline__ void last_block(const Output& o, int a0, int c0,
   }
 }
 
+template <int kCtas>
 __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
                                           uint32_t staging, uint32_t tmem) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -612,9 +637,9 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
     if (!group_all(r.group, ok)) return;
     tmem_after_sync();
     const uint32_t from =
-        tmem + acc * kTileN + ((uint32_t)(quarter * 32) << 16);
-    const int a0 = row0(*l), blocks = block_count(*l), phase = l->phase;
-    const int b0 = l->j * kTileN, m = l->height;
+        tmem + acc * kTile<kCtas> + ((uint32_t)(quarter * 32) << 16);
+    const int a0 = row0<kCtas>(*l), b0 = l->j * kTile<kCtas>;
+    const int blocks = block_count<kCtas>(*l), phase = l->phase, m = l->height;
     const bool last = l->last, tall = l->tall;
     r.i = a0 + r.row;
     const float s = phase == kGram ? 1.f / (l->scale * l->scale)
@@ -637,9 +662,11 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
       tmem_ld32(from + c * kMuonCols, y);
       wait_on(sh, p, &sh.in[b], (uint32_t)(n / kBuffers) & 1u);
       if (phase == kGram) {
-        symmetric_block<false>(pb, pc, m, diag, 0.f, s, a0, c0, r, y);
+        symmetric_block<false>(pb, pc, m, diag, 0.f, s, mirror<kCtas>(a0, c0),
+                               c0, r, y);
       } else if (phase == kSquare) {
-        symmetric_block<true>(pb, pc, m, diag, row_v, s, a0, c0, r, y);
+        symmetric_block<true>(pb, pc, m, diag, row_v, s, mirror<kCtas>(a0, c0),
+                              c0, r, y);
       } else if (!last) {
         apply_block<false>(tall, pa, pa + row_v, r, y);
       } else {
@@ -653,13 +680,16 @@ __device__ __forceinline__ void turn_over(Shared& sh, const MuonParams& p,
     tmem_before_sync();
     __syncwarp();
     if (lane == 0) {
-      remote_arrive(at_rank(&sh.acc_empty[acc], 0));
+      if (kCtas == 2) remote_arrive(at_rank(&sh.acc_empty[acc], 0));
+      else mbar_arrive(&sh.acc_empty[acc]);
       mbar_arrive(&sh.read[slot]);
     }
   }
 }
 
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kStepThreads, 1)
+template <int kCtas>
+__global__ void __cluster_dims__(kCtas, 1, 1)
+    __launch_bounds__(kStepThreads, 1)
 muon_steps_kernel(const __grid_constant__ MuonParams p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ Shared sh;
@@ -673,7 +703,7 @@ muon_steps_kernel(const __grid_constant__ MuonParams p) {
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.acc_full[i], 1);
-      mbar_init(&sh.acc_empty[i], 8 * kGroups);
+      mbar_init(&sh.acc_empty[i], 4 * kGroups * kCtas);
     }
     for (int i = 0; i < kBuffers; ++i) {
       mbar_init(&sh.in[i], 1);
@@ -689,60 +719,72 @@ muon_steps_kernel(const __grid_constant__ MuonParams p) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   }
-  if (warp == 2) pair_tmem_alloc_all(&sh.tmem);
+  if (warp == 2) {
+    if (kCtas == 2) pair_tmem_alloc_all(&sh.tmem);
+    else tmem_alloc_all(&sh.tmem);
+  }
   for (int i = threadIdx.x; i < p.n_mats * kMuonMaps; i += kStepThreads)
     take_map(reinterpret_cast<const CUtensorMap*>(p.mats + i / kMuonMaps) +
              i % kMuonMaps);
   tmem_before_sync();
   __syncthreads();
-  cluster_sync();        // both CTAs' barriers are there
+  if (kCtas == 2) cluster_sync();        // both CTAs' barriers are there
   tmem_after_sync();
-  const uint32_t tmem = sh.tmem, rank = cluster_rank();
+  const uint32_t tmem = sh.tmem, rank = kCtas == 2 ? cluster_rank() : 0;
   if (warp == 0) {
-    if (elect_lane()) copy_operands(sh, p, smem, rank);
+    if (elect_lane()) copy_operands<kCtas>(sh, p, smem, rank);
     __syncwarp();
   } else if (warp == 1) {
-    if (elect_lane()) multiply(sh, p, smem, tmem, rank);
+    if (elect_lane()) multiply<kCtas>(sh, p, smem, tmem, rank);
     __syncwarp();
   } else if (warp == 2) {
-    if (elect_lane()) copy_in(sh, p, staging);
+    if (elect_lane()) copy_in<kCtas>(sh, p, staging);
     __syncwarp();
   } else if (warp == 3) {
-    if (elect_lane()) copy_out(sh, p, staging);
+    if (elect_lane()) copy_out<kCtas>(sh, p, staging);
     __syncwarp();
   } else {
-    turn_over(sh, p, staging, tmem);
+    turn_over<kCtas>(sh, p, staging, tmem);
   }
   tmem_before_sync();
   __syncthreads();
-  cluster_sync();        // neither CTA's memory is used any more
+  if (kCtas == 2) cluster_sync();        // neither's memory is used any more
   tmem_after_sync();
-  if (warp == 2) pair_tmem_free_all(tmem);
+  if (warp == 2) {
+    if (kCtas == 2) pair_tmem_free_all(tmem);
+    else tmem_free_all(tmem);
+  }
 }
 
 }  // namespace
 
-cudaError_t muon_steps_setup(int sms, int* pairs) {
+template <int kCtas>
+cudaError_t muon_setup(int sms, int* units) {
   cudaError_t e = cudaFuncSetAttribute(
-      muon_steps_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      muon_steps_kernel<kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize,
       (int)kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = 2;
+  at.val.clusterDim.x = kCtas;
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(sms / 2 * 2));
+  cfg.gridDim = dim3((unsigned)(sms / kCtas * kCtas));
   cfg.blockDim = dim3(kStepThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  e = cudaOccupancyMaxActiveClusters(pairs, muon_steps_kernel, &cfg);
-  if (e == cudaSuccess && *pairs < 1) e = cudaErrorNotSupported;
+  e = cudaOccupancyMaxActiveClusters(units, muon_steps_kernel<kCtas>, &cfg);
+  if (e == cudaSuccess && *units < 1) e = cudaErrorNotSupported;
   return e;
 }
 
-cudaError_t muon_launch_steps(const MuonParams& p, int pairs,
+cudaError_t muon_steps_setup(int sms, int* ctas, int* pairs) {
+  const cudaError_t e = muon_setup<1>(sms, ctas);
+  return e == cudaSuccess ? muon_setup<2>(sms, pairs) : e;
+}
+
+cudaError_t muon_launch_steps(const MuonParams& p, bool pair, int units,
                               cudaStream_t stream) {
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeCooperative;
@@ -753,12 +795,13 @@ cudaError_t muon_launch_steps(const MuonParams& p, int pairs,
   cfg.stream = stream;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  // a process that has fewer SMs than the device takes fewer pairs
+  // a process that has fewer SMs than the device takes fewer CTAs
   cudaError_t e = cudaErrorCooperativeLaunchTooLarge;
-  for (int n = std::min(pairs, p.total);
+  for (int n = std::min(units, p.total);
        n > 0 && e == cudaErrorCooperativeLaunchTooLarge; n /= 2) {
-    cfg.gridDim = dim3(2u * (unsigned)n);
-    e = cudaLaunchKernelEx(&cfg, muon_steps_kernel, p);
+    cfg.gridDim = dim3((unsigned)(pair ? 2 * n : n));
+    e = cudaLaunchKernelEx(
+        &cfg, pair ? muon_steps_kernel<2> : muon_steps_kernel<1>, p);
     if (e == cudaErrorCooperativeLaunchTooLarge) cudaGetLastError();
   }
   return e;

@@ -270,6 +270,65 @@ def test_step_in_a_graph_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(w, want))
 
 
+# enough work beside a test's own matrices for the larger tiles
+MANY = [(700, 600)] * 20
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["gauss", "low rank"])
+def test_direction_of_many(dtype, kind):
+    shapes = MANY + SHAPES + [(1024, 260), (300, 2050)]
+    g = _gen(11)
+    u = [_matrix(r, c, g, kind).to(DT[dtype]) for r, c in shapes]
+    o = [torch.empty(s, device=DEV, dtype=torch.bfloat16) for s in shapes]
+    plan = MuonPlan(shapes, grad_dtype=dtype)
+    plan.bind_direction(u, o)
+    plan.direction(B.make_muon_hyper())
+    for x, y, s in zip(u, o, shapes):
+        _near(y, _exact(x), TOL + UBF / 2, s)
+    assert plan.query() == 0
+    first = [y.clone() for y in o]
+    plan.direction(B.make_muon_hyper())
+    assert all(torch.equal(a, b) for a, b in zip(first, o))
+
+
+def test_step_of_many():
+    """The step, and an Inf that stays in its own matrix."""
+    shapes = MANY + [(64, 32), (130, 40), (257, 129), (300, 1000)]
+    g = _gen(12)
+    gr = [_matrix(*s, g).bfloat16() for s in shapes]
+    w = [_matrix(*s, g, std=0.05).float() for s in shapes]
+    m = [_matrix(*s, g, std=3e-4).float() for s in shapes]
+    copy = [torch.zeros(s, device=DEV, dtype=torch.bfloat16) for s in shapes]
+    wd, md = [x.double() for x in w], [x.double() for x in m]
+    plan = MuonPlan(shapes, grad_dtype="bf16", copy_dtype="bf16")
+    plan.bind(w, gr, m, copy)
+    lr = torch.full((1,), 0.02, device=DEV)
+    beta, lam, eta = 0.9, 0.1, float(lr)
+    plan.step(B.make_muon_hyper(momentum=beta, weight_decay=lam), lr)
+    for k, (r, c) in enumerate(shapes):
+        gd = gr[k].double()
+        md[k] = beta * md[k] + (1 - beta) * gd
+        x = _exact((1 - beta) * gd + beta * md[k])
+        size = math.sqrt(max(1.0, r / c))
+        wd[k] = wd[k] * (1 - eta * lam) - eta * size * x
+        terms = beta * md[k].abs() + gd.abs()
+        assert ((m[k].double() - md[k]).abs() <= 8 * U32 * terms).all()
+        off = float((w[k].double() - wd[k]).norm())
+        assert off <= (eta * size * TOL * float(x.norm()) +
+                       4 * U32 * float(wd[k].norm())), k
+        assert torch.equal(copy[k], w[k].bfloat16())
+    assert plan.query() == 0
+    good = [x.clone() for x in w]
+    gr[3][5, 7] = float("inf")
+    for x, y in zip(w, good):
+        x.copy_(y)
+    plan.step(B.make_muon_hyper(momentum=beta, weight_decay=lam), lr)
+    assert plan.query(clear=True) == B.LAMB_STATUS_NONFINITE
+    assert torch.isnan(w[3]).any()
+    assert all(torch.isfinite(x).all() for k, x in enumerate(w) if k != 3)
+
+
 def test_refusals():
     shapes = [(8, 8), (8, 4)]
     plan = MuonPlan(shapes, grad_dtype="bf16")
