@@ -12,16 +12,15 @@
 // whatever the words: ids are Zipf-like, most words have few tokens and a mask
 // token thousands.  A chunk writes the rows of the words that lie inside it and
 // leaves the sum of a word that goes on; one more launch adds those, in order.
-// Rows of words without a token are cleared by other CTAs of the same launch.  Sums
-// are fp32.
+// Sums are fp32.  Rows of words without a token are cleared during the sort.
 //
 // Launches follow one another early (griddepcontrol): count, a move for each digit
 // (which counts the next digit), sums, joins; up to 4096 tokens are sorted in one.
 //
 // Measured: lookup of 65536 x 768 (fp32 to bf16) 27 us, 5.1 TB/s; gradient of 65536
-// x 1024 (bf16) into a fresh table 70 us, of which the sort takes 18, the sums 40 and
-// the joins 10: 27 us of HBM traffic, the rest latency of the longest word and of
-// four launches in front; 4095 x 768 added to a tied table 23 us.
+// x 1024 (bf16) into a fresh table 71 us, of which the sort takes 22 with the clearing,
+// the sums 38 and the joins 8: 27 us of HBM traffic, the rest latency of the longest
+// word and of four launches in front; 4095 x 768 added to a tied table 20 us.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -41,7 +40,6 @@ constexpr int kSortTiles = 128;        // at most: each reads all tiles' counts
 // 32 113, 64 85, 128 70.
 constexpr int kLeastChunk = 16;
 int chunk_of(int64_t n) { return n <= 8192 ? 16 : n <= 32768 ? 64 : 128; }
-constexpr int kClearRows = 64;         // rows of the table a clearing CTA looks at
 constexpr int kJoinThreads = 256, kJoinBatch = 8;
 constexpr uint32_t kStatusBadIndex = LAMB_STATUS_BAD_INDEX;
 
@@ -105,6 +103,43 @@ embed_kernel(const TI* __restrict__ table, int64_t table_stride,
   }
 }
 
+// ---- rows of zeros ------------------------------------------------------------
+// The rows of a fresh table gradient are cleared by further CTAs of the sort's
+// launches, whose own are too few to fill the GPU; the sums write the words with
+// tokens again.  Instead of it, looking every word up in the sorted list beside the
+// sums (us, V = 30522): 1 x 768 tokens to fp32 33 (now 19), 512 x 768 37 (25), 8192 x
+// 1024 to bf16 41 (34), 65536 x 1024 to bf16 73 (76: a third is written twice).
+constexpr int kClearRows = 32;         // of a CTA
+
+struct Clear {
+  void* out;
+  int64_t stride;          // elements of `unit` bytes
+  int64_t first, rows;     // of this launch
+  int width, unit;
+};
+
+template <class T>
+__device__ __forceinline__ void clear_rows(const Clear& c, int64_t v0, T zero) {
+  const int64_t end = min(v0 + kClearRows, c.first + c.rows);
+  const int lane = threadIdx.x & 31;
+  for (int64_t v = v0 + (threadIdx.x >> 5); v < end; v += blockDim.x >> 5) {
+    T* row = reinterpret_cast<T*>(c.out) + v * c.stride;
+    for (int d = lane; d < c.width; d += 32) row[d] = zero;
+  }
+}
+__device__ void clear_part(const Clear& c, int part) {
+  const int64_t v0 = c.first + (int64_t)part * kClearRows;
+  if (c.unit == 16) clear_rows(c, v0, make_uint4(0, 0, 0, 0));
+  else if (c.unit == 4) clear_rows(c, v0, 0u);
+  else clear_rows(c, v0, (uint16_t)0);
+}
+unsigned clear_ctas(const Clear& c) {
+  return (unsigned)lm_ceil_div(c.rows, kClearRows);
+}
+__global__ void __launch_bounds__(kSortThreads) clear_kernel(Clear clear) {
+  clear_part(clear, blockIdx.x);
+}
+
 // ---- sort -------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(int64_t id, int64_t vocab,
                                            uint32_t* status) {
@@ -151,10 +186,14 @@ __global__ void __launch_bounds__(kSortThreads)
 digit_move_kernel(const int64_t* ids, const uint32_t* keys, const int32_t* pos,
                   int n, int64_t vocab, int rounds, int shift,
                   const int32_t* hist, int32_t* next_hist, uint32_t* keys_out,
-                  int32_t* pos_out, uint32_t* status) {
+                  int32_t* pos_out, uint32_t* status, int tiles, Clear clear) {
   __shared__ int32_t count[kSortWarps][256];
   __shared__ int32_t half[2][2][256];      // [half][before the tile, in all]
   __shared__ int32_t scan[256];
+  if ((int)blockIdx.x >= tiles) {
+    let_next_launch();
+    return clear_part(clear, blockIdx.x - tiles);
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int i = threadIdx.x; i < kSortWarps * 256; i += kSortThreads)
     count[i >> 8][i & 255] = 0;
@@ -162,7 +201,7 @@ digit_move_kernel(const int64_t* ids, const uint32_t* keys, const int32_t* pos,
   after_prior_launch();
   {   // all tiles' counts of a digit, half of the tiles a thread
     const int d = threadIdx.x & 255, h = threadIdx.x >> 8;
-    const int tiles = gridDim.x, mid = (tiles + 1) / 2;
+    const int mid = (tiles + 1) / 2;
     int before = 0, total = 0;
 #pragma unroll 16
     for (int t = h * mid; t < (h ? tiles : mid); ++t) {
@@ -246,7 +285,8 @@ constexpr int kSmallSort = kSmallThreads * kSmallItems;
 
 __global__ void __launch_bounds__(kSmallThreads)
 sort_small_kernel(const int64_t* ids, int n, int64_t vocab, int passes,
-                  uint32_t* keys_out, int32_t* pos_out, uint32_t* status) {
+                  uint32_t* keys_out, int32_t* pos_out, uint32_t* status,
+                  Clear clear) {
   constexpr int kWarps = kSmallThreads / 32;
   __shared__ uint32_t sm_key[kSmallSort];
   __shared__ uint16_t sm_pos[kSmallSort];
@@ -255,6 +295,7 @@ sort_small_kernel(const int64_t* ids, int n, int64_t vocab, int passes,
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t past = 0xffffffffu;        // sorts behind every key
   let_next_launch();
+  if (blockIdx.x) return clear_part(clear, blockIdx.x - 1);
   uint32_t key[kSmallItems], pos[kSmallItems];
 #pragma unroll
   for (int i = 0; i < kSmallItems; ++i) {
@@ -348,26 +389,51 @@ __device__ __forceinline__ void load_row(const T* p, int d, int width,
     }
   }
 }
+__device__ __forceinline__ void fetch_line(const void* p) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
+// Adding to fp32 is left to the memory, which nobody waits for: each element is
+// added to once in a call, so no order matters.  (It takes subnormals for zeros.)
+// 32768 x 768 tokens added 62 us with a read, 50 so.  A bf16 element is read, so that
+// its sum is rounded once; its line is fetched with the batch: 65536 x 1024 115 us
+// without, 97 with.
+__device__ __forceinline__ void add4(float* p, const float (&x)[4]) {
+  asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p),
+               "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3])
+               : "memory");
+}
+__device__ __forceinline__ void add4(__nv_bfloat16*, const float (&)[4]) {}
+__device__ __forceinline__ void add1(float* p, float x) {
+  asm volatile("red.global.add.f32 [%0], %1;" ::"l"(p), "f"(x) : "memory");
+}
+__device__ __forceinline__ void add1(__nv_bfloat16*, float) {}
+
 template <class T, int kN, bool kVec>
 __device__ __forceinline__ void write_row(T* p, int d, int width,
                                           const float (&s)[kN], float scale,
                                           bool add) {
+  const bool in_memory = sizeof(T) == 4 && add;
   float x[kN];
 #pragma unroll
   for (int j = 0; j < kN; ++j) x[j] = 0.f;
-  if (add) load_row<T, kN, kVec>(p, d, width, x);
+  if (add && !in_memory) load_row<T, kN, kVec>(p, d, width, x);
 #pragma unroll
-  for (int j = 0; j < kN; ++j) x[j] = add ? x[j] + s[j] * scale : s[j] * scale;
+  for (int j = 0; j < kN; ++j)
+    x[j] = add && !in_memory ? x[j] + s[j] * scale : s[j] * scale;
   if (kVec) {
 #pragma unroll
     for (int q = 0; q < kN; q += 4) {
       const float v[4] = {x[q], x[q + 1], x[q + 2], x[q + 3]};
-      store4(p + d + q, v);
+      if (in_memory) add4(p + d + q, v);
+      else store4(p + d + q, v);
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < kN; ++j)
-      if (d + j < width) store1(p + d + j, x[j]);
+    for (int j = 0; j < kN; ++j) {
+      if (d + j >= width) continue;
+      if (in_memory) add1(p + d + j, x[j]);
+      else store1(p + d + j, x[j]);
+    }
   }
 }
 
@@ -407,8 +473,7 @@ struct Raw {
 
 // tx threads take a chunk's rows, 16 bytes of each; kEmbedThreads / tx chunks a
 // CTA.  kBatch rows are on their way at a time: HBM's latency over rows that lie
-// anywhere takes some 100 KB in flight on an SM.  The CTAs past the chunks clear
-// rows without a token.
+// anywhere takes some 100 KB in flight on an SM.
 constexpr int kBatch = 16, kLeastTx = 8;
 
 template <class TG, class TT, bool kVec>
@@ -416,36 +481,13 @@ __global__ void __launch_bounds__(kEmbedThreads)
 embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
                   const uint32_t* __restrict__ keys,
                   const int32_t* __restrict__ pos, int n, int64_t vocab,
-                  int width, int chunk, int tx, int chunk_ctas,
-                  float* __restrict__ part, float scale, bool add,
+                  int width, int chunk, int tx, float* __restrict__ part, float scale, bool add,
                   TT* __restrict__ out, int64_t out_stride) {
   typedef Raw<TG, kVec> R;
   constexpr int kN = R::kN;
   extern __shared__ uint32_t sh_key[];       // the CTA's keys and neighbours
   let_next_launch();
   after_prior_launch();
-  if ((int)blockIdx.x >= chunk_ctas) {
-    const int64_t v0 = (int64_t)(blockIdx.x - chunk_ctas) * kClearRows;
-    if (threadIdx.x < kClearRows) {     // is the word in the sorted list?
-      const uint32_t v = (uint32_t)(v0 + threadIdx.x);
-      int lo = 0, hi = n;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (keys[mid] < v) lo = mid + 1; else hi = mid;
-      }
-      sh_key[threadIdx.x] = lo < n && keys[lo] == v;
-    }
-    __syncthreads();
-    for (int r = threadIdx.x >> 5; r < kClearRows; r += kEmbedThreads / 32) {
-      const int64_t v = v0 + r;
-      if (v >= vocab || sh_key[r]) continue;
-      TT* dst = out + v * out_stride;
-      float zero[kN] = {};
-      for (int d = (threadIdx.x & 31) * kN; d < width; d += 32 * kN)
-        write_row<TT, kN, kVec>(dst, d, width, zero, 1.f, false);
-    }
-    return;
-  }
   const int ty = kEmbedThreads / tx;
   int32_t* const sh_pos = reinterpret_cast<int32_t*>(sh_key) + ty * chunk + 2;
   const int chunk0 = blockIdx.x * ty, first = chunk0 * chunk;
@@ -476,6 +518,9 @@ embed_sums_kernel(const TG* __restrict__ grad, int64_t stride,
         const int i = i0 + u;
         if (i < m && key[i] < (uint32_t)vocab)
           x[u].load(grad + (int64_t)sh_pos[at0 + i] * stride, d, width);
+        if (sizeof(TT) == 2 && add && i < m && key[i] < (uint32_t)vocab &&
+            key[i + 1] != key[i])
+          fetch_line(out + (int64_t)key[i] * out_stride + d);
       }
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
@@ -581,13 +626,11 @@ cudaError_t launch_sums(const lamb_vocab* v, const void* grad, int64_t gs,
   const int chunk = chunk_of(n), ty = kEmbedThreads / tx;
   const int chunks = (int)lm_ceil_div(n, chunk);
   const int ctas = (int)lm_ceil_div(chunks, ty);
-  const size_t smem =
-      std::max<size_t>(2 * (size_t)ty * chunk + 2, kClearRows) * 4;
-  const int64_t clears = add ? 0 : lm_ceil_div(v->vocab, kClearRows);
+  const size_t smem = (2 * (size_t)ty * chunk + 2) * 4;
   cudaError_t e = lm_launch(
-      embed_sums_kernel<TG, TT, kVec>, (unsigned)(ctas + clears), kEmbedThreads,
-      smem, stream, n > 0, (const TG*)grad, gs, v->keys[in], v->pos[in], n,
-      v->vocab, v->width, chunk, tx, ctas, v->part, scale, add, (TT*)out, os);
+      embed_sums_kernel<TG, TT, kVec>, (unsigned)ctas, kEmbedThreads, smem,
+      stream, true, (const TG*)grad, gs, v->keys[in], v->pos[in], n, v->vocab,
+      v->width, chunk, tx, v->part, scale, add, (TT*)out, os);
   if (e == cudaSuccess && chunks > 1)
     e = lm_launch(embed_join_kernel<TT, kVec>, (unsigned)(chunks - 1),
                   kJoinThreads, 0, stream, true, v->keys[in], n, v->vocab,
@@ -704,22 +747,44 @@ extern "C" lamb_status_t lamb_vocab_embed_grad(
   const unsigned tiles = (unsigned)lm_ceil_div(n, kSortThreads * rounds);
   cudaError_t e = cudaSuccess;
   int in = 0;
+  // what is to be cleared, a part with each pass of the sort
+  const size_t size = lm_elem_size(table_dtype);
+  const uint64_t bytes = (uint64_t)table_stride * size,
+                 used = (uint64_t)v->width * size;
+  const int unit =
+      ((uint64_t)table_grad | bytes | used) % 16 == 0 ? 16 : (int)size;
+  const auto clear = [&](int k, int parts) {
+    const int64_t from = accumulate ? 0 : v->vocab * k / parts;
+    const int64_t to = accumulate ? 0 : v->vocab * (k + 1) / parts;
+    return Clear{table_grad,       (int64_t)(bytes / unit), from,
+                 to - from,        (int)(used / unit),      unit};
+  };
+  if (!n) {
+    clear_kernel<<<clear_ctas(clear(0, 1)), kSortThreads, 0, stream>>>(
+        clear(0, 1));
+    e = cudaGetLastError();
+    return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "clear launch");
+  }
   // (4095 tokens: 31 us with a launch a pass, 29 with one in all)
   const bool small = n <= kSmallSort;
-  if (n && small)
-    e = lm_launch(sort_small_kernel, 1, kSmallThreads, 0, stream, false, ids, n,
-                  v->vocab, v->sort_passes, v->keys[0], v->pos[0], v->status);
-  if (n && !small)
+  if (small)
+    e = lm_launch(sort_small_kernel, 1 + clear_ctas(clear(0, 1)),
+                  kSmallThreads, 0, stream, false, ids, n, v->vocab,
+                  v->sort_passes, v->keys[0], v->pos[0], v->status,
+                  clear(0, 1));
+  else
     e = lm_launch(digit_count_kernel, tiles, kSortThreads, 0, stream, false,
                   ids, n, v->vocab, rounds, v->sort_passes, v->hist, v->status);
   for (int pass = 0; e == cudaSuccess && !small && pass < v->sort_passes;
        ++pass) {
     int32_t* hist = v->hist + (int64_t)pass * kSortTiles * 256;
-    e = lm_launch(digit_move_kernel, tiles, kSortThreads, 0, stream, true,
+    const Clear c = clear(pass, v->sort_passes);
+    e = lm_launch(digit_move_kernel, tiles + clear_ctas(c), kSortThreads, 0,
+                  stream, true,
                   pass ? nullptr : ids, v->keys[in], pass ? v->pos[in] : nullptr,
                   n, v->vocab, rounds, 8 * pass, hist,
                   pass + 1 < v->sort_passes ? hist + kSortTiles * 256 : nullptr,
-                  v->keys[in ^ 1], v->pos[in ^ 1], v->status);
+                  v->keys[in ^ 1], v->pos[in ^ 1], v->status, (int)tiles, c);
     in ^= 1;
   }
   if (e != cudaSuccess) return lm_cuda_fail(e, "sort launch");
