@@ -23,9 +23,9 @@
 // layout, with h (rows of dW).  dh's sums over pieces and over parts of a long piece
 // stay in fp32.  8 T V D operations in all.
 //
-// Measured: loss of 8192 x 30522 x 768 (6963 labels) 204 us, 1.6 PFLOP/s; loss and
-// gradients of 9830 x 30522 x 1024 1534 us, 1.57 PFLOP/s of the 8 T V D: bound by
-// the tensor cores under the power limit.  77 x 30522 x 1024 83 us: W is read twice
+// Measured: loss of 8192 x 30522 x 768 (6963 labels) 201 us, 1.6 PFLOP/s; loss and
+// gradients of 9830 x 30522 x 1024 1524 us, 1.58 PFLOP/s of the 8 T V D: bound by
+// the tensor cores under the power limit.  77 x 30522 x 1024 80 us: W is read twice
 // from HBM and dW written, 28 us of it; the rest is six launches' latency.
 #include <cuda_bf16.h>
 
