@@ -847,7 +847,8 @@ int64_t head_parts(int64_t units, int64_t h_tiles, int64_t k_blocks) {
 // Columns of a piece of the vocabulary, in whole tiles: of the counts of pieces
 // that the workspace allows, the one whose products' tiles (rows of dW over all
 // tokens, rows of dh over the piece) fall best on `units` CTAs or pairs.  9830 x
-// 30522 x 1024, us: the fewest pieces 1827, so chosen 1639.
+// 30522 x 1024, us: the fewest pieces 1564, so chosen 1527; 2458 x 30522 x 768, two
+// pieces either way, 329 to 335.
 int64_t piece_width(const lamb_vocab* v, int64_t n, int rows, int units) {
   const int64_t whole = lm_round_up(n, kRowsWhole);
   const int64_t most = v->dlogits_elems / whole / kTileN * kTileN;
