@@ -247,6 +247,12 @@ int64_t small_smem(int64_t m, int64_t n) {
   return (m * lm_round_up(m, 4) + m * lm_round_up(m | 1, 4) +
           2 * m * small_pitch(n)) * 4;
 }
+// What no such matrix passes (a row's pitch is at most seven elements above it).
+// The kernel's limit belongs to the device, not to a plan: it is always this.
+constexpr int kSmallSmem =
+    (kSmallSide * kSmallSide + kSmallSide * (kSmallSide + 4) +
+     2 * ((int)kSmallElems + 7 * kSmallSide)) * 4;
+static_assert(kSmallSmem <= 227 * 1024 - 2048, "a CTA's shared memory");
 
 // out = b in + c (in in^T), or in in^T (kPlain), both symmetric: blocks of 4 x 4
 // (the task's places are in `where`), each by 16 neighbouring lanes that take
@@ -407,10 +413,10 @@ muon_small_kernel(const MuonMatrix* mats, const MuonPtrs* ptrs,
 }
 
 template <class TG, bool kStep>
-cudaError_t small_smem_limit(int64_t bytes) {
+cudaError_t allow_small_smem() {
   return cudaFuncSetAttribute(muon_small_kernel<TG, kStep>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)bytes);
+                              kSmallSmem);
 }
 
 }  // namespace
@@ -807,10 +813,10 @@ extern "C" lamb_status_t lamb_muon_create(
     for (int k : L.small)
       p->small_bytes = std::max(p->small_bytes,
                                 small_smem(L.mats[k].m, L.mats[k].n));
-    if (e == cudaSuccess) e = small_smem_limit<__nv_bfloat16, true>(p->small_bytes);
-    if (e == cudaSuccess) e = small_smem_limit<__nv_bfloat16, false>(p->small_bytes);
-    if (e == cudaSuccess) e = small_smem_limit<float, true>(p->small_bytes);
-    if (e == cudaSuccess) e = small_smem_limit<float, false>(p->small_bytes);
+    if (e == cudaSuccess) e = allow_small_smem<__nv_bfloat16, true>();
+    if (e == cudaSuccess) e = allow_small_smem<__nv_bfloat16, false>();
+    if (e == cudaSuccess) e = allow_small_smem<float, true>();
+    if (e == cudaSuccess) e = allow_small_smem<float, false>();
     if (e == cudaSuccess && p->n_small)
       e = cudaMemcpy(p->small, L.small.data(), L.small.size() * sizeof(int),
                      cudaMemcpyHostToDevice);

@@ -1,0 +1,69 @@
+"""GPU tests of the language-model operators where two plans, two streams, a
+refused call or extreme values meet.  Bounds as in the operators' other tests.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_1904_00962_gb300 import binding as B
+from paper_1904_00962_gb300.muon import MuonPlan
+from paper_1904_00962_gb300.vocab import VocabPlan
+from test_muon_gpu import TOL, _exact, _matrix, _near
+from test_vocab_gpu import (DEV, U32, UBF, _close, _gen, _head_reference,
+                            _randn)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib(gpu):
+    B.load()
+
+
+# ---------------------------------------------------------------------------
+# plans beside one another
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_later_muon_plan_leaves_an_earlier_one_its_shared_memory(dtype):
+    """The small matrices' kernel takes as much of it as the plan's largest
+    needs: plans of less, or without such a matrix, come after one of more."""
+    g = _gen(20)
+    shapes = [(64, 128), (256, 300)]
+    u = [_matrix(*s, g).to(dtype) for s in shapes]
+    o = [torch.empty(s, device=DEV, dtype=torch.bfloat16) for s in shapes]
+    kind = "f32" if dtype == torch.float32 else "bf16"
+    plan = MuonPlan(shapes, grad_dtype=kind)
+    plan.bind_direction(u, o)
+    later = [MuonPlan([(256, 256)]), MuonPlan([(4, 4)], grad_dtype="bf16")]
+    plan.direction(B.make_muon_hyper())
+    for x, y in zip(u, o):
+        _near(y, _exact(x), TOL + UBF / 2)
+    w = [_matrix(*s, g, std=0.05).float() for s in shapes]
+    m = [torch.zeros(s, device=DEV) for s in shapes]
+    plan.bind(w, u, m)
+    before = [x.double() for x in w]
+    lr = torch.full((1,), 0.02, device=DEV)
+    plan.step(B.make_muon_hyper(weight_decay=0.0, scale="one"), lr)
+    for x, y, z in zip(w, before, u):
+        moved = (y - x.double()) / 0.02
+        want = _exact(z.double() * 0.0975)  # (1 - b) (1 + b) g, b = 0.95
+        # the weights' own fp32 digits beside the direction's error
+        off = float((moved - want).norm())
+        assert off <= TOL * float(want.norm()) + \
+            4 * U32 / 0.02 * float(y.norm())
+    assert plan.query() == 0 and all(p.query() == 0 for p in later)
+
+
+def test_every_small_matrix_fits_shared_memory():
+    """The sides at which such a matrix needs most."""
+    shapes = [(64, 128), (25, 819), (819, 25), (1, 20480), (5, 4096), (3, 6826),
+              (64, 64), (2, 10239)]
+    g = _gen(21)
+    u = [_matrix(*s, g).float() for s in shapes]
+    o = [torch.empty(s, device=DEV, dtype=torch.bfloat16) for s in shapes]
+    plan = MuonPlan(shapes)
+    plan.bind_direction(u, o)
+    plan.direction(B.make_muon_hyper())
+    for x, y, s in zip(u, o, shapes):
+        _near(y, _exact(x), TOL + UBF / 2, s)
