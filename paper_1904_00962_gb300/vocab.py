@@ -3,9 +3,14 @@
 ``VocabPlan`` holds a vocabulary plan of the C library (include/lamb.h) and
 checks, before every call, that the tensors are what the call takes: type,
 shape, device and contiguous rows.  It does no arithmetic; the kernels run on
-PyTorch's current stream unless one is given.
+PyTorch's current stream unless one is given.  A result that the plan allocates
+belongs to the stream that writes it, as if it were made under
+``torch.cuda.stream``: another stream that uses it waits for that one first, and
+tells the allocator of its own use (``Tensor.record_stream``).
 """
 from __future__ import annotations
+
+import contextlib
 
 import torch
 
@@ -63,6 +68,17 @@ class VocabPlan:
             return torch._C._cuda_getCurrentRawStream(self._index)
         return stream if isinstance(stream, int) else stream.cuda_stream
 
+    def _allocating(self, stream):
+        """A context whose new tensors' memory goes on in the order of `stream`
+        (the current one: None)."""
+        if stream is None:
+            return contextlib.nullcontext()
+        if isinstance(stream, int):
+            # (0 and 1 are CUDA's names of the default stream)
+            stream = torch.cuda.default_stream(self.device) if stream < 2 else \
+                torch.cuda.ExternalStream(stream, device=self.device)
+        return torch.cuda.stream(stream)
+
     def _tokens(self, name, t):
         if t.dim() != 1:
             raise ValueError(f"{name}: one dimension is needed")
@@ -75,8 +91,9 @@ class VocabPlan:
         `out` if it is given.  Ids below 0 give rows of zeros."""
         n = self._tokens("ids", ids)
         if out is None:
-            out = torch.empty((n, self.width), dtype=dtype or table.dtype,
-                              device=self.device)
+            with self._allocating(stream):
+                out = torch.empty((n, self.width), dtype=dtype or table.dtype,
+                                  device=self.device)
         B.lamb_vocab_embed(
             self.handle, *self._matrix("table", table, self.vocab, _BOTH),
             self._vector("ids", ids, n, torch.int64), n, scale,
@@ -96,10 +113,11 @@ class VocabPlan:
         return table_grad
 
     # -- vocabulary head --------------------------------------------------------
-    def _head(self, hidden, weight, labels, token_loss, loss):
+    def _head(self, hidden, weight, labels, token_loss, loss, stream):
         n = self._tokens("labels", labels)
         if loss is None:
-            loss = torch.empty(1, dtype=torch.float32, device=self.device)
+            with self._allocating(stream):
+                loss = torch.empty(1, dtype=torch.float32, device=self.device)
         h, _, hs = self._matrix("hidden", hidden, n, _BF16)
         w, _, ws = self._matrix("weight", weight, self.vocab, _BF16)
         y = self._vector("labels", labels, n, torch.int64)
@@ -113,7 +131,7 @@ class VocabPlan:
         """Mean cross entropy (a float tensor of one element) of
         hidden @ weight.T against the labels; labels below 0 do not count."""
         _, loss, ins, outs = self._head(hidden, weight, labels, token_loss,
-                                        loss)
+                                        loss, stream)
         B.lamb_vocab_loss(self.handle, *ins, *outs, self._stream(stream))
         return loss
 
@@ -124,7 +142,7 @@ class VocabPlan:
         grad_weight written or (`accumulate`) added to.  `scale`: None or a
         float tensor of one element."""
         n, loss, ins, outs = self._head(hidden, weight, labels, token_loss,
-                                        loss)
+                                        loss, stream)
         gh, _, ghs = self._matrix("grad_hidden", grad_hidden, n, _BF16)
         gw, code, gws = self._matrix("grad_weight", grad_weight, self.vocab,
                                      _BOTH)

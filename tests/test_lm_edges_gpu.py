@@ -67,3 +67,36 @@ def test_every_small_matrix_fits_shared_memory():
     plan.direction(B.make_muon_hyper())
     for x, y, s in zip(u, o, shapes):
         _near(y, _exact(x), TOL + UBF / 2, s)
+
+
+@pytest.mark.parametrize("how", ["stream", "handle", "default"])
+def test_results_belong_to_the_stream_that_writes_them(how):
+    """Memory of a result that is dropped goes on in its stream's order: the
+    current stream does not get it."""
+    g = _gen(30)
+    vocab, width, n = 500, 1000, 1700
+    tab = _randn((vocab, width), g)
+    ids = torch.randint(vocab, (n,), generator=g, device=DEV)
+    h, w = tab[:40].bfloat16(), tab.bfloat16()
+    plan = VocabPlan(vocab, width, n)
+    s = torch.cuda.Stream()
+    given = {"stream": s, "handle": s.cuda_stream, "default": 0}[how]
+    current = torch.cuda.Stream() if how == "default" else \
+        torch.cuda.current_stream()
+    want = plan.loss(h, w, ids[:40]).clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(current):
+        for call, value, like in (
+                (lambda: plan.embed(tab, ids, stream=given), tab[ids], (n, width)),
+                (lambda: plan.loss(h, w, ids[:40], stream=given), want, (1,)),
+                (lambda: plan.loss_grad(h, w, ids[:40], torch.empty_like(h),
+                                        torch.empty_like(w), stream=given),
+                 want, (1,))):
+            torch.cuda.synchronize()
+            got = call()
+            torch.cuda.synchronize()
+            assert torch.equal(got, value)
+            at = got.data_ptr()
+            del got
+            new = [torch.empty(like, device=DEV) for _ in range(8)]
+            assert at not in [x.data_ptr() for x in new]
