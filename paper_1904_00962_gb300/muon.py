@@ -2,7 +2,7 @@
 
 ``MuonPlan`` holds a plan of the C library (include/lamb.h) for a list of
 matrices and checks the tensors it is bound to; it does no arithmetic.  The
-bound tensors are kept alive with the plan.
+bound tensors are kept alive with the plan, until others take their place.
 """
 from __future__ import annotations
 
@@ -31,7 +31,7 @@ class MuonPlan:
             decay_mask, _dtype_code(grad_dtype), _dtype_code(copy_dtype),
             self.device.index or 0)
 
-    def _ptrs(self, name, tensors, dtype):
+    def _checked(self, name, tensors, dtype):
         tensors = list(tensors)
         if len(tensors) != len(self.shapes):
             raise ValueError(f"{name}: {len(self.shapes)} tensors are needed")
@@ -42,8 +42,15 @@ class MuonPlan:
                                  f"of shape {shape} is needed")
             if not t.is_cuda or t.get_device() != (self.device.index or 0):
                 raise ValueError(f"{name}[{k}] is not on {self.device}")
-        self._bound[name] = tensors
-        return [t.data_ptr() for t in tensors]
+        return tensors
+
+    def _bind(self, call, stream, **lists):
+        """Hands the lists' addresses to the C call.  The plan goes on with the
+        tensors it had, and keeps them, unless all of it succeeds."""
+        call(self.handle, *([t.data_ptr() for t in ts]
+                            for ts in lists.values()),
+             stream=self._stream(stream))
+        self._bound.update(lists)
 
     def _stream(self, stream):
         """A raw stream handle: PyTorch's current one of the plan's device, or
@@ -58,19 +65,20 @@ class MuonPlan:
         if (copy is not None) != (self.copy_dtype is not None):
             raise ValueError("copy: needed iff the plan has a copy_dtype")
         f32 = torch.float32
-        B.lamb_muon_bind(
-            self.handle, self._ptrs("w", w, f32),
-            self._ptrs("g", g, _TORCH[self.grad_dtype]),
-            self._ptrs("m", m, f32),
-            None if copy is None else
-            self._ptrs("copy", copy, torch.bfloat16), self._stream(stream))
+        lists = dict(w=self._checked("w", w, f32),
+                     g=self._checked("g", g, _TORCH[self.grad_dtype]),
+                     m=self._checked("m", m, f32))
+        if copy is not None:
+            lists["copy"] = self._checked("copy", copy, torch.bfloat16)
+        self._bind(B.lamb_muon_bind, stream, **lists)
 
     def bind_direction(self, u, o, stream=None):
         """The inputs (of the gradients' type) and bf16 outputs of
         `direction`."""
-        B.lamb_muon_bind_direction(
-            self.handle, self._ptrs("u", u, _TORCH[self.grad_dtype]),
-            self._ptrs("o", o, torch.bfloat16), self._stream(stream))
+        self._bind(
+            B.lamb_muon_bind_direction, stream,
+            u=self._checked("u", u, _TORCH[self.grad_dtype]),
+            o=self._checked("o", o, torch.bfloat16))
 
     def step(self, hyper, d_lr: torch.Tensor, stream=None):
         """One update; d_lr: a float tensor of one element on the device."""

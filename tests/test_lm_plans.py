@@ -70,3 +70,74 @@ def test_results_are_allocated_for_the_stream_that_writes_them(monkeypatch,
                         raising=False)
     plan.embed(table, ids)
     assert made == [None] and calls[-1][1][-1] == 5
+
+
+class _OnGpu:
+    """What a plan asks of a tensor."""
+    is_cuda = True
+
+    def __init__(self, shape, dtype):
+        self.shape, self.dtype = shape, dtype
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return 0
+
+    def data_ptr(self):
+        return 256
+
+
+def _muon(monkeypatch, shapes, **kw):
+    monkeypatch.setattr(B, "lamb_muon_create", lambda *a: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 5,
+                        raising=False)
+    return MuonPlan(shapes, **kw)
+
+
+def _all_bound(plan):
+    return [t for ts in plan._bound.values() for t in ts]
+
+
+def test_a_refused_binding_keeps_the_earlier_tensors(monkeypatch):
+    """The device's table still holds their addresses."""
+    shapes = [(4, 4), (4, 2)]
+    plan = _muon(monkeypatch, shapes)
+    bound, fail = [], []
+
+    def c_bind(*args, stream):
+        if fail:
+            raise B.LambError(B.LAMB_ERR_CUDA, "copy failed")
+        bound.append(args)
+    monkeypatch.setattr(B, "lamb_muon_bind", c_bind)
+    monkeypatch.setattr(B, "lamb_muon_bind_direction", c_bind)
+    f32, bf16 = torch.float32, torch.bfloat16
+
+    def tensors(dtype=f32):
+        return [_OnGpu(s, dtype) for s in shapes]
+    first = w, g, m = tensors(), tensors(), tensors()
+    plan.bind(*first)
+    u, o = tensors(), tensors(bf16)
+    plan.bind_direction(u, o)
+    held = w + g + m + u + o
+    assert set(map(id, _all_bound(plan))) == set(map(id, held))
+    for bad in ((tensors(), tensors(bf16), m), (tensors(), g[:1], m),
+                (tensors(), tensors(), tensors(bf16))):
+        with pytest.raises(ValueError):
+            plan.bind(*bad)
+    with pytest.raises(ValueError):
+        plan.bind_direction(tensors(), tensors())
+    fail.append(True)
+    with pytest.raises(B.LambError):
+        plan.bind(tensors(), tensors(), tensors())
+    with pytest.raises(B.LambError):
+        plan.bind_direction(tensors(), tensors(bf16))
+    assert len(bound) == 2
+    assert set(map(id, _all_bound(plan))) >= set(map(id, held))
+    # and a binding that succeeds replaces them
+    fail.clear()
+    new = tensors(), tensors(), tensors()
+    plan.bind(*new)
+    assert set(map(id, _all_bound(plan))) == \
+        set(map(id, sum(new, []) + u + o))
