@@ -14,7 +14,8 @@
 // leaves, of each 256 columns of a row, the maximum and the sum of exponentials
 // (fp32); a small kernel joins them in a fixed order.  The label's own column is
 // left out of those: with R the sum of exp(l_v - l_y) over the others, the loss is
-// log1p(R), which keeps its digits where the label is nearly sure.
+// log1p(R), which keeps its digits where the label is nearly sure.  So does the
+// label's entry of the logits' gradient, -R / (1 + R): p - 1 would have none left.
 //
 // The gradients take the vocabulary in pieces: a piece's logits are multiplied
 // again, the epilogue writes their gradient in bf16 to a workspace (the rounding
@@ -289,8 +290,8 @@ struct StatsWork {
 __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const float2* stats, int64_t stride, int v_tiles,
             const float* label_logit, const int32_t* row_token, int tokens,
-            const int32_t* n_rows, float* lse2, float* token_loss, float* loss,
-            const float* scale, float* coef, double* block_sums,
+            const int32_t* n_rows, float* lse2, float* entry, float* token_loss,
+            float* loss, const float* scale, float* coef, double* block_sums,
             uint32_t* ticket) {
   __shared__ double sh_loss[kJoinRows];
   __shared__ uint32_t last;
@@ -340,6 +341,8 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
           at + log2f(sum * exp2_fast(top - at) + exp2_fast(y - at));
       const float others = sum * exp2_fast(top - y);
       lse2[r] = lse;
+      entry[r] = others <= 1.f ? -others / (1.f + others)
+                               : 1.f / (1.f + others) - 1.f;
       l = others <= 1.f ? log1pf(others) : (lse - y) * kLn2;
       if (token_loss) token_loss[token] = l;
     }
@@ -374,6 +377,7 @@ struct DlogitsParams {
   const int32_t* n_rows;
   const int32_t* labels;
   const float* lse2;
+  const float* entry;     // p - 1 of the row's label
   const float* coef;
   uint32_t* status;
   int v_tiles, vocab, v0, k_blocks;
@@ -426,6 +430,7 @@ struct DlogitsWork {
     const bool real = r < s.rows;
     const int label = real ? p.labels[r] : -1;
     const float l2 = real ? p.lse2[r] : 0.f;
+    const float entry = real ? p.entry[r] : 0.f;
     const float coef = *p.coef;
     for (int c = 0; c < kTileN / 64; ++c) {
       const int v = g.b0 + c * 64;
@@ -441,7 +446,7 @@ struct DlogitsWork {
         if (label >= first && label < first + 32) {
 #pragma unroll
           for (int i = 0; i < 32; ++i)
-            if (label == first + i) x[i] -= 1.f;
+            if (label == first + i) x[i] = entry;
         }
         if (!real || first + 32 > p.vocab) {
 #pragma unroll
@@ -833,7 +838,7 @@ lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
   e = lm_launch(join_kernel, (unsigned)lm_ceil_div(n, kJoinRows), kJoinThreads,
                 0, stream, true, v->stats, v->max_tokens, p.v_tiles,
                 v->label_logit, v->row_token, (int)n, v->n_rows, v->lse2,
-                token_loss, loss, scale, v->coef, v->block_sums, v->ticket);
+                v->label_entry, token_loss, loss, scale, v->coef, v->block_sums, v->ticket);
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "head join launch");
 }
 
@@ -925,6 +930,7 @@ void lm_head_carve(lamb_vocab* v, LmArena* a) {
   a->take(&v->stats, lm_ceil_div(v->vocab, kTileN) * n);
   a->take(&v->label_logit, n);
   a->take(&v->lse2, n);
+  a->take(&v->label_entry, n);
   a->take(&v->block_sums, lm_ceil_div(n, kJoinRows));
   a->take(&v->ticket, 1);
   a->take(&v->coef, 1);
@@ -1047,6 +1053,7 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
   d.n_rows = v->n_rows;
   d.labels = v->row_label;
   d.lse2 = v->lse2;
+  d.entry = v->label_entry;
   d.coef = v->coef;
   d.status = v->status;
   d.vocab = (int)v->vocab;

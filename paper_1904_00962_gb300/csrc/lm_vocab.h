@@ -29,6 +29,7 @@ struct lamb_vocab {
   float2* stats = nullptr;      // [vocab tiles][max_tokens]
   float* label_logit = nullptr;
   float* lse2 = nullptr;
+  float* label_entry = nullptr; // the label's entry of the softmax, less one
   double* block_sums = nullptr;
   uint32_t* ticket = nullptr;
   float* coef = nullptr;        // scale / number of labels

@@ -100,3 +100,62 @@ def test_results_belong_to_the_stream_that_writes_them(how):
             del got
             new = [torch.empty(like, device=DEV) for _ in range(8)]
             assert at not in [x.data_ptr() for x in new]
+
+
+# ---------------------------------------------------------------------------
+# the head where labels are nearly sure
+# ---------------------------------------------------------------------------
+def _sure_rows(n, vocab, width, word, g):
+    """Hidden rows whose label is `word`, its probability between a quarter and
+    1 - 1e-6.  Column 0 of W is that word's alone and no hidden row has it, so
+    grad_hidden[:, 0] is the label's entry of the logits' gradient itself."""
+    w = _randn((vocab, width), g, 0.05, torch.bfloat16)
+    w[:, 0] = 0.0
+    way = w[word].float() / w[word].float().norm()
+    w[word, 0] = 1.0
+    h = _randn((n, width), g)
+    top = torch.linspace(8.0, 27.0, n, device=DEV)[:, None]
+    at = (w[word].float() * way).sum()
+    h = h - (h @ way)[:, None] * way + top / at * way
+    h[:, 0] = 0.0
+    return h.bfloat16(), w
+
+
+@pytest.mark.parametrize("n,vocab,width,word", [
+    (77, 701, 128, 300), (300, 5003, 96, 4999), (1, 300, 64, 0)])
+def test_sure_labels_keep_their_digits(n, vocab, width, word):
+    """The token losses and the label's entries of the gradient, each against
+    itself.  With R the sum of exp(l_v - l_y) over the other words both are
+    functions of R, whose relative error is that of two logits (a product's sum
+    of `width` terms is within 2^-23 of the sum of their sizes for each), of
+    base-2 exponents formed in fp32, and of a sum of `vocab` terms."""
+    g = _gen(vocab)
+    h, w = _sure_rows(n, vocab, width, word, g)
+    y = torch.full((n,), word, device=DEV)
+    logits = h.double() @ w.double().T
+    others = logits.clone()
+    others[:, word] = -math.inf
+    r = torch.exp(torch.logsumexp(others, 1) - logits[:, word])
+    want = torch.log1p(r)
+    entry = -r / (1.0 + r) / n
+    e_logit = (width + 2) * 2 * U32 * (h.double().abs() @
+                                       w.double().abs().T).amax(1)
+    rel = 2 * e_logit + 8 * U32 * logits.abs().amax(1) + 2.0 ** -20 + \
+        (vocab + 2) * U32
+    if n > 1:      # what the inputs are for
+        assert float(r.min()) < 2e-6 and float(r.max()) > 1e-2
+        assert float(rel.max()) < 2e-3
+
+    plan = VocabPlan(vocab, width, n)
+    token = torch.empty(n, device=DEV)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    plan.loss_grad(h, w, y, dh, dw, token_loss=token)
+    _close(token, want, want * (rel + 2.0 ** -21))
+    # one bf16 term: rounded as the logits' gradient, once more on its way out
+    e_entry = entry.abs() * (rel + UBF)
+    _close(dh[:, 0], entry, e_entry)
+    dw_want = entry @ h.double()
+    _close(dw[word], dw_want, e_entry @ h.double().abs() +
+           (n + 2) * 2 * U32 * (entry.abs() @ h.double().abs()) +
+           UBF * dw_want.abs())
+    assert plan.query() == 0
