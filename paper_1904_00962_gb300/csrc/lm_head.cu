@@ -8,7 +8,9 @@
 // gradient, so it is left out before the first product: the rows that have a
 // label are gathered, and all sizes below come from their number on the device.
 // (Whatever an absent row holds, an Inf or NaN too, then reaches nothing.)
-// Exponentials are taken in base 2: x' = x log2 e.
+// Exponentials are taken in base 2: x' = x log2 e.  Beyond kFarLogit the rounding
+// of x' is no longer small beside one (at -1e10 it makes an exponent of 328), so
+// there the difference of the logits is taken first.
 //
 // The loss is one product on the tensor cores (lm_gemm.cuh) whose epilogue
 // leaves, of each 256 columns of a row, the maximum and the sum of exponentials
@@ -51,6 +53,17 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// Logits (times log2 e) up to this size are scaled before they are subtracted, by
+// one fused operation: their exponent is within 2^-14 then.
+constexpr float kFarLogit = 1024.f;
+
+// e^(from - to) as sums kept relative to `from` are taken over to `to`.
+__device__ __forceinline__ float exp_between(float from, float to) {
+  const float b = to * kLog2e;
+  return exp2_fast(fabsf(b) < kFarLogit ? __fmul_rn(from, kLog2e) - b
+                                        : (from - to) * kLog2e);
 }
 
 // ---- rows with a label ------------------------------------------------------
@@ -267,16 +280,22 @@ struct StatsWork {
       float m = x[0];
 #pragma unroll
       for (int i = 1; i < 32; ++i) m = fmaxf(m, x[i]);
-      m = fmaxf(m * kLog2e, top);
+      m = fmaxf(m, top);
       // a row of nothing but -inf keeps the sum 0
-      const float at = m == -INFINITY ? 0.f : m;
+      const float to = m == -INFINITY ? 0.f : m;
+      float at = to * kLog2e;
+      if (fabsf(at) >= kFarLogit) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] -= to;
+        at = 0.f;
+      }
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int i = 0; i < 32; i += 2) {
         s0 += exp2_fast(fmaf(x[i], kLog2e, -at));
         s1 += exp2_fast(fmaf(x[i + 1], kLog2e, -at));
       }
-      sum = sum * exp2_fast(top - at) + (s0 + s1);
+      sum = sum * exp_between(top, to) + (s0 + s1);
       top = m;
     }
     if (r < s.rows)
@@ -286,12 +305,14 @@ struct StatsWork {
 
 // Joins a row's statistics in the order of the vocabulary: eight threads a row,
 // then those eight; then the mean over the rows (fp64, fixed order) by the CTA
-// that finishes last.
+// that finishes last.  Of each row the gradients get x: what is taken off its logits
+// (0 but for far ones), y: log2 of the sum of the exponentials of the rest, z: its
+// label's entry.
 __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const float2* stats, int64_t stride, int v_tiles,
             const float* label_logit, const int32_t* row_token, int tokens,
-            const int32_t* n_rows, float* lse2, float* entry, float* token_loss,
-            float* loss, const float* scale, float* coef, double* block_sums,
+            const int32_t* n_rows, float4* row_lse, float* token_loss, float* loss,
+            const float* scale, float* coef, double* block_sums,
             uint32_t* ticket) {
   __shared__ double sh_loss[kJoinRows];
   __shared__ uint32_t last;
@@ -304,7 +325,7 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
   float top = -INFINITY, sum = 0.f, y = 0.f;
   int token = 0;
   if (r < tokens) {
-    y = label_logit[r] * kLog2e;
+    y = label_logit[r];
     token = row_token[r];
     const int a = v_tiles * part / 8, b = v_tiles * (part + 1) / 8;
     for (int k0 = a; k0 < b; k0 += 16) {      // sixteen on their way
@@ -317,9 +338,9 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
 #pragma unroll
       for (int u = 0; u < 16; ++u) m = fmaxf(m, s[u].x);
       const float at = m == -INFINITY ? 0.f : m;
-      sum *= exp2_fast(top - at);
+      sum *= exp_between(top, at);
 #pragma unroll
-      for (int u = 0; u < 16; ++u) sum += s[u].y * exp2_fast(s[u].x - at);
+      for (int u = 0; u < 16; ++u) sum += s[u].y * exp_between(s[u].x, at);
       top = m;
     }
   }
@@ -329,7 +350,7 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
     const float os = __shfl_xor_sync(0xffffffffu, sum, o);
     const float m = fmaxf(top, ot);
     const float at = m == -INFINITY ? 0.f : m;
-    sum = sum * exp2_fast(top - at) + os * exp2_fast(ot - at);
+    sum = sum * exp_between(top, at) + os * exp_between(ot, at);
     top = m;
   }
   if (part == 0) {
@@ -337,13 +358,18 @@ join_kernel(const float2* stats, int64_t stride, int v_tiles,
     if (r < rows) {
       const float m = fmaxf(top, y);
       const float at = m == -INFINITY ? 0.f : m;
-      const float lse =
-          at + log2f(sum * exp2_fast(top - at) + exp2_fast(y - at));
-      const float others = sum * exp2_fast(top - y);
-      lse2[r] = lse;
-      entry[r] = others <= 1.f ? -others / (1.f + others)
-                               : 1.f / (1.f + others) - 1.f;
-      l = others <= 1.f ? log1pf(others) : (lse - y) * kLn2;
+      const float at2 = at * kLog2e;
+      const bool far = fabsf(at2) >= kFarLogit;
+      const float off = far ? at : 0.f;
+      const float lse = (far ? 0.f : at2) + log2f(sum * exp_between(top, at) +
+                                                  exp_between(y, at));
+      // (a label at +inf has no value: inf - inf)
+      const float others = y < INFINITY ? sum * exp_between(top, y) : NAN;
+      row_lse[r] = make_float4(off, lse,
+                               others <= 1.f ? -others / (1.f + others)
+                                             : 1.f / (1.f + others) - 1.f,
+                               0.f);
+      l = others < INFINITY ? log1pf(others) : fmaf(lse, kLn2, off - y);
       if (token_loss) token_loss[token] = l;
     }
     sh_loss[i] = l;
@@ -376,8 +402,7 @@ struct DlogitsParams {
   CUtensorMap hidden, weight, out;   // out: the piece's columns
   const int32_t* n_rows;
   const int32_t* labels;
-  const float* lse2;
-  const float* entry;     // p - 1 of the row's label
+  const float4* row_lse;  // of join_kernel
   const float* coef;
   uint32_t* status;
   int v_tiles, vocab, v0, k_blocks;
@@ -429,8 +454,7 @@ struct DlogitsWork {
     const int r = g.a0 + epi.row;
     const bool real = r < s.rows;
     const int label = real ? p.labels[r] : -1;
-    const float l2 = real ? p.lse2[r] : 0.f;
-    const float entry = real ? p.entry[r] : 0.f;
+    const float4 row = real ? p.row_lse[r] : make_float4(0.f, 0.f, 0.f, 0.f);
     const float coef = *p.coef;
     for (int c = 0; c < kTileN / 64; ++c) {
       const int v = g.b0 + c * 64;
@@ -439,14 +463,18 @@ struct DlogitsWork {
       for (int h = 0; h < 2; ++h) {
         float x[32];
         tmem_ld32(acc + c * 64 + h * 32, x);
+        if (row.x != 0.f) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[i] -= row.x;
+        }
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          x[i] = exp2_fast(fmaf(x[i], kLog2e, -l2));
+          x[i] = exp2_fast(fmaf(x[i], kLog2e, -row.y));
         const int first = v + h * 32;
         if (label >= first && label < first + 32) {
 #pragma unroll
           for (int i = 0; i < 32; ++i)
-            if (label == first + i) x[i] = entry;
+            if (label == first + i) x[i] = row.z;
         }
         if (!real || first + 32 > p.vocab) {
 #pragma unroll
@@ -837,8 +865,9 @@ lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
   if (e != cudaSuccess) return lm_cuda_fail(e, "head loss launch");
   e = lm_launch(join_kernel, (unsigned)lm_ceil_div(n, kJoinRows), kJoinThreads,
                 0, stream, true, v->stats, v->max_tokens, p.v_tiles,
-                v->label_logit, v->row_token, (int)n, v->n_rows, v->lse2,
-                v->label_entry, token_loss, loss, scale, v->coef, v->block_sums, v->ticket);
+                v->label_logit, v->row_token, (int)n, v->n_rows,
+                v->row_lse, token_loss, loss, scale, v->coef, v->block_sums,
+                v->ticket);
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "head join launch");
 }
 
@@ -929,8 +958,7 @@ void lm_head_carve(lamb_vocab* v, LmArena* a) {
   a->take(&v->counts, lm_ceil_div(n, kCountRows));
   a->take(&v->stats, lm_ceil_div(v->vocab, kTileN) * n);
   a->take(&v->label_logit, n);
-  a->take(&v->lse2, n);
-  a->take(&v->label_entry, n);
+  a->take(&v->row_lse, n);
   a->take(&v->block_sums, lm_ceil_div(n, kJoinRows));
   a->take(&v->ticket, 1);
   a->take(&v->coef, 1);
@@ -1052,8 +1080,7 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
   if (!ok) return lm_fail(LAMB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   d.n_rows = v->n_rows;
   d.labels = v->row_label;
-  d.lse2 = v->lse2;
-  d.entry = v->label_entry;
+  d.row_lse = v->row_lse;
   d.coef = v->coef;
   d.status = v->status;
   d.vocab = (int)v->vocab;

@@ -28,8 +28,7 @@ struct lamb_vocab {
   int32_t* counts = nullptr;    // labels in runs of tokens
   float2* stats = nullptr;      // [vocab tiles][max_tokens]
   float* label_logit = nullptr;
-  float* lse2 = nullptr;
-  float* label_entry = nullptr; // the label's entry of the softmax, less one
+  float4* row_lse = nullptr;
   double* block_sums = nullptr;
   uint32_t* ticket = nullptr;
   float* coef = nullptr;        // scale / number of labels

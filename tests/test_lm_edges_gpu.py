@@ -159,3 +159,78 @@ def test_sure_labels_keep_their_digits(n, vocab, width, word):
            (n + 2) * 2 * U32 * (entry.abs() @ h.double().abs()) +
            UBF * dw_want.abs())
     assert plan.query() == 0
+
+
+# ---------------------------------------------------------------------------
+# masks of the lowest values
+# ---------------------------------------------------------------------------
+LOWS = [-1e4, -1e10, -1e30, float(torch.finfo(torch.bfloat16).min)]
+
+
+@pytest.mark.parametrize("low", LOWS)
+@pytest.mark.parametrize("n", [40, 200])
+def test_tiles_of_masked_words(n, low):
+    """Words from 200 on are masked by a low value in W's first column, which
+    every hidden row has as one: whole tiles hold nothing else.  The others'
+    loss and gradients are those of a vocabulary without them."""
+    g = _gen(n)
+    vocab, width, real = 900, 64, 200
+    h = _randn((n, width), g, 1.0, torch.bfloat16)
+    w = _randn((vocab, width), g, 0.1, torch.bfloat16)
+    h[:, 0] = 1.0
+    w[:, 0] = 0.0
+    y = torch.arange(n, device=DEV) % real
+    y[3] = -1
+    ref = _head_reference(h, w[:real], y)
+    w[real:] = 0.0
+    w[real:, 0] = low
+    plan = VocabPlan(vocab, width, n)
+    token = torch.empty(n, device=DEV)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    loss = plan.loss_grad(h, w, y, dh, dw, token_loss=token)
+    _close(token, ref["token"], ref["token"] * 2 ** -20 + ref["e_token"])
+    _close(loss[0], ref["loss"], ref["loss"] * 2 ** -20 + ref["e_token"])
+    _close(dh, ref["dh"], ref["dh_err"] + UBF * ref["dh"].abs())
+    _close(dw[:real], ref["dw"], ref["dw_err"] + UBF * ref["dw"].abs())
+    assert (dw[real:] == 0).all()
+
+
+@pytest.mark.parametrize("low", LOWS + [1e10, 1e30])
+@pytest.mark.parametrize("n,vocab", [(5, 300), (150, 700)])
+def test_rows_whose_mask_leaves_nothing(n, vocab, low):
+    """Every word has the same logit, however low or high: the loss is ln V and
+    the softmax 1 / V."""
+    g = _gen(vocab)
+    width = 64
+    h = _randn((n, width), g, 1.0, torch.bfloat16)
+    w = torch.zeros(vocab, width, device=DEV, dtype=torch.bfloat16)
+    h[:, 0] = 1.0
+    w[:, 0] = low
+    y = torch.arange(n, device=DEV) * 7 % vocab
+    dl = torch.full((n, vocab), 1.0 / vocab, device=DEV, dtype=torch.float64)
+    dl[torch.arange(n, device=DEV), y] -= 1.0
+    dl /= n
+    want = dl.T @ h.double()
+    plan = VocabPlan(vocab, width, n)
+    token = torch.empty(n, device=DEV)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    loss = plan.loss_grad(h, w, y, dh, dw, token_loss=token)
+    ln_v = torch.full((n,), math.log(vocab), device=DEV, dtype=torch.float64)
+    _close(token, ln_v, ln_v * 2.0 ** -18)      # sums of V equal terms: exact
+    _close(loss[0], ln_v[0], ln_v[0] * 2.0 ** -18)
+    # the logits' gradient in bf16 (2^-9, the exponentials 2^-20), n terms
+    size = dl.abs().T @ h.double().abs()
+    _close(dw, want, (2.0 ** -9 + 2.0 ** -18 + (n + 2) * 2 * U32) * size +
+           UBF * want.abs())
+    assert (dh[:, 1:] == 0).all()               # W is zero there
+
+
+def test_an_infinite_logit_of_the_label_is_not_a_loss_of_zero():
+    """inf - inf: the formula has no value, and neither have the results."""
+    h = torch.ones(1, 16, device=DEV, dtype=torch.bfloat16)
+    w = torch.zeros(300, 16, device=DEV, dtype=torch.bfloat16)
+    w[7, 3] = math.inf
+    plan = VocabPlan(300, 16, 1)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    loss = plan.loss_grad(h, w, torch.tensor([7], device=DEV), dh, dw)
+    assert torch.isnan(loss).all() and torch.isnan(dw[7]).all()
