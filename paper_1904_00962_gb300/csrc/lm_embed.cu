@@ -601,18 +601,13 @@ bool vec_ok(const void* p, int dtype, int64_t stride, int width, int cols = 4) {
 }
 
 template <class TI, class TO>
-void launch_embed(const lamb_vocab* v, const void* table, int64_t ts,
+cudaError_t launch_embed(const lamb_vocab* v, const void* table, int64_t ts,
                   const int64_t* ids, int64_t n, float scale, void* out,
                   int64_t os, bool vec, cudaStream_t stream) {
   const unsigned grid = (unsigned)lm_ceil_div(n, kEmbedThreads / 32);
-  if (vec)
-    embed_kernel<TI, TO, true><<<grid, kEmbedThreads, 0, stream>>>(
-        (const TI*)table, ts, ids, n, v->width, v->vocab, scale, (TO*)out, os,
-        v->status);
-  else
-    embed_kernel<TI, TO, false><<<grid, kEmbedThreads, 0, stream>>>(
-        (const TI*)table, ts, ids, n, v->width, v->vocab, scale, (TO*)out, os,
-        v->status);
+  return lm_launch(vec ? embed_kernel<TI, TO, true> : embed_kernel<TI, TO, false>,
+                   grid, kEmbedThreads, 0, stream, false, (const TI*)table, ts,
+                   ids, n, v->width, v->vocab, scale, (TO*)out, os, v->status);
 }
 
 template <class TG, class TT, bool kVec>
@@ -711,19 +706,19 @@ extern "C" lamb_status_t lamb_vocab_embed(
                    vec_ok(out, out_dtype, out_stride, v->width);
   const float s = (float)scale;
   typedef __nv_bfloat16 bf;
+  cudaError_t e;
   if (table_dtype == LAMB_F32 && out_dtype == LAMB_F32)
-    launch_embed<float, float>(v, table, table_stride, ids, n_tokens, s, out,
-                               out_stride, vec, stream);
+    e = launch_embed<float, float>(v, table, table_stride, ids, n_tokens, s, out,
+                                   out_stride, vec, stream);
   else if (table_dtype == LAMB_F32)
-    launch_embed<float, bf>(v, table, table_stride, ids, n_tokens, s, out,
-                            out_stride, vec, stream);
+    e = launch_embed<float, bf>(v, table, table_stride, ids, n_tokens, s, out,
+                                out_stride, vec, stream);
   else if (out_dtype == LAMB_F32)
-    launch_embed<bf, float>(v, table, table_stride, ids, n_tokens, s, out,
-                            out_stride, vec, stream);
+    e = launch_embed<bf, float>(v, table, table_stride, ids, n_tokens, s, out,
+                                out_stride, vec, stream);
   else
-    launch_embed<bf, bf>(v, table, table_stride, ids, n_tokens, s, out,
-                         out_stride, vec, stream);
-  const cudaError_t e = cudaGetLastError();
+    e = launch_embed<bf, bf>(v, table, table_stride, ids, n_tokens, s, out,
+                             out_stride, vec, stream);
   return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "embed launch");
 }
 
@@ -760,9 +755,8 @@ extern "C" lamb_status_t lamb_vocab_embed_grad(
                  to - from,        (int)(used / unit),      unit};
   };
   if (!n) {
-    clear_kernel<<<clear_ctas(clear(0, 1)), kSortThreads, 0, stream>>>(
-        clear(0, 1));
-    e = cudaGetLastError();
+    e = lm_launch(clear_kernel, clear_ctas(clear(0, 1)), kSortThreads, 0, stream,
+                  false, clear(0, 1));
     return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "clear launch");
   }
   // (4095 tokens: 31 us with a launch a pass, 29 with one in all)

@@ -831,12 +831,14 @@ cudaError_t head_inputs(const lamb_vocab* v, const void* hidden, int64_t hs,
                   token_loss, (__nv_bfloat16*)grad_hidden, gs, v->status);
   if (e != cudaSuccess) return e;
   if (!lm_mappable(weight, ws)) {
-    rows_copy_kernel<<<grid_for(v->vocab * v->width, v->sms), 256, 0, stream>>>(
-        in->weight, ws, v->vocab, v->width, v->weight_copy, in->pitch);
+    e = lm_launch(rows_copy_kernel,
+                  (unsigned)grid_for(v->vocab * v->width, v->sms), 256, 0, stream,
+                  false, in->weight, ws, v->vocab, v->width, v->weight_copy,
+                  in->pitch);
     in->weight = v->weight_copy;
     in->weight_stride = in->pitch;
   }
-  return cudaGetLastError();
+  return e;
 }
 
 lamb_status_t head_loss(lamb_vocab* v, const HeadInputs& in, int64_t n,
@@ -1027,10 +1029,10 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
   if (!n) {
     e = cudaMemsetAsync(loss, 0, sizeof(float), stream);
     if (e == cudaSuccess && !accumulate) {
-      clear_rows_kernel<<<grid_for(v->vocab * v->width, v->sms), 256, 0,
-                          stream>>>(grad_weight, f32, v->vocab, v->width,
-                                    grad_weight_stride);
-      e = cudaGetLastError();
+      e = lm_launch(clear_rows_kernel,
+                    (unsigned)grid_for(v->vocab * v->width, v->sms), 256, 0,
+                    stream, false, grad_weight, (int)f32, v->vocab, v->width,
+                    grad_weight_stride);
     }
     return e == cudaSuccess ? LAMB_OK : lm_cuda_fail(e, "clearing the gradient");
   }

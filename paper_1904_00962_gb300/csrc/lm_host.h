@@ -22,7 +22,10 @@ inline lamb_status_t lm_fail(lamb_status_t st, const char* fmt, ...) {
   return st;
 }
 
+// The runtime's record of the error is taken back: it is reported here, once, and
+// would be the next launch's otherwise.
 inline lamb_status_t lm_cuda_fail(cudaError_t e, const char* what) {
+  (void)cudaGetLastError();
   return lm_fail(e == cudaErrorMemoryAllocation ? LAMB_ERR_OOM : LAMB_ERR_CUDA,
                  "%s: %s (%d)", what, cudaGetErrorString(e), (int)e);
 }
@@ -60,7 +63,7 @@ struct LmArena {
 
 inline int lm_elem_size(int dtype) { return dtype == LAMB_F32 ? 4 : 2; }
 
-// Launches a kernel.  after_prior: it may start while the launch in front of it in
+// Launches a kernel; its own error, whatever an earlier call left.  after_prior: it may start while the launch in front of it in
 // the stream still runs, and waits for that one itself (after_prior_launch).
 template <class... P, class... A>
 cudaError_t lm_launch(void (*kernel)(P...), unsigned grid, unsigned block,
@@ -94,6 +97,7 @@ inline EncodeTiled lm_encoder() {
                                        cudaEnableDefault, &found) !=
           cudaSuccess ||
       found != cudaDriverEntryPointSuccess) {
+    (void)cudaGetLastError();
     return nullptr;
   }
   return reinterpret_cast<EncodeTiled>(fn);

@@ -599,23 +599,24 @@ lamb_status_t muon_check(const lamb_muon* p, const lamb_muon_hyper_t* h) {
   return LAMB_OK;
 }
 
+// The small matrices, and what comes in front of the others' products.  A launch that
+// is refused is the last of the call.
 template <class TG, bool kStep>
-void muon_small(const lamb_muon* p, const MuonPtrs* ptrs, const MuonConsts& k,
-                int steps, const float* d_lr, cudaStream_t stream) {
+cudaError_t muon_front(const lamb_muon* p, const MuonPtrs* ptrs,
+                       const MuonConsts& k, int steps, const float* d_lr,
+                       cudaStream_t stream) {
+  cudaError_t e = cudaSuccess;
   if (p->n_small)
-    muon_small_kernel<TG, kStep>
-        <<<p->n_small, kSmallThreads, (size_t)p->small_bytes, stream>>>(
-            p->mats, ptrs, p->small, k, steps, d_lr, p->status);
-}
-
-template <class TG, bool kStep>
-void muon_front(const lamb_muon* p, const MuonPtrs* ptrs, const MuonConsts& k,
-                cudaStream_t stream) {
-  if (!p->n_chunks) return;
-  muon_norm_kernel<TG, kStep><<<p->n_chunks, kMuonThreads, 0, stream>>>(
-      ptrs, p->chunks, k, p->part);
-  muon_start_kernel<TG, kStep><<<p->n_chunks, kMuonThreads, 0, stream>>>(
-      p->mats, ptrs, p->chunks, k, p->part, p->done, p->status);
+    e = lm_launch(muon_small_kernel<TG, kStep>, (unsigned)p->n_small,
+                  kSmallThreads, (size_t)p->small_bytes, stream, false, p->mats,
+                  ptrs, p->small, k, steps, d_lr, p->status);
+  if (e != cudaSuccess || !p->n_chunks) return e;
+  e = lm_launch(muon_norm_kernel<TG, kStep>, (unsigned)p->n_chunks, kMuonThreads,
+                0, stream, false, ptrs, p->chunks, k, p->part);
+  if (e != cudaSuccess) return e;
+  return lm_launch(muon_start_kernel<TG, kStep>, (unsigned)p->n_chunks,
+                   kMuonThreads, 0, stream, false, p->mats, ptrs, p->chunks, k,
+                   p->part, p->done, p->status);
 }
 
 lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
@@ -638,23 +639,15 @@ lamb_status_t muon_run(lamb_muon* p, const lamb_muon_hyper_t* h,
   q.k.nesterov = (h->flags & LAMB_MUON_FLAG_NESTEROV) != 0;
   q.k.scale_kind = h->scale_kind;
   typedef __nv_bfloat16 bf;
+  cudaError_t e;
   if (d_lr && p->grad_bf16)
-    muon_small<bf, true>(p, q.ptrs, q.k, h->steps, d_lr, stream);
+    e = muon_front<bf, true>(p, q.ptrs, q.k, h->steps, d_lr, stream);
   else if (d_lr)
-    muon_small<float, true>(p, q.ptrs, q.k, h->steps, d_lr, stream);
+    e = muon_front<float, true>(p, q.ptrs, q.k, h->steps, d_lr, stream);
   else if (p->grad_bf16)
-    muon_small<bf, false>(p, q.ptrs, q.k, h->steps, d_lr, stream);
+    e = muon_front<bf, false>(p, q.ptrs, q.k, h->steps, nullptr, stream);
   else
-    muon_small<float, false>(p, q.ptrs, q.k, h->steps, d_lr, stream);
-  if (d_lr && p->grad_bf16)
-    muon_front<bf, true>(p, q.ptrs, q.k, stream);
-  else if (d_lr)
-    muon_front<float, true>(p, q.ptrs, q.k, stream);
-  else if (p->grad_bf16)
-    muon_front<bf, false>(p, q.ptrs, q.k, stream);
-  else
-    muon_front<float, false>(p, q.ptrs, q.k, stream);
-  cudaError_t e = cudaGetLastError();
+    e = muon_front<float, false>(p, q.ptrs, q.k, h->steps, nullptr, stream);
   if (e == cudaSuccess && p->step_tiles) {
     q.tiles = p->tiles;
     q.done = p->done;

@@ -8,6 +8,7 @@ import torch
 
 from paper_1904_00962_gb300 import binding as B
 from paper_1904_00962_gb300.muon import MuonPlan
+from paper_1904_00962_gb300.state import DeviceState, LambPlan
 from paper_1904_00962_gb300.vocab import VocabPlan
 from test_muon_gpu import TOL, _exact, _matrix, _near
 from test_vocab_gpu import (DEV, U32, UBF, _close, _gen, _head_reference,
@@ -234,3 +235,44 @@ def test_an_infinite_logit_of_the_label_is_not_a_loss_of_zero():
     dh, dw = torch.empty_like(h), torch.empty_like(w)
     loss = plan.loss_grad(h, w, torch.tensor([7], device=DEV), dh, dw)
     assert torch.isnan(loss).all() and torch.isnan(dw[7]).all()
+
+
+# ---------------------------------------------------------------------------
+# after a refused call
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("refused", ["memory", "device", "another's device"])
+def test_a_failed_plan_is_not_the_next_call_s_error(refused):
+    """A plan of 2 TB is refused by the allocation, one on a device that is not
+    there by the runtime: the error belongs to that call alone."""
+    words = VocabPlan(10, 16, 8)
+    muon = MuonPlan([(8, 8), (80, 70)])
+    state = DeviceState([100])
+    lamb = LambPlan(state)
+    tab = torch.ones(10, 16, device=DEV)
+    odd = torch.ones(10, 17, device=DEV, dtype=torch.bfloat16)[:, :16]
+    ids = torch.arange(8, device=DEV)
+    u = [torch.ones(s, device=DEV) for s in muon.shapes]
+    o = [torch.empty(s, device=DEV, dtype=torch.bfloat16) for s in muon.shapes]
+    muon.bind_direction(u, o)
+    one = torch.ones(1, device=DEV)
+    step = torch.ones(1, dtype=torch.int64, device=DEV)
+    fail = {"memory": lambda: VocabPlan(2 ** 30, 2 ** 10, 64),
+            "device": lambda: MuonPlan([(8, 8)], device="cuda:99"),
+            "another's device": lambda: B.lamb_plan_create([8], device=99)}
+    calls = [lambda: words.embed(tab, ids),
+             lambda: words.embed_grad(tab[:0], ids[:0], tab.clone()),
+             lambda: words.embed_grad(tab[:8], ids, tab.clone()),
+             lambda: words.loss(odd[:8], odd, ids),
+             lambda: words.loss_grad(odd[:0], odd, ids[:0], odd[:0],
+                                     odd.clone()),
+             lambda: muon.direction(B.make_muon_hyper())]
+    if refused != "another's device":
+        calls.append(lambda: lamb.lamb_step(B.make_hyper(), step, one))
+    for call in calls:
+        with pytest.raises(B.LambError) as e:
+            fail[refused]()
+        assert e.value.status in (B.LAMB_ERR_OOM, B.LAMB_ERR_CUDA,
+                                  B.LAMB_ERR_INVALID_ARG)
+        call()
+    torch.cuda.synchronize()
+    assert words.query() == 0 and muon.query() == 0 and lamb.query() == 0
