@@ -9,7 +9,7 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
-from .state import _dtype_code
+from .state import _dtype_code, _with_index
 
 _TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
 
@@ -22,7 +22,7 @@ class MuonPlan:
                  copy_dtype=None, device="cuda:0"):
         self.shapes = [(int(r), int(c)) for r, c in shapes]
         self.grad_dtype, self.copy_dtype = grad_dtype, copy_dtype
-        self.device = torch.device(device)
+        self.device = _with_index(device)
         self._bound = {}
         if decay_mask is not None and len(decay_mask) != len(self.shapes):
             raise ValueError("decay_mask: one entry a matrix is needed")

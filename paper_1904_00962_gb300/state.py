@@ -22,6 +22,14 @@ def _dtype_code(name):
             "bf16": B.LAMB_BF16}[name]
 
 
+def _with_index(device):
+    """The device by its number: "cuda" is PyTorch's current one."""
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    return device
+
+
 class DeviceState:
     def __init__(self, sizes, *, grad_dtype="f32", copy_dtype=None,
                  device="cuda:0", with_v=True, align_elems=ALIGN_ELEMS,

@@ -15,6 +15,7 @@ import contextlib
 import torch
 
 from . import binding as B
+from .state import _with_index
 
 _BF16 = {torch.bfloat16: B.LAMB_BF16}
 _BOTH = {torch.float32: B.LAMB_F32, torch.bfloat16: B.LAMB_BF16}
@@ -25,7 +26,7 @@ class VocabPlan:
     `width` columns, for up to `max_tokens` tokens a call."""
 
     def __init__(self, vocab, width, max_tokens, *, device="cuda:0"):
-        self.device = torch.device(device)
+        self.device = _with_index(device)
         self.vocab, self.width = int(vocab), int(width)
         self.max_tokens = int(max_tokens)
         self._index = self.device.index or 0

@@ -141,3 +141,17 @@ def test_a_refused_binding_keeps_the_earlier_tensors(monkeypatch):
     plan.bind(*new)
     assert set(map(id, _all_bound(plan))) == \
         set(map(id, sum(new, []) + u + o))
+
+
+def test_cuda_is_the_current_device(monkeypatch):
+    made = []
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(B, "lamb_vocab_create",
+                        lambda *a: made.append(a[-1]) or 0)
+    monkeypatch.setattr(B, "lamb_muon_create",
+                        lambda *a: made.append(a[-1]) or 0)
+    plans = [VocabPlan(10, 16, 8, device="cuda"),
+             MuonPlan([(4, 4)], device=torch.device("cuda")),
+             VocabPlan(10, 16, 8, device="cuda:1"), MuonPlan([(4, 4)])]
+    assert made == [3, 3, 1, 0]
+    assert [p.device.index for p in plans] == [3, 3, 1, 0]
