@@ -62,6 +62,11 @@ class VocabPlan:
             raise ValueError(f"{name} is not on {self.device}")
         return t.data_ptr()
 
+    def _scalar(self, name, t):
+        """A float tensor of one element, of no dimension or one."""
+        return self._vector(name, t.reshape(1) if t.dim() == 0 else t, 1,
+                            torch.float32)
+
     def _stream(self, stream):
         """A raw stream handle: PyTorch's current one of the plan's device, or
         the given one."""
@@ -124,7 +129,7 @@ class VocabPlan:
         y = self._vector("labels", labels, n, torch.int64)
         tl = 0 if token_loss is None else \
             self._vector("token_loss", token_loss, n, torch.float32)
-        lp = self._vector("loss", loss, 1, torch.float32)
+        lp = self._scalar("loss", loss)
         return n, loss, (h, hs, w, ws, y, n), (tl or None, lp)
 
     def loss(self, hidden, weight, labels, *, token_loss=None, loss=None,
@@ -147,8 +152,7 @@ class VocabPlan:
         gh, _, ghs = self._matrix("grad_hidden", grad_hidden, n, _BF16)
         gw, code, gws = self._matrix("grad_weight", grad_weight, self.vocab,
                                      _BOTH)
-        sp = None if scale is None else \
-            self._vector("scale", scale, 1, torch.float32)
+        sp = None if scale is None else self._scalar("scale", scale)
         B.lamb_vocab_loss_grad(self.handle, *ins, sp, *outs, gh, ghs, gw, code,
                                gws, int(accumulate), self._stream(stream))
         return loss

@@ -155,3 +155,28 @@ def test_cuda_is_the_current_device(monkeypatch):
              VocabPlan(10, 16, 8, device="cuda:1"), MuonPlan([(4, 4)])]
     assert made == [3, 3, 1, 0]
     assert [p.device.index for p in plans] == [3, 3, 1, 0]
+
+
+def test_one_element_has_no_dimension_or_one(monkeypatch):
+    """The scale and the loss of one element, as a loss or a gradient scaler
+    has them."""
+    calls = []
+    plan = _words(monkeypatch, calls=calls)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 5,
+                        raising=False)
+    rows = torch.zeros(4, 16, dtype=torch.bfloat16)
+    weight, y = torch.zeros(10, 16, dtype=torch.bfloat16), torch.arange(4)
+    for scale, loss in ((torch.ones(()), torch.zeros(())),
+                        (torch.ones(1), torch.zeros(1))):
+        assert plan.loss(rows, weight, y, loss=loss) is loss
+        assert calls[-1][1][-2] == loss.data_ptr()
+        plan.loss_grad(rows, weight, y, rows.clone(), weight.clone(),
+                       scale=scale, loss=loss)
+        assert calls[-1][1][7] == scale.data_ptr()
+    n = len(calls)
+    for scale in (torch.ones(2), torch.ones((), dtype=torch.float64),
+                  torch.ones(1, 1)):
+        with pytest.raises(ValueError):
+            plan.loss_grad(rows, weight, y, rows.clone(), weight.clone(),
+                           scale=scale)
+    assert len(calls) == n
