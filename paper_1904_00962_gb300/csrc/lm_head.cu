@@ -1057,7 +1057,9 @@ extern "C" lamb_status_t lamb_vocab_loss_grad(
   GradsParams g;
   // (the copy of W has rows of whole blocks; the user's only if the width is)
   g.weight_blocks = v->width % 64 == 0 || in.weight == v->weight_copy;
-  g.weight_out = !f32 && !accumulate &&
+  // (a tensor store leaves out whole units of 16 bytes only: where a row ends inside
+  // one, the rest of it is the caller's)
+  g.weight_out = !f32 && !accumulate && v->width % 8 == 0 &&
                  lm_mappable(grad_weight, grad_weight_stride);
   const bool ok =
       lm_map(v->encode, &d.hidden, true, v->rows, whole, v->width, in.pitch,

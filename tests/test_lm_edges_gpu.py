@@ -276,3 +276,48 @@ def test_a_failed_plan_is_not_the_next_call_s_error(refused):
         call()
     torch.cuda.synchronize()
     assert words.query() == 0 and muon.query() == 0 and lamb.query() == 0
+
+
+# ---------------------------------------------------------------------------
+# what lies beside a result
+# ---------------------------------------------------------------------------
+def _framed(rows, width, pad, shift, dtype):
+    """A [rows, width] view of rows of width + pad, and whether all beside it
+    in its buffer is still as it was."""
+    buf = torch.full((rows * (width + pad) + shift + 64,), 7.0, device=DEV,
+                     dtype=dtype)
+    mine = torch.zeros_like(buf, dtype=torch.bool)
+    at = slice(shift, shift + rows * (width + pad))
+    mine[at].view(rows, width + pad)[:, :width] = True
+    view = buf[at].view(rows, width + pad)[:, :width]
+    return view, lambda: bool((buf[~mine] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("width,pad,shift", [
+    (1, 7, 0), (37, 3, 8), (44, 4, 0), (63, 1, 0), (64, 8, 0), (100, 28, 8),
+    (257, 7, 0), (30, 2, 1)])
+def test_columns_beside_a_result_are_left_alone(dtype, add, width, pad, shift):
+    """Columns between the width and the row stride belong to others."""
+    g = _gen(width)
+    n, vocab = 150, 700
+    plan = VocabPlan(vocab, width, n)
+    tab = _randn((vocab, width), g, 0.1, torch.bfloat16)
+    h = _randn((n, width), g, 1.0, torch.bfloat16)
+    y = torch.randint(vocab, (n,), generator=g, device=DEV)
+    y[::5] = -1
+    out, out_ok = _framed(n, width, pad, shift, dtype)
+    plan.embed(tab, y, out=out)
+    assert out_ok()
+    for rows in (n, 60):                       # pairs of CTAs, single ones
+        dw, dw_ok = _framed(vocab, width, pad, shift, dtype)
+        dh, dh_ok = _framed(rows, width, pad, shift, torch.bfloat16)
+        token, token_ok = _framed(1, rows, 0, shift, torch.float32)
+        dw.zero_()
+        plan.loss_grad(h[:rows], tab, y[:rows], dh, dw, accumulate=add,
+                       token_loss=token[0])
+        assert dw_ok() and dh_ok() and token_ok()
+        plan.embed_grad(dh, y[:rows], dw, accumulate=add)
+        assert dw_ok()
+    assert plan.query() == 0
