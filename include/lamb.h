@@ -668,7 +668,8 @@ LAMB_API lamb_status_t lamb_vocab_embed(
 /* The lookup's gradient: table_grad[v] = scale * sum of grad_out[t] over the
  * tokens with ids[t] = v, in fp32 and in a fixed order.  accumulate = 0 writes
  * every row of table_grad (zeros where a word has no token); accumulate = 1 adds
- * to the rows that have tokens and leaves the others alone.  grad_out and
+ * to the rows that have tokens and leaves the others alone (an fp32 element below
+ * 2^-126 in size, before or after the addition, may count as 0).  grad_out and
  * table_grad are LAMB_F32 or LAMB_BF16 each. */
 LAMB_API lamb_status_t lamb_vocab_embed_grad(
     struct lamb_vocab* plan, const void* grad_out, int32_t grad_dtype,
@@ -682,7 +683,10 @@ LAMB_API lamb_status_t lamb_vocab_embed_grad(
  *   token_loss  NULL or DEVICE float [n_tokens]: lse_t - logit of the label, 0
  *               where the label is absent
  *   loss        DEVICE float: the mean over the labels that are present (0 if
- *               there are none) */
+ *               there are none); NaN or Inf where the formula's is, which no
+ *               status bit tells
+ * A weight that does not start on 16 bytes or whose row stride is no multiple of 8
+ * is copied in every call. */
 LAMB_API lamb_status_t lamb_vocab_loss(
     struct lamb_vocab* plan, const void* hidden, int64_t hidden_stride,
     const void* weight, int64_t weight_stride, const int64_t* labels,
@@ -695,7 +699,7 @@ LAMB_API lamb_status_t lamb_vocab_loss(
  *   grad_weight  bf16 or fp32 [vocab, width]; accumulate = 1 adds to it
  * The gradient of the logits is rounded to bf16 on its way into the two products
  * with weight and hidden, whose sums are fp32: an fp32 grad_weight holds sums of
- * such terms. */
+ * such terms.  Exponentials and partial sums below 2^-126 may count as 0. */
 LAMB_API lamb_status_t lamb_vocab_loss_grad(
     struct lamb_vocab* plan, const void* hidden, int64_t hidden_stride,
     const void* weight, int64_t weight_stride, const int64_t* labels,

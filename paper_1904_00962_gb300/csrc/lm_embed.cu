@@ -3,8 +3,9 @@
 //   out[t]  = s E[id_t]                         (a row of zeros for id_t < 0)
 //   dE[v] (+)= s sum over t with id_t = v of dY[t]
 //
-// Lookup: a copy with a gather, bound by HBM (each row read and written once); a
-// warp takes a row, 16 bytes a lane.
+// Lookup: a copy with a gather (each row read and written once); a warp takes a row,
+// four columns a lane at a time.  Bound by loads in flight: DRAM is 44% busy, as words
+// that come again and half of what is written stay in L2.
 //
 // Gradient: the token positions are sorted by id (stable, least significant digit
 // first, 8 bits a pass), so that every word's rows are added in the order of the
@@ -17,10 +18,11 @@
 // Launches follow one another early (griddepcontrol): count, a move for each digit
 // (which counts the next digit), sums, joins; up to 4096 tokens are sorted in one.
 //
-// Measured: lookup of 65536 x 768 (fp32 to bf16) 27 us, 5.1 TB/s; gradient of 65536
-// x 1024 (bf16) into a fresh table 71 us, of which the sort takes 22 with the clearing,
-// the sums 38 and the joins 8: 27 us of HBM traffic, the rest latency of the longest
-// word and of four launches in front; 4095 x 768 added to a tied table 20 us.
+// Measured: lookup of 65536 x 768 (fp32 to bf16) 28 us, 5.0 TB/s of its own bytes;
+// gradient of 65536 x 1024 (bf16) into a fresh table 73 us, of which the sort takes 23
+// with the clearing, the sums 38 and the joins 8: 27 us of HBM traffic, the rest
+// latency of the longest word and of four launches in front; 4095 x 768 added to a tied
+// table 20 us.
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -27,8 +27,8 @@
 // stay in fp32.  8 T V D operations in all.
 //
 // Measured: loss of 8192 x 30522 x 768 (6963 labels) 201 us, 1.6 PFLOP/s; loss and
-// gradients of 9830 x 30522 x 1024 1524 us, 1.58 PFLOP/s of the 8 T V D: bound by
-// the tensor cores under the power limit.  77 x 30522 x 1024 80 us: W is read twice
+// gradients of 9830 x 30522 x 1024 1521 us, 1.58 PFLOP/s of the 8 T V D: bound by
+// the tensor cores under the power limit.  77 x 30522 x 1024 81 us: W is read twice
 // from HBM and dW written, 28 us of it; the rest is six launches' latency.
 #include <cuda_bf16.h>
 
@@ -743,7 +743,8 @@ slabs_kernel(const float* slabs, int count, int64_t slab, int pitch, int width,
   }
 }
 
-// Rows of a bf16 matrix that no tensor map can read, on 16-byte boundaries.
+// Rows of a bf16 matrix that no tensor map can read, on 16-byte boundaries: a pass over
+// all of W in each call with such a W, element by element.
 __global__ void __launch_bounds__(256)
 rows_copy_kernel(const __nv_bfloat16* in, int64_t in_stride, int64_t rows,
                  int width, __nv_bfloat16* out, int64_t out_stride) {

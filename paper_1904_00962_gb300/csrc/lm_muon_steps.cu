@@ -28,9 +28,10 @@
 // Measured: one 1024 x 1024 matrix 139 us with the momentum's launches, 15 products
 // one behind another; one BERT-large layer (four 1024 x 1024, two 4096 x 1024) 308
 // us, bound by the chain of a matrix' products (64 blocks of K, the epilogue's drain,
-// the counters); all matrices of BERT-base 1350 us, bound by HBM: X, D and E take
-// some 1.2 GB a step and do not fit L2.  Sets that do (56 MB each) wait for one
-// another's products instead: 1500 us.  On the way there (both cases, us, with the momentum's
+// the counters); all matrices of BERT-base 1355 us: X, D and E do not fit L2 and pass
+// DRAM every step, 6.5 GB in all at 4.8 TB/s (61% of its peak, 0.71 of a copy's rate),
+// the tensor pipe 43% busy.  Sets that do fit (56 MB each) wait for one another's
+// products instead: 1500 us.  On the way there (both cases, us, with the momentum's
 // launches): a launch a product with a CTA a tile 550 / 2909, one launch 419 / 2336,
 // all matrices in two sets 419 / 1812, pairs of CTAs 353 / 1683.  X in fp32 beside hi
 // in place of lo: 411 / 1963.
