@@ -729,7 +729,8 @@ LAMB_API lamb_status_t lamb_vocab_destroy(struct lamb_vocab* plan);
  * s is update_scale times 1, sqrt(max(1, rows / cols)) or 0.2 sqrt(max(rows,
  * cols)).  The products take 16-bit operands (11 significant bits, the large
  * terms apart in 32): X is within about 1e-3 of the exact one in the Frobenius
- * norm.  Sums of squares of u are formed in fp32: entries beyond 1e19 in size
+ * norm, within 5e-3 where one direction is all there is (rank one, equal entries)
+ * and roundings do not average out.  Sums of squares of u are formed in fp32: entries beyond 1e19 in size
  * make a norm infinite (LAMB_STATUS_NONFINITE), those below 1e-20 count as 0.
  * The same bits in every run.
  * ------------------------------------------------------------------------- */

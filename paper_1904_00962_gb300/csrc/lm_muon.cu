@@ -15,7 +15,8 @@
 //     beta_i = b l_i + c (l_i^2 + (D D)_ii)
 //   and X <- (a + beta_i) X + E X takes X whole from the pair.
 // The direction is then within 3e-4 .. 1e-3 of the exact one (Gaussian, low-rank
-// and power-law spectra, 10 x 10 to 1536 x 1600): half a bf16 rounding; with G
+// and power-law spectra, 10 x 10 to 1536 x 1600; up to 4.4e-3 where all entries are
+// equal or the rank is one, at short sides of 100 to 300): half a bf16 rounding; with G
 // rounded as it is, 1.7e-3 .. 1.2e-2, in bf16 1.3e-2 .. 1e-1.  Scales that are
 // powers of two keep the entries inside fp16's range.
 //
