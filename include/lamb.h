@@ -745,7 +745,10 @@ typedef struct {
   double weight_decay;   /* lambda >= 0, decoupled; where the mask is 1       */
   double eps;            /* >= 0                                             */
   double a, b, c;        /* of the odd polynomial, up to 16 in size; the usual
-                            ones are 3.4445, -4.7750, 2.0315                 */
+                            ones are 3.4445, -4.7750, 2.0315.  With s the
+                            largest singular value on the way, s <= 8 and
+                            |b| s^2 + |c| s^4 <= 255 (fp16's range), or X is
+                            not finite; the usual ones keep s below 1.3      */
   double update_scale;
   int32_t steps;         /* 1 .. 64, usually 5                               */
   int32_t scale_kind;    /* LAMB_MUON_SCALE_*                                */
