@@ -474,15 +474,18 @@ NormLayout grad_layout(int width, bool vec, bool bf16) {
 
 }  // namespace
 
-// Shared-memory limits on the current device of the kernels for a width.
+// Shared-memory limits on the current device of the kernels for a width.  A limit is
+// its kernel's, and one for all plans: a CTA's rows are of many widths, so that theirs is
+// what the widest ones need (fp32: 196,608 bytes).
 cudaError_t norm_grad_setup(int width) {
   cudaError_t e = cudaSuccess;
   for (int t = 0; t < 4 && e == cudaSuccess; ++t) {
     const NormLayout l = grad_layout(width, true, t == 3);
     const GradKernel k = grad_kernel_of(l, t & 1, t & 2);
+    const int most_threads = l.wide ? 32 * kNormMostWarps : kNormThreads;
     if (k.smem)
       e = cudaFuncSetAttribute(k.run, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               k.smem * l.threads);
+                               k.smem * most_threads);
   }
   return e;
 }

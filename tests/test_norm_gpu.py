@@ -322,3 +322,25 @@ def test_norm_calls_refuse(gpu):
             call()
         assert e.value.status == B.LAMB_ERR_INVALID_ARG
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("widths", [(8192, 4096, 2048, 1024, 520),
+                                    (520, 1024, 2048, 4096, 8192)])
+@pytest.mark.parametrize("g_type,h_type", [(BF16, BF16), (BF16, F32),
+                                           (F32, BF16), (F32, F32)])
+def test_norm_grad_of_plans_that_live_together(gpu, widths, g_type, h_type):
+    """Plans of other widths that are made later leave a plan's launches as they are."""
+    n = 5
+    plans = [NormPlan(d, n, eps=EPS) for d in widths]
+    for d, plan in zip(widths, plans):
+        h, dy = _rows(n, d, h_type, 1), _rows(n, d, g_type, 2)
+        w, dw = _weight(d, BF16), torch.empty(d, device="cuda")
+        dh = torch.empty_like(h)
+        plan.norm_grad(dy, h, w, dh, dw)
+        want, size, ww, wsize = _grads(h, dy, w, None)
+        rounding = _half(h_type) if h_type == BF16 else 0
+        _close(dh, want, 2 * ROUNDS * size + rounding * want.abs())
+        _close(dw, ww, 256 * 2.0 ** -24 * wsize)
+    torch.cuda.synchronize()
+    for plan in plans:
+        plan.destroy()
