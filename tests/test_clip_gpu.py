@@ -229,3 +229,19 @@ def test_clip_tensors_on_16_and_32_bytes(gpu, g_type, o_type, shift):
     factor = torch.zeros(1, device="cuda")
     norm = plan.clip(0.5, factor=factor)
     _check(out or grads, before, norm, factor, 0.5)
+
+
+@pytest.mark.parametrize("sizes", [[16384 * 1003 + 77], [16385, 3, 40000] * 350])
+@pytest.mark.parametrize("g_type,o_type", [("f32", None), ("bf16", "f32")])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_clip_of_more_chunks_than_ctas(gpu, sizes, g_type, o_type, shift):
+    """A thousand pieces of 16,384 elements and more: several for each CTA."""
+    grads = _grads(sizes, g_type, shift=shift)
+    before = [g.clone() for g in grads]
+    plan = ClipPlan(sizes, grad_dtype=g_type, out_dtype=o_type)
+    out = _grads(sizes, o_type, seed=2, shift=shift) if o_type else grads
+    plan.bind(grads, out if o_type else None)
+    factor = torch.zeros(1, device="cuda")
+    norm = plan.clip(0.5, factor=factor)
+    _check(out, before, norm, factor, 0.5)
+    assert plan.query() == 0

@@ -344,3 +344,23 @@ def test_norm_grad_of_plans_that_live_together(gpu, widths, g_type, h_type):
     torch.cuda.synchronize()
     for plan in plans:
         plan.destroy()
+
+
+@pytest.mark.parametrize("n,d,shift", [(1300, 8200, 0), (700, 20999, 0),
+                                       (1000, 5001, 0), (640, 2048, 1),
+                                       (9000, 257, 0), (30000, 31, 3)])
+@pytest.mark.parametrize("g_type,h_type", [(BF16, BF16), (F32, F32)])
+def test_norm_grad_of_more_rows_than_ctas(gpu, n, d, shift, g_type, h_type):
+    """Walked rows and rows taken column by column, several of them for each CTA: as
+    many additions as in test_norm_grad."""
+    h = _rows(n, d, h_type, 1, shift=shift)
+    dy = _rows(n, d, g_type, 2, shift=shift)
+    dh_in = _rows(n, d, h_type, 3, shift=shift)
+    w, dw = _weight(d, BF16), _weight(d, F32, 9)
+    dw0, dh = dw.double(), torch.empty_like(h)
+    with NormPlanOf(d, n) as plan:
+        plan.norm_grad(dy, h, w, dh, dw, grad_in=dh_in, accumulate=True)
+        want, size, ww, wsize = _grads(h, dy, w, dh_in)
+        rounding = _half(h_type) if h_type == BF16 else 0
+        _close(dh, want, 2 * ROUNDS * size + rounding * want.abs())
+        _close(dw, ww + dw0, 256 * 2.0 ** -24 * (wsize + dw0.abs()))
