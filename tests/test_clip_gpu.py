@@ -245,3 +245,24 @@ def test_clip_of_more_chunks_than_ctas(gpu, sizes, g_type, o_type, shift):
     norm = plan.clip(0.5, factor=factor)
     _check(out, before, norm, factor, 0.5)
     assert plan.query() == 0
+
+
+@pytest.mark.parametrize("g_type,o_type", [("f32", "f32"), ("f32", "bf16"),
+                                           ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("g_shift,o_shift", [(4, 0), (0, 4), (4, 4), (4, 8), (8, 0)])
+def test_clip_where_one_of_both_is_off_its_boundary(gpu, g_type, o_type, g_shift,
+                                                    o_shift):
+    """A gradient and its result that start at different places: eight elements of
+    either may lie across a boundary while the other's do not."""
+    sizes = [20000, 16384, 31, 8]
+    grads = _grads(sizes, g_type, shift=g_shift)
+    before = [g.clone() for g in grads]
+    out = _grads(sizes, o_type, shift=o_shift, seed=3)
+    for ts, t, shift in ((grads, g_type, g_shift), (out, o_type, o_shift)):
+        wide = 8 * TYPES[t].itemsize
+        assert all((x.data_ptr() % wide == 0) == (shift % 8 == 0) for x in ts)
+    plan = ClipPlan(sizes, grad_dtype=g_type, out_dtype=o_type)
+    plan.bind(grads, out)
+    factor = torch.zeros(1, device="cuda")
+    norm = plan.clip(0.5, factor=factor)
+    _check(out, before, norm, factor, 0.5)
