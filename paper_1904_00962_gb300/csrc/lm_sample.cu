@@ -1315,6 +1315,13 @@ __device__ __forceinline__ void Draw<T, kStaged>::find_kept_tabled(Kept& kept) {
       kept.tie = values.value(f.bin);
     } else {
       const float end = __uint_as_float(__float_as_uint(values.gap) - 1);
+      if (!by && values.gap_number == values.last) {
+        // (the words below `lower` were counted in the gap: they have no mass, and with
+        // some of them among the first top_k all that have one are)
+        sum = 0;
+        each([&](float x, uint32_t) { sum += fabsf(x) < values.gap; });
+        if (before.count + row_sum(sum) < top_k) continue;
+      }
       kept.tie = cut(key_of(-end), key_of(end), by, target, before);
       if (!by && by_mass) {
         // (counting left no masses)
