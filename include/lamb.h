@@ -891,7 +891,8 @@ LAMB_API lamb_status_t lamb_norm_destroy(struct lamb_norm* plan);
  *     out = f g
  * where s is a scale that the gradients get anyway (the inverse of a loss scale or
  * of the number of micro-batches).  N covers gradients of any size (sums are scaled
- * where fp32 would overflow or vanish); it is rounded to fp32 in `norm` alone.  If an
+ * where fp32 would overflow or vanish), and f of any size keeps its digits in `out`
+ * (down to 2^-252); both are rounded to fp32 in `norm` and `factor` alone.  If an
  * element is Inf or NaN, N is Inf or NaN, f = s and LAMB_STATUS_GRAD_NONFINITE is
  * set: nothing is clipped (a step with LAMB_FLAG_SKIP_NONFINITE then skips itself).
  * The same bits in every run.

@@ -266,3 +266,31 @@ def test_clip_where_one_of_both_is_off_its_boundary(gpu, g_type, o_type, g_shift
     factor = torch.zeros(1, device="cuda")
     norm = plan.clip(0.5, factor=factor)
     _check(out, before, norm, factor, 0.5)
+
+
+@pytest.mark.parametrize("o_type", [None, "f32", "bf16"])
+@pytest.mark.parametrize("g_type", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("max_norm", [1.0, 1e-6, 1e-30])
+def test_clip_by_a_factor_below_the_normal_numbers(gpu, o_type, g_type, shift,
+                                                   max_norm):
+    """The factor is 2^-131 to 2^-231.  A result passes the norm's error and the
+    roundings of the factor's two parts, of a product and of the result's type."""
+    sizes = [100000, 31, 16384]
+    grads = _grads(sizes, g_type, 2e37, shift=shift)
+    before = [g.clone() for g in grads]
+    plan = ClipPlan(sizes, grad_dtype=g_type, out_dtype=o_type)
+    out = _grads(sizes, o_type, seed=2, shift=shift) if o_type else grads
+    plan.bind(grads, out if o_type else None)
+    norm, factor = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    plan.clip(max_norm, norm=norm, factor=factor)
+    f = max_norm / _norm(before)
+    assert 0 < f < 2.0 ** -129
+    assert abs(float(factor) - f) <= 2.0 ** -149
+    for x, g in zip(out, before):
+        exact = g.double() * f
+        half = torch.finfo(x.dtype).eps / 2
+        err = (x.double() - exact).abs()
+        least = 2.0 ** -149 if x.dtype == torch.float32 else 2.0 ** -133
+        assert (err <= (NORM + 3 * 2.0 ** -24 + half) * exact.abs() + least).all()
+    assert plan.query() == 0
