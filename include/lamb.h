@@ -833,7 +833,8 @@ LAMB_API lamb_status_t lamb_muon_destroy(struct lamb_muon* plan);
  * what stands in front of a language model's head and between its layers.
  *     h = x + residual, rounded to the residual's type;  h = x without one
  *     r = 1 / sqrt(mean of h^2 + eps);  y = h r weight
- * Sums are fp32: a row with entries beyond 1e19 in size gets r = 0.  Matrices are
+ * Sums are fp32: a row whose squares add up beyond 3.4e38 (entries of 1.8e19 /
+ * sqrt(width) in size) gets r = 0, and nothing of grad_out goes through it.  Matrices are
  * given as above; weights are vectors of `width` LAMB_F32 or LAMB_BF16.  Calls
  * enqueue on `stream`, allocate nothing and do not synchronise: capturable.
  * lamb_norm_forward uses no workspace; calls of lamb_norm_grad with one plan share

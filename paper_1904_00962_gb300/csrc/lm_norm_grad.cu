@@ -4,7 +4,8 @@
 //   g = dy w,  c = r^2 mean(g h),  dh = r (g - c h) + dh_in
 //   dw_j (+)= sum over the rows of dy_j h_j r
 //
-// r is formed again from h, which is read anyway.  A row's two sums go over the
+// r is formed again from h, which is read anyway; h r comes before dy's factor, as dy h
+// may leave fp32's range where dy h r is in it.  A row's two sums go over the
 // threads that hold it; a CTA keeps dw's terms of its rows in registers, leaves one
 // fp32 row of sums, and a second launch adds those in order: the same bits in every
 // run, whatever the order in which CTAs finish.
@@ -34,6 +35,11 @@ struct NormGradArgs {
   int lanes;
   float eps, inv_width;
 };
+
+// c of a row; 0 where r is 0, because the squares' sum is beyond fp32, whatever gh is.
+__device__ __forceinline__ float correction(float gh, float r, float inv_width) {
+  return r > 0.f ? gh * inv_width * r * r : 0.f;
+}
 
 // Both sums over a row's threads.  `turn` alternates from row to row, so that one
 // barrier a row is enough.
@@ -252,7 +258,7 @@ norm_grad_ring_kernel(const NormGradArgs a) {
     gh += more;
     over_row2<kWide>(hh, gh, lanes, sums, stage);
     const float r = rsqrtf(fmaf(hh, a.inv_width, a.eps));
-    const float c = gh * a.inv_width * r * r;
+    const float c = correction(gh, r, a.inv_width);
     const Two r2 = two(r, r), minus_rc2 = two(-r * c, -r * c);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
@@ -271,7 +277,7 @@ norm_grad_ring_kernel(const NormGradArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         // (zeros where there is no such column or row)
-        dw[i][j] = fma2(mul2(g[j], h[j]), r2, dw[i][j]);
+        dw[i][j] = fma2(g[j], mul2(h[j], r2), dw[i][j]);
         apart(fma2(h[j], minus_rc2, fma2(mul2(g[j], w[j]), r2, in[j])), out[2 * j],
               out[2 * j + 1]);
       }
@@ -339,7 +345,7 @@ norm_grad_rows_kernel(const NormGradArgs a) {
     over_row2<kWide>(hh, gh, lanes, sums, turn);
     turn ^= 1;
     const float r = rsqrtf(fmaf(hh, a.inv_width, a.eps));
-    const float c = gh * a.inv_width * r * r;
+    const float c = correction(gh, r, a.inv_width);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       float w[8], h[8], g[8], in[8];
@@ -383,7 +389,7 @@ __global__ void __launch_bounds__(kNormWalk) norm_grad_walk_kernel(
     over_row2<true>(hh, gh, 32, sums, turn);
     turn ^= 1;
     const float r = rsqrtf(fmaf(hh, a.inv_width, a.eps));
-    const float k = gh * a.inv_width * r * r;
+    const float k = correction(gh, r, a.inv_width);
     for (int c = threadIdx.x; c < a.width; c += kNormWalk) {
       const float x = get1(h + c), g = get1(dy + c);
       const float w = weight1(a.weight, a.weight_bf16, c);

@@ -364,3 +364,47 @@ def test_norm_grad_of_more_rows_than_ctas(gpu, n, d, shift, g_type, h_type):
         rounding = _half(h_type) if h_type == BF16 else 0
         _close(dh, want, 2 * ROUNDS * size + rounding * want.abs())
         _close(dw, ww + dw0, 256 * 2.0 ** -24 * (wsize + dw0.abs()))
+
+
+LAYOUTS = [(1024, 0), (1024, 1), (2048, 0), (2048, 1), (64, 0), (64, 1), (8200, 0)]
+
+
+@pytest.mark.parametrize("d,shift", LAYOUTS)
+def test_norm_grad_of_tiny_rows(gpu, d, shift):
+    """grad_out h is below the normal numbers of 32 bits, grad_out h r is not."""
+    n, eps = 6, 1e-20
+    h = _rows(n, d, F32, 1, shift=shift)
+    dy = _rows(n, d, F32, 2, shift=shift)
+    h *= 1e-15
+    dy *= 1e-28
+    plan = NormPlan(d, n, eps=eps)
+    dh, dw = torch.empty_like(h), torch.empty(d, device="cuda")
+    plan.norm_grad(dy, h, None, dh, dw)
+    x, g = h.double(), dy.double()
+    r = (x.square().mean(1, keepdim=True) + eps).rsqrt()
+    terms = g * x * r
+    _close(dw, terms.sum(0), 256 * 2.0 ** -24 * terms.abs().sum(0))
+    # (each of the row's products is off by half of 2^-149, too)
+    c = (g * x).mean(1, keepdim=True) * r * r
+    size = r * (g.abs() + (g * x).abs().mean(1, keepdim=True) * r * r * x.abs())
+    _close(dh, r * (g - c * x), 2 * ROUNDS * size + 2.0 ** -148 * r ** 3 * x.abs())
+
+
+@pytest.mark.parametrize("d,shift", LAYOUTS)
+def test_norm_grad_of_rows_whose_squares_overflow(gpu, d, shift):
+    """Such rows have r = 0: nothing goes through them, whatever grad_out h is."""
+    n = 4
+    h, dy = _rows(n, d, F32, 1, shift=shift), _rows(n, d, F32, 2, shift=shift)
+    dh_in, w = _rows(n, d, F32, 3, shift=shift), _weight(d, F32)
+    h[1] = 3e20 * (1 + torch.rand(d, device="cuda"))
+    dy[1] = 1e19 * (1 + torch.rand(d, device="cuda"))
+    h[2] = -2e19
+    plan = NormPlan(d, n, eps=EPS)
+    dh, dw = torch.empty_like(h), torch.empty(d, device="cuda")
+    y = plan.norm(h, w)
+    plan.norm_grad(dy, h, w, dh, dw, grad_in=dh_in)
+    assert (y[1:3] == 0).all() and torch.equal(dh[1:3], dh_in[1:3])
+    rows = [0, 3]
+    want, size, ww, wsize = _grads(h[rows], dy[rows], w, dh_in[rows])
+    _close(dh[rows], want, 2 * ROUNDS * size)
+    _close(dw, ww, 256 * 2.0 ** -24 * wsize)
