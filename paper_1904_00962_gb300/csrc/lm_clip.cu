@@ -45,7 +45,6 @@ struct ClipChunk {
 struct ClipArgs {
   const ClipChunk* chunks;
   int n_chunks;
-  int apply;                  // 0: the norm and the factor alone
   const float* d_scale;       // NULL: 1
   double max_norm;
   double* part;               // of each CTA
