@@ -856,7 +856,8 @@ LAMB_API lamb_status_t lamb_norm_create(int32_t width, int64_t max_rows,
  *   out       F32, BF16 (rounded once; may be x), or E4M3 with scales
  *   scales    E4M3: DEVICE float [n_rows][ceil(width / block)] (block 32 or 128
  *             columns, or 0: a scale a row): s = max(largest |y| of the block,
- *             2^-100) / 448, out = y / s to nearest.  A block with a NaN has
+ *             2^-100) / 448, out = y (1 / s) to nearest, a product of
+ *             fp32 numbers (within 2^-23 of y / s).  A block with a NaN has
  *             s = NaN */
 LAMB_API lamb_status_t lamb_norm_forward(
     struct lamb_norm* plan, const void* x, int32_t x_dtype, int64_t x_stride,

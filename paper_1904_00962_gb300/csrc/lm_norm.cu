@@ -3,7 +3,7 @@
 //   h = x + residual, rounded to the residual's type and stored;  h = x without
 //   r = 1 / sqrt(mean of h^2 + eps)
 //   y = h r w, in fp32 or bf16, or in e4m3 with a scale for each block of columns:
-//       s = max(largest |y| of the block, 2^-100) / 448,  q = e4m3(y / s)
+//       s = max(largest |y| of the block, 2^-100) / 448,  q = e4m3(y (1 / s))
 //
 // The norm is that of h as it is stored, so that the gradient (lm_norm_grad.cu),
 // which reads h, is the gradient of this function.  Sums of squares are fp32.
