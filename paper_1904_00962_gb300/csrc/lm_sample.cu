@@ -185,9 +185,11 @@ __device__ __forceinline__ Ratio ratio_of(float x) {
   return {(b & 0x7fffffu) | (e ? 0x800000u : 0u), 150 - max(e, 1)};
 }
 
-// Numbers in the order of logits; -0 is 0.
+// Numbers in the order of logits; -0 is 0, and a NaN is beyond all others.  (From the bits
+// alone: a NaN that a sum gives has no certain sign.)
 __device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __float_as_uint(x + 0.f);
+  const uint32_t bits = __float_as_uint(x);
+  const uint32_t b = bits == 0x80000000u ? 0u : bits;
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(uint32_t k) {
