@@ -725,8 +725,8 @@ LAMB_API lamb_status_t lamb_vocab_loss_grad(
  * top_k below 1 as all, a top_p not above 0 or a min_p not up to 1 as the first word
  * alone.  Masses p are whole numbers of 2^-44 (2^-38 at 2^24 words, the most; rounded
  * down), good to 2^-34 above 2^-6 and to 2^-28 of themselves below, and added without
- * rounding: a sum of them is good to about 2^-36.  Logits further apart than 1e38 are
- * taken as infinitely far apart.  Uses no workspace: calls of one plan may overlap. */
+ * rounding: a sum of them is good to about 2^-36 of itself and to a unit for each of
+ * its words.  Logits further apart than 1e38 are taken as infinitely far apart.  Uses no workspace: calls of one plan may overlap. */
 LAMB_API lamb_status_t lamb_vocab_sample(
     struct lamb_vocab* plan, const void* logits, int32_t dtype, int64_t stride,
     int64_t n_rows, const float* uniform, double temperature,

@@ -14,7 +14,8 @@
 //
 // Bound by memory: the gradients are read twice, once for N.  The second time goes
 // backwards, so that what the first left in L2 is met there.  336e6 fp32 gradients to
-// bf16 487 us, 6.6 and 6.9 TB/s; 109e6 of bf16 within the bound 39, 5.6.  Other numbers
+// bf16 494 us, 6.6 and 6.9 TB/s (1,570 element by element, where tensors are off their
+// boundary); 109e6 of bf16 within the bound 41, 5.6.  Other numbers
 // of groups of a thread and of CTAs an SM are slower: (8, 4) 579 us, (4, 6) 538, (16, 2)
 // 531 and (2, 8) 522 of the first, against 503 of (8, 3) then.
 #include <math.h>

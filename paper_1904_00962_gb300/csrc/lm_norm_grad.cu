@@ -162,7 +162,7 @@ __device__ __forceinline__ void leave_part(const NormGradArgs& a,
 
 // Rows that can be taken 16 bytes at a time.  They pass through a ring of two in shared
 // memory, so that a row is on its way while the one in front is worked on, and are
-// worked on two numbers at a time.  Bound by memory: 65,536 x 1,024 in bf16 in 86 us, 6.2
+// worked on two numbers at a time.  Bound by memory: 65,536 x 1,024 in bf16 in 85 us, 6.3
 // TB/s (119 with rows loaded into registers when they are wanted, 100 one number at a
 // time, 112 so with a ring of three).
 template <class TG, class TH, int kN, bool kWide>
@@ -297,7 +297,8 @@ norm_grad_ring_kernel(const NormGradArgs a) {
   leave_part<kN, kWide, true>(a, sum, lanes, reinterpret_cast<float*>(ring_memory));
 }
 
-// Other rows are loaded into registers, column by column.
+// Other rows are loaded into registers, column by column, when they are wanted: 30,000 x
+// 757 in bf16 66 us, 2.7 TB/s.
 template <class TG, class TH, int kN, bool kWide>
 __global__ void __launch_bounds__(kWide ? 32 * kNormMostWarps : kNormThreads,
                                   kWide ? 1 : ctas_by_registers(kN, false))
@@ -367,7 +368,8 @@ norm_grad_rows_kernel(const NormGradArgs a) {
 }
 
 // Rows that do not fit a CTA's registers: two looks at memory a row, and dw's sums in
-// the CTA's row of parts.
+// the CTA's row of parts.  4,096 x 16,384 in bf16 671 us, 0.8 TB/s of bytes that it cannot
+// do without.
 template <class TG, class TH>
 __global__ void __launch_bounds__(kNormWalk) norm_grad_walk_kernel(
     const NormGradArgs a) {

@@ -27,9 +27,11 @@
 // What CTAs tell one another they store into each other's shared memory.
 //
 // Bound by instructions and, with few rows, by the exchanges: reading the words is a tenth
-// of it.  1,024 rows of 30,522 words in bf16 without a filter 57 us (81 without the
-// table, 204 with the long form of each mass), 128 of 131,071 with top_p 67 (146, 186),
+// of it.  1,024 rows of 30,522 words in bf16 without a filter 53 us (81 without the
+// table, 204 with the long form of each mass), 128 of 131,071 with top_p 62 (146, 186),
 // 64 of 30,522 in fp32 with settings of their own 35, one with top_k and top_p 12.
+// 1,024 rows of 30,522 in fp32: 48 greedy, 103 without a filter, 290 with top_p 0.9.  All
+// forms are one kernel of 64 registers, which spills some 300 bytes.
 // Among many words pairs are slow: a cut among 250 took 12 us more so than by parts.
 // Tried and dropped: CTAs of 128 threads, eight on an SM, that read the row again (105
 // and 194 us of the first two before the table); fp32 masses with a bound on their error,
@@ -1666,7 +1668,7 @@ extern "C" lamb_status_t lamb_vocab_sample(
   const int bins = (a.cuts ? sizeof(DrawCuts) : 0) +
                    table_bytes(lm_elem_size(dtype), a.cuts);
   // CTAs of a row: while two of all of them fit on each SM, and until two of one row
-  // do; of 4,096 columns at least.  (1,024 rows of 30,522 by one CTA 81 us, by two 101;
+  // do; of 4,096 columns at least.  (Then, 1,024 rows of 30,522 by one CTA 81 us, by two 101;
   // 64 by two 43, four 41, eight 46; 128 rows of 131,071 in bf16 by two, which are alone
   // on their SMs, 209, by four 146, eight 194.)
   const int size = lm_elem_size(dtype);
