@@ -1668,7 +1668,7 @@ extern "C" lamb_status_t lamb_vocab_sample(
   const int bins = (a.cuts ? sizeof(DrawCuts) : 0) +
                    table_bytes(lm_elem_size(dtype), a.cuts);
   // CTAs of a row: while two of all of them fit on each SM, and until two of one row
-  // do; of 4,096 columns at least.  (Then, 1,024 rows of 30,522 by one CTA 81 us, by two 101;
+  // do; of 4,096 columns at least.  (Before the table, 1,024 rows of 30,522 by one CTA 81 us, by two 101;
   // 64 by two 43, four 41, eight 46; 128 rows of 131,071 in bf16 by two, which are alone
   // on their SMs, 209, by four 146, eight 194.)
   const int size = lm_elem_size(dtype);
